@@ -283,6 +283,72 @@ int slp_mean_loss(const float* losses /*device*/, int n, float* mean_out /*devic
 int slp_count_correct_static(const void* logits /*device*/, const int32_t* targets /*device*/, int batch, int classes,
                              int dt, int accumulate, int64_t* correct_out /*device*/, slp_stream stream);
 
+/* ---- segments in 8 bits ----------------------------------------------------------------
+ * Products of 8-bit matrices run at twice the bf16 rate and read half the bytes.  An 8-bit matrix here is two device buffers:
+ *   q       [rows][ldq]   e4m3 values (OCP: 4 exponent and 3 fraction bits, largest 448, no infinity), one byte each; q on a 16-byte boundary,
+ *                         ldq a multiple of 16, the bytes from the last column up to the next multiple of 16 zero;
+ *   scales  [rows / block, rounded up][lds]   one byte e for each 128 consecutive columns (and, block = 128, each 128 rows): the values
+ *                         stand for q * 2^(e - 127); 255 is NaN.  On a 4-byte boundary, lds a multiple of 4 and at least the number of
+ *                         blocks of a row; bytes past that number are not interpreted.
+ * block is 1 (activations and gradients: a scale for each 128 elements of a row) or 128 (weights: one for each 128 x 128 block, which the
+ * transposed matrix shares).  Scales are powers of two because the matrix instruction applies those by itself.  Quantising picks the least
+ * power of two, not below 2^-127, under which the block's largest magnitude fits 448, and rounds to nearest even: nothing saturates.  A block
+ * that holds an infinity or a NaN gets the scale 255, so that whatever is computed from it is NaN.
+ * Rows that are not a multiple of 4096 bytes apart are read faster (fewer of them share a memory channel).
+ * The calls take the leading dimensions of every matrix in elements, 64 bits wide; float32 and bf16 matrices may start at any element.  An
+ * empty matrix (0 rows) is a call without effect.  Common errors: SLP_ERR_ARG (null pointer, negative size, unknown dtype or block),
+ * SLP_ERR_SHAPE (a leading dimension below the row, rows or columns above 2^24, more than 2^40 elements, an 8-bit row above 2^22 bytes), SLP_ERR_ALLOC (alignment, workspace),
+ * SLP_ERR_DEVICE. */
+
+/* Matrix x[rows][cols] (dtype dt, device) to 8 bits: row-major to q and scales (both or neither null), transposed to qt[cols][ldqt] and
+ * scales_t with the rows of x as its columns (both or neither null; at least one of the two layouts).  A transposed copy with block = 1
+ * has scales of its own, one for each 128 rows of x; with block = 128 it holds the same values and scales as the row-major one.
+ * mask (dtype dt, may be NULL): elements whose mask is not > 0 count as zero -- the ReLU's derivative from its output.  column_sums (float32
+ * [cols], may be NULL): the sums of the (masked) columns, the bias's gradient, added in a fixed order; needs workspace. */
+size_t slp_quantize_workspace_bytes(int rows, int cols);
+int slp_quantize(const void* x /*device*/, int64_t ldx, const void* mask /*device, may be NULL*/, int64_t ldmask, int dt, int rows, int cols, int block,
+                 void* q, int64_t ldq, void* scales, int64_t lds, void* qt, int64_t ldqt, void* scales_t, int64_t ldst,
+                 float* column_sums /*device, may be NULL*/, void* workspace /*device*/, size_t workspace_bytes, slp_stream stream);
+
+/* out[M][N] = act(A B^T + bias): A [M][K] and B [N][K] 8-bit matrices, each with its own block; bias float32 [N] or NULL; act the ReLU
+ * where relu is not 0 (a NaN stays one); out of dtype dt.  Sums are float32; where dt is SLP_BF16 the matrix
+ * instruction keeps about 15 bits below the largest of neighbouring products (some 2e-5 of the result, a hundredth of what rounding it to bf16 costs),
+ * where dt is SLP_F32 all of float32.  Forward: A the input, B the weights.  Gradient of the input:
+ * A the gradient of the output, B the transposed weights.  Gradient of the weights: A and B the transposed gradient and input.
+ * K = 0 leaves act(bias).  The workspace holds partial products of a contraction that is split over the chip; 256-byte aligned, its size is
+ * 0 for most large products. */
+size_t slp_product_workspace_bytes(int M, int N, int K);
+int slp_product(const void* a /*device*/, int64_t lda, const void* a_scales, int64_t ldsa, int a_block, const void* b, int64_t ldb,
+                const void* b_scales, int64_t ldsb, int b_block, const float* bias /*device, may be NULL*/, int relu, int M, int N, int K,
+                void* out /*device*/, int64_t ldo, int dt, void* workspace /*device*/, size_t workspace_bytes, slp_stream stream);
+
+/* Root-mean-square norm of x + residual:
+ *   h = x + residual (added in float32, rounded to dt; h = x where residual is NULL);  n = 1 / sqrt(mean over the row of h^2 + eps);  y = h n gamma
+ * x, residual, h, y: [rows][dim] of dtype dt; gamma float32 [dim], NULL for ones; rstd float32 [rows] receives n.  h must be given where
+ * residual is, and may be x or residual; y, rstd and the 8-bit output (q and scales together, block 1) may be NULL.  The norm and the 8-bit values
+ * are of h as stored. */
+int slp_rmsnorm(const void* x /*device*/, int64_t ldx, const void* residual /*device, may be NULL*/, int64_t ldr, const float* gamma, float eps, int dt,
+                int rows, int dim, void* h, int64_t ldh, void* y, int64_t ldy, void* q, int64_t ldq, void* scales, int64_t lds, float* rstd, slp_stream stream);
+
+/* Its backward pass, from dy (the gradient of y; rounding to 8 bits passes it on), h and rstd as the forward call left them and dh, the gradient that reaches h past
+ * the norm (NULL: none):  dx_j = dh_j + n (gamma_j dy_j - h_j n^2 mean over the row of gamma dy h), the gradient of x and of the residual alike;
+ * dgamma_j (float32, may be NULL) = sum over the rows of dy_j h_j n, added in a fixed order.  dx may be dy or dh.  Workspace: 256-byte aligned. */
+size_t slp_rmsnorm_backward_workspace_bytes(int rows, int dim);
+int slp_rmsnorm_backward(const void* dy /*device*/, int64_t lddy, const void* h, int64_t ldh, const float* gamma, const float* rstd, const void* dh, int64_t lddh, int dt,
+                         int rows, int dim, void* dx, int64_t lddx, float* dgamma, void* workspace, size_t workspace_bytes, slp_stream stream);
+
+/* ---- the norm of all gradients together ---------------------------------------------------------------
+ * tensors[i] (device) holds counts[i] contiguous elements of dtype dts[i]; the three arrays are host memory and are not kept.
+ * slp_gradient_norm: *norm_out = sqrt of the sum of all squares (float32; squares and sums are float64, in a fixed order).
+ * slp_clip_gradients: out[i] = c tensors[i] with c = min(1, max_norm / (norm + 1e-6)); out[i] may be tensors[i] (out NULL: all of them), where c = 1 costs
+ * nothing.  A norm that is not finite leaves the values as they are: look at *norm_out and skip the update.  norm_out may be NULL.
+ * Workspace: 256-byte aligned.  Errors: SLP_ERR_ARG (null array or tensor, negative count, unknown dtype, max_norm not > 0), SLP_ERR_ALLOC, SLP_ERR_DEVICE. */
+size_t slp_gradient_norm_workspace_bytes(const int64_t* counts /*host*/, int n);
+int slp_gradient_norm(const void* const* tensors /*host*/, const int64_t* counts /*host*/, const int* dts /*host*/, int n, float* norm_out /*device*/,
+                      void* workspace /*device*/, size_t workspace_bytes, slp_stream stream);
+int slp_clip_gradients(const void* const* tensors /*host*/, void* const* out /*host, may be NULL*/, const int64_t* counts /*host*/, const int* dts /*host*/, int n,
+                       float max_norm, float* norm_out /*device, may be NULL*/, void* workspace /*device*/, size_t workspace_bytes, slp_stream stream);
+
 /* ---- measurement hooks -------------------------------------------------------------
  * When enabled, every matrix-product launch of the segment is bracketed by HIP
  * events on its stream.  slp_segment_profile_read synchronises the recorded events,

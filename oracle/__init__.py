@@ -10,6 +10,8 @@ Contents
 rng.py      counter-based generator (Philox4x32-10) and the transforms that turn
             its words into synthetic intermediate labels (paper Eq. 1), input
             noise for interior segments and initial weights.
+eightbit.py 8-bit matrices, their products, the root-mean-square norm with its backward pass, clipping by
+            the norm of all gradients.
 segment.py  one training step of one network segment (forward, loss, backward
             confined to the segment, SGD with momentum) in float64, with an
             optional emulation of bf16 storage points.

@@ -6,6 +6,7 @@ tensors used as raw device memory; the stream passed to the library is torch's
 current stream, so ordinary torch stream semantics apply.
 """
 
+import collections
 import ctypes
 import os
 
@@ -74,6 +75,16 @@ def lib():
         "slp_count_correct": (i32, [vp, vp, i32, i32, i32, vp, sz, i32, vp, vp]),
         "slp_mean_loss": (i32, [vp, i32, vp, vp]),
         "slp_count_correct_static": (i32, [vp, vp, i32, i32, i32, i32, vp, vp]),
+        "slp_quantize_workspace_bytes": (sz, [i32, i32]),
+        "slp_quantize": (i32, [vp, i64, vp, i64, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]),
+        "slp_product_workspace_bytes": (sz, [i32, i32, i32]),
+        "slp_product": (i32, [vp, i64, vp, i64, i32, vp, i64, vp, i64, i32, vp, i32, i32, i32, i32, vp, i64, i32, vp, sz, vp]),
+        "slp_rmsnorm": (i32, [vp, i64, vp, i64, vp, f32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp]),
+        "slp_rmsnorm_backward_workspace_bytes": (sz, [i32, i32]),
+        "slp_rmsnorm_backward": (i32, [vp, i64, vp, i64, vp, vp, vp, i64, i32, i32, i32, vp, i64, vp, vp, sz, vp]),
+        "slp_gradient_norm_workspace_bytes": (sz, [ctypes.POINTER(i64), i32]),
+        "slp_gradient_norm": (i32, [ctypes.POINTER(vp), ctypes.POINTER(i64), ctypes.POINTER(i32), i32, vp, vp, sz, vp]),
+        "slp_clip_gradients": (i32, [ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.POINTER(i64), ctypes.POINTER(i32), i32, f32, vp, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -90,7 +101,9 @@ EXPORTS = ["slp_last_error", "slp_make_synthetic_labels", "slp_make_segment_inpu
            "slp_segment_profile_enable", "slp_segment_profile_read", "slp_probe_mfma_rate",
            "slp_segment_set_graph", "slp_segment_set_overlap", "slp_segment_join", "slp_count_correct", "slp_mean_loss",
            "slp_count_correct_static", "slp_segment_set_fused_update", "slp_segment_target_errors",
-           "slp_segment_graph_stats"]
+           "slp_segment_graph_stats", "slp_quantize_workspace_bytes", "slp_quantize", "slp_product_workspace_bytes",
+           "slp_product", "slp_rmsnorm", "slp_rmsnorm_backward_workspace_bytes", "slp_rmsnorm_backward",
+           "slp_gradient_norm_workspace_bytes", "slp_gradient_norm", "slp_clip_gradients"]
 
 
 def _check(code):
@@ -170,6 +183,162 @@ def mean_loss(losses, out=None):
         out = torch.empty(1, dtype=torch.float32, device=losses.device)
     _check(lib().slp_mean_loss(_ptr(losses), losses.numel(), _ptr(out), _stream()))
     return out
+
+
+# ---- segments in 8 bits -----------------------------------------------------------------------------------------
+# A matrix in 8 bits: q [rows, cols] (float8_e4m3fn, rows on 16-byte boundaries), scales [rows / block, cols / 128] (both rounded up,
+# float8_e8m0fnu, rows on 4-byte boundaries), block 1 or 128 rows that share a scale.
+Quantized = collections.namedtuple("Quantized", "q scales block")
+QuantizeResult = collections.namedtuple("QuantizeResult", "rows transposed column_sums")
+NormResult = collections.namedtuple("NormResult", "h rstd y y8")
+
+
+def _float_dtype(t):
+    """The library's number for a matrix's element type."""
+    if t.dtype is torch.bfloat16:
+        return BF16
+    assert t.dtype is torch.float32, "float32 or bfloat16 (got %s)" % t.dtype
+    return F32
+
+
+def _matrix(t, like=None):
+    """Leading dimension of a matrix on the device whose rows are contiguous (of the shape and type of `like`)."""
+    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.size(1) <= 1)
+    if like is not None:
+        assert t.dtype is like.dtype and t.shape == like.shape and t.device == like.device
+    return t.stride(0) if t.size(0) > 1 else max(t.stride(0), t.size(1))
+
+
+def _vector(t, n):
+    """Address of a contiguous float32 vector of n elements on the device, or None."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype is torch.float32 and t.is_contiguous() and t.numel() == n
+    return t.data_ptr()
+
+
+def empty_quantized(rows, cols, block=1, device="cuda"):
+    """Room for a matrix in 8 bits: rows on 128-byte boundaries and not a multiple of 4 KB apart (they are read faster then)."""
+    ld = -(-cols // 128) * 128
+    if ld % 4096 == 0:
+        ld += 128
+    blocks, srows = -(-cols // 128), -(-rows // block)
+    lds = -(-blocks // 4) * 4
+    q = torch.empty((rows, ld), dtype=torch.float8_e4m3fn, device=device)
+    scales = torch.empty((srows, lds), dtype=torch.float8_e8m0fnu, device=device)
+    return Quantized(q.as_strided((rows, cols), (ld, 1)), scales.as_strided((srows, blocks), (lds, 1)), block)
+
+
+def _eight(m, rows, cols):
+    """(q, its leading dimension, scales, theirs) of a matrix in 8 bits."""
+    if m is None:
+        return None, 0, None, 0
+    q, scales, block = m
+    assert q.is_cuda and q.dtype is torch.float8_e4m3fn and tuple(q.shape) == (rows, cols) and (q.stride(1) == 1 or cols <= 1)
+    assert scales.is_cuda and scales.dtype is torch.float8_e8m0fnu and tuple(scales.shape) == (-(-rows // block), -(-cols // 128))
+    assert scales.stride(1) == 1 or scales.size(1) <= 1
+    return q.data_ptr(), q.stride(0), scales.data_ptr(), scales.stride(0)
+
+
+def _workspace(size, device):
+    return torch.empty(size, dtype=torch.uint8, device=device) if size else None
+
+
+def quantize(x, block=1, rows=True, transposed=False, mask=None, column_sums=False):
+    """slp_quantize: x in 8 bits, row-major (`rows`) and transposed as asked, with a scale for each 128 elements of a row of the
+    result (block=1) or each 128 x 128 block (block=128).  Elements whose `mask` is not positive count as zero; column_sums: also
+    the sums of x's (masked) columns."""
+    ldx, dt, (m, n) = _matrix(x), _float_dtype(x), x.shape
+    ldmask = _matrix(mask, x) if mask is not None else 0
+    r = empty_quantized(m, n, block, x.device) if rows else None
+    t = empty_quantized(n, m, block, x.device) if transposed else None
+    sums = torch.empty(n, dtype=torch.float32, device=x.device) if column_sums else None
+    size = lib().slp_quantize_workspace_bytes(m, n) if column_sums else 0
+    work = _workspace(size, x.device)
+    _check(lib().slp_quantize(_ptr(x), ldx, _ptr(mask), ldmask, dt, m, n, block, *_eight(r, m, n), *_eight(t, n, m), _ptr(sums), _ptr(work), size, _stream()))
+    return QuantizeResult(r, t, sums)
+
+
+def product(a, b, bias=None, relu=False, dtype=BF16, out=None):
+    """slp_product: act(a b^T + bias) of two Quantized matrices with the same number of columns, as a matrix of `dtype` (or into
+    `out`, whose type decides then)."""
+    (m, k), n = a.q.shape, b.q.size(0)
+    if out is None:
+        out = torch.empty((m, n), dtype=_torch_dtype(dtype), device=a.q.device)
+    else:
+        assert tuple(out.shape) == (m, n)
+    size = lib().slp_product_workspace_bytes(m, n, k)
+    work = _workspace(size, out.device)
+    _check(lib().slp_product(*_eight(a, m, k), a.block, *_eight(b, n, k), b.block, _vector(bias, n), int(bool(relu)), m, n, k, _ptr(out), _matrix(out),
+                             _float_dtype(out), _ptr(work), size, _stream()))
+    return out
+
+
+def rmsnorm(x, gamma=None, residual=None, eps=1e-6, normed=False, quantized=True):
+    """slp_rmsnorm: h = x + residual (x itself without one), rstd, the norm y in x's type if `normed`, and y8 in 8 bits if `quantized`."""
+    ldx, dt, (m, n) = _matrix(x), _float_dtype(x), x.shape
+    h, ldr, ldh = x, 0, 0
+    if residual is not None:
+        ldr = _matrix(residual, x)
+        h = torch.empty((m, n), dtype=x.dtype, device=x.device)
+        ldh = n
+    y = torch.empty((m, n), dtype=x.dtype, device=x.device) if normed else None
+    y8 = empty_quantized(m, n, 1, x.device) if quantized else None
+    rstd = torch.empty(m, dtype=torch.float32, device=x.device)
+    _check(lib().slp_rmsnorm(_ptr(x), ldx, _ptr(residual), ldr, _vector(gamma, n), eps, dt, m, n, _ptr(h) if ldh else None, ldh, _ptr(y), n,
+                             *_eight(y8, m, n), _ptr(rstd), _stream()))
+    return NormResult(h, rstd, y, y8)
+
+
+def rmsnorm_backward(dy, h, gamma, rstd, dh=None, gamma_grad=True):
+    """slp_rmsnorm_backward: (the gradient of x and of the residual, the gradient of gamma or None)."""
+    dt, (m, n) = _float_dtype(h), h.shape
+    dx = torch.empty((m, n), dtype=h.dtype, device=h.device)
+    dgamma = torch.empty(n, dtype=torch.float32, device=h.device) if gamma_grad else None
+    size = lib().slp_rmsnorm_backward_workspace_bytes(m, n)
+    work = _workspace(size, h.device)
+    _check(lib().slp_rmsnorm_backward(_ptr(dy), _matrix(dy, h), _ptr(h), _matrix(h), _vector(gamma, n), _vector(rstd, m), _ptr(dh),
+                                      _matrix(dh, h) if dh is not None else 0, dt, m, n, _ptr(dx), n, _ptr(dgamma), _ptr(work), size, _stream()))
+    return dx, dgamma
+
+
+def _tensor_list(tensors):
+    n = len(tensors)
+    for t in tensors:
+        assert t.is_cuda and t.is_contiguous()
+    return ((ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors]), (ctypes.c_int64 * n)(*[t.numel() for t in tensors]),
+            (ctypes.c_int * n)(*[_float_dtype(t) for t in tensors]), n)
+
+
+def gradient_norm(tensors):
+    """slp_gradient_norm: the norm of all tensors' values together, as a device scalar."""
+    ptrs, counts, dts, n = _tensor_list(tensors)
+    assert n > 0
+    device = tensors[0].device
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    size = lib().slp_gradient_norm_workspace_bytes(counts, n)
+    work = _workspace(size, device)
+    _check(lib().slp_gradient_norm(ptrs, counts, dts, n, _ptr(norm), _ptr(work), size, _stream()))
+    return norm
+
+
+def clip_gradients(tensors, max_norm, out=None):
+    """slp_clip_gradients: scales the tensors together to a norm of at most max_norm, in place or into `out` (tensors of the same
+    sizes and types).  Returns the norm before, a device scalar; where it is not finite the values are left as they are."""
+    ptrs, counts, dts, n = _tensor_list(tensors)
+    assert n > 0
+    to = None
+    if out is not None:
+        assert len(out) == n
+        for t, o in zip(tensors, out):
+            assert o.is_cuda and o.is_contiguous() and o.dtype is t.dtype and o.numel() == t.numel()
+        to = (ctypes.c_void_p * n)(*[o.data_ptr() for o in out])
+    device = tensors[0].device
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    size = lib().slp_gradient_norm_workspace_bytes(counts, n)
+    work = _workspace(size, device)
+    _check(lib().slp_clip_gradients(ptrs, to, counts, dts, n, max_norm, _ptr(norm), _ptr(work), size, _stream()))
+    return norm
 
 
 class Segment:

@@ -36,6 +36,11 @@ UNITS = {
     "chain.hip": [],
     "probe.hip": [],
     "accuracy.hip": [],
+    "operators.hip": [],
+    "norm.hip": [],
+    "quantize.hip": [],
+    "product.hip": [],
+    "clip.hip": [],
 }
 
 

@@ -12,15 +12,16 @@
 #include <algorithm>
 #include <vector>
 
+#include "host_errors.h"
 #include "slp_kernels.h"
 
 using namespace slp;
 
 namespace {
-
 thread_local char g_err[512] = "";
+}
 
-int fail(int code, const char* fmt, ...) {
+int slp::fail(int code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
@@ -28,11 +29,7 @@ int fail(int code, const char* fmt, ...) {
   return code;
 }
 
-#define HIP_TRY(expr)                                                                             \
-  do {                                                                                            \
-    hipError_t e__ = (expr);                                                                      \
-    if (e__ != hipSuccess) return fail(SLP_ERR_DEVICE, "%s: %s", #expr, hipGetErrorString(e__)); \
-  } while (0)
+namespace {
 
 constexpr size_t kAlign = 256;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }

@@ -1,0 +1,115 @@
+// Device helpers of the 8-bit operators: vectors of 8 elements at any alignment, e4m3 values and their power-of-two scales.
+#pragma once
+
+#include "eightbit.h"
+
+namespace slp {
+namespace {
+
+typedef __bf16 bf16;
+typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+
+// Vectors that start at any element of a row (global memory takes them at any address).
+struct __attribute__((packed, aligned(2))) AnyBf16x8 { bf16x8 v; };
+struct __attribute__((packed, aligned(2))) AnyBf16x4 { bf16x4 v; };
+struct __attribute__((packed, aligned(4))) AnyF32x4 { f32x4 v; };
+
+// v[j] = p[j], 0 for j >= n
+__device__ __forceinline__ void load8(const bf16* p, int n, float (&v)[8]) {
+  if (n >= 8) {
+    const bf16x8 x = ((const AnyBf16x8*)p)->v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)x[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? (float)p[j] : 0.0f;
+  }
+}
+__device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
+  if (n >= 8) {
+    const f32x4 a = ((const AnyF32x4*)p)->v, b = ((const AnyF32x4*)(p + 4))->v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[j] = a[j];
+      v[4 + j] = b[j];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : 0.0f;
+  }
+}
+// p[j] = v[j] for j < n, rounded to the type
+__device__ __forceinline__ void store8(bf16* p, int n, const float (&v)[8]) {
+  if (n >= 8) {
+    bf16x8 x;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = (bf16)v[j];
+    ((AnyBf16x8*)p)->v = x;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) p[j] = (bf16)v[j];
+  }
+}
+__device__ __forceinline__ void store8(float* p, int n, const float (&v)[8]) {
+  if (n >= 8) {
+    ((AnyF32x4*)p)->v = f32x4{v[0], v[1], v[2], v[3]};
+    ((AnyF32x4*)(p + 4))->v = f32x4{v[4], v[5], v[6], v[7]};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) p[j] = v[j];
+  }
+}
+
+// Lane i of a row of 16 takes the value of the lane that the control names.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
+}
+constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
+__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint32_t max_of_16(uint32_t x) {
+  x = umax(x, dpp<kSwap1>(x));
+  x = umax(x, dpp<kSwap2>(x));
+  x = umax(x, dpp<kHalfMirror>(x));
+  return umax(x, dpp<kMirror>(x));
+}
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float x) { return x + __builtin_bit_cast(float, dpp<CTRL>(__builtin_bit_cast(uint32_t, x))); }
+__device__ __forceinline__ float sum_of_64(float x) {
+  x = add_dpp<kSwap1>(x);
+  x = add_dpp<kSwap2>(x);
+  x = add_dpp<kHalfMirror>(x);
+  x = add_dpp<kMirror>(x);
+  x += __shfl_xor(x, 16, 64);
+  return x + __shfl_xor(x, 32, 64);
+}
+
+// |v| as an integer that orders like the value, infinities and NaN above all others
+__device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu; }
+// The scale 2^e of a block as e + 127: the least e >= -127 with max|x| <= 448 2^e (448 = 1.75 2^8, the largest e4m3 value).  With max|x| =
+// f 2^k, 1 <= f < 2, e is k - 8, one more where f > 1.75: the carry of adding 0.25 - 2^-23 to the fraction.  A block that holds an infinity
+// or a NaN gets 255, the scale's own NaN: everything computed from it is NaN, as it would be from the block itself.
+__device__ __forceinline__ uint32_t scale_of(uint32_t amax) {
+  const int e = (int)((amax + 0x1FFFFFu) >> 23) - 8;
+  return amax >= 0x7F800000u ? 255u : (uint32_t)(e > 0 ? e : 0);
+}
+// 2^-e; NaN for the scale 255
+__device__ __forceinline__ float inverse_scale(uint32_t scale) {
+  return __builtin_bit_cast(float, scale == 255u ? 0x7FC00000u : (254u - scale) << 23);
+}
+// Four values to e4m3, round to nearest even.  None is above 448 after scaling, so nothing saturates.
+__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) {
+  int o = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  o = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, o, true);
+  return (uint32_t)o;
+}
+
+}  // namespace
+}  // namespace slp
