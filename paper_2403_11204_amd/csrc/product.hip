@@ -20,6 +20,8 @@
 #include "eightbit_device.h"
 
 #include <mutex>
+#include <type_traits>
+#include <utility>
 
 namespace slp {
 namespace {
@@ -84,19 +86,17 @@ __device__ __forceinline__ void store4(const ProductArgs& g, int m, int n, f32x4
   }
 }
 __device__ __forceinline__ f32x4 finished(const ProductArgs& g, f32x4 v, f32x4 bias) {
+  const float least = g.relu ? 0.0f : -INFINITY;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    v[e] += bias[e];
-    if (g.relu) v[e] = v[e] < 0.0f ? 0.0f : v[e];       // (a NaN stays one)
-  }
+  for (int e = 0; e < 4; ++e) v[e] = __builtin_elementwise_maximum(v[e] + bias[e], least);       // (a NaN stays one)
   return v;
 }
+// bias[n .. n + 3]; what is past its end is the last one, for columns that nobody stores
 __device__ __forceinline__ f32x4 bias4(const ProductArgs& g, int n) {
   f32x4 b = {0.0f, 0.0f, 0.0f, 0.0f};
   if (g.bias) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (n + e < g.N) b[e] = g.bias[n + e];
+    for (int e = 0; e < 4; ++e) b[e] = g.bias[n + e < g.N ? n + e : g.N - 1];
   }
   return b;
 }
@@ -217,6 +217,362 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const ProductArgs g, 
 #endif
 }
 
+// f(0), f(1), ... f(N - 1) with the index as a constant.
+template <typename F, int... I>
+__device__ __forceinline__ void static_for_impl(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, typename F>
+__device__ __forceinline__ void static_for(F f) { static_for_impl(f, std::make_integer_sequence<int, N>{}); }
+
+// workgroup -> 256x256 tile.  Consecutive workgroups go round the XCDs: all of them work on one 16 x 16 region of tiles at a time where
+// the tiles divide into such, on contiguous runs of tile columns 8 tiles high otherwise.
+__device__ __forceinline__ void big_tile(const ProductArgs& g, int& tm, int& tn) {
+  const int tilesM = (g.M + 255) / 256, tilesN = (g.N + 255) / 256, pid = blockIdx.x, xcd = pid % kXcds, q = pid / kXcds;
+  if (tilesM % 16 == 0 && tilesN % 16 == 0) {
+    const int r = q / 32, sl = q % 32, regions = tilesM / 16;
+    tm = (r % regions) * 16 + (xcd % 2) * 8 + sl % 8;
+    tn = (r / regions) * 16 + (xcd / 2) * 4 + sl / 8;
+    return;
+  }
+  const int total = tilesM * tilesN, base = total / kXcds, rem = total % kXcds, tid = xcd * base + (xcd < rem ? xcd : rem) + q;
+  const int width = 8 * tilesN, first = tid / width * 8, rows = tilesM - first < 8 ? tilesM - first : 8;
+  tm = first + tid % width % rows;
+  tn = tid % width / rows;
+}
+
+// Large products: a 256x256 tile on 4 wavefronts of 128 x 128, one on each SIMD, accumulators in 256 AGPRs, two LDS stages of 64 KB, a k-tile
+// of 128 (one scale).  One wavefront on a SIMD has nobody to fill its issue slots, so everything else goes between the MFMAs, a few
+// instructions at a time.  The scales of 4 k-tiles come as one dword for each row into a ring of two, and from there as a byte beside
+// each fragment.  MFMAs and loads are assembly: the accumulators stay where they are, and a load's LDS address (m0) is set in front of an MFMA.
+//
+// bf16 outputs: a k-tile is 64 MFMAs of 32 cycles, in 4 strips of 2 A fragments against all 8 B fragments.  B's fragments stay in
+// registers for the whole k-tile; A's are read a strip ahead.
+//   strip 1  barrier X: nobody reads this k-tile's B rows any more;  strips 1, 2: the 8 loads of k-tile kt + 2 into them
+//   strip 3  barrier Y: k-tile kt + 1 has landed, nobody reads this one's A rows;  strips 3, 0: the 8 loads of kt + 2 into those;
+//            strips 3 and 0 read kt + 1's B fragments, one every third MFMA, each behind the last that uses its predecessor and 6 ahead of
+//            the first that uses it
+// The loop starts at strip 1, where the compiler, which waits for every LDS read at a loop's head, finds only those that strip needs.
+//
+// float32 outputs (EXACT): a k-tile is 2 sub-steps of 64 k, each 128 bf16 MFMAs of 16 cycles in the same 4 strips.  Both operands pass through a
+// conversion on the way, 128 of them a sub-step, one behind each MFMA: B's fragments, double-buffered, behind the even ones, A's, a strip
+// ahead, behind the odd ones; the bytes are read from LDS 14 MFMAs before their conversion starts.
+//   sub-step 1, MFMA   0  barrier Z: k-tile kt + 1 has landed, nobody reads this one's B rows;  4 .. 60: the 8 loads of kt + 2 into them
+//                     72  barrier X: nobody reads this one's A rows;  76 .. 132 (into the next sub-step): the 8 loads of kt + 2 into those
+constexpr int kBigScales = 2 * 512 * 128, kBigSmem = kBigScales + 2 * 512 * 4;
+template <bool EXACT>
+__global__ __launch_bounds__(256) void product_long_kernel(const ProductArgs g) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef __attribute__((ext_vector_type(4))) int i32x4;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  constexpr int A_BYTES = 256 * 128, STAGE = 512 * 128;
+  int tm, tn;
+  big_tile(g, tm, tn);
+  const int m0 = tm * 256, n0 = tn * 256;
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, wm = w & 1, wn = w >> 1, lgrp = lane >> 4, lrow = lane & 15;
+  const int nk = (g.K + 127) / 128, Kr = (g.K + 15) & ~15;
+  const int ra = g.M - m0 < 256 ? g.M - m0 : 256, rb = g.N - n0 < 256 ? g.N - n0 : 256;
+  // a buffer resource by words: as an operand of assembly it has to be a vector
+  auto rsrc = [](const void* p, int64_t bytes) {
+    const uint64_t a = (uint64_t)(uintptr_t)p;
+    return i32x4{(int)(uint32_t)a, (int)(uint32_t)(a >> 32), (int)bytes, 0x00020000};
+  };
+  const i32x4 rsrcA = rsrc(g.a + (int64_t)m0 * g.lda, (ra - 1) * g.lda + Kr), rsrcB = rsrc(g.b + (int64_t)n0 * g.ldb, (rb - 1) * g.ldb + Kr);
+  // load i < 8 fills rows [32 i, 32 i + 32) of A's tile, i >= 8 of B's; wavefront w rows 8w .. 8w + 7 of those
+  const int prow = w * 8 + (lane >> 3), chunk = (lane & 7) ^ ((prow >> 1) & 7);
+  uint32_t voff[16];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    voff[i] = prow + 32 * i < ra ? (uint32_t)((prow + 32 * i) * g.lda + chunk * 16) : kOutOfRange;
+    voff[8 + i] = prow + 32 * i < rb ? (uint32_t)((prow + 32 * i) * g.ldb + chunk * 16) : kOutOfRange;
+  }
+  // scales: wavefront w loads rows 64 w .. 64 w + 63 of A's and of B's
+  const int srow = 64 * w + lane, sfA = m0 >> g.shift_a, sfB = n0 >> g.shift_b, slA = ((m0 + ra - 1) >> g.shift_a) - sfA, slB = ((n0 + rb - 1) >> g.shift_b) - sfB;
+  const i32x4 rsrcSA = rsrc(g.sa + sfA * g.ldsa, slA * g.ldsa + ((nk + 3) & ~3)), rsrcSB = rsrc(g.sb + sfB * g.ldsb, slB * g.ldsb + ((nk + 3) & ~3));
+  const uint32_t soffA = srow < ra ? (uint32_t)((((m0 + srow) >> g.shift_a) - sfA) * g.ldsa) : kOutOfRange;
+  const uint32_t soffB = srow < rb ? (uint32_t)((((n0 + srow) >> g.shift_b) - sfB) * g.ldsb) : kOutOfRange;
+  typedef __attribute__((address_space(3))) void* lds_ptr_t;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
+  const uint32_t lds_wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds0 + w * 1024));
+  const uint32_t lds_scale = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds0 + kBigScales + w * 256));
+
+  f32x4 acc[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  // Chunks past K become zero fills: one that is past it in a k-tile is past it in all that follow.
+  auto clip = [&](int kt) {
+    if (kt * 128 + 128 > Kr) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (kt * 128 + chunk * 16 >= Kr) voff[i] = kOutOfRange;
+    }
+  };
+  // The k offset is a scalar; k-tiles past the end, whose offsets are out of range already, take 0, so that no sum of the two wraps.
+  auto koff_of = [&](int kt) { return (uint32_t)(kt < nk ? kt : 0) * 128u; };
+  // The statements name the m0 they set, so that one set by the compiler for an access of its own does not pass for still set behind them; it
+  // warns of every register it reserves.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+#define SLP_LOAD_ARGS(i, base_, koff_)                                                                                             \
+  [base] "s"(base_), [row] "i"((i) < 8 ? (i) * 4096 : A_BYTES + ((i) - 8) * 4096), [off] "v"(voff[i]), [rsrc] "s"((i) < 8 ? rsrcA : rsrcB), \
+      [koff] "s"(koff_)
+  auto load = [&](int i, uint32_t base, uint32_t koff) {
+    asm volatile("s_add_u32 m0, %[base], %[row]\n\ts_nop 1\n\tbuffer_load_dwordx4 %[off], %[rsrc], %[koff] offen lds"
+                 : : SLP_LOAD_ARGS(i, base, koff) : "memory", "scc", "m0");
+  };
+  auto load_scales = [&](int group) {
+    const uint32_t at = lds_scale + (group & 1) * 2048, koff = (uint32_t)(group * 4 < nk ? group * 4 : 0);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 1\n\tbuffer_load_dword %1, %2, %3 offen lds" : : "s"(at), "v"(soffA), "s"(rsrcSA), "s"(koff) : "memory", "m0");
+    asm volatile("s_add_u32 m0, %0, 0x400\n\ts_nop 1\n\tbuffer_load_dword %1, %2, %3 offen lds" : : "s"(at), "v"(soffB), "s"(rsrcSB), "s"(koff) : "memory", "scc", "m0");
+  };
+  const uint32_t x0 = (uint32_t)((lgrp ^ ((lane >> 1) & 7)) << 4), x1 = x0 ^ 64;       // a lane's two pieces of a row
+  const uint32_t fa = (uint32_t)((wm * 128 + lrow) * 128), fb = (uint32_t)(A_BYTES + (wn * 128 + lrow) * 128);
+  const uint32_t fsa = (uint32_t)(kBigScales + (wm * 128 + lrow) * 4), fsb = (uint32_t)(kBigScales + (256 + wn * 128 + lrow) * 4);
+  auto scale_at = [&](int kt) {                  // k-tile nk takes the last one's: zeros times any scale of the row's own
+    const int k = kt < nk ? kt : nk - 1;
+    return (uint32_t)((k >> 2 & 1) * 2048 + (k & 3));
+  };
+  // pair m of a sub-step's fragments: strip m / 16; columns forwards, but backwards in strip 1, so that mostly one operand changes from one
+  // to the next
+  constexpr auto col_of = [](int m) { return m / 16 == 1 ? 7 - m % 16 / 2 : m % 16 / 2; };
+  constexpr auto row_of = [](int m) { return 2 * (m / 16) + ((m / 2 & 1) ? 1 - m % 2 : m % 2); };
+#define SLP_FENCE() __builtin_amdgcn_sched_barrier(0)
+#define SLP_BARRIER(cnt)                                            \
+  do {                                                              \
+    asm volatile("" ::: "memory");                                  \
+    __builtin_amdgcn_s_waitcnt(cnt);                                \
+    asm volatile("" ::: "memory");                                  \
+    __builtin_amdgcn_s_barrier();                                   \
+    asm volatile("" ::: "memory");                                  \
+  } while (0)
+  const int rowW = m0 + wm * 128, colW = n0 + wn * 128;
+  f32x4 bias[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) bias[j] = bias4(g, colW + j * 16 + 4 * lgrp);
+  // k-tiles 0 and 1 and the first group of scales; the last 4 loads of A's rows of k-tile 1 go out beside the first MFMAs
+  clip(0);
+  load_scales(0);
+  static_for<16>([&](auto i) { load(i, lds_wave, 0u); });
+  clip(1);
+  static_for<8>([&](auto i) { load(8 + i, lds_wave + STAGE, koff_of(1)); });
+
+  if constexpr (!EXACT) {
+  static_for<4>([&](auto i) { load(i, lds_wave + STAGE, koff_of(1)); });
+  i32x8 a[4], b[8];              // A fragments of strips with even and odd number, 2 each
+  int sa[4], sb[8];
+  auto bytes = [&](int stage, uint32_t at) {
+    const u32x4 lo = *(const u32x4*)(smem + stage * STAGE + at + x0), hi = *(const u32x4*)(smem + stage * STAGE + at + x1);
+    return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  };
+  auto read_a = [&](int kt, int f) {             // fragment f of the 8
+    const int r = f & 3;
+    a[r] = bytes(kt & 1, fa + f * 2048);
+    sa[r] = smem[fsa + scale_at(kt) + f * 64];
+  };
+  auto read_b = [&](int kt, int f) {
+    b[f] = bytes(kt & 1, fb + f * 2048);
+    sb[f] = smem[fsb + scale_at(kt) + f * 64];
+  };
+#define SLP_MFMA "v_mfma_scale_f32_16x16x128_f8f6f4 %[acc], %[b], %[a], %[acc], %[sb], %[sa] op_sel_hi:[0,0,0]"
+#define SLP_MFMA_ARGS(i, j) [b] "v"(b[j]), [a] "v"(a[(i) & 3]), [sb] "v"(sb[j]), [sa] "v"(sa[(i) & 3])
+  auto mma = [&](int i, int j) { asm volatile(SLP_MFMA : [acc] "+a"(acc[i][j]) : SLP_MFMA_ARGS(i, j)); };
+  // where the compiler may have touched a scale just before: an MFMA reads what a vector instruction wrote two instructions later at the earliest
+  auto mma_first = [&](int i, int j) { asm volatile("s_nop 1\n\t" SLP_MFMA : [acc] "+a"(acc[i][j]) : SLP_MFMA_ARGS(i, j)); };
+  auto mma_load = [&](int i, int j, int l, uint32_t base, uint32_t koff) {        // the MFMA is the wait state that m0 needs
+    asm volatile("s_add_u32 m0, %[base], %[row]\n\t" SLP_MFMA "\n\tbuffer_load_dwordx4 %[off], %[rsrc], %[koff] offen lds"
+                 : [acc] "+a"(acc[i][j]) : SLP_MFMA_ARGS(i, j), SLP_LOAD_ARGS(l, base, koff) : "memory", "scc", "m0");
+  };
+  // strip S of k-tile kt; loads go to k-tile kl
+  auto strip = [&](auto sc, int kt, int kl) {
+    constexpr int S = decltype(sc)::value;
+    const uint32_t base = lds_wave + (kl & 1) * STAGE, koff = koff_of(kl);
+    static_for<16>([&](auto pc) {
+      constexpr int p = decltype(pc)::value, m = 16 * S + p, i = row_of(m), j = col_of(m);
+      // fragments: A's of the next strip, B's and the first of A's of the next k-tile in strip 3
+      if constexpr (S < 3 && (p == 2 || p == 5)) read_a(kt, 2 * S + 2 + (p == 5));
+      if constexpr (S == 3 && (p == 1 || p == 3)) read_a(kt + 1, p == 3);
+      if constexpr (S == 3 && p % 3 == 2) read_b(kt + 1, p / 3);
+      if constexpr (S == 0 && p % 3 == 1 && p < 8) read_b(kt, 5 + p / 3);
+      constexpr int l = (S == 1 || S == 2) ? 8 + (S - 1) * 4 + p / 4 : (S == 3 ? 0 : 4) + p / 4;
+      if constexpr (p % 4 == 2) mma_load(i, j, l, base, koff);
+      else if constexpr (p < 2) mma_first(i, j);
+      else mma(i, j);
+      SLP_FENCE();
+    });
+  };
+  constexpr std::integral_constant<int, 0> s0{};
+  constexpr std::integral_constant<int, 1> s1{};
+  constexpr std::integral_constant<int, 2> s2{};
+  constexpr std::integral_constant<int, 3> s3{};
+
+  SLP_BARRIER(SLP_VMCNT(12));
+#pragma unroll
+  for (int f = 0; f < 5; ++f) read_b(0, f);
+  read_a(0, 0);
+  read_a(0, 1);
+  strip(s0, 0, 1);
+  for (int kt = 0; kt < nk; ++kt) {
+    SLP_BARRIER(0xC07F);                                   // X: every LDS read so far has returned
+    clip(kt + 2);
+    if ((kt & 3) == 0) load_scales(kt / 4 + 1);
+    SLP_FENCE();
+    strip(s1, kt, kt + 2);
+    strip(s2, kt, kt + 2);
+    SLP_BARRIER(SLP_VMCNT_LGKM0(8));                       // Y
+    strip(s3, kt, kt + 2);
+    strip(s0, kt + 1, kt + 2);                             // (of k-tile nk, too: all zeros)
+  }
+#undef SLP_MFMA
+#undef SLP_MFMA_ARGS
+  } else {
+  bf16x8 a[2][2][2], b[2][8][2];           // [strip's or sub-step's parity][fragment][32 k]
+  u32x4 rawa[2], rawb[2];
+  int sa[2], sb[2];
+  // bytes of fragment f of sub-step kk of k-tile kt
+  auto read_a = [&](int kt, int kk, int f) {
+    rawa[f & 1] = *(const u32x4*)(smem + (kt & 1) * STAGE + fa + f * 2048 + (kk ? x1 : x0));
+    sa[f & 1] = smem[fsa + scale_at(kt) + f * 64];
+  };
+  auto read_b = [&](int kt, int kk, int f) {
+    rawb[f & 1] = *(const u32x4*)(smem + (kt & 1) * STAGE + fb + f * 2048 + (kk ? x1 : x0));
+    sb[f & 1] = smem[fsb + scale_at(kt) + f * 64];
+  };
+  // conversion e of the 8 of a fragment: 2 values, with their scale (the instruction reads its exponent's bits)
+  auto convert = [&](const u32x4& raw, int scale, bf16x8 (&to)[2], auto ec) {
+    constexpr int e = decltype(ec)::value;
+    const bf16x2 v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[e / 2], __builtin_bit_cast(float, scale << 23), e % 2 == 1);
+    to[e / 4][2 * (e % 4)] = v[0];
+    to[e / 4][2 * (e % 4) + 1] = v[1];
+  };
+#define SLP_MFMA "v_mfma_f32_16x16x32_bf16 %[acc], %[b], %[a], %[acc]"
+#define SLP_MFMA_ARGS(kk, i, j, q) [b] "v"(b[kk][j][q]), [a] "v"(a[(i) / 2 & 1][(i) & 1][q])
+  auto mma = [&](int kk, int i, int j, int q) { asm volatile(SLP_MFMA : [acc] "+a"(acc[i][j]) : SLP_MFMA_ARGS(kk, i, j, q)); };
+  auto mma_load = [&](int kk, int i, int j, int q, int l, uint32_t base, uint32_t koff) {
+    asm volatile("s_add_u32 m0, %[base], %[row]\n\t" SLP_MFMA "\n\tbuffer_load_dwordx4 %[off], %[rsrc], %[koff] offen lds"
+                 : [acc] "+a"(acc[i][j]) : SLP_MFMA_ARGS(kk, i, j, q), SLP_LOAD_ARGS(l, base, koff) : "memory", "scc", "m0");
+  };
+  // Sub-step KK of k-tile kt.  MFMA p: pair p / 2, 32 k p % 2.
+  auto substep = [&](auto kc, int kt) {
+    constexpr int KK = decltype(kc)::value;
+    const int kn = KK ? kt + 1 : kt;               // k-tile of the next sub-step
+    const uint32_t base0 = lds_wave + ((kt & 1) ^ 1) * STAGE, koff0 = koff_of(kt + 1), base1 = lds_wave + (kt & 1) * STAGE, koff1 = koff_of(kt + 2);
+    static_for<128>([&](auto pc) {
+      constexpr int p = decltype(pc)::value, i = row_of(p / 2), j = col_of(p / 2), q = p % 2, S = p / 32;
+      if constexpr (KK == 1 && p == 0) SLP_BARRIER(SLP_VMCNT_LGKM0(0));            // Z
+      if constexpr (KK == 1 && p == 2) clip(kt + 2);
+      if constexpr (KK == 1 && p == 72) SLP_BARRIER(0xC07F);                       // X
+      // bytes: B's of the next sub-step, A's of the strip after the next (14 MFMAs ahead of the conversions)
+      if constexpr (p % 16 == 0) read_b(kn, KK ^ 1, p / 16);
+      if constexpr (p % 16 == 3 || p % 32 == 19) {
+        constexpr int f = 2 * S + (p % 32 == 19 ? 4 : 3);                          // fragments 3 .. 10: 8, 9 and 10 are the next sub-step's 0, 1 and 2
+        if constexpr (f < 8) read_a(kt, KK, f);
+        else read_a(kn, KK ^ 1, f - 8);
+      }
+      constexpr bool loads = KK == 1 ? (p >= 4 && p <= 60 && p % 8 == 4) || (p >= 76 && p % 8 == 4) : p == 4;
+      if constexpr (!loads) mma(KK, i, j, q);
+      else if constexpr (KK == 0) mma_load(KK, i, j, q, 7, base0, koff0);
+      else if constexpr (p <= 60) mma_load(KK, i, j, q, 8 + (p - 4) / 8, base1, koff1);
+      else mma_load(KK, i, j, q, (p - 76) / 8, base1, koff1);
+      if constexpr (p % 2 == 0) {
+        constexpr int at = p - 14 >= 0 ? p - 14 : p - 14 + 128, f = at / 16, e = at % 16 / 2;
+        if constexpr (p >= 14) convert(rawb[f & 1], sb[f & 1], b[KK ^ 1][f], std::integral_constant<int, e>{});
+        else convert(rawb[f & 1], sb[f & 1], b[KK][f], std::integral_constant<int, e>{});        // the current sub-step's last fragment
+      } else {
+        constexpr int f = p % 32 / 16, e = p % 16 / 2;
+        convert(rawa[f], sa[f], a[(S + 1) & 1][f], std::integral_constant<int, e>{});
+      }
+      SLP_FENCE();
+    });
+  };
+  constexpr std::integral_constant<int, 0> k0{};
+  constexpr std::integral_constant<int, 1> k1{};
+  static_for<7>([&](auto i) { load(i, lds_wave + STAGE, koff_of(1)); });
+  SLP_BARRIER(SLP_VMCNT(15));
+  // what a sub-step finds: B's fragments but the last one's conversions, the first strip of A's, the bytes of the fragment behind each
+  static_for<7>([&](auto f) {
+    read_b(0, 0, f);
+    static_for<8>([&](auto e) { convert(rawb[f & 1], sb[f & 1], b[0][f], e); });
+  });
+  read_b(0, 0, 7);
+  static_for<1>([&](auto) { convert(rawb[1], sb[1], b[0][7], std::integral_constant<int, 0>{}); });
+  static_for<2>([&](auto f) {
+    read_a(0, 0, f);
+    static_for<8>([&](auto e) { convert(rawa[f], sa[f], a[0][f], e); });
+  });
+  read_a(0, 0, 2);
+  SLP_FENCE();
+  for (int kt = 0; kt < nk; ++kt) {
+    if ((kt & 3) == 0) load_scales(kt / 4 + 1);
+    SLP_FENCE();
+    substep(k0, kt);
+    substep(k1, kt);
+  }
+  }
+  // the last zero fills have landed, and the matrix pipe is done with the accumulators (the compiler does not see MFMAs in assembly)
+  __builtin_amdgcn_s_waitcnt(SLP_VMCNT_LGKM0(0));
+  asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 64; ++i) asm volatile("" : "+a"(acc[i / 8][i % 8]));
+#undef SLP_FENCE
+#undef SLP_BARRIER
+#undef SLP_LOAD_ARGS
+#undef SLP_MFMA
+#undef SLP_MFMA_ARGS
+#pragma clang diagnostic pop
+
+  if constexpr (EXACT) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        asm volatile("" : "+a"(acc[i][j]));
+        store4(g, rowW + i * 16 + lrow, colW + j * 16 + 4 * lgrp, finished(g, acc[i][j], bias[j]));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    return;
+  }
+  // A wavefront stages its 128 x 128 outputs in a 32 KB of the stages that is its own, rows of 256 bytes whose 16-byte piece c sits at
+  // c ^ (row mod 16), and writes whole row segments.
+  __syncthreads();
+  unsigned char* const st = smem + w * 32768;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      asm volatile("" : "+a"(acc[i][j]));
+      const f32x4 v = finished(g, acc[i][j], bias[j]);
+      const bf16x4 o = {(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+      *(u32x2*)(st + (i * 16 + lrow) * 256 + (((2 * j + (lgrp >> 1)) ^ lrow) << 4) + (lgrp & 1) * 8) = __builtin_bit_cast(u32x2, o);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  const int c = lane & 15, n = colW + 8 * c;
+  if (n < g.N) {
+    bf16* const out = (bf16*)g.out + (int64_t)rowW * g.ldo + n;
+#pragma unroll
+    for (int b0 = 0; b0 < 32; b0 += 8) {
+      bf16x8 val[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int r = (b0 + q) * 4 + lgrp;
+        val[q] = *(const bf16x8*)(st + r * 256 + ((c ^ (r & 15)) << 4));
+      }
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int r = (b0 + q) * 4 + lgrp;
+        if (rowW + r < g.M) {
+          if (n + 8 <= g.N) ((AnyBf16x8*)(out + r * g.ldo))->v = val[q];
+          else
+            for (int e = 0; e < g.N - n; ++e) out[r * g.ldo + e] = val[q][e];
+        }
+      }
+    }
+  }
+#endif
+}
+
 // The parts of a split contraction added up in order, then bias, ReLU and rounding.
 __global__ __launch_bounds__(256) void join_kernel(const ProductArgs g, int parts) {
   const int quads = (g.N + 3) / 4;
@@ -263,6 +619,24 @@ hipError_t launch_tile(const ProductArgs& g, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <bool EXACT>
+hipError_t configure_long() {
+  static std::once_flag once;
+  static hipError_t result = hipSuccess;
+  std::call_once(once, [] { result = hipFuncSetAttribute((const void*)product_long_kernel<EXACT>, hipFuncAttributeMaxDynamicSharedMemorySize, kBigSmem); });
+  return result;
+}
+template <bool EXACT>
+hipError_t launch_long(const ProductArgs& g, hipStream_t s) {
+  hipError_t e = configure_long<EXACT>();
+  if (e != hipSuccess) return e;
+  product_long_kernel<EXACT><<<(unsigned)(((g.M + 255) / 256) * ((g.N + 255) / 256)), 256, kBigSmem, s>>>(g);
+  return hipGetLastError();
+}
+
+// 256x256 tiles where they keep most of the 256 compute units busy.
+bool big_tiles(int M, int N) { return (int64_t)((M + 255) / 256) * ((N + 255) / 256) >= 192; }
+
 bool wide_tiles(int M, int N) { return (int64_t)((M + 127) / 128) * ((N + 127) / 128) >= 192; }
 
 }  // namespace
@@ -273,6 +647,7 @@ size_t product_floats(int M, int N, int K) {
 }
 
 hipError_t launch_product(const ProductArgs& g, hipStream_t s) {
+  if (big_tiles(g.M, g.N) && g.K > 0) return g.out_dtype == 0 ? launch_long<true>(g, s) : launch_long<false>(g, s);
   const bool wide = wide_tiles(g.M, g.N);
   if (g.out_dtype == 0) return wide ? launch_tile<128, 128, 2, true>(g, s) : launch_tile<64, 64, 4, true>(g, s);
   return wide ? launch_tile<128, 128, 2, false>(g, s) : launch_tile<64, 64, 4, false>(g, s);
@@ -282,6 +657,8 @@ hipError_t product_configure_all() {
   hipError_t e = configure_tile<128, 128, 2, false>();
   if (e == hipSuccess) e = configure_tile<64, 64, 4, false>();
   if (e == hipSuccess) e = configure_tile<128, 128, 2, true>();
+  if (e == hipSuccess) e = configure_long<false>();
+  if (e == hipSuccess) e = configure_long<true>();
   return e == hipSuccess ? configure_tile<64, 64, 4, true>() : e;
 }
 
