@@ -104,7 +104,123 @@ hipError_t rmsnorm_of(const NormArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// ---- backward, any width: the rows' products first, then the columns --------------------------------------------------------
+// ---- backward: rows dealt out to teams of WAVES wavefronts, gamma and the sums for its gradient in registers, each lane CH chunks ----
+template <typename T> struct Raw;
+template <> struct Raw<bf16> { bf16x8 v; };
+template <> struct Raw<float> { f32x4 v[2]; };
+__device__ __forceinline__ void fetch8(const bf16* p, int n, Raw<bf16>& r) {
+  if (n >= 8) r.v = ((const AnyBf16x8*)p)->v;
+  else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r.v[j] = j < n ? p[j] : (bf16)0.0f;
+  }
+}
+__device__ __forceinline__ void fetch8(const float* p, int n, Raw<float>& r) {
+  if (n >= 8) {
+    r.v[0] = ((const AnyF32x4*)p)->v;
+    r.v[1] = ((const AnyF32x4*)(p + 4))->v;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r.v[j / 4][j % 4] = j < n ? p[j] : 0.0f;
+  }
+}
+__device__ __forceinline__ float item(const Raw<bf16>& r, int j) { return (float)r.v[j]; }
+__device__ __forceinline__ float item(const Raw<float>& r, int j) { return r.v[j / 4][j % 4]; }
+
+// One reading of everything: a row waits in registers for its product, while the next row's loads are under way (AHEAD).
+template <typename T, int WAVES, int CH, bool AHEAD>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_backward_kernel(const NormBackArgs a, float* __restrict__ partials) {
+  constexpr int TEAM = WAVES * 64, TEAMS = WAVES == 1 ? 4 : 1;
+  __shared__ float part[2][WAVES];
+  __shared__ float sums[WAVES == 1 ? 4 : 1][WAVES == 1 ? CH * 512 : 1];
+  const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, team = WAVES == 1 ? threadIdx.x >> 6 : 0;
+  const int D = a.dim, step = gridDim.x * TEAMS;
+  const float over = 1.0f / (float)D;
+  float g[CH][8], acc[CH][8];
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int c = 8 * (i * TEAM + t);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      g[i][j] = 1.0f;
+      acc[i][j] = 0.0f;
+    }
+    if (a.gamma) load8(a.gamma + c, D - c, g[i]);
+  }
+  Raw<T> y[CH], x[CH], d[CH];
+  auto fetch = [&](int64_t row, Raw<T>(&y)[CH], Raw<T>(&x)[CH], Raw<T>(&d)[CH]) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int c = 8 * (i * TEAM + t);
+      fetch8((const T*)a.dy + row * a.lddy + c, D - c, y[i]);
+      fetch8((const T*)a.h + row * a.ldh + c, D - c, x[i]);
+      if (a.dh) fetch8((const T*)a.dh + row * a.lddh + c, D - c, d[i]);
+    }
+  };
+  int64_t row = (int64_t)blockIdx.x * TEAMS + team;
+  if (AHEAD && row < a.rows) fetch(row, y, x, d);
+  for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
+    if (!AHEAD) fetch(row, y, x, d);
+    const float n = a.rstd[row];
+    float dot = 0.0f;
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float yx = item(y[i], j) * item(x[i], j);
+        dot += g[i][j] * yx;
+        acc[i][j] += yx * n;
+      }
+    Raw<T> y2[CH], x2[CH], d2[CH];
+    if (AHEAD && row + step < a.rows) fetch(row + step, y2, x2, d2);
+    dot = sum_of_64(dot);
+    if (WAVES > 1) {
+      if ((t & 63) == 0) part[turn][t >> 6] = dot;
+      __syncthreads();
+      dot = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) dot += part[turn][w];
+    }
+    const float k = dot * over * n * n * n;          // (in this order nothing leaves the range that the result stays in)
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int c = 8 * (i * TEAM + t);
+      float o[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        o[j] = n * (g[i][j] * item(y[i], j)) - item(x[i], j) * k;
+        if (a.dh) o[j] += item(d[i], j);
+      }
+      store8((T*)a.dx + row * a.lddx + c, D - c, o);
+    }
+    if (AHEAD) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        y[i] = y2[i];
+        x[i] = x2[i];
+        d[i] = d2[i];
+      }
+    }
+  }
+  if (!a.dgamma) return;
+  if (WAVES == 1) {                    // the four teams' sums in order
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sums[team][8 * (i * TEAM + t) + j] = acc[i][j];
+    __syncthreads();
+    for (int c = threadIdx.x; c < D; c += 256)
+      partials[(int64_t)blockIdx.x * D + c] = (sums[0][c] + sums[WAVES == 1 ? 1 : 0][c]) + (sums[WAVES == 1 ? 2 : 0][c] + sums[WAVES == 1 ? 3 : 0][c]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int c = 8 * (i * TEAM + t);
+      store8(partials + (int64_t)blockIdx.x * D + c, D - c, acc[i]);
+    }
+  }
+}
+
+// ---- backward, rows past 16384: the rows' products first, then the columns --------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(256) void rmsnorm_dots_kernel(const NormBackArgs a, float* dots) {
   __shared__ float part[4];
@@ -157,41 +273,66 @@ __global__ __launch_bounds__(256) void rmsnorm_columns_kernel(const NormBackArgs
   if (a.dgamma) store8(partials + (int64_t)blockIdx.y * a.dim + c, left, acc);
 }
 
-int column_groups(int rows) { return rows < 256 ? rows : 256; }
+constexpr int kOnePass = 16384;       // longest row that a workgroup's registers hold
+
+// Partial sums of gamma's gradient: workgroups of the one-pass kernel, or strands of rows.
+int backward_groups(int rows, int dim) {
+  const int teams = dim <= 1024 ? (rows + 3) / 4 : rows, most = dim <= 1024 ? 1024 : dim <= 4096 ? 512 : 256;
+  return teams < most ? teams : most;
+}
 
 template <typename T>
 hipError_t rmsnorm_backward_of(const NormBackArgs& a, hipStream_t s) {
-  float *dots = a.work, *partials = a.work + (a.rows + 3) / 4 * 4;
-  rmsnorm_dots_kernel<T><<<a.rows, 256, 0, s>>>(a, dots);
-  const int groups = column_groups(a.rows);
-  rmsnorm_columns_kernel<T><<<dim3((a.dim + 2047) / 2048, groups), 256, 0, s>>>(a, dots, partials);
+  constexpr bool narrow = sizeof(T) == 2;
+  const int groups = backward_groups(a.rows, a.dim);
+  float* partials = a.work;
+  if (a.dim <= 512) rmsnorm_backward_kernel<T, 1, 1, true><<<groups, 256, 0, s>>>(a, partials);
+  else if (a.dim <= 1024) rmsnorm_backward_kernel<T, 1, 2, true><<<groups, 256, 0, s>>>(a, partials);
+  else if (a.dim <= 2048) rmsnorm_backward_kernel<T, 4, 1, true><<<groups, 256, 0, s>>>(a, partials);
+  else if (a.dim <= 4096) rmsnorm_backward_kernel<T, 4, 2, true><<<groups, 256, 0, s>>>(a, partials);
+  else if (a.dim <= 8192) rmsnorm_backward_kernel<T, 8, 2, true><<<groups, 512, 0, s>>>(a, partials);
+  else if (a.dim <= kOnePass) rmsnorm_backward_kernel<T, 8, 4, narrow><<<groups, 512, 0, s>>>(a, partials);
+  else {
+    float* dots = a.work;
+    partials = a.work + (a.rows + 3) / 4 * 4;
+    rmsnorm_dots_kernel<T><<<a.rows, 256, 0, s>>>(a, dots);
+    rmsnorm_columns_kernel<T><<<dim3((a.dim + 2047) / 2048, groups), 256, 0, s>>>(a, dots, partials);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.dgamma) return e;
   return launch_sum_rows(partials, groups, a.dim, a.dgamma, s);
 }
 
-// One column a thread of 64, 4 strands of rows.
-__global__ __launch_bounds__(256) void sum_rows_kernel(const float* __restrict__ in, int n, int cols, float* __restrict__ out) {
-  __shared__ float part[4][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), strand = threadIdx.x >> 6;
+// 32 columns (a line) and 32 strands of rows a workgroup.
+__global__ __launch_bounds__(1024) void sum_rows_kernel(const float* __restrict__ in, int n, int cols, float* __restrict__ out) {
+  __shared__ float part[32][33];
+  const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   float sum = 0.0f;
-  if (c < cols)
-    for (int i = strand; i < n; i += 4) sum += in[(int64_t)i * cols + c];
-  part[strand][threadIdx.x & 63] = sum;
+  if (c < cols) {
+#pragma unroll 8
+    for (int i = strand; i < n; i += 32) sum += in[(int64_t)i * cols + c];
+  }
+  part[strand][lane] = sum;
   __syncthreads();
-  if (strand == 0 && c < cols) out[c] = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+  // strand s of column c: lane s of the 32 that add column c up
+  sum = part[lane][strand];
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 32);
+  if (lane == 0 && blockIdx.x * 32 + strand < cols) out[blockIdx.x * 32 + strand] = sum;
 }
 
 }  // namespace
 
 hipError_t launch_sum_rows(const float* in, int n, int cols, float* out, hipStream_t s) {
-  sum_rows_kernel<<<(cols + 63) / 64, 256, 0, s>>>(in, n, cols, out);
+  sum_rows_kernel<<<(cols + 31) / 32, 1024, 0, s>>>(in, n, cols, out);
   return hipGetLastError();
 }
 
 hipError_t launch_rmsnorm(int dtype, const NormArgs& a, hipStream_t s) { return dtype == 1 ? rmsnorm_of<bf16>(a, s) : rmsnorm_of<float>(a, s); }
 
-size_t rmsnorm_backward_floats(int rows, int dim) { return (size_t)((rows + 3) / 4 * 4) + (size_t)column_groups(rows) * dim; }
+size_t rmsnorm_backward_floats(int rows, int dim) {
+  return (dim > kOnePass ? (size_t)((rows + 3) / 4 * 4) : 0) + (size_t)backward_groups(rows, dim) * dim;
+}
 
 hipError_t launch_rmsnorm_backward(int dtype, const NormBackArgs& a, hipStream_t s) {
   return dtype == 1 ? rmsnorm_backward_of<bf16>(a, s) : rmsnorm_backward_of<float>(a, s);
