@@ -217,6 +217,81 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const ProductArgs g, 
 #endif
 }
 
+// Few rows (a request's, a short last batch): bound by reading B once.  A workgroup takes 16 rows of B, its wavefronts take turns along the
+// contraction, STEP k-tiles at a time whose loads are all under way together, from memory straight into the fragments' registers; the parts are
+// added up in the order of the wavefronts.  MF fragments of 16 rows of A.  Both output types take the exact form: the conversions hide behind
+// the loads.  Microseconds on the device, this kernel / tiles with a split contraction and a second launch that joins the parts: 1 x 4096 x
+// 4096 5.2 / 8.4 (16.8 MB from caches at 6 TB/s behind 2.5 us of launch and latency), 1 x 16384 x 16384 47.5 / 50.8 (5.7 TB/s), 16 x 4096 x 4096
+// 7.1 / 9.0, 64 x 1024 x 1024 5.4 / 6.9.  32 rows of B a workgroup, which halves the reading of A: 7.0, 52.1, 9.0, -.
+template <int MF, int STEP>
+__global__ __launch_bounds__(1024) void product_rows_kernel(const ProductArgs g) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, waves = blockDim.x >> 6, lgrp = lane >> 4, lrow = lane & 15;
+  const int n0 = blockIdx.x * 16, nk = (g.K + 127) / 128, Kr = (g.K + 15) & ~15;
+  const int ra = g.M < 16 * MF ? g.M : 16 * MF, rb = g.N - n0 < 16 ? g.N - n0 : 16;
+  const int sfirst = n0 >> g.shift_b, sblocks = ((n0 + rb - 1) >> g.shift_b) - sfirst;
+  const __amdgpu_buffer_rsrc_t rsrcA = rsrc_of(g.a, (ra - 1) * g.lda + Kr), rsrcB = rsrc_of(g.b + n0 * g.ldb, (rb - 1) * g.ldb + Kr);
+  const __amdgpu_buffer_rsrc_t rsrcSA = rsrc_of(g.sa, ((ra - 1) >> g.shift_a) * g.ldsa + nk), rsrcSB = rsrc_of(g.sb + sfirst * g.ldsb, sblocks * g.ldsb + nk);
+  // rows past the end read as zeros, under a scale of zero
+  uint32_t oa[MF], osa[MF];
+#pragma unroll
+  for (int i = 0; i < MF; ++i) {
+    const int m = 16 * i + lrow;
+    oa[i] = m < ra ? (uint32_t)(m * g.lda + lgrp * 16) : kOutOfRange;
+    osa[i] = m < ra ? (uint32_t)((m >> g.shift_a) * g.ldsa) : kOutOfRange;
+  }
+  const uint32_t ob = lrow < rb ? (uint32_t)(lrow * g.ldb + lgrp * 16) : kOutOfRange;
+  const uint32_t osb = lrow < rb ? (uint32_t)((((n0 + lrow) >> g.shift_b) - sfirst) * g.ldsb) : kOutOfRange;
+  f32x4 acc[MF];
+#pragma unroll
+  for (int i = 0; i < MF; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  auto sixteen = [&](__amdgpu_buffer_rsrc_t r, uint32_t row, int k) {       // bytes k + 16 lgrp .. of a row, zeros past K
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, k + lgrp * 16 < Kr ? row + (uint32_t)k : kOutOfRange, 0, 0));
+  };
+  auto piece = [&](__amdgpu_buffer_rsrc_t r, uint32_t row, int kt) {
+    const u32x4 lo = sixteen(r, row, kt * 128), hi = sixteen(r, row, kt * 128 + 64);
+    return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  };
+  auto scale = [&](__amdgpu_buffer_rsrc_t r, uint32_t row, int kt) {        // (past the end: the last one, for zeros)
+    return (int)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, row + (uint32_t)(kt < nk ? kt : nk - 1), 0, 0);
+  };
+  for (int k0 = w * STEP; k0 < nk; k0 += waves * STEP) {
+    i32x8 vb[STEP], va[STEP][MF];
+    int sb[STEP], sa[STEP][MF];
+#pragma unroll
+    for (int s = 0; s < STEP; ++s) {
+      vb[s] = piece(rsrcB, ob, k0 + s);
+      sb[s] = scale(rsrcSB, osb, k0 + s);
+#pragma unroll
+      for (int i = 0; i < MF; ++i) {
+        va[s][i] = piece(rsrcA, oa[i], k0 + s);
+        sa[s][i] = scale(rsrcSA, osa[i], k0 + s);
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < STEP; ++s) {
+      Fragment<true> b, a;
+      b.set(vb[s], sb[s]);
+#pragma unroll
+      for (int i = 0; i < MF; ++i) {
+        a.set(va[s][i], sa[s][i]);
+        acc[i] = mma(b, a, acc[i]);
+      }
+    }
+  }
+  f32x4* const part = (f32x4*)smem;
+#pragma unroll
+  for (int i = 0; i < MF; ++i) part[(i * waves + w) * 64 + lane] = acc[i];
+  __syncthreads();
+  for (int i = w; i < MF; i += waves) {
+    f32x4 sum = part[i * waves * 64 + lane];
+    for (int v = 1; v < waves; ++v) sum += part[(i * waves + v) * 64 + lane];
+    store4(g, 16 * i + lrow, n0 + 4 * lgrp, finished(g, sum, bias4(g, n0 + 4 * lgrp)));
+  }
+#endif
+}
+
 // f(0), f(1), ... f(N - 1) with the index as a constant.
 template <typename F, int... I>
 __device__ __forceinline__ void static_for_impl(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
@@ -637,16 +712,38 @@ hipError_t launch_long(const ProductArgs& g, hipStream_t s) {
 // 256x256 tiles where they keep most of the 256 compute units busy.
 bool big_tiles(int M, int N) { return (int64_t)((M + 255) / 256) * ((N + 255) / 256) >= 192; }
 
+// Whether a product runs on product_rows_kernel.  Its workgroups read A as often as there are 16 rows of B, and a compute unit reads 16 rows in 0.7 us
+// per 1024 k (1.2 with 16 rows of A, 3 with 64); tiles take a second launch, 3.5 us, unless they are enough not to split the contraction.
+// Microseconds, this / tiles: 1 x 2048 x 8192 8.1 / 9.2, 1 x 1000 x 16384 15.6 / 12.3, 1 x 8192 x 8192 13.4 / 15.8, 8 x 16384 x 16384 58 / 51, 16 x 4096 x 4096
+// 7.1 / 9.0, 16 x 512 x 8192 11.3 / 11.0, 32 x 4096 x 4096 9.9 / 9.5, 32 x 4096 x 1024 4.1 / 7.1, 64 x 4096 x 1024 5.5 / 7.7, 64 x 512 x 4096 15.3 / 8.8,
+// and against tiles in one launch 16 x 16384 x 1024 6.3 / 5.8, 32 x 16384 x 512 5.6 / 4.9.
+bool few_rows(int M, int N, int K) {
+  if (M <= 4) return K <= 8192 || N >= 4096;
+  return M <= 64 && (int64_t)M * K <= 65536 && (N + 63) / 64 < 192;
+}
+
 bool wide_tiles(int M, int N) { return (int64_t)((M + 127) / 128) * ((N + 127) / 128) >= 192; }
 
 }  // namespace
 
 size_t product_floats(int M, int N, int K) {
+  if (few_rows(M, N, K) || big_tiles(M, N)) return 0;
   const int t = wide_tiles(M, N) ? 128 : 64, parts = parts_of(M, N, K, t, t);
   return parts > 1 ? (size_t)parts * M * ((N + 3) & ~3) : 0;
 }
 
+template <int MF, int STEP>
+hipError_t launch_rows(const ProductArgs& g, hipStream_t s) {
+  const int steps = ((g.K + 127) / 128 + STEP - 1) / STEP, waves = steps > 16 ? 16 : steps > 1 ? steps : 1;
+  product_rows_kernel<MF, STEP><<<(unsigned)((g.N + 15) / 16), waves * 64, MF * waves * 1024, s>>>(g);
+  return hipGetLastError();
+}
+
 hipError_t launch_product(const ProductArgs& g, hipStream_t s) {
+  if (few_rows(g.M, g.N, g.K)) {
+    if (g.M <= 16) return launch_rows<1, 2>(g, s);
+    return g.M <= 32 ? launch_rows<2, 2>(g, s) : launch_rows<4, 1>(g, s);
+  }
   if (big_tiles(g.M, g.N) && g.K > 0) return g.out_dtype == 0 ? launch_long<true>(g, s) : launch_long<false>(g, s);
   const bool wide = wide_tiles(g.M, g.N);
   if (g.out_dtype == 0) return wide ? launch_tile<128, 128, 2, true>(g, s) : launch_tile<64, 64, 4, true>(g, s);

@@ -72,9 +72,9 @@ def test_product():
     refused(ALLOC, product(ldsa=6), b"4-byte")
     refused(ALLOC, product(out=P + 1), b"element")
     refused(ALLOC, product(bias=P + 2), b"bias")
-    need = api.lib().slp_product_workspace_bytes(4, 64, 16384)
+    need = api.lib().slp_product_workspace_bytes(100, 64, 16384)
     assert need > 0
-    big = dict(m=4, n=64, k=16384, lda=16384, ldb=16384, ldsa=128, ldsb=128, ldo=64)
+    big = dict(m=100, n=64, k=16384, lda=16384, ldb=16384, ldsa=128, ldsb=128, ldo=64)
     refused(ALLOC, product(**big, size=need - 1), b"workspace")
     refused(ALLOC, product(**big, work=None), b"workspace")
     assert product(m=0) == 0 and product(n=0, ldo=0) == 0
