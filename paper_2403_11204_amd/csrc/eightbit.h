@@ -65,7 +65,6 @@ struct ProductArgs {
 };
 size_t product_floats(int M, int N, int K);
 hipError_t launch_product(const ProductArgs& a, hipStream_t s);
-hipError_t product_configure_all();
 
 constexpr int kClipTensors = 48;      // a launch takes (kernel arguments)
 struct ClipTable {

@@ -114,7 +114,8 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const ProductArgs g, 
   constexpr int A_BYTES = BM * 128, DATA = (BM + BN) * 128, STAGE = DATA + 4 * 256;      // + a dword of scales for each row
   constexpr int LA = BM / 32, LB = BN / 32, NLD = LA + LB + 1;                           // loads a lane per k-tile
   constexpr int MI = BM / 32, NI = BN / 32;
-  static_assert(BM + BN <= 256, "one load of scales per wavefront");
+  constexpr int AW = (BM + 63) / 64, BW = (BN + 63) / 64;                                // wavefronts that load A's and B's scales
+  static_assert(AW + BW <= 4, "one load of scales per wavefront");
   const int tilesM = (g.M + BM - 1) / BM, tilesN = (g.N + BN - 1) / BN, total = tilesM * tilesN;
   int tid;
   {
@@ -140,13 +141,13 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const ProductArgs g, 
 #pragma unroll
   for (int i = 0; i < LB; ++i) voff[LA + i] = prow + 32 * i < rb ? (uint32_t)((prow + 32 * i) * g.ldb + chunk * 16) : kOutOfRange;
   // scales: wavefront w loads the dwords that hold a k-tile's scales for 64 of the tile's rows, A's and then B's
-  const bool sA = 64 * w < BM;
-  const int srow = 64 * w + lane - (sA ? 0 : BM);
+  const bool sA = w < AW;
+  const int srow = 64 * (sA ? w : w - AW) + lane;
   const int sm = sA ? m0 : n0, sshift = sA ? g.shift_a : g.shift_b, sfirst = sm >> sshift;
   const int64_t slds = sA ? g.ldsa : g.ldsb;
   const int slast = ((sm + (sA ? ra : rb) - 1) >> sshift) - sfirst;
   const __amdgpu_buffer_rsrc_t rsrcS = rsrc_of((sA ? g.sa : g.sb) + sfirst * slds, slast * slds + ((nk + 3) & ~3));
-  const uint32_t soff = srow < (sA ? ra : rb) && srow >= 0 ? (uint32_t)((((sm + srow) >> sshift) - sfirst) * slds) : kOutOfRange;
+  const uint32_t soff = srow < (sA ? ra : rb) ? (uint32_t)((((sm + srow) >> sshift) - sfirst) * slds) : kOutOfRange;
 
   typedef __attribute__((address_space(3))) void* lds_ptr_t;
   const int lds_wave = __builtin_amdgcn_readfirstlane(w * 1024), lds_scale = __builtin_amdgcn_readfirstlane(DATA + w * 256);
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const ProductArgs g, 
   };
   const uint32_t fragA = (uint32_t)((wm * (BM / 2) + lrow) * 128), fragB = (uint32_t)(A_BYTES + (wn * (BN / 2) + lrow) * 128);
   const uint32_t x0 = (uint32_t)((lgrp ^ ((lane >> 1) & 7)) << 4), x1 = x0 ^ 64;
-  const uint32_t scaleA = (uint32_t)(DATA + (wm * (BM / 2) + lrow) * 4), scaleB = (uint32_t)(DATA + (BM + wn * (BN / 2) + lrow) * 4);
+  const uint32_t scaleA = (uint32_t)(DATA + (wm * (BM / 2) + lrow) * 4), scaleB = (uint32_t)(DATA + AW * 256 + (wn * (BN / 2) + lrow) * 4);
 
   f32x4 acc[MI][NI];
 #pragma unroll
@@ -660,60 +661,14 @@ __global__ __launch_bounds__(256) void join_kernel(const ProductArgs g, int part
   store4(g, m, n, finished(g, sum, bias4(g, n)));
 }
 
-template <int BM, int BN, int NS, bool EXACT>
-hipError_t configure_tile() {
-  static std::once_flag once;
-  static hipError_t result = hipSuccess;
-  std::call_once(once, [] {
-    result = hipFuncSetAttribute((const void*)product_tile_kernel<BM, BN, NS, EXACT>, hipFuncAttributeMaxDynamicSharedMemorySize, NS * ((BM + BN) * 128 + 1024));
-  });
-  return result;
-}
+// ---- host side -------------------------------------------------------------------------------
+int64_t tiles_of(int M, int N, int BM, int BN) { return (int64_t)((M + BM - 1) / BM) * ((N + BN - 1) / BN); }
 
-// Parts of the contraction: as many as give each of the 256 compute units a workgroup, of 4 k-tiles at least.
-int parts_of(int M, int N, int K, int BM, int BN) {
-  const int64_t tiles = (int64_t)((M + BM - 1) / BM) * ((N + BN - 1) / BN);
-  const int nk = (K + 127) / 128;
-  int64_t parts = tiles >= 192 ? 1 : 256 / tiles;
-  if (parts > nk / 4) parts = nk / 4;
-  return parts < 1 ? 1 : (int)parts;
-}
+// Which kernel a product runs on.
+enum Shape { kRows, kBig, k128, k128x64, k64, k32x64, k32, kSplit };
 
-template <int BM, int BN, int NS, bool EXACT>
-hipError_t launch_tile(const ProductArgs& g, hipStream_t s) {
-  hipError_t e = configure_tile<BM, BN, NS, EXACT>();
-  if (e != hipSuccess) return e;
-  const unsigned tiles = (unsigned)(((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN));
-  const int nk = (g.K + 127) / 128, wanted = parts_of(g.M, g.N, g.K, BM, BN);
-  const int kper = nk > wanted ? (nk + wanted - 1) / wanted : 1, parts = nk > 1 ? (nk + kper - 1) / kper : 1;
-  hipLaunchKernelGGL((product_tile_kernel<BM, BN, NS, EXACT>), dim3(tiles, parts), dim3(256), NS * ((BM + BN) * 128 + 1024), s, g, kper);
-  e = hipGetLastError();
-  if (e != hipSuccess || parts == 1) return e;
-  const int64_t quads = (int64_t)g.M * ((g.N + 3) / 4);
-  join_kernel<<<(unsigned)((quads + 255) / 256), 256, 0, s>>>(g, parts);
-  return hipGetLastError();
-}
-
-template <bool EXACT>
-hipError_t configure_long() {
-  static std::once_flag once;
-  static hipError_t result = hipSuccess;
-  std::call_once(once, [] { result = hipFuncSetAttribute((const void*)product_long_kernel<EXACT>, hipFuncAttributeMaxDynamicSharedMemorySize, kBigSmem); });
-  return result;
-}
-template <bool EXACT>
-hipError_t launch_long(const ProductArgs& g, hipStream_t s) {
-  hipError_t e = configure_long<EXACT>();
-  if (e != hipSuccess) return e;
-  product_long_kernel<EXACT><<<(unsigned)(((g.M + 255) / 256) * ((g.N + 255) / 256)), 256, kBigSmem, s>>>(g);
-  return hipGetLastError();
-}
-
-// 256x256 tiles where they keep most of the 256 compute units busy.
-bool big_tiles(int M, int N) { return (int64_t)((M + 255) / 256) * ((N + 255) / 256) >= 192; }
-
-// Whether a product runs on product_rows_kernel.  Its workgroups read A as often as there are 16 rows of B, and a compute unit reads 16 rows in 0.7 us
-// per 1024 k (1.2 with 16 rows of A, 3 with 64); tiles take a second launch, 3.5 us, unless they are enough not to split the contraction.
+// Whether it is product_rows_kernel.  Its workgroups read A as often as there are 16 rows of B, and a compute unit reads 16 rows in 0.7 us per
+// 1024 k (1.2 with 16 rows of A, 3 with 64); tiles with a split contraction take a second launch, 3.5 us.
 // Microseconds, this / tiles: 1 x 2048 x 8192 8.1 / 9.2, 1 x 1000 x 16384 15.6 / 12.3, 1 x 8192 x 8192 13.4 / 15.8, 8 x 16384 x 16384 58 / 51, 16 x 4096 x 4096
 // 7.1 / 9.0, 16 x 512 x 8192 11.3 / 11.0, 32 x 4096 x 4096 9.9 / 9.5, 32 x 4096 x 1024 4.1 / 7.1, 64 x 4096 x 1024 5.5 / 7.7, 64 x 512 x 4096 15.3 / 8.8,
 // and against tiles in one launch 16 x 16384 x 1024 6.3 / 5.8, 32 x 16384 x 512 5.6 / 4.9.
@@ -722,14 +677,60 @@ bool few_rows(int M, int N, int K) {
   return M <= 64 && (int64_t)M * K <= 65536 && (N + 63) / 64 < 192;
 }
 
-bool wide_tiles(int M, int N) { return (int64_t)((M + 127) / 128) * ((N + 127) / 128) >= 192; }
+// All microseconds on the device, operands in the caches.  256x256 tiles where they keep most of the 256 compute units busy, sooner with a bf16
+// output, whose k-tiles are half as long: 1700 x 6000 x 2000 (168 tiles) 28.7 against 37.5 on smaller ones, 3000 x 3000 x 1000 (144) 20.4 / 20.1, 2048 x
+// 4096 x 4096 (128) 45 / 39; float32 3000 x 3000 x 1000 33.6 / 28.8, 2472 x 4096 x 2700 (160) 65.3 / 65.3.
+// A long contraction on few tiles is split: 714 x 174 x 4096 10.5 in 4 parts, 12.5 on 32x32 tiles in one; 1000 x 512 x 8192 20.6 / 29; 451 x 453 x 4096
+// 10.0 / 10.6; but 192 x 128 x 2048 7.5 / 7.5 and below that one launch is faster.
+// Otherwise the smallest tiles that leave each compute unit one workgroup: 32x32 against 32x64 and 64x64 on 226 x 679 x 837 (176 tiles) 4.5 / 5.1 / 5.8, 462 x 1024 x
+// 146 (480) 4.0 / 3.8 / 4.2, 618 x 1341 x 256 (840) 5.4 / 4.5 / 4.4.  Larger ones as soon as they fill the chip, of which a compute unit holds 4 (64x64), 3
+// (128x64) and 2 (128x128): 64x64 against 128x64 on 491 x 5192 x 24 (328 of the latter) 6.3 / 7.0, 392 x 4096 x 540 (256) 7.8 / 8.5, 436 x 8192 x 2512 (512) 20.1 /
+// 16.6; 128x64 against 128x128 on 2048 x 4096 x 1024 (512 of the latter) 18.1 / 15.9, 1024 x 8192 x 8192 (512) 102 / 69, 3000 x 3000 x 1000 float32 (576)
+// 28.8 / 32.9, 440 x 10342 x 324 (324) 8.6 / 10.5.
+Shape shape_of(int M, int N, int K, int dtype) {
+  const int nk = (K + 127) / 128;
+  if (few_rows(M, N, K)) return kRows;
+  if (K > 0 && tiles_of(M, N, 256, 256) >= (dtype == 1 ? 144 : 192)) return kBig;
+  if (nk >= 28 && tiles_of(M, N, 64, 64) <= 256) return kSplit;
+  if (tiles_of(M, N, 32, 32) <= 256) return k32;
+  if (tiles_of(M, N, 32, 64) <= 256) return k32x64;
+  if (tiles_of(M, N, 128, 64) < 480) return k64;
+  const int64_t t128 = tiles_of(M, N, 128, 128);
+  return t128 >= 384 && t128 <= 512 && nk >= 4 ? k128 : k128x64;
+}
 
-}  // namespace
+// Parts of a split contraction: two workgroups for each compute unit, 8 k-tiles at least (1000 x 512 x 8192, 128 tiles, in 2, 4 and 8 parts 22.7, 20.6, 23.0
+// us; 64 x 64 x 16384 in 8 12.0).
+int parts_of(int M, int N, int K) {
+  const int64_t t = 512 / tiles_of(M, N, 64, 64);
+  const int most = (K + 127) / 128 / 8;
+  return t < most ? (int)t : most;
+}
 
-size_t product_floats(int M, int N, int K) {
-  if (few_rows(M, N, K) || big_tiles(M, N)) return 0;
-  const int t = wide_tiles(M, N) ? 128 : 64, parts = parts_of(M, N, K, t, t);
-  return parts > 1 ? (size_t)parts * M * ((N + 3) & ~3) : 0;
+template <int BM, int BN, int NS, bool EXACT>
+hipError_t launch_tile(const ProductArgs& g, int wanted, hipStream_t s) {
+  constexpr int smem = NS * ((BM + BN) * 128 + 1024);
+  static std::once_flag once;          // one attribute call per instantiation, also when two host threads launch first together
+  static hipError_t result = hipSuccess;
+  std::call_once(once, [] { result = hipFuncSetAttribute((const void*)product_tile_kernel<BM, BN, NS, EXACT>, hipFuncAttributeMaxDynamicSharedMemorySize, smem); });
+  if (result != hipSuccess) return result;
+  const int nk = (g.K + 127) / 128, kper = wanted > 1 ? (nk + wanted - 1) / wanted : nk, parts = wanted > 1 ? (nk + kper - 1) / kper : 1;
+  hipLaunchKernelGGL((product_tile_kernel<BM, BN, NS, EXACT>), dim3((unsigned)tiles_of(g.M, g.N, BM, BN), parts), dim3(256), smem, s, g, kper);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || parts == 1) return e;
+  const int64_t quads = (int64_t)g.M * ((g.N + 3) / 4);
+  join_kernel<<<(unsigned)((quads + 255) / 256), 256, 0, s>>>(g, parts);
+  return hipGetLastError();
+}
+
+template <bool EXACT>
+hipError_t launch_long(const ProductArgs& g, hipStream_t s) {
+  static std::once_flag once;
+  static hipError_t result = hipSuccess;
+  std::call_once(once, [] { result = hipFuncSetAttribute((const void*)product_long_kernel<EXACT>, hipFuncAttributeMaxDynamicSharedMemorySize, kBigSmem); });
+  if (result != hipSuccess) return result;
+  product_long_kernel<EXACT><<<(unsigned)tiles_of(g.M, g.N, 256, 256), 256, kBigSmem, s>>>(g);
+  return hipGetLastError();
 }
 
 template <int MF, int STEP>
@@ -739,24 +740,34 @@ hipError_t launch_rows(const ProductArgs& g, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_product(const ProductArgs& g, hipStream_t s) {
-  if (few_rows(g.M, g.N, g.K)) {
-    if (g.M <= 16) return launch_rows<1, 2>(g, s);
-    return g.M <= 32 ? launch_rows<2, 2>(g, s) : launch_rows<4, 1>(g, s);
+template <bool EXACT>
+hipError_t launch_shape(const ProductArgs& g, Shape shape, hipStream_t s) {
+  switch (shape) {
+    case kRows:
+      if (g.M <= 16) return launch_rows<1, 2>(g, s);
+      return g.M <= 32 ? launch_rows<2, 2>(g, s) : launch_rows<4, 1>(g, s);
+    case kBig: return launch_long<EXACT>(g, s);
+    case k128: return launch_tile<128, 128, 2, EXACT>(g, 1, s);
+    case k128x64: return launch_tile<128, 64, 2, EXACT>(g, 1, s);
+    case k64: return launch_tile<64, 64, 2, EXACT>(g, 1, s);
+    case k32x64: return launch_tile<32, 64, 3, EXACT>(g, 1, s);
+    case k32: return launch_tile<32, 32, 4, EXACT>(g, 1, s);
+    default: return launch_tile<64, 64, 3, EXACT>(g, parts_of(g.M, g.N, g.K), s);
   }
-  if (big_tiles(g.M, g.N) && g.K > 0) return g.out_dtype == 0 ? launch_long<true>(g, s) : launch_long<false>(g, s);
-  const bool wide = wide_tiles(g.M, g.N);
-  if (g.out_dtype == 0) return wide ? launch_tile<128, 128, 2, true>(g, s) : launch_tile<64, 64, 4, true>(g, s);
-  return wide ? launch_tile<128, 128, 2, false>(g, s) : launch_tile<64, 64, 4, false>(g, s);
 }
 
-hipError_t product_configure_all() {
-  hipError_t e = configure_tile<128, 128, 2, false>();
-  if (e == hipSuccess) e = configure_tile<64, 64, 4, false>();
-  if (e == hipSuccess) e = configure_tile<128, 128, 2, true>();
-  if (e == hipSuccess) e = configure_long<false>();
-  if (e == hipSuccess) e = configure_long<true>();
-  return e == hipSuccess ? configure_tile<64, 64, 4, true>() : e;
+}  // namespace
+
+// (of the larger one for the two output types)
+size_t product_floats(int M, int N, int K) {
+  if (shape_of(M, N, K, 0) != kSplit && shape_of(M, N, K, 1) != kSplit) return 0;
+  const int parts = parts_of(M, N, K);
+  return parts > 1 ? (size_t)parts * M * ((N + 3) & ~3) : 0;
+}
+
+hipError_t launch_product(const ProductArgs& g, hipStream_t s) {
+  const Shape shape = shape_of(g.M, g.N, g.K, g.out_dtype);
+  return g.out_dtype == 0 ? launch_shape<true>(g, shape, s) : launch_shape<false>(g, shape, s);
 }
 
 }  // namespace slp

@@ -143,7 +143,7 @@ def test_empty_matrices():
 
 # ---- products -----------------------------------------------------------------------------------------------------
 SHAPES = [(1, 1, 1), (1, 16, 16), (1, 47, 60), (1, 1000, 784), (2, 64, 128), (3, 65, 129), (5, 200, 3001), (8, 130, 640), (15, 129, 1500), (16, 512, 2048), (17, 96, 400),
-          (33, 100, 1000), (64, 64, 64), (64, 333, 4100), (100, 129, 777), (130, 260, 131), (256, 512, 1024), (300, 700, 1500), (1000, 777, 300), (1410, 80, 784), (2000, 2100, 200),
+          (33, 100, 1000), (64, 64, 64), (64, 333, 4100), (100, 129, 777), (130, 260, 131), (256, 512, 1024), (300, 700, 1500), (1000, 777, 300), (1410, 80, 784), (130, 2000, 131), (70, 300, 9000), (2000, 2100, 200), (2000, 4090, 600),
           (4100, 4200, 144), (4096, 4096, 3200)]
 
 
