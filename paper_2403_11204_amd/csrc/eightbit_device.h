@@ -67,6 +67,29 @@ __device__ __forceinline__ void store8(float* p, int n, const float (&v)[8]) {
   }
 }
 
+// 8 elements as they are in memory.
+template <typename T> struct Raw;
+template <> struct Raw<bf16> { bf16x8 v; };
+template <> struct Raw<float> { f32x4 v[2]; };
+__device__ __forceinline__ void fetch8(const bf16* p, int n, Raw<bf16>& r) {
+  if (n >= 8) r.v = ((const AnyBf16x8*)p)->v;
+  else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r.v[j] = j < n ? p[j] : (bf16)0.0f;
+  }
+}
+__device__ __forceinline__ void fetch8(const float* p, int n, Raw<float>& r) {
+  if (n >= 8) {
+    r.v[0] = ((const AnyF32x4*)p)->v;
+    r.v[1] = ((const AnyF32x4*)(p + 4))->v;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r.v[j / 4][j % 4] = j < n ? p[j] : 0.0f;
+  }
+}
+__device__ __forceinline__ float item(const Raw<bf16>& r, int j) { return (float)r.v[j]; }
+__device__ __forceinline__ float item(const Raw<float>& r, int j) { return r.v[j / 4][j % 4]; }
+
 // Lane i of a row of 16 takes the value of the lane that the control names.
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp(uint32_t x) {
@@ -80,15 +103,30 @@ __device__ __forceinline__ uint32_t max_of_16(uint32_t x) {
   x = umax(x, dpp<kHalfMirror>(x));
   return umax(x, dpp<kMirror>(x));
 }
+// Over the lanes l, l ^ 16, l ^ 32 and l ^ 48: two instructions that exchange halves and quarters of the wavefront between two registers.
+__device__ __forceinline__ uint32_t max_of_rows(uint32_t x) {
+  u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(x, x, false, false));
+  x = umax(r[0], r[1]);
+  r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(x, x, false, false));
+  return umax(r[0], r[1]);
+}
+__device__ __forceinline__ float sum_of_rows(float x) {
+  uint32_t u = __builtin_bit_cast(uint32_t, x);
+  u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(u, u, false, false));
+  uint32_t a = r[0], b = r[1];         // (a bit cast of a vector's element takes the first one's)
+  u = __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b));
+  r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(u, u, false, false));
+  a = r[0];
+  b = r[1];
+  return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+}
 template <int CTRL>
 __device__ __forceinline__ float add_dpp(float x) { return x + __builtin_bit_cast(float, dpp<CTRL>(__builtin_bit_cast(uint32_t, x))); }
 __device__ __forceinline__ float sum_of_64(float x) {
   x = add_dpp<kSwap1>(x);
   x = add_dpp<kSwap2>(x);
   x = add_dpp<kHalfMirror>(x);
-  x = add_dpp<kMirror>(x);
-  x += __shfl_xor(x, 16, 64);
-  return x + __shfl_xor(x, 32, 64);
+  return sum_of_rows(add_dpp<kMirror>(x));
 }
 
 // |v| as an integer that orders like the value, infinities and NaN above all others

@@ -105,28 +105,6 @@ hipError_t rmsnorm_of(const NormArgs& a, hipStream_t s) {
 }
 
 // ---- backward: rows dealt out to teams of WAVES wavefronts, gamma and the sums for its gradient in registers, each lane CH chunks ----
-template <typename T> struct Raw;
-template <> struct Raw<bf16> { bf16x8 v; };
-template <> struct Raw<float> { f32x4 v[2]; };
-__device__ __forceinline__ void fetch8(const bf16* p, int n, Raw<bf16>& r) {
-  if (n >= 8) r.v = ((const AnyBf16x8*)p)->v;
-  else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) r.v[j] = j < n ? p[j] : (bf16)0.0f;
-  }
-}
-__device__ __forceinline__ void fetch8(const float* p, int n, Raw<float>& r) {
-  if (n >= 8) {
-    r.v[0] = ((const AnyF32x4*)p)->v;
-    r.v[1] = ((const AnyF32x4*)(p + 4))->v;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) r.v[j / 4][j % 4] = j < n ? p[j] : 0.0f;
-  }
-}
-__device__ __forceinline__ float item(const Raw<bf16>& r, int j) { return (float)r.v[j]; }
-__device__ __forceinline__ float item(const Raw<float>& r, int j) { return r.v[j / 4][j % 4]; }
-
 // One reading of everything: a row waits in registers for its product, while the next row's loads are under way (AHEAD).
 template <typename T, int WAVES, int CH, bool AHEAD>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_backward_kernel(const NormBackArgs a, float* __restrict__ partials) {

@@ -33,90 +33,83 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs a
   if ((threadIdx.x & 15) == 0) a.scales[row * a.lds + b] = (uint8_t)scale;
 }
 
-// Everything else, a 128 x 128 tile a workgroup: a thread holds 8 rows of 8 columns.  The transposed bytes go through LDS, a row of 128
-// bytes for each column of the tile; the 16-byte piece p of column c sits at p ^ (c / 8 mod 8), so that the lanes of a wavefront, which write 16
-// columns 8 apart, spread over the banks.
+// Everything else, a 128 x 128 tile a workgroup of 8 wavefronts: a thread holds 4 rows of 8 columns.  The transposed bytes go through LDS, a row
+// of 128 bytes for each column of the tile; the 16-byte piece p of column c sits at p ^ (c / 8 mod 8), so that the lanes of a wavefront, which
+// write 16 columns 8 apart, spread over the banks.
 template <typename T, int BLOCK>
-__global__ __launch_bounds__(256) void quantize_tile_kernel(const QuantizeArgs a) {
+__global__ __launch_bounds__(512) void quantize_tile_kernel(const QuantizeArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t turned[128 * 128];
-  __shared__ uint32_t cmax[4][128];
-  __shared__ float csum[4][128];
+  __shared__ uint32_t cmax[8][128];
+  __shared__ float csum[8][128];
   const int t = threadIdx.x, wave = t >> 6, g = t >> 4, cc = t & 15;
-  const int tiles = (a.cols + 127) / 128;
-  const int64_t tm = blockIdx.x / tiles;
-  const int tn = blockIdx.x % tiles;
+  const int tilesM = (a.rows + 127) / 128, tilesN = (a.cols + 127) / 128;
+  const int64_t tm = blockIdx.x / tilesN;
+  const int tn = blockIdx.x % tilesN;
   const int64_t m0 = tm * 128;
   const int c0 = tn * 128 + cc * 8, left = a.cols - c0;
-  float v[8][8];
+  float v[4][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t row = m0 + 8 * g + i;
-    const int n = row < a.rows ? left : 0;
-    load8((const T*)a.x + row * a.ldx + c0, n, v[i]);
-    if (a.mask) {
-      float m[8];
-      load8((const T*)a.mask + row * a.ldmask + c0, n, m);
+  for (int i = 0; i < 4; ++i) {
+    const int64_t row = m0 + 4 * g + i;
+    load8((const T*)a.x + row * a.ldx + c0, row < a.rows ? left : 0, v[i]);
+  }
+  if (a.mask) {
+    float m[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t row = m0 + 4 * g + i;
+      load8((const T*)a.mask + row * a.ldmask + c0, row < a.rows ? left : 0, m[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (!(m[j] > 0.0f)) v[i][j] = 0.0f;
-    }
+        if (!(m[i][j] > 0.0f)) v[i][j] = 0.0f;
   }
-  // largest magnitudes: of the rows (16 lanes each), of the columns (a thread's 8 rows, 4 lanes of a wavefront, 4 wavefronts)
-  uint32_t rmax[8], kmax[8];
-  float sum[8];
+  // largest magnitudes: of the rows (16 lanes each), of the columns (a thread's 4 rows, 4 lanes of a wavefront, 8 wavefronts)
+  uint32_t rmax[4] = {0, 0, 0, 0}, kmax[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) rmax[i] = kmax[i] = 0;
+  for (int j = 0; j < 8; ++j) {
+    float sum = 0.0f;
+    kmax[j] = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int i = 0; i < 4; ++i) {
       const uint32_t m = magnitude(v[i][j]);
       rmax[i] = umax(rmax[i], m);
       kmax[j] = umax(kmax[j], m);
-      sum[j] += v[i][j];
+      sum += v[i][j];
     }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    kmax[j] = umax(kmax[j], __shfl_xor(kmax[j], 16, 64));
-    kmax[j] = umax(kmax[j], __shfl_xor(kmax[j], 32, 64));
-    if ((t & 63) < 16) cmax[wave][cc * 8 + j] = kmax[j];
+    if (BLOCK == 128 || a.qt) {
+      kmax[j] = max_of_rows(kmax[j]);
+      if ((t & 63) < 16) cmax[wave][cc * 8 + j] = kmax[j];
+    }
     if (a.sums) {
-      sum[j] += __shfl_xor(sum[j], 16, 64);
-      sum[j] += __shfl_xor(sum[j], 32, 64);
-      if ((t & 63) < 16) csum[wave][cc * 8 + j] = sum[j];
+      sum = sum_of_rows(sum);
+      if ((t & 63) < 16) csum[wave][cc * 8 + j] = sum;
     }
   }
   __syncthreads();
-  if (a.sums && t < 128 && tn * 128 + t < a.cols)
-    a.work[tm * a.cols + tn * 128 + t] = (csum[0][t] + csum[1][t]) + (csum[2][t] + csum[3][t]);
-  uint32_t kscale[8];
+  if (a.sums && t < 128 && tn * 128 + t < a.cols) {
+    float sum = csum[0][t];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int c = cc * 8 + j;
-    kmax[j] = umax(umax(cmax[0][c], cmax[1][c]), umax(cmax[2][c], cmax[3][c]));
+    for (int w = 1; w < 8; ++w) sum += csum[w][t];
+    (tilesM == 1 ? a.sums : a.work + tm * a.cols)[tn * 128 + t] = sum;
   }
+  uint32_t all = 0;
   if (BLOCK == 128) {
-    uint32_t all = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) all = umax(all, kmax[j]);
-    all = scale_of(max_of_16(all));
-#pragma unroll
-    for (int j = 0; j < 8; ++j) kscale[j] = all;
+    for (int w = 0; w < 8; ++w) all = umax(all, umax(cmax[w][t & 63], cmax[w][64 + (t & 63)]));
+    all = scale_of(max_of_rows(max_of_16(all)));
     if (t == 0) {
       if (a.q) a.scales[tm * a.lds + tn] = (uint8_t)all;
       if (a.qt) a.scales_t[(int64_t)tn * a.ldst + tm] = (uint8_t)all;
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) kscale[j] = scale_of(kmax[j]);
   }
   if (a.q) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t row = m0 + 8 * g + i;
-      const uint32_t scale = BLOCK == 128 ? kscale[0] : scale_of(max_of_16(rmax[i]));
+    for (int i = 0; i < 4; ++i) {
+      const int64_t row = m0 + 4 * g + i;
+      const uint32_t scale = BLOCK == 128 ? all : scale_of(max_of_16(rmax[i]));
       const float up = inverse_scale(scale);
       if (row < a.rows) {
         if (c0 < ((a.cols + 15) & ~15))
@@ -130,15 +123,21 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(const QuantizeArgs a
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int c = cc * 8 + j;
-      const float up = inverse_scale(kscale[j]);
-      *(u32x2*)(turned + c * 128 + (((g >> 1) ^ (cc & 7)) << 4) + (g & 1) * 8) =
-          u32x2{to_e4m3(v[0][j] * up, v[1][j] * up, v[2][j] * up, v[3][j] * up), to_e4m3(v[4][j] * up, v[5][j] * up, v[6][j] * up, v[7][j] * up)};
-      if (BLOCK == 1 && g == 0 && c0 + j < a.cols) a.scales_t[(int64_t)(c0 + j) * a.ldst + tm] = (uint8_t)kscale[j];
+      uint32_t scale = all;
+      if (BLOCK == 1) {
+        uint32_t k = 0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) k = umax(k, cmax[w][c]);
+        scale = scale_of(k);
+        if (g == 0 && c0 + j < a.cols) a.scales_t[(int64_t)(c0 + j) * a.ldst + tm] = (uint8_t)scale;
+      }
+      const float up = inverse_scale(scale);
+      *(uint32_t*)(turned + c * 128 + (((g >> 2) ^ (cc & 7)) << 4) + (g & 3) * 4) = to_e4m3(v[0][j] * up, v[1][j] * up, v[2][j] * up, v[3][j] * up);
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int c = i * 32 + (t >> 3), p = t & 7;
+    for (int i = 0; i < 2; ++i) {
+      const int c = i * 64 + (t >> 3), p = t & 7;
       if (tn * 128 + c < a.cols && m0 + 16 * p < a.rows)          // zeros up to the next 16 bytes
         *(u32x4*)(a.qt + (int64_t)(tn * 128 + c) * a.ldqt + m0 + 16 * p) = *(const u32x4*)(turned + c * 128 + ((p ^ ((c >> 3) & 7)) << 4));
     }
@@ -155,16 +154,16 @@ hipError_t quantize_of(const QuantizeArgs& a, hipStream_t s) {
     return hipGetLastError();
   }
   const unsigned tiles = (unsigned)tile_count(a);
-  if (a.block == 128) quantize_tile_kernel<T, 128><<<tiles, 256, 0, s>>>(a);
-  else quantize_tile_kernel<T, 1><<<tiles, 256, 0, s>>>(a);
+  if (a.block == 128) quantize_tile_kernel<T, 128><<<tiles, 512, 0, s>>>(a);
+  else quantize_tile_kernel<T, 1><<<tiles, 512, 0, s>>>(a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.sums) return e;
+  if (e != hipSuccess || !a.sums || a.rows <= 128) return e;      // (a single tile's height has stored its sums itself)
   return launch_sum_rows(a.work, (a.rows + 127) / 128, a.cols, a.sums, s);
 }
 
 }  // namespace
 
-size_t quantize_floats(int rows, int cols) { return (size_t)((rows + 127) / 128) * cols; }
+size_t quantize_floats(int rows, int cols) { return rows <= 128 ? 0 : (size_t)((rows + 127) / 128) * cols; }
 
 hipError_t launch_quantize(int dtype, const QuantizeArgs& a, hipStream_t s) { return dtype == 1 ? quantize_of<bf16>(a, s) : quantize_of<float>(a, s); }
 

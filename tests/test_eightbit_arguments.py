@@ -43,8 +43,8 @@ def test_quantize():
     refused(ALLOC, quantize(ldq=392), b"16-byte")
     refused(ALLOC, quantize(scales=P + 1), b"4-byte")
     refused(ALLOC, quantize(lds=5), b"4-byte")
-    refused(ALLOC, quantize(sums=P, work=P, size=4 * 300 - 1), b"1200")
-    refused(ALLOC, quantize(sums=P, work=P + 64, size=1 << 20), b"256-byte")
+    refused(ALLOC, quantize(rows=200, sums=P, work=P, size=2 * 4 * 300 - 1), b"2400")
+    refused(ALLOC, quantize(rows=200, sums=P, work=P + 64, size=1 << 20), b"256-byte")
     assert quantize(rows=0) == 0 and quantize(cols=0, ldx=0) == 0
     assert api.lib().slp_quantize_workspace_bytes(129, 5) == 40 and api.lib().slp_quantize_workspace_bytes(-1, 5) == 0
 
