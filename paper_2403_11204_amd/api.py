@@ -82,7 +82,7 @@ def lib():
         "slp_rmsnorm": (i32, [vp, i64, vp, i64, vp, f32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp]),
         "slp_rmsnorm_backward_workspace_bytes": (sz, [i32, i32]),
         "slp_rmsnorm_backward": (i32, [vp, i64, vp, i64, vp, vp, vp, i64, i32, i32, i32, vp, i64, vp, vp, sz, vp]),
-        "slp_gradient_norm_workspace_bytes": (sz, [ctypes.POINTER(i64), i32]),
+        "slp_gradient_norm_workspace_bytes": (sz, [i32]),
         "slp_gradient_norm": (i32, [ctypes.POINTER(vp), ctypes.POINTER(i64), ctypes.POINTER(i32), i32, vp, vp, sz, vp]),
         "slp_clip_gradients": (i32, [ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.POINTER(i64), ctypes.POINTER(i32), i32, f32, vp, vp, sz, vp]),
     }
@@ -360,9 +360,9 @@ def gradient_norm(tensors):
     """slp_gradient_norm: the norm of all tensors' values together, as a device scalar."""
     (ptrs, counts, dts, n), device, L = _tensor_list(tensors), tensors[0].device, lib()
     norm = _empty((), dtype=_FL, device=device)
-    size = L.slp_gradient_norm_workspace_bytes(counts, n)
-    work = _empty(size, dtype=torch.uint8, device=device) if size else None
-    _check(L.slp_gradient_norm(ptrs, counts, dts, n, norm.data_ptr(), _ptr(work), size, _stream()))
+    size = L.slp_gradient_norm_workspace_bytes(n)
+    work = _empty(size, dtype=torch.uint8, device=device)
+    _check(L.slp_gradient_norm(ptrs, counts, dts, n, norm.data_ptr(), work.data_ptr(), size, _stream()))
     return norm
 
 
@@ -375,9 +375,9 @@ def clip_gradients(tensors, max_norm, out=None):
         assert len(out) == n and all(o.is_cuda and o.is_contiguous() and o.dtype is t.dtype and o.shape == t.shape for t, o in zip(tensors, out))
         to = _table(n)[0](*[o.data_ptr() for o in out])
     norm = _empty((), dtype=_FL, device=device)
-    size = L.slp_gradient_norm_workspace_bytes(counts, n)
-    work = _empty(size, dtype=torch.uint8, device=device) if size else None
-    code = L.slp_clip_gradients(ptrs, to, counts, dts, n, max_norm, norm.data_ptr(), _ptr(work), size, _stream())
+    size = L.slp_gradient_norm_workspace_bytes(n)
+    work = _empty(size, dtype=torch.uint8, device=device)
+    code = L.slp_clip_gradients(ptrs, to, counts, dts, n, max_norm, norm.data_ptr(), work.data_ptr(), size, _stream())
     if code:
         _check(code)
     return norm

@@ -27,34 +27,55 @@ __device__ __forceinline__ double total(const double* __restrict__ partials, int
   return sum_of_256(x);
 }
 
-// f(tensor, first element, elements) for each chunk of this workgroup: chunks are dealt out in turns.
+// f(tensor, its chunk) for each chunk of this workgroup.  Chunks are dealt out in turns, to one workgroup for each compute unit, so that all of
+// them read and write within 8 MB at a time: 549 million float32 values, norm / clipping 334 / 1141 us (6.5 TB/s / 5.8 for 6.6 GB) against 349 / 1172
+// with two workgroups each and 375 / 1201 with four; 455 / 1357 with chunks of 16 KB, 355 / 1187 with 64 KB.
 template <typename F>
 __device__ __forceinline__ void each_chunk(const ClipTable& t, F f) {
   int i = 0;
   for (int c = blockIdx.x; c < t.chunk0[t.n]; c += gridDim.x) {
     while (c >= t.chunk0[i + 1]) ++i;
-    const int64_t first = (int64_t)(c - t.chunk0[i]) * kClipChunk, left = t.count[i] - first;
-    f(i, first, (int)(left < kClipChunk ? left : kClipChunk));
+    f(i, c - t.chunk0[i]);
+  }
+}
+
+// Chunk c of a tensor: a thread's elements of it, 8 at a time, all loads under way together; f(first of 8, how many of them exist, they).
+template <typename T, typename F>
+__device__ __forceinline__ void each_eight(const T* p, int64_t count, int c, F f) {
+  constexpr int kElements = kClipChunk / (int)sizeof(T), kVectors = kElements / (256 * 8);
+  const int64_t first = (int64_t)c * kElements, left = count - first;
+  const int n = left < kElements ? (int)left : kElements;
+  Raw<T> v[kVectors];
+#pragma unroll
+  for (int i = 0; i < kVectors; ++i) {
+    const int k = (i * 256 + threadIdx.x) * 8;
+    fetch8(p + first + k, n - k, v[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kVectors; ++i) {
+    const int k = (i * 256 + threadIdx.x) * 8;
+    f(first + k, n - k, v[i]);
   }
 }
 
 template <typename T>
-__device__ __forceinline__ double squares(const T* p, int n) {
+__device__ __forceinline__ double squares(const T* p, int64_t count, int c) {
   double sum = 0.0;
-  for (int k = threadIdx.x * 8; k < n; k += 256 * 8) {
-    float v[8];
-    load8(p + k, n - k, v);
+  each_eight(p, count, c, [&](int64_t, int, const Raw<T>& v) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum += (double)v[j] * (double)v[j];
-  }
+    for (int j = 0; j < 8; ++j) {
+      const double x = (double)item(v, j);
+      sum += x * x;
+    }
+  });
   return sum;
 }
 
 __global__ __launch_bounds__(256) void square_sums_kernel(const ClipTable t, double* __restrict__ partials) {
   double sum = 0.0;
-  each_chunk(t, [&](int i, int64_t first, int n) {
-    if ((t.bf16 >> i) & 1) sum += squares((const bf16*)t.in[i] + first, n);
-    else sum += squares((const float*)t.in[i] + first, n);
+  each_chunk(t, [&](int i, int c) {
+    if ((t.bf16 >> i) & 1) sum += squares((const bf16*)t.in[i], t.count[i], c);
+    else sum += squares((const float*)t.in[i], t.count[i], c);
   });
   sum = sum_of_256(sum);
   if (threadIdx.x == 0) partials[blockIdx.x] = sum;
@@ -66,25 +87,24 @@ __global__ __launch_bounds__(256) void norm_of_kernel(const double* __restrict__
 }
 
 template <typename T>
-__device__ __forceinline__ void scaled(const T* in, T* out, int n, float c) {
-  for (int k = threadIdx.x * 8; k < n; k += 256 * 8) {
-    float v[8];
-    load8(in + k, n - k, v);
+__device__ __forceinline__ void scaled(const T* in, T* out, int64_t count, int c, float by) {
+  each_eight(in, count, c, [&](int64_t k, int n, const Raw<T>& v) {
+    float o[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= c;
-    store8(out + k, n - k, v);
-  }
+    for (int j = 0; j < 8; ++j) o[j] = item(v, j) * by;
+    store8(out + k, n, o);
+  });
 }
 
 __global__ __launch_bounds__(256) void scale_kernel(const ClipTable t, const double* __restrict__ partials, int n, float max_norm, float* __restrict__ norm) {
   const double x = sqrt(total(partials, n));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)x;
   const double ratio = (double)max_norm / (x + 1e-6);
-  const float c = x < INFINITY && ratio < 1.0 ? (float)ratio : 1.0f;
-  each_chunk(t, [&](int i, int64_t first, int n) {
-    if (c == 1.0f && t.in[i] == t.out[i]) return;
-    if ((t.bf16 >> i) & 1) scaled((const bf16*)t.in[i] + first, (bf16*)t.out[i] + first, n, c);
-    else scaled((const float*)t.in[i] + first, (float*)t.out[i] + first, n, c);
+  const float by = x < INFINITY && ratio < 1.0 ? (float)ratio : 1.0f;
+  each_chunk(t, [&](int i, int c) {
+    if (by == 1.0f && t.in[i] == t.out[i]) return;
+    if ((t.bf16 >> i) & 1) scaled((const bf16*)t.in[i], (bf16*)t.out[i], t.count[i], c, by);
+    else scaled((const float*)t.in[i], (float*)t.out[i], t.count[i], c, by);
   });
 }
 

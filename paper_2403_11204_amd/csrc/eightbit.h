@@ -75,8 +75,8 @@ struct ClipTable {
   uint64_t bf16;                      // bit i: tensor i holds bf16
   int n;
 };
-constexpr int64_t kClipChunk = 8192;  // elements
-constexpr int kClipMaxGroups = 1024;  // workgroups of one launch at most
+constexpr int kClipChunk = 32768;     // bytes
+constexpr int kClipMaxGroups = 256;   // workgroups of one launch at most
 // partials[0 .. groups) = sums of squares, one a workgroup
 hipError_t launch_square_sums(const ClipTable& t, int groups, double* partials, hipStream_t s);
 // *norm = sqrt(sum of partials)

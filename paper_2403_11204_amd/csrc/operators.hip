@@ -56,16 +56,16 @@ int check_work(const char* who, const void* p, size_t bytes, size_t need) {
   } while (0)
 
 int chunk_groups(int64_t chunks) { return (int)(chunks < 1 ? 1 : chunks < kClipMaxGroups ? chunks : kClipMaxGroups); }
-int64_t chunks_of(int64_t count) { return (count + kClipChunk - 1) / kClipChunk; }
+int64_t chunks_of(int64_t count, int dt) { return (count * (int64_t)size_of(dt) + kClipChunk - 1) / kClipChunk; }
 
 // Partial sums of all launches; -1 where a tensor has more chunks than fit.
-int clip_partials(const int64_t* counts, int n) {
+int clip_partials(const int64_t* counts, const int* dts, int n) {
   int64_t all = 0;
   for (int i = 0; i < n; i += kClipTensors) {
     int64_t chunks = 0;
     for (int k = i; k < n && k < i + kClipTensors; ++k) {
       if (counts[k] < 0 || counts[k] > ((int64_t)1 << 43)) return -1;
-      chunks += chunks_of(counts[k]);
+      chunks += chunks_of(counts[k], dts[k]);
       if (chunks > INT32_MAX) return -1;
     }
     all += chunk_groups(chunks);
@@ -85,9 +85,9 @@ int clip_run(const char* who, const void* const* in, void* const* out, const int
     if (counts[i] && (off(in[i], size_of(dts[i])) || (scale && out && off(out[i], size_of(dts[i])))))
       return fail(SLP_ERR_ALLOC, "%s: tensor %d is not on an element's boundary", who, i);
   }
-  const int partials = clip_partials(counts, n);
+  const int partials = clip_partials(counts, dts, n);
   if (partials < 0) return fail(SLP_ERR_SHAPE, "%s: too many elements", who);
-  SLP_CHECK(check_work(who, workspace, workspace_bytes, slp_gradient_norm_workspace_bytes(counts, n)));
+  SLP_CHECK(check_work(who, workspace, workspace_bytes, slp_gradient_norm_workspace_bytes(n)));
   double* const sums = (double*)workspace;
   for (int pass = 0; pass < (scale ? 2 : 1); ++pass) {
     int done = 0;
@@ -98,7 +98,7 @@ int clip_run(const char* who, const void* const* in, void* const* out, const int
         t.out[t.n] = out ? out[k] : const_cast<void*>(in[k]);
         t.count[t.n] = counts[k];
         t.bf16 |= (uint64_t)(dts[k] == SLP_BF16) << t.n;
-        t.chunk0[t.n + 1] = t.chunk0[t.n] + (int)chunks_of(counts[k]);
+        t.chunk0[t.n + 1] = t.chunk0[t.n] + (int)chunks_of(counts[k], dts[k]);
         ++t.n;
       }
       const int groups = chunk_groups(t.chunk0[t.n]);
@@ -222,10 +222,8 @@ int slp_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, int64_t ld
   return SLP_OK;
 }
 
-size_t slp_gradient_norm_workspace_bytes(const int64_t* counts, int n) {
-  if (n < 0 || (n && !counts)) return 0;
-  const int partials = n ? clip_partials(counts, n) : 1;
-  return partials < 0 ? 0 : (size_t)partials * sizeof(double);
+size_t slp_gradient_norm_workspace_bytes(int n) {
+  return n < 0 ? 0 : (size_t)(n / kClipTensors + 1) * kClipMaxGroups * sizeof(double);
 }
 
 int slp_gradient_norm(const void* const* tensors, const int64_t* counts, const int* dts, int n, float* norm_out, void* workspace,
