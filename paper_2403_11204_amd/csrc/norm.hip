@@ -10,23 +10,94 @@
 namespace slp {
 namespace {
 
-// A chunk is 8 consecutive columns, the columns of a scale are 16 lanes'.  WAVES wavefronts share a row, each lane CH chunks of it in
-// registers; MANY: rows longer than that, read twice.
-template <typename T, int WAVES, int CH, bool MANY>
+// A chunk is 8 consecutive columns, the columns of a scale are 16 lanes'.  What follows the row's rstd n, for one chunk (v: h, g: gamma).
+template <typename T>
+__device__ __forceinline__ void finish_chunk(const NormArgs& a, int64_t row, int c, float n, const float (&g)[8], float (&v)[8]) {
+  const int D = a.dim;
+  uint32_t amax = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    v[j] = 8 * c + j < D ? v[j] * n * g[j] : 0.0f;        // (0 times an infinite n)
+    amax = umax(amax, magnitude(v[j]));
+  }
+  if (a.y) store8((T*)a.y + row * a.ldy + 8 * c, D - 8 * c, v);
+  if (a.q) {
+    const uint32_t scale = scale_of(max_of_16(amax));
+    const float up = inverse_scale(scale);
+    if (8 * c < ((D + 15) & ~15))                         // zeros up to the next 16 bytes
+      *(u32x2*)(a.q + row * a.ldq + 8 * c) = u32x2{to_e4m3(v[0] * up, v[1] * up, v[2] * up, v[3] * up), to_e4m3(v[4] * up, v[5] * up, v[6] * up, v[7] * up)};
+    if ((threadIdx.x & 15) == 0 && 8 * c < D) a.scales[row * a.lds + c / 16] = (uint8_t)scale;
+  }
+}
+
+// Rows dealt out to teams of WAVES wavefronts, each lane CH chunks of a row in registers; the next row's loads are under way while this one is
+// added up and stored.  Bound by memory: 8192 x 16384 bf16 with the residual 173 us (939 MB, 5.4 TB/s), 4096 x 8192 44 us (235 MB, 5.3 TB/s), on 512
+// workgroups of several wavefronts; a workgroup for each row 181 and 49 us, 256 workgroups 171 and 45 (8192 x 4096 45 -> 59), 1024 177 and 45.
+template <typename T, int WAVES, int CH>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_kernel(const NormArgs a) {
-  constexpr int TEAM = WAVES * 64, ROWS = WAVES == 1 ? 4 : 1;
-  __shared__ float part[WAVES];
-  const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
-  const int64_t row = (int64_t)blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x >> 6 : 0);
-  if (row >= a.rows) return;           // (a whole wavefront, and no barrier where a workgroup holds several rows)
+  constexpr int TEAM = WAVES * 64, TEAMS = WAVES == 1 ? 4 : 1;
+  __shared__ float part[2][WAVES];
+  const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, D = a.dim, step = gridDim.x * TEAMS;
+  float g[CH][8];
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g[i][j] = 1.0f;
+    if (a.gamma) load8(a.gamma + 8 * (i * TEAM + t), D - 8 * (i * TEAM + t), g[i]);
+  }
+  Raw<T> x[CH], r[CH];
+  auto fetch = [&](int64_t row) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int c = 8 * (i * TEAM + t);
+      fetch8((const T*)a.x + row * a.ldx + c, D - c, x[i]);
+      if (a.r) fetch8((const T*)a.r + row * a.ldr + c, D - c, r[i]);
+    }
+  };
+  int64_t row = (int64_t)blockIdx.x * TEAMS + (WAVES == 1 ? threadIdx.x >> 6 : 0);
+  if (row < a.rows) fetch(row);
+  for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
+    float v[CH][8], ss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int c = 8 * (i * TEAM + t);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[i][j] = item(x[i], j);
+        if (a.r) v[i][j] = (float)(T)(v[i][j] + item(r[i], j));
+        ss += v[i][j] * v[i][j];
+      }
+      if (a.h) store8((T*)a.h + row * a.ldh + c, D - c, v[i]);
+    }
+    if (row + step < a.rows) fetch(row + step);
+    ss = sum_of_64(ss);
+    if (WAVES > 1) {
+      if ((t & 63) == 0) part[turn][t >> 6] = ss;
+      __syncthreads();
+      ss = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) ss += part[turn][w];
+    }
+    const float n = 1.0f / sqrtf(ss / (float)D + a.eps);
+    if (a.rstd && t == 0) a.rstd[row] = n;
+    if (a.y || a.q) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) finish_chunk<T>(a, row, i * TEAM + t, n, g[i], v[i]);
+    }
+  }
+}
+
+constexpr int kOnePass = 16384;       // longest row that a workgroup's registers hold
+
+// Longer rows, read twice: a workgroup of 16 wavefronts for each.
+template <typename T>
+__global__ __launch_bounds__(1024) void rmsnorm_long_kernel(const NormArgs a) {
+  __shared__ float part[16];
+  const int64_t row = blockIdx.x;
+  const int D = a.dim, chunks = (D + 127) / 128 * 16;
   const T* x = (const T*)a.x + row * a.ldx;
   const T* r = a.r ? (const T*)a.r + row * a.ldr : nullptr;
   T* h = a.h ? (T*)a.h + row * a.ldh : nullptr;
-  const int D = a.dim;
-  const int padded = (D + 127) / 128 * 16;        // chunks, the last scale's whole
-
-  float v[CH][8];
-  float ss = 0.0f;
   auto load = [&](int c, float (&o)[8]) {
     load8(x + 8 * c, D - 8 * c, o);
     if (r) {
@@ -36,76 +107,48 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_kernel(
       for (int j = 0; j < 8; ++j) o[j] = (float)(T)(o[j] + u[j]);
     }
   };
-  for (int c0 = 0; c0 < padded; c0 += CH * TEAM) {
+  float ss = 0.0f;
+  for (int c = threadIdx.x; c < chunks; c += 1024) {
+    float v[8];
+    load(c, v);
+    if (h) store8(h + 8 * c, D - 8 * c, v);
 #pragma unroll
-    for (int i = 0; i < CH; ++i) load(c0 + i * TEAM + t, v[i]);
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int c = c0 + i * TEAM + t;
-      if (h) store8(h + 8 * c, D - 8 * c, v[i]);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) ss += v[i][j] * v[i][j];
-    }
-    if (!MANY) break;
+    for (int j = 0; j < 8; ++j) ss += v[j] * v[j];
   }
   ss = sum_of_64(ss);
-  if (WAVES > 1) {
-    if ((t & 63) == 0) part[t >> 6] = ss;
-    __syncthreads();
-    ss = 0.0f;
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = ss;
+  __syncthreads();
+  ss = 0.0f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) ss += part[w];
-  }
+  for (int w = 0; w < 16; ++w) ss += part[w];
   const float n = 1.0f / sqrtf(ss / (float)D + a.eps);
-  if (a.rstd && t == 0) a.rstd[row] = n;
+  if (a.rstd && threadIdx.x == 0) a.rstd[row] = n;
   if (!a.y && !a.q) return;
-  for (int c0 = 0; c0 < padded; c0 += CH * TEAM) {
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int c = c0 + i * TEAM + t;
-      if (MANY) {
-        if (h) load8(h + 8 * c, D - 8 * c, v[i]);
-        else load(c, v[i]);
-      }
-      float g[8];
-      uint32_t amax = 0;
-      if (a.gamma) load8(a.gamma + 8 * c, D - 8 * c, g);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        v[i][j] *= n;
-        if (a.gamma) v[i][j] *= g[j];
-        if (8 * c + j >= D) v[i][j] = 0.0f;           // (0 times an infinite n)
-        amax = umax(amax, magnitude(v[i][j]));
-      }
-      if (a.y) store8((T*)a.y + row * a.ldy + 8 * c, D - 8 * c, v[i]);
-      if (a.q) {
-        const uint32_t scale = scale_of(max_of_16(amax));
-        const float up = inverse_scale(scale);
-        if (8 * c < ((D + 15) & ~15))                 // zeros up to the next 16 bytes
-          *(u32x2*)(a.q + row * a.ldq + 8 * c) = u32x2{to_e4m3(v[i][0] * up, v[i][1] * up, v[i][2] * up, v[i][3] * up),
-                                                      to_e4m3(v[i][4] * up, v[i][5] * up, v[i][6] * up, v[i][7] * up)};
-        if ((t & 15) == 0 && 8 * c < D) a.scales[row * a.lds + c / 16] = (uint8_t)scale;
-      }
-    }
-    if (!MANY) break;
+  for (int c = threadIdx.x; c < chunks; c += 1024) {
+    float v[8], g[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
+    if (h) load8(h + 8 * c, D - 8 * c, v);
+    else load(c, v);
+    if (a.gamma) load8(a.gamma + 8 * c, D - 8 * c, g);
+    finish_chunk<T>(a, row, c, n, g, v);
   }
 }
 
 template <typename T>
 hipError_t rmsnorm_of(const NormArgs& a, hipStream_t s) {
-  const dim3 quads((a.rows + 3) / 4), rows(a.rows);
-  if (a.dim <= 512) rmsnorm_kernel<T, 1, 1, false><<<quads, 256, 0, s>>>(a);
-  else if (a.dim <= 1024) rmsnorm_kernel<T, 1, 2, false><<<quads, 256, 0, s>>>(a);
-  else if (a.dim <= 2048) rmsnorm_kernel<T, 4, 1, false><<<rows, 256, 0, s>>>(a);
-  else if (a.dim <= 4096) rmsnorm_kernel<T, 4, 2, false><<<rows, 256, 0, s>>>(a);
-  else if (a.dim <= 8192) rmsnorm_kernel<T, 8, 2, false><<<rows, 512, 0, s>>>(a);
-  else if (a.dim <= 16384) rmsnorm_kernel<T, 8, 4, false><<<rows, 512, 0, s>>>(a);
-  else rmsnorm_kernel<T, 16, 2, true><<<rows, 1024, 0, s>>>(a);
+  const int quads = (a.rows + 3) / 4, few = quads < 2048 ? quads : 2048, rows = a.rows < 512 ? a.rows : 512;
+  if (a.dim <= 512) rmsnorm_kernel<T, 1, 1><<<few, 256, 0, s>>>(a);
+  else if (a.dim <= 1024) rmsnorm_kernel<T, 1, 2><<<few, 256, 0, s>>>(a);
+  else if (a.dim <= 2048) rmsnorm_kernel<T, 4, 1><<<rows, 256, 0, s>>>(a);
+  else if (a.dim <= 4096) rmsnorm_kernel<T, 4, 2><<<rows, 256, 0, s>>>(a);
+  else if (a.dim <= 8192) rmsnorm_kernel<T, 8, 2><<<rows, 512, 0, s>>>(a);
+  else if (a.dim <= kOnePass) rmsnorm_kernel<T, 8, 4><<<rows, 512, 0, s>>>(a);
+  else rmsnorm_long_kernel<T><<<a.rows, 1024, 0, s>>>(a);
   return hipGetLastError();
 }
 
 // ---- backward: rows dealt out to teams of WAVES wavefronts, gamma and the sums for its gradient in registers, each lane CH chunks ----
-// One reading of everything: a row waits in registers for its product, while the next row's loads are under way (AHEAD).
+// One reading of everything: a row waits in registers for its product, while the next row's loads are under way (AHEAD).  Bound by memory: 4096 x
+// 8192 bf16 with the gradient past the norm 51 us (268 MB, 5.3 TB/s), and 5 for the sums over the workgroups.
 template <typename T, int WAVES, int CH, bool AHEAD>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_backward_kernel(const NormBackArgs a, float* __restrict__ partials) {
   constexpr int TEAM = WAVES * 64, TEAMS = WAVES == 1 ? 4 : 1;
@@ -250,8 +293,6 @@ __global__ __launch_bounds__(256) void rmsnorm_columns_kernel(const NormBackArgs
   }
   if (a.dgamma) store8(partials + (int64_t)blockIdx.y * a.dim + c, left, acc);
 }
-
-constexpr int kOnePass = 16384;       // longest row that a workgroup's registers hold
 
 // Partial sums of gamma's gradient: workgroups of the one-pass kernel, or strands of rows.
 int backward_groups(int rows, int dim) {
