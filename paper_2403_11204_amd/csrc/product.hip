@@ -597,22 +597,37 @@ __global__ __launch_bounds__(256) void product_long_kernel(const ProductArgs g) 
 #undef SLP_MFMA_ARGS
 #pragma clang diagnostic pop
 
+  // A wavefront stages its 128 x 128 outputs in a 32 KB of the stages that is its own, float32 64 rows at a time, in rows of 256 or 512 bytes whose
+  // 16-byte piece c sits at c ^ (row mod 16), and writes whole row segments.
+  __syncthreads();
+  unsigned char* const st = smem + w * 32768;
   if constexpr (EXACT) {
+    const int c = lane & 31, n = colW + 4 * c;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int half = 0; half < 2; ++half) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        asm volatile("" : "+a"(acc[i][j]));
-        store4(g, rowW + i * 16 + lrow, colW + j * 16 + 4 * lgrp, finished(g, acc[i][j], bias[j]));
-        __builtin_amdgcn_sched_barrier(0);
+      for (int j = 0; j < 8; ++j) {
+#pragma unroll
+        for (int i = 4 * half; i < 4 * half + 4; ++i) {
+          asm volatile("" : "+a"(acc[i][j]));
+          *(f32x4*)(st + ((i & 3) * 16 + lrow) * 512 + (((4 * j + lgrp) ^ lrow) << 4)) = finished(g, acc[i][j], bias[j]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+#pragma unroll
+      for (int b0 = 0; b0 < 32; b0 += 8) {
+        f32x4 val[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int r = (b0 + q) * 2 + (lane >> 5);
+          val[q] = *(const f32x4*)(st + r * 512 + ((c ^ (r & 15)) << 4));
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) store4(g, rowW + 64 * half + (b0 + q) * 2 + (lane >> 5), n, val[q]);
       }
     }
     return;
   }
-  // A wavefront stages its 128 x 128 outputs in a 32 KB of the stages that is its own, rows of 256 bytes whose 16-byte piece c sits at
-  // c ^ (row mod 16), and writes whole row segments.
-  __syncthreads();
-  unsigned char* const st = smem + w * 32768;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
 #pragma unroll
@@ -679,7 +694,8 @@ bool few_rows(int M, int N, int K) {
 
 // All microseconds on the device, operands in the caches.  256x256 tiles where they keep most of the 256 compute units busy, sooner with a bf16
 // output, whose k-tiles are half as long: 1700 x 6000 x 2000 (168 tiles) 28.7 against 37.5 on smaller ones, 3000 x 3000 x 1000 (144) 20.4 / 20.1, 2048 x
-// 4096 x 4096 (128) 45 / 39; float32 3000 x 3000 x 1000 33.6 / 28.8, 2472 x 4096 x 2700 (160) 65.3 / 65.3.
+// 4096 x 4096 (128) 45 / 39; float32 3000 x 3000 x 1000 33.6 / 28.8, 2472 x 4096 x 2700 (160) 65.3 / 65.3;
+// short contractions with a float32 output, which are all stores: 4096 x 8192 x 64 42 / 33, 256 45 / 40, 512 57 / 54, 784 68 / 75.
 // A long contraction on few tiles is split: 714 x 174 x 4096 10.5 in 4 parts, 12.5 on 32x32 tiles in one; 1000 x 512 x 8192 20.6 / 29; 451 x 453 x 4096
 // 10.0 / 10.6; but 192 x 128 x 2048 7.5 / 7.5 and below that one launch is faster.
 // Otherwise the smallest tiles that leave each compute unit one workgroup: 32x32 against 32x64 and 64x64 on 226 x 679 x 837 (176 tiles) 4.5 / 5.1 / 5.8, 462 x 1024 x
@@ -690,7 +706,7 @@ bool few_rows(int M, int N, int K) {
 Shape shape_of(int M, int N, int K, int dtype) {
   const int nk = (K + 127) / 128;
   if (few_rows(M, N, K)) return kRows;
-  if (K > 0 && tiles_of(M, N, 256, 256) >= (dtype == 1 ? 144 : 192)) return kBig;
+  if (K > (dtype == 1 ? 0 : 256) && tiles_of(M, N, 256, 256) >= (dtype == 1 ? 144 : 192)) return kBig;
   if (nk >= 28 && tiles_of(M, N, 64, 64) <= 256) return kSplit;
   if (tiles_of(M, N, 32, 32) <= 256) return k32;
   if (tiles_of(M, N, 32, 64) <= 256) return k32x64;
