@@ -138,15 +138,23 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t amax) {
   const int e = (int)((amax + 0x1FFFFFu) >> 23) - 8;
   return amax >= 0x7F800000u ? 255u : (uint32_t)(e > 0 ? e : 0);
 }
-// 2^-e; NaN for the scale 255
-__device__ __forceinline__ float inverse_scale(uint32_t scale) {
-  return __builtin_bit_cast(float, scale == 255u ? 0x7FC00000u : (254u - scale) << 23);
+// The scale as the conversions take it, which read its exponent's bits.
+__device__ __forceinline__ float scale_value(uint32_t scale) { return __builtin_bit_cast(float, scale << 23); }
+// Values over their scale to e4m3, round to nearest even.  None is above 448, so nothing saturates.
+typedef __attribute__((ext_vector_type(2))) short i16x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d, float scale) {
+  i16x2 o = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(i16x2{0, 0}, a, b, scale, false);
+  o = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(o, c, d, scale, true);
+  return __builtin_bit_cast(uint32_t, o);
 }
-// Four values to e4m3, round to nearest even.  None is above 448 after scaling, so nothing saturates.
-__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) {
-  int o = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  o = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, o, true);
-  return (uint32_t)o;
+__device__ __forceinline__ uint32_t to_e4m3(uint32_t ab, uint32_t cd, float scale) {        // pairs of bf16
+  i16x2 o = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(i16x2{0, 0}, __builtin_bit_cast(bf16x2, ab), scale, false);
+  o = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(o, __builtin_bit_cast(bf16x2, cd), scale, true);
+  return __builtin_bit_cast(uint32_t, o);
+}
+__device__ __forceinline__ u32x2 to_e4m3(const float (&v)[8], float scale) {
+  return u32x2{to_e4m3(v[0], v[1], v[2], v[3], scale), to_e4m3(v[4], v[5], v[6], v[7], scale)};
 }
 
 }  // namespace

@@ -23,9 +23,7 @@ __device__ __forceinline__ void finish_chunk(const NormArgs& a, int64_t row, int
   if (a.y) store8((T*)a.y + row * a.ldy + 8 * c, D - 8 * c, v);
   if (a.q) {
     const uint32_t scale = scale_of(max_of_16(amax));
-    const float up = inverse_scale(scale);
-    if (8 * c < ((D + 15) & ~15))                         // zeros up to the next 16 bytes
-      *(u32x2*)(a.q + row * a.ldq + 8 * c) = u32x2{to_e4m3(v[0] * up, v[1] * up, v[2] * up, v[3] * up), to_e4m3(v[4] * up, v[5] * up, v[6] * up, v[7] * up)};
+    if (8 * c < ((D + 15) & ~15)) *(u32x2*)(a.q + row * a.ldq + 8 * c) = to_e4m3(v, scale_value(scale));      // zeros up to the next 16 bytes
     if ((threadIdx.x & 15) == 0 && 8 * c < D) a.scales[row * a.lds + c / 16] = (uint8_t)scale;
   }
 }

@@ -31,8 +31,6 @@ constexpr uint32_t kOutOfRange = 0x80000000u;     // byte offset past the end of
 #define SLP_VMCNT(n) ((((n) & 15) | 0x0F70 | (((n) >> 4) << 14)))
 #define SLP_VMCNT_LGKM0(n) (SLP_VMCNT(n) & 0xF0FF)
 
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-
 // A lane's 32 values of a fragment and the scale of its row, as either form takes them.
 template <bool EXACT> struct Fragment;
 template <> struct Fragment<false> {
@@ -46,7 +44,7 @@ template <> struct Fragment<false> {
 template <> struct Fragment<true> {
   bf16x8 v[4];
   __device__ __forceinline__ void set(const i32x8& bytes, int s) {
-    const float scale = __builtin_bit_cast(float, s << 23);       // the conversion reads the exponent's bits
+    const float scale = scale_value((uint32_t)s);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)bytes[i], scale, false);
@@ -517,7 +515,7 @@ __global__ __launch_bounds__(256) void product_long_kernel(const ProductArgs g) 
   // conversion e of the 8 of a fragment: 2 values, with their scale (the instruction reads its exponent's bits)
   auto convert = [&](const u32x4& raw, int scale, bf16x8 (&to)[2], auto ec) {
     constexpr int e = decltype(ec)::value;
-    const bf16x2 v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[e / 2], __builtin_bit_cast(float, scale << 23), e % 2 == 1);
+    const bf16x2 v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[e / 2], scale_value((uint32_t)scale), e % 2 == 1);
     to[e / 4][2 * (e % 4)] = v[0];
     to[e / 4][2 * (e % 4) + 1] = v[1];
   };

@@ -6,6 +6,69 @@
 namespace slp {
 namespace {
 
+// The steps on 8 elements of a row, two bf16 elements an instruction where there is one for it.  Magnitudes are compared as integers, which order like
+// the values; kMags registers hold those of the columns.
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+template <typename T> constexpr int kMags = sizeof(T) == 2 ? 4 : 8;
+__device__ __forceinline__ uint32_t word(const Raw<bf16>& v, int i) { return __builtin_bit_cast(u32x4, v.v)[i]; }
+__device__ __forceinline__ u16x2 halves(uint32_t w) { return __builtin_bit_cast(u16x2, w); }
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(halves(a), halves(b))); }
+
+// zero where m is not > 0
+__device__ __forceinline__ void keep_positive(Raw<bf16>& v, const Raw<bf16>& m) {
+  u32x4 o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    // as integers the positive values and infinity are 1 .. 0x7F80: all ones where 0x7F80 - (m - 1), stopped at zero, is not zero
+    u16x2 d = __builtin_elementwise_sub_sat(u16x2{0x7F80, 0x7F80}, halves(word(m, i)) - u16x2{1, 1});
+    d = u16x2{0, 0} - __builtin_elementwise_min(d, u16x2{1, 1});
+    o[i] = word(v, i) & __builtin_bit_cast(uint32_t, d);
+  }
+  v.v = __builtin_bit_cast(bf16x8, o);
+}
+__device__ __forceinline__ void keep_positive(Raw<float>& v, const Raw<float>& m) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (!(m.v[j / 4][j % 4] > 0.0f)) v.v[j / 4][j % 4] = 0.0f;
+}
+// largest magnitude of the 8 elements; columns' raised to theirs
+__device__ __forceinline__ uint32_t magnitudes(const Raw<bf16>& v, uint32_t (&columns)[4]) {
+  uint32_t all = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t m = word(v, i) & 0x7FFF7FFFu;
+    columns[i] = max_halves(columns[i], m);
+    all = max_halves(all, m);
+  }
+  return umax(all & 0xFFFF0000u, all << 16);
+}
+__device__ __forceinline__ uint32_t magnitudes(const Raw<float>& v, uint32_t (&columns)[8]) {
+  uint32_t all = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t m = magnitude(item(v, j));
+    columns[j] = umax(columns[j], m);
+    all = umax(all, m);
+  }
+  return all;
+}
+__device__ __forceinline__ uint32_t column(const uint32_t (&columns)[4], int j) { return j & 1 ? columns[j / 2] & 0xFFFF0000u : columns[j / 2] << 16; }
+__device__ __forceinline__ uint32_t column(const uint32_t (&columns)[8], int j) { return columns[j]; }
+__device__ __forceinline__ u32x2 row_e4m3(const Raw<bf16>& v, float scale) {
+  return u32x2{to_e4m3(word(v, 0), word(v, 1), scale), to_e4m3(word(v, 2), word(v, 3), scale)};
+}
+__device__ __forceinline__ u32x2 row_e4m3(const Raw<float>& v, float scale) {
+  return u32x2{to_e4m3(v.v[0][0], v.v[0][1], v.v[0][2], v.v[0][3], scale), to_e4m3(v.v[1][0], v.v[1][1], v.v[1][2], v.v[1][3], scale)};
+}
+// element j of four rows
+__device__ __forceinline__ uint32_t column_e4m3(const Raw<bf16> (&v)[4], int j, float scale) {
+  const uint32_t pick = j & 1 ? 0x07060302u : 0x05040100u;          // the high or the low half of both words
+  return to_e4m3(__builtin_amdgcn_perm(word(v[1], j / 2), word(v[0], j / 2), pick), __builtin_amdgcn_perm(word(v[3], j / 2), word(v[2], j / 2), pick), scale);
+}
+__device__ __forceinline__ uint32_t column_e4m3(const Raw<float> (&v)[4], int j, float scale) {
+  return to_e4m3(item(v[0], j), item(v[1], j), item(v[2], j), item(v[3], j), scale);
+}
+
 // Row-major alone, a scale for each 128 elements of a row: a chunk of 8 elements a lane, 16 lanes a scale, a workgroup 16 scales.
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs a) {
@@ -14,22 +77,16 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs a
   const int64_t row = at / blocks;
   const int b = (int)(at % blocks), c = b * 128 + (threadIdx.x & 15) * 8, left = a.cols - c;
   if (row >= a.rows) return;           // (16 lanes together)
-  float v[8];
-  load8((const T*)a.x + row * a.ldx + c, left, v);
+  Raw<T> v;
+  fetch8((const T*)a.x + row * a.ldx + c, left, v);
   if (a.mask) {
-    float m[8];
-    load8((const T*)a.mask + row * a.ldmask + c, left, m);
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (!(m[j] > 0.0f)) v[j] = 0.0f;
+    Raw<T> m;
+    fetch8((const T*)a.mask + row * a.ldmask + c, left, m);
+    keep_positive(v, m);
   }
-  uint32_t amax = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) amax = umax(amax, magnitude(v[j]));
-  const uint32_t scale = scale_of(max_of_16(amax));
-  const float up = inverse_scale(scale);
-  if (c < ((a.cols + 15) & ~15))
-    *(u32x2*)(a.q + row * a.ldq + c) = u32x2{to_e4m3(v[0] * up, v[1] * up, v[2] * up, v[3] * up), to_e4m3(v[4] * up, v[5] * up, v[6] * up, v[7] * up)};
+  uint32_t columns[kMags<T>] = {};
+  const uint32_t scale = scale_of(max_of_16(magnitudes(v, columns)));
+  if (c < ((a.cols + 15) & ~15)) *(u32x2*)(a.q + row * a.ldq + c) = row_e4m3(v, scale_value(scale));
   if ((threadIdx.x & 15) == 0) a.scales[row * a.lds + b] = (uint8_t)scale;
 }
 
@@ -39,52 +96,45 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs a
 template <typename T, int BLOCK>
 __global__ __launch_bounds__(512) void quantize_tile_kernel(const QuantizeArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t turned[128 * 128];
-  __shared__ uint32_t cmax[8][128];
-  __shared__ float csum[8][128];
+  __shared__ __attribute__((aligned(16))) uint32_t cmax[8][128];
+  __shared__ __attribute__((aligned(16))) float csum[8][128];
   const int t = threadIdx.x, wave = t >> 6, g = t >> 4, cc = t & 15;
   const int tilesM = (a.rows + 127) / 128, tilesN = (a.cols + 127) / 128;
   const int64_t tm = blockIdx.x / tilesN;
   const int tn = blockIdx.x % tilesN;
   const int64_t m0 = tm * 128;
   const int c0 = tn * 128 + cc * 8, left = a.cols - c0;
-  float v[4][8];
+  Raw<T> v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int64_t row = m0 + 4 * g + i;
-    load8((const T*)a.x + row * a.ldx + c0, row < a.rows ? left : 0, v[i]);
+    fetch8((const T*)a.x + row * a.ldx + c0, row < a.rows ? left : 0, v[i]);
   }
   if (a.mask) {
-    float m[4][8];
+    Raw<T> m[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int64_t row = m0 + 4 * g + i;
-      load8((const T*)a.mask + row * a.ldmask + c0, row < a.rows ? left : 0, m[i]);
+      fetch8((const T*)a.mask + row * a.ldmask + c0, row < a.rows ? left : 0, m[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (!(m[i][j] > 0.0f)) v[i][j] = 0.0f;
+    for (int i = 0; i < 4; ++i) keep_positive(v[i], m[i]);
   }
   // largest magnitudes: of the rows (16 lanes each), of the columns (a thread's 4 rows, 4 lanes of a wavefront, 8 wavefronts)
-  uint32_t rmax[4] = {0, 0, 0, 0}, kmax[8];
+  uint32_t rmax[4], columns[kMags<T>] = {};
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    float sum = 0.0f;
-    kmax[j] = 0;
+  for (int i = 0; i < 4; ++i) rmax[i] = magnitudes(v[i], columns);
+  if (BLOCK == 128 || a.qt) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t m = magnitude(v[i][j]);
-      rmax[i] = umax(rmax[i], m);
-      kmax[j] = umax(kmax[j], m);
-      sum += v[i][j];
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t k = max_of_rows(column(columns, j));
+      if ((t & 63) < 16) cmax[wave][cc * 8 + j] = k;
     }
-    if (BLOCK == 128 || a.qt) {
-      kmax[j] = max_of_rows(kmax[j]);
-      if ((t & 63) < 16) cmax[wave][cc * 8 + j] = kmax[j];
-    }
-    if (a.sums) {
-      sum = sum_of_rows(sum);
+  }
+  if (a.sums) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float sum = sum_of_rows((item(v[0], j) + item(v[1], j)) + (item(v[2], j) + item(v[3], j)));
       if ((t & 63) < 16) csum[wave][cc * 8 + j] = sum;
     }
   }
@@ -110,11 +160,8 @@ __global__ __launch_bounds__(512) void quantize_tile_kernel(const QuantizeArgs a
     for (int i = 0; i < 4; ++i) {
       const int64_t row = m0 + 4 * g + i;
       const uint32_t scale = BLOCK == 128 ? all : scale_of(max_of_16(rmax[i]));
-      const float up = inverse_scale(scale);
       if (row < a.rows) {
-        if (c0 < ((a.cols + 15) & ~15))
-          *(u32x2*)(a.q + row * a.ldq + c0) = u32x2{to_e4m3(v[i][0] * up, v[i][1] * up, v[i][2] * up, v[i][3] * up),
-                                                   to_e4m3(v[i][4] * up, v[i][5] * up, v[i][6] * up, v[i][7] * up)};
+        if (c0 < ((a.cols + 15) & ~15)) *(u32x2*)(a.q + row * a.ldq + c0) = row_e4m3(v[i], scale_value(scale));
         if (BLOCK == 1 && cc == 0) a.scales[row * a.lds + tn] = (uint8_t)scale;
       }
     }
@@ -131,8 +178,7 @@ __global__ __launch_bounds__(512) void quantize_tile_kernel(const QuantizeArgs a
         scale = scale_of(k);
         if (g == 0 && c0 + j < a.cols) a.scales_t[(int64_t)(c0 + j) * a.ldst + tm] = (uint8_t)scale;
       }
-      const float up = inverse_scale(scale);
-      *(uint32_t*)(turned + c * 128 + (((g >> 2) ^ (cc & 7)) << 4) + (g & 3) * 4) = to_e4m3(v[0][j] * up, v[1][j] * up, v[2][j] * up, v[3][j] * up);
+      *(uint32_t*)(turned + c * 128 + (((g >> 2) ^ (cc & 7)) << 4) + (g & 3) * 4) = column_e4m3(v, j, scale_value(scale));
     }
     __syncthreads();
 #pragma unroll
