@@ -193,194 +193,73 @@ QuantizeResult = collections.namedtuple("QuantizeResult", "rows transposed colum
 NormResult = collections.namedtuple("NormResult", "h rstd y y8")
 
 
-_F8, _E8, _BF, _FL = torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.bfloat16, torch.float32
-_empty, _empty_like = torch.empty, torch.empty_like
+_native = None
 
 
-def _float_dtype(t):
-    """The library's number for a matrix's element type."""
-    if t.dtype is _BF:
-        return BF16
-    assert t.dtype is _FL, "float32 or bfloat16 (got %s)" % t.dtype
-    return F32
+def _binding():
+    """The compiled binding of the calls below, loaded once.  They take the device a few microseconds: checks, outputs and arguments put together
+    in Python would take the host more than that."""
+    global _native
+    if _native is None:
+        lib()                                    # (says what to do if nothing has been built)
+        from . import _binding as native
+        _native = native
+    return _native
 
 
-def _matrix(t):
-    """Leading dimension of a matrix on the device whose rows are contiguous."""
-    assert t.is_cuda and t.dim() == 2
-    ld, one = t.stride()
-    if one != 1 or ld < t.size(1):               # (a side of one element may have any stride)
-        m, n = t.shape
-        assert one == 1 or n <= 1, "rows must be contiguous"
-        if m <= 1 or ld == 1:
-            ld = max(ld, n)
-    return ld
-
-
-def _like(t, x):
-    """Leading dimension of a matrix of x's shape, type and place."""
-    assert t.dtype is x.dtype and t.shape == x.shape and t.device == x.device
-    return _matrix(t)
-
-
-def _vector(t, n):
-    """Address of a contiguous float32 vector of n elements on the device, or None."""
-    if t is None:
-        return None
-    assert t.is_cuda and t.dtype is _FL and t.is_contiguous() and t.numel() == n
-    return t.data_ptr()
-
-
-def _room(rows, cols, block, device):
-    """empty_quantized's matrix, and (address, leading dimension) of its values and of its scales."""
-    ld = (cols + 127) & -128
-    if ld % 4096 == 0 and rows > 16:
-        ld += 128
-    blocks, srows = (cols + 127) >> 7, rows if block == 1 else (rows + 127) >> 7
-    lds = (blocks + 3) & -4
-    q = _empty((rows, ld), dtype=_F8, device=device)
-    scales = _empty((srows, lds), dtype=_E8, device=device)
-    at = (q.data_ptr(), ld, scales.data_ptr(), lds)
-    if ld != cols:
-        q = q.as_strided((rows, cols), (ld, 1))
-    if lds != blocks:
-        scales = scales.as_strided((srows, blocks), (lds, 1))
-    return Quantized(q, scales, block), at
+def _outputs(r):
+    """What the binding gives back: outputs, or the library's error code."""
+    if r.__class__ is int:
+        _check(r)
+    return r
 
 
 def empty_quantized(rows, cols, block=1, device="cuda"):
     """Room for a matrix in 8 bits: rows on 128-byte boundaries and, where there are many, not a multiple of 4 KB apart (they are read
     faster then)."""
-    return _room(rows, cols, block, device)[0]
-
-
-_NOTHING = (None, 0, None, 0)
-
-
-def _eight(m, rows, cols):
-    """(address, leading dimension) of the values and of the scales of a matrix in 8 bits."""
-    if m is None:
-        return _NOTHING
-    q, scales, block = m
-    assert q.is_cuda and q.dtype is _F8 and q.shape == (rows, cols) and scales.is_cuda and scales.dtype is _E8
-    assert scales.shape == (rows if block == 1 else (rows + 127) >> 7, (cols + 127) >> 7)
-    (ld, one), (lds, sone) = q.stride(), scales.stride()
-    assert (one == 1 or cols <= 1) and (sone == 1 or cols <= 128), "rows must be contiguous"
-    return q.data_ptr(), ld, scales.data_ptr(), lds
+    ld, blocks, srows = (cols + 127) & -128, (cols + 127) >> 7, -(-rows // block)
+    if ld % 4096 == 0 and rows > 16:
+        ld += 128
+    lds = (blocks + 3) & -4
+    q = torch.empty((rows, ld), dtype=torch.float8_e4m3fn, device=device)
+    scales = torch.empty((srows, lds), dtype=torch.float8_e8m0fnu, device=device)
+    return Quantized(q.as_strided((rows, cols), (ld, 1)), scales.as_strided((srows, blocks), (lds, 1)), block)
 
 
 def quantize(x, block=1, rows=True, transposed=False, mask=None, column_sums=False):
     """slp_quantize: x in 8 bits, row-major (`rows`) and transposed as asked, with a scale for each 128 elements of a row of the
     result (block=1) or each 128 x 128 block (block=128).  Elements whose `mask` is not positive count as zero; column_sums: also
     the sums of x's (masked) columns."""
-    ldx, dt, (m, n), device, L = _matrix(x), _float_dtype(x), x.shape, x.device, lib()
-    ldmask = _like(mask, x) if mask is not None else 0
-    r, at_r = _room(m, n, block, device) if rows else (None, _NOTHING)
-    t, at_t = _room(n, m, block, device) if transposed else (None, _NOTHING)
-    sums = work = None
-    size = 0
-    if column_sums:
-        sums = _empty(n, dtype=_FL, device=device)
-        size = L.slp_quantize_workspace_bytes(m, n)
-        work = _empty(size, dtype=torch.uint8, device=device) if size else None
-    code = L.slp_quantize(x.data_ptr(), ldx, _ptr(mask), ldmask, dt, m, n, block, *at_r, *at_t, _ptr(sums), _ptr(work), size, _stream())
-    if code:
-        _check(code)
-    return QuantizeResult(r, t, sums)
+    q, s, qt, st, sums = _outputs(_binding().quantize(x, block, rows, transposed, mask, column_sums, _stream()))
+    return QuantizeResult(Quantized(q, s, block) if rows else None, Quantized(qt, st, block) if transposed else None, sums)
 
 
 def product(a, b, bias=None, relu=False, dtype=BF16, out=None):
     """slp_product: act(a b^T + bias) of two Quantized matrices with the same number of columns, as a matrix of `dtype` (or into
     `out`, whose type decides then)."""
-    (m, k), n, L = a[0].shape, b[0].size(0), lib()
-    if out is None:
-        out, ldo = _empty((m, n), dtype=_BF if dtype == BF16 else _FL, device=a[0].device), n
-    else:
-        assert out.shape == (m, n)
-        ldo, dtype = _matrix(out), _float_dtype(out)
-    at_a, at_b = _eight(a, m, k), _eight(b, n, k)
-    size = L.slp_product_workspace_bytes(m, n, k)
-    work = _empty(size, dtype=torch.uint8, device=out.device) if size else None
-    code = L.slp_product(*at_a, a[2], *at_b, b[2], _vector(bias, n), 1 if relu else 0, m, n, k, out.data_ptr(), ldo, dtype, _ptr(work), size, _stream())
-    if code:
-        _check(code)
-    return out
+    return _outputs(_binding().product(a[0], a[1], a[2], b[0], b[1], b[2], bias, relu, dtype, out, _stream()))
 
 
 def rmsnorm(x, gamma=None, residual=None, eps=1e-6, normed=False, quantized=True):
     """slp_rmsnorm: h = x + residual (x itself without one), rstd, the norm y in x's type if `normed`, and y8 in 8 bits if `quantized`."""
-    ldx, dt, (m, n), device = _matrix(x), _float_dtype(x), x.shape, x.device
-    h, ldr, to = x, 0, None
-    if residual is not None:
-        ldr = _like(residual, x)
-        h = _empty_like(x) if ldx == n else _empty((m, n), dtype=x.dtype, device=device)
-        to = h.data_ptr()
-    y = _empty((m, n), dtype=x.dtype, device=device) if normed else None
-    y8, at = _room(m, n, 1, device) if quantized else (None, _NOTHING)
-    rstd = _empty(m, dtype=_FL, device=device)
-    code = lib().slp_rmsnorm(x.data_ptr(), ldx, _ptr(residual), ldr, _vector(gamma, n), eps, dt, m, n, to, n, _ptr(y), n, *at, rstd.data_ptr(), _stream())
-    if code:
-        _check(code)
-    return NormResult(h, rstd, y, y8)
+    h, rstd, y, q, s = _outputs(_binding().rmsnorm(x, gamma, residual, eps, normed, quantized, _stream()))
+    return NormResult(h, rstd, y, Quantized(q, s, 1) if quantized else None)
 
 
 def rmsnorm_backward(dy, h, gamma, rstd, dh=None, gamma_grad=True):
     """slp_rmsnorm_backward: (the gradient of x and of the residual, the gradient of gamma or None)."""
-    ldh, dt, (m, n), device, L = _matrix(h), _float_dtype(h), h.shape, h.device, lib()
-    lddy, lddh = _like(dy, h), _like(dh, h) if dh is not None else 0
-    dx = _empty((m, n), dtype=h.dtype, device=device)
-    dgamma = _empty(n, dtype=_FL, device=device) if gamma_grad else None
-    size = L.slp_rmsnorm_backward_workspace_bytes(m, n)
-    work = _empty(size, dtype=torch.uint8, device=device) if size else None
-    code = L.slp_rmsnorm_backward(dy.data_ptr(), lddy, h.data_ptr(), ldh, _vector(gamma, n), _vector(rstd, m), _ptr(dh), lddh, dt, m, n, dx.data_ptr(), n,
-                                  _ptr(dgamma), _ptr(work), size, _stream())
-    if code:
-        _check(code)
-    return dx, dgamma
-
-
-_tables = {}
-
-
-def _table(n):
-    """The ctypes arrays of a list of n tensors: (addresses, sizes, types) as C types, made once for each n."""
-    if n not in _tables:
-        _tables[n] = ctypes.c_void_p * n, ctypes.c_int64 * n, ctypes.c_int * n
-    return _tables[n]
-
-
-def _tensor_list(tensors):
-    n = len(tensors)
-    assert n > 0 and all(t.is_cuda and t.is_contiguous() for t in tensors)
-    addresses, sizes, types = _table(n)
-    return addresses(*[t.data_ptr() for t in tensors]), sizes(*[t.numel() for t in tensors]), types(*[_float_dtype(t) for t in tensors]), n
+    return _outputs(_binding().rmsnorm_backward(dy, h, gamma, rstd, dh, gamma_grad, _stream()))
 
 
 def gradient_norm(tensors):
     """slp_gradient_norm: the norm of all tensors' values together, as a device scalar."""
-    (ptrs, counts, dts, n), device, L = _tensor_list(tensors), tensors[0].device, lib()
-    norm = _empty((), dtype=_FL, device=device)
-    size = L.slp_gradient_norm_workspace_bytes(n)
-    work = _empty(size, dtype=torch.uint8, device=device)
-    _check(L.slp_gradient_norm(ptrs, counts, dts, n, norm.data_ptr(), work.data_ptr(), size, _stream()))
-    return norm
+    return _outputs(_binding().gradient_norm(tensors, _stream()))
 
 
 def clip_gradients(tensors, max_norm, out=None):
     """slp_clip_gradients: scales the tensors together to a norm of at most max_norm, in place or into `out` (tensors of the same
     sizes and types).  Returns the norm before, a device scalar; where it is not finite the values are left as they are."""
-    (ptrs, counts, dts, n), device, L = _tensor_list(tensors), tensors[0].device, lib()
-    to = None
-    if out is not None:
-        assert len(out) == n and all(o.is_cuda and o.is_contiguous() and o.dtype is t.dtype and o.shape == t.shape for t, o in zip(tensors, out))
-        to = _table(n)[0](*[o.data_ptr() for o in out])
-    norm = _empty((), dtype=_FL, device=device)
-    size = L.slp_gradient_norm_workspace_bytes(n)
-    work = _empty(size, dtype=torch.uint8, device=device)
-    code = L.slp_clip_gradients(ptrs, to, counts, dts, n, max_norm, norm.data_ptr(), work.data_ptr(), size, _stream())
-    if code:
-        _check(code)
-    return norm
+    return _outputs(_binding().clip_gradients(tensors, max_norm, out, _stream()))
 
 
 class Segment:

@@ -1,4 +1,4 @@
-"""Builds libslp.so (the C-ABI library) in-tree with hipcc for gfx950.
+"""Builds libslp.so (the C-ABI library) in-tree with hipcc for gfx950, and _binding.so, the operators' binding to torch tensors.
 
     python -m paper_2403_11204_amd.build
 
@@ -17,6 +17,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libslp.so")
+BINDING = os.path.join(HERE, "_binding.so")
 BUILD = os.path.join(ROOT, "_build")
 
 COMMON = [
@@ -66,14 +67,43 @@ def _compile(unit, extra, verbose):
     return obj
 
 
+def _run(cmd, what, verbose):
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("%s failed:\n%s" % (what, r.stdout))
+
+
+def _compile_binding(verbose):
+    """The operators' way from torch tensors to the C ABI (csrc/binding.cpp), host code against torch's headers."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    obj = os.path.join(BUILD, "binding.o")
+    cmd = ["g++", "-std=c++17", "-O2", "-fPIC", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"]]
+    for path in cpp_extension.include_paths():
+        cmd += ["-isystem", path]
+    _run(cmd + ["-c", os.path.join(CSRC, "binding.cpp"), "-o", obj], "g++ on binding.cpp", verbose)
+    return obj
+
+
+def _link_binding(obj, verbose):
+    from torch.utils import cpp_extension
+    libs = [a for path in cpp_extension.library_paths() for a in ("-L", path)]
+    _run(["g++", "-shared", "-o", BINDING, obj, "-L", HERE, "-l:libslp.so", "-Wl,-rpath,$ORIGIN"] + libs + ["-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"], "linking _binding.so", verbose)
+
+
 def build(verbose=True):
     os.makedirs(BUILD, exist_ok=True)
     with ThreadPoolExecutor(max_workers=4) as ex:
+        binding = ex.submit(_compile_binding, verbose)
         objs = list(ex.map(lambda kv: _compile(kv[0], kv[1], verbose), UNITS.items()))
-    cmd = [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", OUT] + objs
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+        binding = binding.result()
+    _run([hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", OUT] + objs, "linking libslp.so", verbose)
+    _link_binding(binding, verbose)
     return OUT
 
 
