@@ -187,7 +187,8 @@ def mean_loss(losses, out=None):
 
 # ---- segments in 8 bits -----------------------------------------------------------------------------------------
 # A matrix in 8 bits: q [rows, cols] (float8_e4m3fn, rows on 16-byte boundaries), scales [rows / block, cols / 128] (both rounded up,
-# float8_e8m0fnu, rows on 4-byte boundaries), block 1 or 128 rows that share a scale.
+# float8_e8m0fnu, rows on 4-byte boundaries), block 1 or 128 rows that share a scale.  Between the last column and the next multiple of 16 the
+# values in memory are zeros: a slice of whole columns ends at a multiple of 128, or where the matrix does.
 Quantized = collections.namedtuple("Quantized", "q scales block")
 QuantizeResult = collections.namedtuple("QuantizeResult", "rows transposed column_sums")
 NormResult = collections.namedtuple("NormResult", "h rstd y y8")

@@ -64,11 +64,11 @@ int64_t like(const at::Tensor& t, const at::Tensor& x) {
   require(t.scalar_type() == x.scalar_type() && t.sizes() == x.sizes() && t.device() == x.device(), "matrices of one shape, type and device are wanted");
   return leading(t);
 }
-// A contiguous float32 vector of n elements on the device, or null for None.
-const float* vector(PyObject* o, int64_t n) {
+// A contiguous float32 vector of n elements beside x, or null for None.
+const float* vector(PyObject* o, int64_t n, const at::Tensor& x) {
   if (!given(o)) return nullptr;
   const at::Tensor& t = tensor(o);
-  require(t.is_cuda() && t.scalar_type() == at::kFloat && t.is_contiguous() && t.numel() == n, "a contiguous float32 vector on the device is wanted");
+  require(t.device() == x.device() && t.scalar_type() == at::kFloat && t.is_contiguous() && t.numel() == n, "a contiguous float32 vector on the same device is wanted");
   return (const float*)t.data_ptr();
 }
 
@@ -103,7 +103,7 @@ Eight eight_given(PyObject* q, PyObject* scales, int64_t block, int64_t cols) {
   e.scales = tensor(scales);
   require(block == 1 || block == 128, "blocks of 1 or 128 rows");
   require(e.q.is_cuda() && e.q.dim() == 2 && e.q.scalar_type() == at::kFloat8_e4m3fn && e.q.size(1) == cols, "values of float8_e4m3fn with as many columns are wanted");
-  require(e.scales.is_cuda() && e.scales.dim() == 2 && e.scales.scalar_type() == at::kFloat8_e8m0fnu && e.scales.size(0) == (e.q.size(0) + block - 1) / block &&
+  require(e.scales.device() == e.q.device() && e.scales.dim() == 2 && e.scales.scalar_type() == at::kFloat8_e8m0fnu && e.scales.size(0) == (e.q.size(0) + block - 1) / block &&
               e.scales.size(1) == (cols + 127) / 128,
           "scales of float8_e8m0fnu, one for each block, are wanted");
   require((e.q.stride(1) == 1 || cols <= 1) && (e.scales.stride(1) == 1 || cols <= 128), "rows must be contiguous");
@@ -177,7 +177,7 @@ PyObject* product(PyObject* const* a) {
   }
   const size_t size = slp_product_workspace_bytes(side(m), side(n), side(cols));
   const at::Tensor work = bytes(size, x.q.device());
-  const int rc = slp_product(x.at, x.ld, x.scales_at, x.lds, (int)ablock, y.at, y.ld, y.scales_at, y.lds, (int)bblock, vector(a[6], n), truth(a[7]), side(m), side(n),
+  const int rc = slp_product(x.at, x.ld, x.scales_at, x.lds, (int)ablock, y.at, y.ld, y.scales_at, y.lds, (int)bblock, vector(a[6], n, x.q), truth(a[7]), side(m), side(n),
                              side(cols), out.data_ptr(), ldo, dt, address(work), size, PyLong_AsVoidPtr(a[10]));
   if (rc) return code(rc);
   return wrapped(out);
@@ -188,7 +188,7 @@ PyObject* rmsnorm(PyObject* const* a) {
   const at::Tensor& x = tensor(a[0]);
   const int64_t ldx = leading(x), m = x.size(0), n = x.size(1);
   const int dt = dtype_of(x);
-  const float* gamma = vector(a[1], n);
+  const float* gamma = vector(a[1], n, x);
   at::Tensor h = x, y;
   const void* r = nullptr;
   void* to = nullptr;
@@ -220,7 +220,7 @@ PyObject* rmsnorm_backward(PyObject* const* a) {
     dh = tensor(a[4]).data_ptr();
   }
   require(given(a[3]), "rstd of the forward pass is wanted");
-  const float *gamma = vector(a[2], n), *rstd = vector(a[3], m);
+  const float *gamma = vector(a[2], n, h), *rstd = vector(a[3], m, h);
   const at::Tensor dx = room({m, n}, h.scalar_type(), h.device());
   at::Tensor dgamma;
   if (truth(a[5])) dgamma = room({n}, at::kFloat, h.device());

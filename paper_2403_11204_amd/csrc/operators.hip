@@ -12,7 +12,7 @@ namespace {
 constexpr int kMaxSide = 1 << 24;
 constexpr int64_t kMaxRow8 = 1 << 22;      // bytes of an 8-bit row: a tile of 256 rows is addressed with 32-bit offsets
 constexpr int64_t kMaxLd = (int64_t)1 << 40;
-constexpr int64_t kMaxElements = (int64_t)1 << 40;      // of a matrix: the grids are 31 bits wide
+constexpr int64_t kMaxElements = (int64_t)1 << 34;      // of a matrix: a grid has fewer than 2^32 threads
 
 bool known(int dt) { return dt == SLP_F32 || dt == SLP_BF16; }
 size_t size_of(int dt) { return dt == SLP_BF16 ? 2 : 4; }
@@ -166,6 +166,8 @@ int slp_product(const void* a, int64_t lda, const void* a_scales, int64_t ldsa, 
   if (K > 0) {
     SLP_CHECK(check_eight(who, "a", a, lda, a_scales, ldsa, K));
     SLP_CHECK(check_eight(who, "b", b, ldb, b_scales, ldsb, K));
+  } else {
+    lda = ldsa = ldb = ldsb = 0;       // unchecked, and the kernels' bounds are made of them
   }
   if (bias && off(bias, 4)) return fail(SLP_ERR_ALLOC, "%s: bias is not on an element's boundary", who);
   SLP_CHECK(check_work(who, workspace, workspace_bytes, slp_product_workspace_bytes(M, N, K)));

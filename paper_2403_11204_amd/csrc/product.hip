@@ -695,7 +695,9 @@ bool few_rows(int M, int N, int K) {
 // All microseconds on the device, operands in the caches.  256x256 tiles where they keep most of the 256 compute units busy, sooner with a bf16
 // output, whose k-tiles are half as long: 1700 x 6000 x 2000 (168 tiles) 28.7 against 37.5 on smaller ones, 3000 x 3000 x 1000 (144) 20.4 / 20.1, 2048 x
 // 4096 x 4096 (128) 45 / 39; float32 3000 x 3000 x 1000 33.6 / 28.8, 2472 x 4096 x 2700 (160) 65.3 / 65.3;
-// short contractions with a float32 output, which are all stores: 4096 x 8192 x 64 42 / 33, 256 45 / 40, 512 57 / 54, 784 68 / 75.
+// short contractions with a float32 output, which are all stores: 4096 x 8192 x 64 42 / 33, 256 45 / 40, 512 57 / 54, 784 68 / 75;
+// and not where most of a tile would lie past a side (60000 rows, 1024 k): 10 columns 26.6 / 12.1, float32 38.6 / 13.9, 100 columns 30.6 / 17.3, 34.5 / 22.8; 200
+// columns 22.8 / 28.8, 35.0 / 40.3.
 // A long contraction on few tiles is split: 714 x 174 x 4096 10.5 in 4 parts, 12.5 on 32x32 tiles in one; 1000 x 512 x 8192 20.6 / 29; 451 x 453 x 4096
 // 10.0 / 10.6; but 192 x 128 x 2048 7.5 / 7.5 and below that one launch is faster.
 // Otherwise the smallest tiles that leave each compute unit one workgroup: 32x32 against 32x64 and 64x64 on 226 x 679 x 837 (176 tiles) 4.5 / 5.1 / 5.8, 462 x 1024 x
@@ -706,7 +708,7 @@ bool few_rows(int M, int N, int K) {
 Shape shape_of(int M, int N, int K, int dtype) {
   const int nk = (K + 127) / 128;
   if (few_rows(M, N, K)) return kRows;
-  if (K > (dtype == 1 ? 0 : 256) && tiles_of(M, N, 256, 256) >= (dtype == 1 ? 144 : 192)) return kBig;
+  if ((M < N ? M : N) > 128 && K > (dtype == 1 ? 0 : 256) && tiles_of(M, N, 256, 256) >= (dtype == 1 ? 144 : 192)) return kBig;
   if (nk >= 28 && tiles_of(M, N, 64, 64) <= 256) return kSplit;
   if (tiles_of(M, N, 32, 32) <= 256) return k32;
   if (tiles_of(M, N, 32, 64) <= 256) return k32x64;

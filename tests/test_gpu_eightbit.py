@@ -405,3 +405,24 @@ def test_another_stream_repetition_and_capture():
         torch.cuda.synchronize()
         got = [t.clone() for t in held]
         assert all(torch.equal(a, b) for a, b in zip(got, everything(x, r, gamma, w, dy)))
+
+
+# ---- outputs of a few columns for many rows, and contractions of nothing ----------------------------------------------
+@pytest.mark.parametrize("m,n", [(37000, 10), (37000, 100), (37000, 128), (37000, 129), (10, 37000)])
+def test_narrow_products_of_many_rows(m, n):
+    k = 300
+    a = api.quantize(torch.randint(-4, 5, (m, k), device=DEV).float()).rows
+    b = api.quantize(torch.randint(-4, 5, (n, k), device=DEV).float(), block=128).rows
+    ref = _dequantized(a) @ _dequantized(b).t().contiguous()         # integers below 2^13
+    assert torch.equal(api.product(a, b, dtype=api.F32).double(), ref)
+    assert torch.equal(api.product(a, b).double(), ref.to(torch.bfloat16).double())
+
+
+@pytest.mark.parametrize("m,n", [(3, 40), (300, 40), (100, 2000)])
+def test_a_contraction_of_nothing_reads_nothing_whatever_its_leading_dimensions(m, n):
+    out = torch.full((m, n), 7.0, device=DEV)
+    bias = torch.arange(n, device=DEV).float()
+    need = api.lib().slp_product_workspace_bytes(m, n, 0)
+    assert need == 0
+    rc = api.lib().slp_product(None, -31, None, -7, 1, None, -(1 << 33), None, 5, 128, bias.data_ptr(), 0, m, n, 0, out.data_ptr(), n, api.F32, None, 0, api._stream())
+    assert rc == 0 and torch.equal(out, bias.expand(m, n))
