@@ -103,13 +103,16 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, int64_t
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00020000);
 }
 
-// BM x BN tile, 4 wavefronts in a 2 x 2 grid, NS LDS stages of a k-tile of 128 each, one barrier a k-tile.  blockIdx.y: part of the
-// contraction (kper k-tiles each); several parts leave float32 partial products for join_kernel.
-template <int BM, int BN, int NS, bool EXACT>
-__global__ __launch_bounds__(256) void product_tile_kernel(const ProductArgs g, int kper) {
+// BM x BN tile, 4 wavefronts in a 2 x 2 grid, NS LDS stages of a k-tile of 128 each, one barrier a k-tile.  NG such groups of wavefronts
+// take a part of the contraction each (kper k-tiles) and are added up in order at the end.  blockIdx.y: part of the contraction of a whole workgroup;
+// several parts leave float32 partial products for join_kernel.
+template <int BM, int BN, int NS, int NG, bool EXACT>
+__global__ __launch_bounds__(256 * NG) void product_tile_kernel(const ProductArgs g, int kper) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  extern __shared__ __attribute__((aligned(16))) unsigned char all_smem[];
   constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128, SCALES = NS * STAGE;        // behind the stages a ring of two groups of scales
+  const int group = NG > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
+  unsigned char* const smem = all_smem + group * (SCALES + 2048);
   constexpr int LA = BM / 32, LB = BN / 32, NLD = LA + LB;                               // loads a lane per k-tile
   constexpr int MI = BM / 32, NI = BN / 32;
   constexpr int AW = (BM + 63) / 64, BW = (BN + 63) / 64;                                // wavefronts that load A's and B's scales
@@ -123,10 +126,10 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const ProductArgs g, 
   constexpr int kGroup = 8;
   const int width = kGroup * tilesN, first = tid / width * kGroup, rows = tilesM - first < kGroup ? tilesM - first : kGroup;
   const int m0 = (first + tid % width % rows) * BM, n0 = tid % width / rows * BN;
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6, wm = w & 1, wn = w >> 1, lgrp = lane >> 4, lrow = lane & 15;
+  const int t = threadIdx.x & 255, lane = t & 63, w = t >> 6, wm = w & 1, wn = w >> 1, lgrp = lane >> 4, lrow = lane & 15;
 
   const int nk = (g.K + 127) / 128, Kr = (g.K + 15) & ~15;
-  const int k0 = blockIdx.y * kper, k1 = k0 + kper < nk ? k0 + kper : nk;
+  const int k0 = (blockIdx.y * NG + group) * kper, k1 = k0 + kper < nk ? k0 + kper : nk;
   const int ra = g.M - m0 < BM ? g.M - m0 : BM, rb = g.N - n0 < BN ? g.N - n0 : BN;        // rows of the tile that exist
   const __amdgpu_buffer_rsrc_t rsrcA = rsrc_of(g.a + (int64_t)m0 * g.lda, (ra - 1) * g.lda + Kr);
   const __amdgpu_buffer_rsrc_t rsrcB = rsrc_of(g.b + (int64_t)n0 * g.ldb, (rb - 1) * g.ldb + Kr);
@@ -173,7 +176,7 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const ProductArgs g, 
 
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s) load(k0 + s, s);
-  for (int kt = k0; kt < k1; ++kt) {
+  for (int kt = k0; kt < (NG > 1 ? k0 + kper : k1); ++kt) {
     // this wavefront's part of k-tile kt has landed and its reads of the last one are done; behind the barrier, everybody's
     __builtin_amdgcn_s_waitcnt(SLP_VMCNT_LGKM0((NS - 2) * NLD));
     asm volatile("" ::: "memory");
@@ -181,6 +184,7 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const ProductArgs g, 
     asm volatile("" ::: "memory");
     const int step = kt - k0;
     load(kt + NS - 1, (step + NS - 1) % NS);
+    if (NG > 1 && kt >= k1) continue;            // (a shorter part takes the others' barriers)
     const unsigned char* const st = smem + step % NS * STAGE;
     const unsigned char* const sc = smem + (kt & 4) * 256 + (kt & 3);
     Fragment<EXACT> a[MI], b[NI];
@@ -198,6 +202,21 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const ProductArgs g, 
       for (int j = 0; j < NI; ++j) acc[i][j] = mma(b[j], a[i], acc[i][j]);
   }
   __builtin_amdgcn_s_waitcnt(SLP_VMCNT(0));      // no load into LDS may outlive the workgroup
+  if constexpr (NG > 1) {
+    // the other groups' sums, 16 bytes of each lane side by side
+    __syncthreads();
+    f32x4* const sums = (f32x4*)all_smem + t;
+    if (group > 0) {
+#pragma unroll
+      for (int i = 0; i < MI * NI; ++i) sums[((group - 1) * MI * NI + i) * 256] = acc[i / NI][i % NI];
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int v = 0; v < NG - 1; ++v)
+#pragma unroll
+      for (int i = 0; i < MI * NI; ++i) acc[i / NI][i % NI] += sums[(v * MI * NI + i) * 256];
+  }
 
 #pragma unroll
   for (int j = 0; j < NI; ++j) {
@@ -221,9 +240,9 @@ __global__ __launch_bounds__(256) void product_tile_kernel(const ProductArgs g, 
 // Few rows (a request's, a short last batch): bound by reading B once.  A workgroup takes 16 rows of B, its wavefronts take turns along the
 // contraction, STEP k-tiles at a time whose loads are all under way together, from memory straight into the fragments' registers; the parts are
 // added up in the order of the wavefronts.  MF fragments of 16 rows of A.  Both output types take the exact form: the conversions hide behind
-// the loads.  Microseconds on the device, this kernel / tiles with a split contraction and a second launch that joins the parts: 1 x 4096 x
-// 4096 5.2 / 8.4 (16.8 MB from caches at 6 TB/s behind 2.5 us of launch and latency), 1 x 16384 x 16384 47.5 / 50.8 (5.7 TB/s), 16 x 4096 x 4096
-// 7.1 / 9.0, 64 x 1024 x 1024 5.4 / 6.9.  32 rows of B a workgroup, which halves the reading of A: 7.0, 52.1, 9.0, -.
+// the loads.  Microseconds on the device, this kernel / tiles: 1 x 4096 x 4096 5.2 / 6.5 (16.8 MB from caches at 6 TB/s behind 2.5 us of launch and
+// latency), 4 x 16384 x 16384 50.3 / 55.6 (5.4 TB/s), 8 x 4096 x 4096 6.1 / 6.5.  32 rows of B a workgroup, which halves the reading of A: 1 x 4096 x
+// 4096 7.0, 1 x 16384 x 16384 52.1 (47.5 with 16).
 template <int MF, int STEP>
 __global__ __launch_bounds__(1024) void product_rows_kernel(const ProductArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -680,16 +699,16 @@ __global__ __launch_bounds__(256) void join_kernel(const ProductArgs g, int part
 int64_t tiles_of(int M, int N, int BM, int BN) { return (int64_t)((M + BM - 1) / BM) * ((N + BN - 1) / BN); }
 
 // Which kernel a product runs on.
-enum Shape { kRows, kBig, k128, k128x64, k64, k32x64, k32, kSplit };
+enum Shape { kRows, kBig, k128, k128x64, k64, k64by2, k32x64, k32x64by2, k32, k32by4, kSplit, kSplit32by4 };
 
 // Whether it is product_rows_kernel.  Its workgroups read A as often as there are 16 rows of B, and a compute unit reads 16 rows in 0.7 us per
-// 1024 k (1.2 with 16 rows of A, 3 with 64); tiles with a split contraction take a second launch, 3.5 us.
-// Microseconds, this / tiles: 1 x 2048 x 8192 8.1 / 9.2, 1 x 1000 x 16384 15.6 / 12.3, 1 x 8192 x 8192 13.4 / 15.8, 8 x 16384 x 16384 58 / 51, 16 x 4096 x 4096
-// 7.1 / 9.0, 16 x 512 x 8192 11.3 / 11.0, 32 x 4096 x 4096 9.9 / 9.5, 32 x 4096 x 1024 4.1 / 7.1, 64 x 4096 x 1024 5.5 / 7.7, 64 x 512 x 4096 15.3 / 8.8,
-// and against tiles in one launch 16 x 16384 x 1024 6.3 / 5.8, 32 x 16384 x 512 5.6 / 4.9.
+// 1024 k (1.2 with 16 rows of A).  Microseconds, this / tiles: 1 x 1000 x 784 2.9 / 3.9, 1 x 4096 x 8192 8.2 / 10.9, 4 x 512 x 8192 8.0 / 7.7, 1 x 1000 x
+// 16384 12.3 / 8.7, 12 x 4096 x 4096 6.6 / 6.5, 8 x 2048 x 8192 9.6 / 8.1, 16 x 1000 x 2000 4.5 / 4.9, 16 x 1000 x 4000 6.9 / 6.4, 32 x 4096 x 1024 4.1 / 4.3,
+// 32 x 1000 x 2000 5.7 / 5.0; with 4 fragments of A 40 x 1000 x 784 4.5 / 4.1, 64 x 64 x 256 3.6 / 3.0, 64 x 1000 x 784 4.8 / 4.1;
+// many columns 16 x 16384 x 1024 6.4 / 5.5, 32 x 16384 x 512 5.6 / 4.7.
 bool few_rows(int M, int N, int K) {
   if (M <= 4) return K <= 8192 || N >= 4096;
-  return M <= 64 && (int64_t)M * K <= 65536 && (N + 63) / 64 < 192;
+  return M <= 32 && (int64_t)M * K <= 32768 && (N + 63) / 64 < 192;
 }
 
 // All microseconds on the device, operands in the caches.  256x256 tiles where they keep most of the 256 compute units busy, sooner with a bf16
@@ -698,8 +717,12 @@ bool few_rows(int M, int N, int K) {
 // short contractions with a float32 output, which are all stores: 4096 x 8192 x 64 42 / 33, 256 45 / 40, 512 57 / 54, 784 68 / 75;
 // and not where most of a tile would lie past a side (60000 rows, 1024 k): 10 columns 26.6 / 12.1, float32 38.6 / 13.9, 100 columns 30.6 / 17.3, 34.5 / 22.8; 200
 // columns 22.8 / 28.8, 35.0 / 40.3.
-// A long contraction on few tiles is split: 714 x 174 x 4096 10.5 in 4 parts, 12.5 on 32x32 tiles in one; 1000 x 512 x 8192 20.6 / 29; 451 x 453 x 4096
-// 10.0 / 10.6; but 192 x 128 x 2048 7.5 / 7.5 and below that one launch is faster.
+// Where there is less than one tile for a compute unit, a k-tile's steps (barrier, LDS, conversion, product) wait for one another; two or four groups of
+// wavefronts with a part of the contraction each fill the gaps, as long as a part is long enough.  32x32 in one group / four: 300 x 300 x 1000 4.8 / 5.1, x 1400
+// 5.7 / 5.4, 200 x 800 x 3001 9.5 / 7.6, 714 x 174 x 4096 10.2 (split, two launches) / 8.3; 32x64 in one / two: 1000 x 512 x 500 4.7 / 5.2, x 800 5.9 / 5.6, x 2048 9.2
+// / 7.8, x 4096 15.8 (split) / 12.0; 64x64 in one / two: 1000 x 1000 x 500 5.9 / 6.3, x 800 7.3 / 6.9, x 4096 21.3 (split) / 15.7, bf16 16.8 / 10.8; 1200 x 1200 x 1500
+// (361 tiles) 11.9 / 12.5, x 3000 19.8 / 18.2, bf16 15.1 / 12.6.  A very long contraction is split over workgroups, too: 64 x 64 x 16384 in one / split 22.1 / 12.5, split
+// on 32x32 in four groups 9.8; 128 x 512 x 8192 12.8 / 11.5 / 9.3; 300 x 300 x 6200 (100 of these tiles) 11.5 / 12.0 / 10.8, 784 x 128 x 60000 (100) 86 / 31 / 50.
 // Otherwise the smallest tiles that leave each compute unit one workgroup: 32x32 against 32x64 and 64x64 on 226 x 679 x 837 (176 tiles) 4.5 / 5.1 / 5.8, 462 x 1024 x
 // 146 (480) 4.0 / 3.8 / 4.2, 618 x 1341 x 256 (840) 5.4 / 4.5 / 4.4.  Larger ones as soon as they fill the chip, of which a compute unit holds 4 (64x64), 3
 // (128x64) and 2 (128x128): 64x64 against 128x64 on 491 x 5192 x 24 (328 of the latter) 6.3 / 7.0, 392 x 4096 x 540 (256) 7.8 / 8.5, 436 x 8192 x 2512 (512) 20.1 /
@@ -709,31 +732,35 @@ Shape shape_of(int M, int N, int K, int dtype) {
   const int nk = (K + 127) / 128;
   if (few_rows(M, N, K)) return kRows;
   if ((M < N ? M : N) > 128 && K > (dtype == 1 ? 0 : 256) && tiles_of(M, N, 256, 256) >= (dtype == 1 ? 144 : 192)) return kBig;
-  if (nk >= 28 && tiles_of(M, N, 64, 64) <= 256) return kSplit;
-  if (tiles_of(M, N, 32, 32) <= 256) return k32;
-  if (tiles_of(M, N, 32, 64) <= 256) return k32x64;
+  const int64_t t64 = tiles_of(M, N, 64, 64), t32 = tiles_of(M, N, 32, 32);
+  if (nk >= 48 && t64 <= 256) return t32 <= 64 ? kSplit32by4 : kSplit;
+  if (t32 <= 256) return nk >= 11 ? k32by4 : k32;
+  if (tiles_of(M, N, 32, 64) <= 256) return nk >= 7 ? k32x64by2 : k32x64;
+  if (nk >= 7 && t64 <= (nk >= 16 ? 384 : 256)) return k64by2;
   if (tiles_of(M, N, 128, 64) < 480) return k64;
   const int64_t t128 = tiles_of(M, N, 128, 128);
   return t128 >= 384 && t128 <= 512 && nk >= 4 ? k128 : k128x64;
 }
 
 // Parts of a split contraction: two workgroups for each compute unit, 8 k-tiles at least (1000 x 512 x 8192, 128 tiles, in 2, 4 and 8 parts 22.7, 20.6, 23.0
-// us; 64 x 64 x 16384 in 8 12.0).
-int parts_of(int M, int N, int K) {
-  const int64_t t = 512 / tiles_of(M, N, 64, 64);
-  const int most = (K + 127) / 128 / 8;
+// us); one with four groups of wavefronts, 16 k-tiles at least.
+int parts_of(Shape shape, int M, int N, int K) {
+  const int nk = (K + 127) / 128;
+  const int64_t t = shape == kSplit ? 512 / tiles_of(M, N, 64, 64) : 256 / tiles_of(M, N, 32, 32);
+  const int most = shape == kSplit ? nk / 8 : nk / 16;
   return t < most ? (int)t : most;
 }
 
-template <int BM, int BN, int NS, bool EXACT>
+template <int BM, int BN, int NS, int NG, bool EXACT>
 hipError_t launch_tile(const ProductArgs& g, int wanted, hipStream_t s) {
-  constexpr int smem = NS * (BM + BN) * 128 + 2048;
+  constexpr int smem = NG * (NS * (BM + BN) * 128 + 2048);
+  static_assert(smem >= (NG - 1) * BM * BN * 4, "room for the groups' sums");
   static std::once_flag once;          // one attribute call per instantiation, also when two host threads launch first together
   static hipError_t result = hipSuccess;
-  std::call_once(once, [] { result = hipFuncSetAttribute((const void*)product_tile_kernel<BM, BN, NS, EXACT>, hipFuncAttributeMaxDynamicSharedMemorySize, smem); });
+  std::call_once(once, [] { result = hipFuncSetAttribute((const void*)product_tile_kernel<BM, BN, NS, NG, EXACT>, hipFuncAttributeMaxDynamicSharedMemorySize, smem); });
   if (result != hipSuccess) return result;
-  const int nk = (g.K + 127) / 128, kper = wanted > 1 ? ((nk + wanted - 1) / wanted + 3) & ~3 : nk, parts = wanted > 1 ? (nk + kper - 1) / kper : 1;
-  hipLaunchKernelGGL((product_tile_kernel<BM, BN, NS, EXACT>), dim3((unsigned)tiles_of(g.M, g.N, BM, BN), parts), dim3(256), smem, s, g, kper);
+  const int nk = (g.K + 127) / 128, all = wanted * NG, kper = all > 1 ? ((nk + all - 1) / all + 3) & ~3 : nk, parts = wanted > 1 ? (nk + NG * kper - 1) / (NG * kper) : 1;
+  hipLaunchKernelGGL((product_tile_kernel<BM, BN, NS, NG, EXACT>), dim3((unsigned)tiles_of(g.M, g.N, BM, BN), parts), dim3(256 * NG), smem, s, g, kper);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || parts == 1) return e;
   const int64_t quads = (int64_t)g.M * ((g.N + 3) / 4);
@@ -762,15 +789,18 @@ template <bool EXACT>
 hipError_t launch_shape(const ProductArgs& g, Shape shape, hipStream_t s) {
   switch (shape) {
     case kRows:
-      if (g.M <= 16) return launch_rows<1, 2>(g, s);
-      return g.M <= 32 ? launch_rows<2, 2>(g, s) : launch_rows<4, 1>(g, s);
+      return g.M <= 16 ? launch_rows<1, 2>(g, s) : launch_rows<2, 2>(g, s);
     case kBig: return launch_long<EXACT>(g, s);
-    case k128: return launch_tile<128, 128, 2, EXACT>(g, 1, s);
-    case k128x64: return launch_tile<128, 64, 2, EXACT>(g, 1, s);
-    case k64: return launch_tile<64, 64, 2, EXACT>(g, 1, s);
-    case k32x64: return launch_tile<32, 64, 3, EXACT>(g, 1, s);
-    case k32: return launch_tile<32, 32, 4, EXACT>(g, 1, s);
-    default: return launch_tile<64, 64, 3, EXACT>(g, parts_of(g.M, g.N, g.K), s);
+    case k128: return launch_tile<128, 128, 2, 1, EXACT>(g, 1, s);
+    case k128x64: return launch_tile<128, 64, 2, 1, EXACT>(g, 1, s);
+    case k64: return launch_tile<64, 64, 2, 1, EXACT>(g, 1, s);
+    case k64by2: return launch_tile<64, 64, 2, 2, EXACT>(g, 1, s);
+    case k32x64: return launch_tile<32, 64, 3, 1, EXACT>(g, 1, s);
+    case k32x64by2: return launch_tile<32, 64, 3, 2, EXACT>(g, 1, s);
+    case k32: return launch_tile<32, 32, 4, 1, EXACT>(g, 1, s);
+    case k32by4: return launch_tile<32, 32, 2, 4, EXACT>(g, 1, s);
+    case kSplit: return launch_tile<64, 64, 3, 1, EXACT>(g, parts_of(shape, g.M, g.N, g.K), s);
+    default: return launch_tile<32, 32, 2, 4, EXACT>(g, parts_of(shape, g.M, g.N, g.K), s);
   }
 }
 
@@ -778,8 +808,13 @@ hipError_t launch_shape(const ProductArgs& g, Shape shape, hipStream_t s) {
 
 // (of the larger one for the two output types)
 size_t product_floats(int M, int N, int K) {
-  if (shape_of(M, N, K, 0) != kSplit && shape_of(M, N, K, 1) != kSplit) return 0;
-  const int parts = parts_of(M, N, K);
+  int parts = 1;
+  for (int dtype = 0; dtype < 2; ++dtype) {
+    const Shape shape = shape_of(M, N, K, dtype);
+    if (shape != kSplit && shape != kSplit32by4) continue;
+    const int p = parts_of(shape, M, N, K);
+    parts = p > parts ? p : parts;
+  }
   return parts > 1 ? (size_t)parts * M * ((N + 3) & ~3) : 0;
 }
 

@@ -45,7 +45,7 @@ def test_no_kernel_spills(unit):
 
 def test_no_product_spills(product):
     found = kernels(product)
-    assert sum("product_long_kernel" in n for n in found) == 2 and sum("product_tile_kernel" in n for n in found) == 12 and sum("product_rows_kernel" in n for n in found) == 3
+    assert sum("product_long_kernel" in n for n in found) == 2 and sum("product_tile_kernel" in n for n in found) == 18 and sum("product_rows_kernel" in n for n in found) == 2
     for name, v in found.items():
         assert v["vgpr_spill_count"] == 0 and v["private_segment_fixed_size"] == 0, (name, v)
         if "product_tile_kernel" in name:

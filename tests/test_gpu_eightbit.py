@@ -426,3 +426,21 @@ def test_a_contraction_of_nothing_reads_nothing_whatever_its_leading_dimensions(
     assert need == 0
     rc = api.lib().slp_product(None, -31, None, -7, 1, None, -(1 << 33), None, 5, 128, bias.data_ptr(), 0, m, n, 0, out.data_ptr(), n, api.F32, None, 0, api._stream())
     assert rc == 0 and torch.equal(out, bias.expand(m, n))
+
+
+@pytest.mark.parametrize("m,n,k", [(714, 174, 1400), (300, 300, 1409), (65, 65, 3000), (1000, 512, 900), (1000, 500, 5000), (700, 900, 1025), (1000, 1000, 4000), (1200, 1100, 2050),
+                                   (64, 64, 16384), (100, 500, 6200), (130, 2000, 7000), (10, 1000, 20001)])
+def test_contractions_shared_by_groups_of_wavefronts_and_workgroups(m, n, k):
+    """Integers: the parts' sums are exact whatever the order; the same call gives the same bits."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(k)
+    a = api.quantize(torch.randint(-4, 5, (m, k), device=DEV, generator=g).float()).rows
+    b = api.quantize(torch.randint(-4, 5, (n, k), device=DEV, generator=g).float(), block=128).rows
+    bias = torch.randint(-9, 10, (n,), device=DEV, generator=g).float()
+    ref = _dequantized(a) @ _dequantized(b).t().contiguous()
+    assert torch.equal(api.product(a, b, dtype=api.F32).double(), ref)
+    assert torch.equal(api.product(a, b, bias=bias, relu=True).double(), (ref + bias).clamp(min=0).to(torch.bfloat16).double())
+    x, y = values((m, k), 3).to(DEV), values((n, k), 4).to(DEV)
+    x, y = api.quantize(x).rows, api.quantize(y).rows
+    for dtype in (api.F32, api.BF16):
+        assert torch.equal(api.product(x, y, dtype=dtype), api.product(x, y, dtype=dtype))
