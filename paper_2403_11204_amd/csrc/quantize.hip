@@ -69,13 +69,13 @@ __device__ __forceinline__ uint32_t column_e4m3(const Raw<float> (&v)[4], int j,
   return to_e4m3(item(v[0], j), item(v[1], j), item(v[2], j), item(v[3], j), scale);
 }
 
-// Row-major alone, a scale for each 128 elements of a row: a chunk of 8 elements a lane, 16 lanes a scale, a workgroup 16 scales.
+// Row-major alone, a scale for each 128 elements of a row: a chunk of 8 elements a lane, 16 lanes a scale, a workgroup 16 scales.  Bound by memory: 8192 x
+// 8192 float32 58 us (338 MB, 5.8 TB/s), 8192 x 16384 bf16 72 us (404 MB, 5.6 TB/s); on tiles, which serve the other forms, the latter takes 77.
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs a) {
-  const int blocks = (a.cols + 127) / 128;
-  const int64_t at = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const uint32_t blocks = (a.cols + 127) / 128, at = blockIdx.x * 16 + (threadIdx.x >> 4);       // (a matrix has fewer than 2^28 scales)
   const int64_t row = at / blocks;
-  const int b = (int)(at % blocks), c = b * 128 + (threadIdx.x & 15) * 8, left = a.cols - c;
+  const int b = at % blocks, c = b * 128 + (threadIdx.x & 15) * 8, left = a.cols - c;
   if (row >= a.rows) return;           // (16 lanes together)
   Raw<T> v;
   fetch8((const T*)a.x + row * a.ldx + c, left, v);
@@ -92,7 +92,9 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs a
 
 // Everything else, a 128 x 128 tile a workgroup of 8 wavefronts: a thread holds 4 rows of 8 columns.  The transposed bytes go through LDS, a row
 // of 128 bytes for each column of the tile; the 16-byte piece p of column c sits at p ^ (c / 8 mod 8), so that the lanes of a wavefront, which
-// write 16 columns 8 apart, spread over the banks.
+// write 16 columns 8 apart, spread over the banks.  8 wavefronts: with 4, which hold twice as much each, a 4096 x 8192 bf16 gradient took 73 us, not 57.
+// Bound by memory where there are many tiles, to both layouts: 8192 x 8192 float32 76 us (405 MB, 5.3 TB/s) with either kind of blocks, 4096 x 8192 bf16
+// with a mask and sums 39 us (203 MB, 5.2 TB/s); by the steps of one tile, 1.5 us behind the 2.5 of an empty launch, where there are few.
 template <typename T, int BLOCK>
 __global__ __launch_bounds__(512) void quantize_tile_kernel(const QuantizeArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t turned[128 * 128];
@@ -125,17 +127,21 @@ __global__ __launch_bounds__(512) void quantize_tile_kernel(const QuantizeArgs a
 #pragma unroll
   for (int i = 0; i < 4; ++i) rmax[i] = magnitudes(v[i], columns);
   if (BLOCK == 128 || a.qt) {
+    u32x4 k[2];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t k = max_of_rows(column(columns, j));
-      if ((t & 63) < 16) cmax[wave][cc * 8 + j] = k;
+    for (int j = 0; j < 8; ++j) k[j / 4][j % 4] = max_of_rows(column(columns, j));
+    if ((t & 63) < 16) {
+      *(u32x4*)&cmax[wave][cc * 8] = k[0];
+      *(u32x4*)&cmax[wave][cc * 8 + 4] = k[1];
     }
   }
   if (a.sums) {
+    f32x4 sum[2];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float sum = sum_of_rows((item(v[0], j) + item(v[1], j)) + (item(v[2], j) + item(v[3], j)));
-      if ((t & 63) < 16) csum[wave][cc * 8 + j] = sum;
+    for (int j = 0; j < 8; ++j) sum[j / 4][j % 4] = sum_of_rows((item(v[0], j) + item(v[1], j)) + (item(v[2], j) + item(v[3], j)));
+    if ((t & 63) < 16) {
+      *(f32x4*)&csum[wave][cc * 8] = sum[0];
+      *(f32x4*)&csum[wave][cc * 8 + 4] = sum[1];
     }
   }
   __syncthreads();
@@ -144,6 +150,18 @@ __global__ __launch_bounds__(512) void quantize_tile_kernel(const QuantizeArgs a
 #pragma unroll
     for (int w = 1; w < 8; ++w) sum += csum[w][t];
     (tilesM == 1 ? a.sums : a.work + tm * a.cols)[tn * 128 + t] = sum;
+  }
+  // the columns' scales, a column a thread, in place of the first wavefront's largest magnitudes (every thread reading all eight took 1.6 us more)
+  if (BLOCK == 1 && a.qt) {
+    if (t < 128) {
+      uint32_t k = cmax[0][t];
+#pragma unroll
+      for (int w = 1; w < 8; ++w) k = umax(k, cmax[w][t]);
+      k = scale_of(k);
+      if (tn * 128 + t < a.cols) a.scales_t[(int64_t)(tn * 128 + t) * a.ldst + tm] = (uint8_t)k;
+      cmax[0][t] = k;
+    }
+    __syncthreads();
   }
   uint32_t all = 0;
   if (BLOCK == 128) {
@@ -170,14 +188,7 @@ __global__ __launch_bounds__(512) void quantize_tile_kernel(const QuantizeArgs a
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int c = cc * 8 + j;
-      uint32_t scale = all;
-      if (BLOCK == 1) {
-        uint32_t k = 0;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) k = umax(k, cmax[w][c]);
-        scale = scale_of(k);
-        if (g == 0 && c0 + j < a.cols) a.scales_t[(int64_t)(c0 + j) * a.ldst + tm] = (uint8_t)scale;
-      }
+      const uint32_t scale = BLOCK == 128 ? all : cmax[0][c];
       *(uint32_t*)(turned + c * 128 + (((g >> 2) ^ (cc & 7)) << 4) + (g & 3) * 4) = column_e4m3(v, j, scale_value(scale));
     }
     __syncthreads();
