@@ -70,7 +70,8 @@ __device__ __forceinline__ uint32_t column_e4m3(const Raw<float> (&v)[4], int j,
 }
 
 // Row-major alone, a scale for each 128 elements of a row: a chunk of 8 elements a lane, 16 lanes a scale, a workgroup 16 scales.  Bound by memory: 8192 x
-// 8192 float32 58 us (338 MB, 5.8 TB/s), 8192 x 16384 bf16 72 us (404 MB, 5.6 TB/s); on tiles, which serve the other forms, the latter takes 77.
+// 8192 float32 58 us (338 MB, 5.8 TB/s), 8192 x 16384 bf16 72 us (404 MB, 5.6 TB/s); the tiles below take 77 for its
+// transposed form.
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs a) {
   const uint32_t blocks = (a.cols + 127) / 128, at = blockIdx.x * 16 + (threadIdx.x >> 4);       // (a matrix has fewer than 2^28 scales)
