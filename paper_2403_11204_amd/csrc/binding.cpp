@@ -94,8 +94,8 @@ Eight eight_room(int64_t rows, int64_t cols, int64_t block, const at::Device& de
   e.at = e.q.data_ptr();
   e.scales_at = e.scales.data_ptr();
   // (in place: each as_strided takes the host another half microsecond)
-  if (e.ld != cols) e.q.unsafeGetTensorImpl()->set_sizes_and_strides({rows, cols}, {e.ld, 1});
-  if (e.lds != blocks) e.scales.unsafeGetTensorImpl()->set_sizes_and_strides({srows, blocks}, {e.lds, 1});
+  if (e.ld != cols) e.q.unsafeGetTensorImpl()->set_sizes_and_strides(at::IntArrayRef({rows, cols}), at::IntArrayRef({e.ld, 1}));
+  if (e.lds != blocks) e.scales.unsafeGetTensorImpl()->set_sizes_and_strides(at::IntArrayRef({srows, blocks}), at::IntArrayRef({e.lds, 1}));
   return e;
 }
 Eight eight_given(PyObject* q, PyObject* scales, int64_t block, int64_t cols) {
