@@ -1,6 +1,6 @@
 // The operators' way from Python tensors to the C ABI (include/slp.h): argument checks, room for the outputs and workspaces from torch's
 // allocator, the call.  An operator on a few rows takes the device 3 to 5 us; written in Python these steps took the host 10 to 17 us
-// a call, here 5 to 9.  Each function returns its outputs, or the library's error code as an integer.  `stream` is a hipStream_t as an integer.
+// a call, here 5 with one launch, 8 to 12 with two.  Each function returns its outputs, or the library's error code as an integer.  `stream` is a hipStream_t as an integer.
 #include <Python.h>
 
 #include <ATen/Functions.h>
@@ -72,8 +72,31 @@ const float* vector(PyObject* o, int64_t n, const at::Tensor& x) {
   return (const float*)t.data_ptr();
 }
 
-at::Tensor room(at::IntArrayRef sizes, at::ScalarType type, const at::Device& device) { return at::empty(sizes, at::TensorOptions().dtype(type).device(device)); }
-at::Tensor bytes(size_t n, const at::Device& device) { return n ? room({(int64_t)n}, at::kByte, device) : at::Tensor(); }
+// Room for a call's outputs and workspace.  Each allocation takes the host 0.6 us: where all of them come to 256 KB at most (a request's
+// rows: the device is done before the host) they are parts of one, on 256-byte boundaries.
+class Room {
+ public:
+  Room(const at::Device& device, size_t all) : device_(device) {
+    if (all <= (256u << 10)) block_ = at::empty({(int64_t)all}, at::TensorOptions().dtype(at::kByte).device(device));
+  }
+  static size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+  at::Tensor take(at::IntArrayRef sizes, at::ScalarType type) {
+    if (!block_.defined()) return at::empty(sizes, at::TensorOptions().dtype(type).device(device_));
+    at::Tensor t = at::detail::make_tensor<at::TensorImpl>(c10::Storage(block_.storage()), block_.key_set(), c10::scalarTypeToTypeMeta(type));
+    const size_t size = t.itemsize();
+    t.unsafeGetTensorImpl()->set_storage_offset((int64_t)(used_ / size));
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+    used_ += padded((size_t)t.numel() * size);
+    require(used_ <= block_.nbytes(), "room counted too small");
+    return t;
+  }
+  at::Tensor bytes(size_t n) { return n ? take({(int64_t)n}, at::kByte) : at::Tensor(); }
+
+ private:
+  at::Device device_;
+  at::Tensor block_;
+  size_t used_ = 0;
+};
 void* address(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 
 // A matrix in 8 bits.
@@ -83,14 +106,21 @@ struct Eight {
   int64_t ld = 0, lds = 0;
 };
 // Room for one: rows on 128-byte boundaries and, where there are many, not a multiple of 4 KB apart; rows of scales on 4-byte boundaries.
-Eight eight_room(int64_t rows, int64_t cols, int64_t block, const at::Device& device) {
+int64_t eight_ld(int64_t rows, int64_t cols) {
+  const int64_t ld = (cols + 127) / 128 * 128;
+  return ld % 4096 == 0 && rows > 16 ? ld + 128 : ld;
+}
+int64_t eight_lds(int64_t cols) { return (cols + 511) / 512 * 4; }
+size_t eight_bytes(int64_t rows, int64_t cols, int64_t block) {
+  return Room::padded((size_t)(rows * eight_ld(rows, cols))) + Room::padded((size_t)((rows + block - 1) / block * eight_lds(cols)));
+}
+Eight eight_room(int64_t rows, int64_t cols, int64_t block, Room& room) {
   Eight e;
   const int64_t blocks = (cols + 127) / 128, srows = (rows + block - 1) / block;
-  e.ld = blocks * 128;
-  if (e.ld % 4096 == 0 && rows > 16) e.ld += 128;
-  e.lds = (blocks + 3) / 4 * 4;
-  e.q = room({rows, e.ld}, at::kFloat8_e4m3fn, device);
-  e.scales = room({srows, e.lds}, at::kFloat8_e8m0fnu, device);
+  e.ld = eight_ld(rows, cols);
+  e.lds = eight_lds(cols);
+  e.q = room.take({rows, e.ld}, at::kFloat8_e4m3fn);
+  e.scales = room.take({srows, e.lds}, at::kFloat8_e8m0fnu);
   e.at = e.q.data_ptr();
   e.scales_at = e.scales.data_ptr();
   // (in place: each as_strided takes the host another half microsecond)
@@ -144,15 +174,15 @@ PyObject* quantize(PyObject* const* a) {
     ldmask = like(tensor(a[4]), x);
     mask = tensor(a[4]).data_ptr();
   }
+  const bool rows = truth(a[2]), transposed = truth(a[3]), column_sums = truth(a[5]);
+  const size_t size = column_sums ? slp_quantize_workspace_bytes(side(m), side(n)) : 0;
+  Room room(x.device(), (rows ? eight_bytes(m, n, block) : 0) + (transposed ? eight_bytes(n, m, block) : 0) + (column_sums ? Room::padded(4 * n) : 0) + Room::padded(size));
   Eight r, t;
-  if (truth(a[2])) r = eight_room(m, n, block, x.device());
-  if (truth(a[3])) t = eight_room(n, m, block, x.device());
-  at::Tensor sums, work;
-  size_t size = 0;
-  if (truth(a[5])) {
-    sums = room({n}, at::kFloat, x.device());
-    work = bytes(size = slp_quantize_workspace_bytes(side(m), side(n)), x.device());
-  }
+  if (rows) r = eight_room(m, n, block, room);
+  if (transposed) t = eight_room(n, m, block, room);
+  at::Tensor sums;
+  if (column_sums) sums = room.take({n}, at::kFloat);
+  const at::Tensor work = room.bytes(size);
   const int rc = slp_quantize(x.data_ptr(), ldx, mask, ldmask, dt, side(m), side(n), (int)block, r.at, r.ld, r.scales_at, r.lds, t.at, t.ld, t.scales_at, t.lds,
                               (float*)address(sums), address(work), size, PyLong_AsVoidPtr(a[6]));
   return rc ? code(rc) : tuple({r.q, r.scales, t.q, t.scales, sums});
@@ -165,19 +195,20 @@ PyObject* product(PyObject* const* a) {
   const Eight x = eight_given(a[0], a[1], ablock, cols), y = eight_given(a[3], a[4], bblock, cols);
   const int64_t m = x.q.size(0), n = y.q.size(0);
   require(x.q.device() == y.q.device(), "matrices on one device are wanted");
+  const size_t size = slp_product_workspace_bytes(side(m), side(n), side(cols));
   at::Tensor out;
   int dt = (int)integer(a[8]);
   int64_t ldo = n;
+  Room room(x.q.device(), Room::padded(size) + (given(a[9]) ? 0 : Room::padded((size_t)(m * n) * (dt == SLP_BF16 ? 2 : 4))));
   if (given(a[9])) {
     out = tensor(a[9]);
     require(out.dim() == 2 && out.size(0) == m && out.size(1) == n && out.device() == x.q.device(), "an output of the product's shape is wanted");
     ldo = leading(out);
     dt = dtype_of(out);
   } else {
-    out = room({m, n}, dt == SLP_BF16 ? at::kBFloat16 : at::kFloat, x.q.device());
+    out = room.take({m, n}, dt == SLP_BF16 ? at::kBFloat16 : at::kFloat);
   }
-  const size_t size = slp_product_workspace_bytes(side(m), side(n), side(cols));
-  const at::Tensor work = bytes(size, x.q.device());
+  const at::Tensor work = room.bytes(size);
   const int rc = slp_product(x.at, x.ld, x.scales_at, x.lds, (int)ablock, y.at, y.ld, y.scales_at, y.lds, (int)bblock, vector(a[6], n, x.q), truth(a[7]), side(m), side(n),
                              side(cols), out.data_ptr(), ldo, dt, address(work), size, PyLong_AsVoidPtr(a[10]));
   if (rc) return code(rc);
@@ -190,6 +221,9 @@ PyObject* rmsnorm(PyObject* const* a) {
   const int64_t ldx = leading(x), m = x.size(0), n = x.size(1);
   const int dt = dtype_of(x);
   const float* gamma = vector(a[1], n, x);
+  const bool normed = truth(a[4]), quantized = truth(a[5]);
+  const size_t matrix = Room::padded((size_t)(m * n) * (dt == SLP_BF16 ? 2 : 4));
+  Room room(x.device(), (given(a[2]) ? matrix : 0) + (normed ? matrix : 0) + (quantized ? eight_bytes(m, n, 1) : 0) + Room::padded(4 * m));
   at::Tensor h = x, y;
   const void* r = nullptr;
   void* to = nullptr;
@@ -197,13 +231,13 @@ PyObject* rmsnorm(PyObject* const* a) {
   if (given(a[2])) {
     ldr = like(tensor(a[2]), x);
     r = tensor(a[2]).data_ptr();
-    h = room({m, n}, x.scalar_type(), x.device());
+    h = room.take({m, n}, x.scalar_type());
     to = h.data_ptr();
   }
-  if (truth(a[4])) y = room({m, n}, x.scalar_type(), x.device());
+  if (normed) y = room.take({m, n}, x.scalar_type());
   Eight e;
-  if (truth(a[5])) e = eight_room(m, n, 1, x.device());
-  const at::Tensor rstd = room({m}, at::kFloat, x.device());
+  if (quantized) e = eight_room(m, n, 1, room);
+  const at::Tensor rstd = room.take({m}, at::kFloat);
   const int rc = slp_rmsnorm(x.data_ptr(), ldx, r, ldr, gamma, (float)number(a[3]), dt, side(m), side(n), to, n, address(y), n, e.at, e.ld, e.scales_at, e.lds,
                              (float*)rstd.data_ptr(), PyLong_AsVoidPtr(a[6]));
   return rc ? code(rc) : tuple({h, rstd, y, e.q, e.scales});
@@ -222,11 +256,12 @@ PyObject* rmsnorm_backward(PyObject* const* a) {
   }
   require(given(a[3]), "rstd of the forward pass is wanted");
   const float *gamma = vector(a[2], n, h), *rstd = vector(a[3], m, h);
-  const at::Tensor dx = room({m, n}, h.scalar_type(), h.device());
-  at::Tensor dgamma;
-  if (truth(a[5])) dgamma = room({n}, at::kFloat, h.device());
   const size_t size = slp_rmsnorm_backward_workspace_bytes(side(m), side(n));
-  const at::Tensor work = bytes(size, h.device());
+  Room room(h.device(), Room::padded((size_t)(m * n) * (dt == SLP_BF16 ? 2 : 4)) + Room::padded(4 * n) + Room::padded(size));
+  const at::Tensor dx = room.take({m, n}, h.scalar_type());
+  at::Tensor dgamma;
+  if (truth(a[5])) dgamma = room.take({n}, at::kFloat);
+  const at::Tensor work = room.bytes(size);
   const int rc = slp_rmsnorm_backward(dy.data_ptr(), lddy, h.data_ptr(), ldh, gamma, rstd, dh, lddh, dt, side(m), side(n), dx.data_ptr(), n, (float*)address(dgamma),
                                       address(work), size, PyLong_AsVoidPtr(a[6]));
   return rc ? code(rc) : tuple({dx, dgamma});
@@ -263,9 +298,9 @@ Tensors tensors(PyObject* list, const Tensors* as) {
 PyObject* gradient_norm(PyObject* const* a) {
   const Tensors in = tensors(a[0], nullptr);
   const int n = (int)in.at.size();
-  const at::Tensor norm = room({}, at::kFloat, in.device);
   const size_t size = slp_gradient_norm_workspace_bytes(n);
-  const at::Tensor work = bytes(size, in.device);
+  Room room(in.device, Room::padded(4) + Room::padded(size));
+  const at::Tensor norm = room.take({}, at::kFloat), work = room.bytes(size);
   const int rc = slp_gradient_norm(in.at.data(), in.counts.data(), in.dts.data(), n, (float*)norm.data_ptr(), address(work), size, PyLong_AsVoidPtr(a[1]));
   if (rc) return code(rc);
   return wrapped(norm);
@@ -277,9 +312,9 @@ PyObject* clip_gradients(PyObject* const* a) {
   const int n = (int)in.at.size();
   Tensors out;
   if (given(a[2])) out = tensors(a[2], &in);
-  const at::Tensor norm = room({}, at::kFloat, in.device);
   const size_t size = slp_gradient_norm_workspace_bytes(n);
-  const at::Tensor work = bytes(size, in.device);
+  Room room(in.device, Room::padded(4) + Room::padded(size));
+  const at::Tensor norm = room.take({}, at::kFloat), work = room.bytes(size);
   const int rc = slp_clip_gradients(in.at.data(), given(a[2]) ? out.at.data() : nullptr, in.counts.data(), in.dts.data(), n, (float)number(a[1]), (float*)norm.data_ptr(),
                                     address(work), size, PyLong_AsVoidPtr(a[3]));
   if (rc) return code(rc);

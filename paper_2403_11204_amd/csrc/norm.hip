@@ -302,7 +302,8 @@ template <typename T>
 hipError_t rmsnorm_backward_of(const NormBackArgs& a, hipStream_t s) {
   constexpr bool narrow = sizeof(T) == 2;
   const int groups = backward_groups(a.rows, a.dim);
-  float* partials = a.work;
+  const bool alone = groups == 1 && a.dim <= kOnePass;          // its sums are the gradient
+  float* partials = alone ? a.dgamma : a.work;
   if (a.dim <= 512) rmsnorm_backward_kernel<T, 1, 1, true><<<groups, 256, 0, s>>>(a, partials);
   else if (a.dim <= 1024) rmsnorm_backward_kernel<T, 1, 2, true><<<groups, 256, 0, s>>>(a, partials);
   else if (a.dim <= 2048) rmsnorm_backward_kernel<T, 4, 1, true><<<groups, 256, 0, s>>>(a, partials);
@@ -316,7 +317,7 @@ hipError_t rmsnorm_backward_of(const NormBackArgs& a, hipStream_t s) {
     rmsnorm_columns_kernel<T><<<dim3((a.dim + 2047) / 2048, groups), 256, 0, s>>>(a, dots, partials);
   }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.dgamma) return e;
+  if (e != hipSuccess || !a.dgamma || alone) return e;
   return launch_sum_rows(partials, groups, a.dim, a.dgamma, s);
 }
 
@@ -348,7 +349,8 @@ hipError_t launch_sum_rows(const float* in, int n, int cols, float* out, hipStre
 hipError_t launch_rmsnorm(int dtype, const NormArgs& a, hipStream_t s) { return dtype == 1 ? rmsnorm_of<bf16>(a, s) : rmsnorm_of<float>(a, s); }
 
 size_t rmsnorm_backward_floats(int rows, int dim) {
-  return (dim > kOnePass ? (size_t)((rows + 3) / 4 * 4) : 0) + (size_t)backward_groups(rows, dim) * dim;
+  const size_t sums = (size_t)backward_groups(rows, dim) * dim;
+  return dim > kOnePass ? (size_t)((rows + 3) / 4 * 4) + sums : sums > (size_t)dim ? sums : 0;
 }
 
 hipError_t launch_rmsnorm_backward(int dtype, const NormBackArgs& a, hipStream_t s) {

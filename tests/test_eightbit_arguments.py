@@ -105,7 +105,7 @@ def test_rmsnorm():
 
 
 def norm_back(**kw):
-    a = dict(dy=P, lddy=300, h=P, ldh=300, gamma=P, rstd=P, dh=None, lddh=0, dt=1, rows=4, dim=300, dx=P, lddx=300, dgamma=P, work=P, size=1 << 40)
+    a = dict(dy=P, lddy=300, h=P, ldh=300, gamma=P, rstd=P, dh=None, lddh=0, dt=1, rows=200, dim=300, dx=P, lddx=300, dgamma=P, work=P, size=1 << 40)
     a.update(kw)
     return api.lib().slp_rmsnorm_backward(*a.values(), None)
 

@@ -444,3 +444,39 @@ def test_contractions_shared_by_groups_of_wavefronts_and_workgroups(m, n, k):
     x, y = api.quantize(x).rows, api.quantize(y).rows
     for dtype in (api.F32, api.BF16):
         assert torch.equal(api.product(x, y, dtype=dtype), api.product(x, y, dtype=dtype))
+
+
+def test_outputs_of_a_small_call_lie_apart_and_outlive_one_another():
+    x, r = (values((3, 200), i, torch.bfloat16).to(DEV) for i in range(2))
+    gamma = torch.ones(200, device=DEV)
+
+    def outputs():
+        n = api.rmsnorm(x, gamma, residual=r, normed=True)
+        q = api.quantize(x, transposed=True, mask=r, column_sums=True)
+        dx, dgamma = api.rmsnorm_backward(x, n.h, gamma, n.rstd)
+        return [n.h, n.rstd, n.y, n.y8.q, n.y8.scales, q.rows.q, q.rows.scales, q.transposed.q, q.transposed.scales, q.column_sums, dx, dgamma, api.gradient_norm([x, r])]
+
+    first = outputs()
+    spans = sorted((t.data_ptr(), t.data_ptr() + (t.numel() and 1 + sum((s - 1) * st for s, st in zip(t.shape, t.stride()))) * t.element_size()) for t in first)
+    assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
+    assert all(t.data_ptr() % 256 == 0 for t in first)
+    kept = [f64(t) if t.dtype != torch.float8_e8m0fnu else bytes_of(t).copy() for t in first]
+    h = first[0]
+    del first
+    for _ in range(50):
+        again = outputs()
+        for t in again:
+            t.view(torch.uint8).fill_(85) if t.is_contiguous() and t.dim() else None
+    assert np.array_equal(f64(h), kept[0])
+    for t, k in zip(outputs(), kept):
+        assert np.array_equal(f64(t) if t.dtype != torch.float8_e8m0fnu else bytes_of(t), k)
+
+
+@pytest.mark.parametrize("rows,dim", [(1, 16384), (1, 1025), (4, 1000), (2, 60), (5, 1000), (2, 4096)])
+def test_rmsnorm_backward_of_few_rows(rows, dim):
+    h, dy = values((rows, dim), 1), values((rows, dim), 2)
+    n = api.rmsnorm(h.to(DEV), quantized=False)
+    dx, dgamma = api.rmsnorm_backward(dy.to(DEV), h.to(DEV), None, n.rstd)
+    terms = f64(dy) * f64(h) * f64(n.rstd)[:, None]
+    assert np.all(np.abs(f64(dgamma) - terms.sum(0)) <= (rows + 4) * U * np.abs(terms).sum(0))
+    assert api.rmsnorm_backward(dy.to(DEV), h.to(DEV), None, n.rstd, gamma_grad=False)[1] is None
