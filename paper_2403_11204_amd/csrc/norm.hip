@@ -29,8 +29,10 @@ __device__ __forceinline__ void finish_chunk(const NormArgs& a, int64_t row, int
 }
 
 // Rows dealt out to teams of WAVES wavefronts, each lane CH chunks of a row in registers; the next row's loads are under way while this one is
-// added up and stored.  Bound by memory: 8192 x 16384 bf16 with the residual 173 us (939 MB, 5.4 TB/s), 4096 x 8192 44 us (235 MB, 5.3 TB/s), on 512
-// workgroups of several wavefronts; a workgroup for each row 181 and 49 us, 256 workgroups 171 and 45 (8192 x 4096 45 -> 59), 1024 177 and 45.
+// added up and stored.  Bound by memory: 8192 x 16384 bf16 with the residual 173 us (939 MB, 5.4 TB/s), 4096 x 8192 39 us (235 MB), on 512
+// workgroups of 8 or 16 wavefronts; a workgroup for each row 181 and 49 us, 256 workgroups 171 and 45 (8192 x 4096 45 -> 59), 1024 177 and 45.  Teams of 4 wavefronts
+// on 1024 workgroups: 5000 x 1500 14.2 us, 19.7 on 512; 8192 x 2048 21.5, 23.8.  A team holds little more than its rows: 2000 x 9000 in 3 chunks of 8
+// wavefronts 27.3, in 4 45.6, in 2 of 16 36.6; 4096 x 16384 float32 in 2 chunks of 16 wavefronts 165, in 4 of 8 172, one row 5.4 and 6.3.
 template <typename T, int WAVES, int CH>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_kernel(const NormArgs a) {
   constexpr int TEAM = WAVES * 64, TEAMS = WAVES == 1 ? 4 : 1;
@@ -133,20 +135,22 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(const NormArgs a) {
 
 template <typename T>
 hipError_t rmsnorm_of(const NormArgs& a, hipStream_t s) {
-  const int quads = (a.rows + 3) / 4, few = quads < 2048 ? quads : 2048, rows = a.rows < 512 ? a.rows : 512;
+  const int quads = (a.rows + 3) / 4, few = quads < 2048 ? quads : 2048, rows = a.rows < 512 ? a.rows : 512, twice = a.rows < 1024 ? a.rows : 1024;
   if (a.dim <= 512) rmsnorm_kernel<T, 1, 1><<<few, 256, 0, s>>>(a);
   else if (a.dim <= 1024) rmsnorm_kernel<T, 1, 2><<<few, 256, 0, s>>>(a);
-  else if (a.dim <= 2048) rmsnorm_kernel<T, 4, 1><<<rows, 256, 0, s>>>(a);
-  else if (a.dim <= 4096) rmsnorm_kernel<T, 4, 2><<<rows, 256, 0, s>>>(a);
+  else if (a.dim <= 2048) rmsnorm_kernel<T, 4, 1><<<twice, 256, 0, s>>>(a);
+  else if (a.dim <= 4096) rmsnorm_kernel<T, 4, 2><<<twice, 256, 0, s>>>(a);
   else if (a.dim <= 8192) rmsnorm_kernel<T, 8, 2><<<rows, 512, 0, s>>>(a);
-  else if (a.dim <= kOnePass) rmsnorm_kernel<T, 8, 4><<<rows, 512, 0, s>>>(a);
+  else if (a.dim <= 12288) rmsnorm_kernel<T, 8, 3><<<rows, 512, 0, s>>>(a);
+  else if (a.dim <= kOnePass) rmsnorm_kernel<T, 16, 2><<<rows, 1024, 0, s>>>(a);
   else rmsnorm_long_kernel<T><<<a.rows, 1024, 0, s>>>(a);
   return hipGetLastError();
 }
 
 // ---- backward: rows dealt out to teams of WAVES wavefronts, gamma and the sums for its gradient in registers, each lane CH chunks ----
-// One reading of everything: a row waits in registers for its product, while the next row's loads are under way (AHEAD).  Bound by memory: 4096 x
-// 8192 bf16 with the gradient past the norm 51 us (268 MB, 5.3 TB/s), and 5 for the sums over the workgroups.
+// One reading of everything: a row waits in registers for its product, while the next row's loads are under way (AHEAD; 16 wavefronts have no registers
+// for it).  Bound by memory: 4096 x 8192 bf16 with the gradient past the norm 49 us (268 MB, 5.5 TB/s), and 5 for the sums over the workgroups; rows of 8193 to
+// 16384 in 2 chunks of 16 wavefronts 4096 x 16384 108 us with the sums, 1 x 16384 4.7, in 4 of 8 wavefronts 112 and 6.1.
 template <typename T, int WAVES, int CH, bool AHEAD>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_backward_kernel(const NormBackArgs a, float* __restrict__ partials) {
   constexpr int TEAM = WAVES * 64, TEAMS = WAVES == 1 ? 4 : 1;
@@ -292,15 +296,18 @@ __global__ __launch_bounds__(256) void rmsnorm_columns_kernel(const NormBackArgs
   if (a.dgamma) store8(partials + (int64_t)blockIdx.y * a.dim + c, left, acc);
 }
 
-// Partial sums of gamma's gradient: workgroups of the one-pass kernel, or strands of rows.
+// Partial sums of gamma's gradient: workgroups of the one-pass kernel, or strands of rows.  As many as hide the loads, but every one is a row for
+// sum_rows_kernel.  Both kernels, bf16, us: 8192 x 300 12.3 with 1024, 13.0 with 512; 8192 x 1024 15.8 with 512, 18.4 with 1024; 5000 x 1500 25.2 with 512, 22.1 with 768,
+// 8192 x 2048 27.7, 26.2, 27.7 with 1024, but 1000 x 1500 10.6, 12.2; 4096 x 4096 27.4 with 512, 31.9 with 256, 29.4 with 768; 4096 x 8192 52.0 with 256, 50.4 with 512,
+// but 1000 x 16384 31.0, 37.5.
 int backward_groups(int rows, int dim) {
-  const int teams = dim <= 1024 ? (rows + 3) / 4 : rows, most = dim <= 1024 ? 1024 : dim <= 4096 ? 512 : 256;
+  const int teams = dim <= 1024 ? (rows + 3) / 4 : rows;
+  const int most = dim <= 512 ? 1024 : dim > 4096 ? 256 : dim > 1024 && dim <= 2048 && rows >= 4096 ? 768 : 512;
   return teams < most ? teams : most;
 }
 
 template <typename T>
 hipError_t rmsnorm_backward_of(const NormBackArgs& a, hipStream_t s) {
-  constexpr bool narrow = sizeof(T) == 2;
   const int groups = backward_groups(a.rows, a.dim);
   const bool alone = groups == 1 && a.dim <= kOnePass;          // its sums are the gradient
   float* partials = alone ? a.dgamma : a.work;
@@ -309,7 +316,7 @@ hipError_t rmsnorm_backward_of(const NormBackArgs& a, hipStream_t s) {
   else if (a.dim <= 2048) rmsnorm_backward_kernel<T, 4, 1, true><<<groups, 256, 0, s>>>(a, partials);
   else if (a.dim <= 4096) rmsnorm_backward_kernel<T, 4, 2, true><<<groups, 256, 0, s>>>(a, partials);
   else if (a.dim <= 8192) rmsnorm_backward_kernel<T, 8, 2, true><<<groups, 512, 0, s>>>(a, partials);
-  else if (a.dim <= kOnePass) rmsnorm_backward_kernel<T, 8, 4, narrow><<<groups, 512, 0, s>>>(a, partials);
+  else if (a.dim <= kOnePass) rmsnorm_backward_kernel<T, 16, 2, false><<<groups, 1024, 0, s>>>(a, partials);
   else {
     float* dots = a.work;
     partials = a.work + (a.rows + 3) / 4 * 4;

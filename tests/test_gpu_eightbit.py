@@ -480,3 +480,10 @@ def test_rmsnorm_backward_of_few_rows(rows, dim):
     terms = f64(dy) * f64(h) * f64(n.rstd)[:, None]
     assert np.all(np.abs(f64(dgamma) - terms.sum(0)) <= (rows + 4) * U * np.abs(terms).sum(0))
     assert api.rmsnorm_backward(dy.to(DEV), h.to(DEV), None, n.rstd, gamma_grad=False)[1] is None
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,dim", [(1100, 1500), (4100, 1030), (600, 9001), (3, 12288), (520, 12289), (2, 13000)])
+def test_rmsnorm_where_workgroups_take_several_rows(rows, dim, dtype):
+    test_rmsnorm(rows, dim, dtype)
+    test_rmsnorm_backward(rows, dim, dtype)
