@@ -487,3 +487,17 @@ def test_rmsnorm_backward_of_few_rows(rows, dim):
 def test_rmsnorm_where_workgroups_take_several_rows(rows, dim, dtype):
     test_rmsnorm(rows, dim, dtype)
     test_rmsnorm_backward(rows, dim, dtype)
+
+
+@pytest.mark.parametrize("m,n,k", [(581, 14917, 256), (581, 14914, 130), (2050, 8200, 200), (247, 1024, 8192), (200, 400, 12000), (1000, 512, 6200), (7759, 234, 4100)])
+def test_products_at_the_borders_of_the_rules(m, n, k):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(n)
+    a = api.quantize(torch.randint(-4, 5, (m, k), device=DEV, generator=g).float()).rows
+    b = api.quantize(torch.randint(-4, 5, (n, k), device=DEV, generator=g).float(), block=128).rows
+    ref = _dequantized(a) @ _dequantized(b).t().contiguous()
+    assert torch.equal(api.product(a, b, dtype=api.F32).double(), ref)
+    assert torch.equal(api.product(a, b).double(), ref.to(torch.bfloat16).double())
+    room = torch.full((m, n + 3), 7.0, dtype=torch.bfloat16, device=DEV)
+    api.product(a, b, out=room[:, 1:n + 1])
+    assert torch.equal(room[:, 1:n + 1].double(), ref.to(torch.bfloat16).double()) and bool((room[:, 0] == 7).all()) and bool((room[:, n + 1:] == 7).all())
