@@ -122,12 +122,13 @@ __device__ __forceinline__ float sum_of_rows(float x) {
 }
 template <int CTRL>
 __device__ __forceinline__ float add_dpp(float x) { return x + __builtin_bit_cast(float, dpp<CTRL>(__builtin_bit_cast(uint32_t, x))); }
-__device__ __forceinline__ float sum_of_64(float x) {
+__device__ __forceinline__ float sum_of_16(float x) {
   x = add_dpp<kSwap1>(x);
   x = add_dpp<kSwap2>(x);
   x = add_dpp<kHalfMirror>(x);
-  return sum_of_rows(add_dpp<kMirror>(x));
+  return add_dpp<kMirror>(x);
 }
+__device__ __forceinline__ float sum_of_64(float x) { return sum_of_rows(sum_of_16(x)); }
 
 // |v| as an integer that orders like the value, infinities and NaN above all others
 __device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu; }

@@ -33,11 +33,13 @@ __device__ __forceinline__ void finish_chunk(const NormArgs& a, int64_t row, int
 // workgroups of 8 or 16 wavefronts; a workgroup for each row 181 and 49 us, 256 workgroups 171 and 45 (8192 x 4096 45 -> 59), 1024 177 and 45.  Teams of 4 wavefronts
 // on 1024 workgroups: 5000 x 1500 14.2 us, 19.7 on 512; 8192 x 2048 21.5, 23.8.  A team holds little more than its rows: 2000 x 9000 in 3 chunks of 8
 // wavefronts 27.3, in 4 45.6, in 2 of 16 36.6; 4096 x 16384 float32 in 2 chunks of 16 wavefronts 165, in 4 of 8 172, one row 5.4 and 6.3.
-template <typename T, int WAVES, int CH>
+// Rows of up to 128 (256, where there are many) on LANES = 16: 8192 x 64 3.8 us, on whole wavefronts 6.2; 100000 x 128 16.2, 43.1; 16384 x 80 float32 5.4, 9.3; 8192 x 200 5.5,
+// 6.8, but 1000 x 129 4.1, 3.3.
+template <typename T, int WAVES, int CH, int LANES = 64>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_kernel(const NormArgs a) {
-  constexpr int TEAM = WAVES * 64, TEAMS = WAVES == 1 ? 4 : 1;
+  constexpr int TEAM = WAVES * LANES, TEAMS = WAVES == 1 ? 256 / LANES : 1;
   __shared__ float part[2][WAVES];
-  const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, D = a.dim, step = gridDim.x * TEAMS;
+  const int t = WAVES == 1 ? threadIdx.x % LANES : threadIdx.x, D = a.dim, step = gridDim.x * TEAMS;
   float g[CH][8];
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
@@ -54,7 +56,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_kernel(
       if (a.r) fetch8((const T*)a.r + row * a.ldr + c, D - c, r[i]);
     }
   };
-  int64_t row = (int64_t)blockIdx.x * TEAMS + (WAVES == 1 ? threadIdx.x >> 6 : 0);
+  int64_t row = (int64_t)blockIdx.x * TEAMS + (WAVES == 1 ? threadIdx.x / LANES : 0);
   if (row < a.rows) fetch(row);
   for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
     float v[CH][8], ss = 0.0f;
@@ -70,7 +72,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_kernel(
       if (a.h) store8((T*)a.h + row * a.ldh + c, D - c, v[i]);
     }
     if (row + step < a.rows) fetch(row + step);
-    ss = sum_of_64(ss);
+    ss = LANES == 16 ? sum_of_16(ss) : sum_of_64(ss);
     if (WAVES > 1) {
       if ((t & 63) == 0) part[turn][t >> 6] = ss;
       __syncthreads();
@@ -135,8 +137,10 @@ __global__ __launch_bounds__(1024) void rmsnorm_long_kernel(const NormArgs a) {
 
 template <typename T>
 hipError_t rmsnorm_of(const NormArgs& a, hipStream_t s) {
-  const int quads = (a.rows + 3) / 4, few = quads < 2048 ? quads : 2048, rows = a.rows < 512 ? a.rows : 512, twice = a.rows < 1024 ? a.rows : 1024;
-  if (a.dim <= 512) rmsnorm_kernel<T, 1, 1><<<few, 256, 0, s>>>(a);
+  const int quads = (a.rows + 3) / 4, few = quads < 2048 ? quads : 2048, sixteens = (quads + 3) / 4 < 2048 ? (quads + 3) / 4 : 2048, rows = a.rows < 512 ? a.rows : 512, twice = a.rows < 1024 ? a.rows : 1024;
+  if (a.dim <= 128) rmsnorm_kernel<T, 1, 1, 16><<<sixteens, 256, 0, s>>>(a);
+  else if (a.dim <= 256 && a.rows >= 4096) rmsnorm_kernel<T, 1, 2, 16><<<sixteens, 256, 0, s>>>(a);
+  else if (a.dim <= 512) rmsnorm_kernel<T, 1, 1><<<few, 256, 0, s>>>(a);
   else if (a.dim <= 1024) rmsnorm_kernel<T, 1, 2><<<few, 256, 0, s>>>(a);
   else if (a.dim <= 2048) rmsnorm_kernel<T, 4, 1><<<twice, 256, 0, s>>>(a);
   else if (a.dim <= 4096) rmsnorm_kernel<T, 4, 2><<<twice, 256, 0, s>>>(a);
@@ -150,13 +154,14 @@ hipError_t rmsnorm_of(const NormArgs& a, hipStream_t s) {
 // ---- backward: rows dealt out to teams of WAVES wavefronts, gamma and the sums for its gradient in registers, each lane CH chunks ----
 // One reading of everything: a row waits in registers for its product, while the next row's loads are under way (AHEAD; 16 wavefronts have no registers
 // for it).  Bound by memory: 4096 x 8192 bf16 with the gradient past the norm 49 us (268 MB, 5.5 TB/s), and 5 for the sums over the workgroups; rows of 8193 to
-// 16384 in 2 chunks of 16 wavefronts 4096 x 16384 108 us with the sums, 1 x 16384 4.7, in 4 of 8 wavefronts 112 and 6.1.
-template <typename T, int WAVES, int CH, bool AHEAD>
+// 16384 in 2 chunks of 16 wavefronts 4096 x 16384 108 us with the sums, 1 x 16384 4.7, in 4 of 8 wavefronts 112 and 6.1.  Up to 256 on LANES = 16: 100000 x 128 19.6 us, on whole wavefronts 44.6; 16384 x 80
+// float32 8.6, 12.5; 1410 x 80 5.7, 6.5; 8192 x 200 8.2, 10.4.
+template <typename T, int WAVES, int CH, bool AHEAD, int LANES = 64>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_backward_kernel(const NormBackArgs a, float* __restrict__ partials) {
-  constexpr int TEAM = WAVES * 64, TEAMS = WAVES == 1 ? 4 : 1;
+  constexpr int TEAM = WAVES * LANES, TEAMS = WAVES == 1 ? 256 / LANES : 1;
   __shared__ float part[2][WAVES];
-  __shared__ float sums[WAVES == 1 ? 4 : 1][WAVES == 1 ? CH * 512 : 1];
-  const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, team = WAVES == 1 ? threadIdx.x >> 6 : 0;
+  __shared__ float sums[TEAMS][WAVES == 1 ? CH * TEAM * 8 : 1];
+  const int t = WAVES == 1 ? threadIdx.x % LANES : threadIdx.x, team = WAVES == 1 ? threadIdx.x / LANES : 0;
   const int D = a.dim, step = gridDim.x * TEAMS;
   const float over = 1.0f / (float)D;
   float g[CH][8], acc[CH][8];
@@ -196,7 +201,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_backwar
       }
     Raw<T> y2[CH], x2[CH], d2[CH];
     if (AHEAD && row + step < a.rows) fetch(row + step, y2, x2, d2);
-    dot = sum_of_64(dot);
+    dot = LANES == 16 ? sum_of_16(dot) : sum_of_64(dot);
     if (WAVES > 1) {
       if ((t & 63) == 0) part[turn][t >> 6] = dot;
       __syncthreads();
@@ -226,14 +231,18 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_backwar
     }
   }
   if (!a.dgamma) return;
-  if (WAVES == 1) {                    // the four teams' sums in order
+  if (WAVES == 1) {                    // the teams' sums in order
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) sums[team][8 * (i * TEAM + t) + j] = acc[i][j];
     __syncthreads();
-    for (int c = threadIdx.x; c < D; c += 256)
-      partials[(int64_t)blockIdx.x * D + c] = (sums[0][c] + sums[WAVES == 1 ? 1 : 0][c]) + (sums[WAVES == 1 ? 2 : 0][c] + sums[WAVES == 1 ? 3 : 0][c]);
+    for (int c = threadIdx.x; c < D; c += 256) {
+      float sum = sums[0][c];
+#pragma unroll
+      for (int w = 1; w < TEAMS; ++w) sum += sums[w][c];
+      partials[(int64_t)blockIdx.x * D + c] = sum;
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
@@ -297,12 +306,12 @@ __global__ __launch_bounds__(256) void rmsnorm_columns_kernel(const NormBackArgs
 }
 
 // Partial sums of gamma's gradient: workgroups of the one-pass kernel, or strands of rows.  As many as hide the loads, but every one is a row for
-// sum_rows_kernel.  Both kernels, bf16, us: 8192 x 300 12.3 with 1024, 13.0 with 512; 8192 x 1024 15.8 with 512, 18.4 with 1024; 5000 x 1500 25.2 with 512, 22.1 with 768,
+// sum_rows_kernel.  Both kernels, bf16, us: 100000 x 128 19.6 with 512, 22.2 with 256, 20.8 with 1024; 8192 x 300 12.3 with 1024, 13.0 with 512; 8192 x 1024 15.8 with 512, 18.4 with 1024; 5000 x 1500 25.2 with 512, 22.1 with 768,
 // 8192 x 2048 27.7, 26.2, 27.7 with 1024, but 1000 x 1500 10.6, 12.2; 4096 x 4096 27.4 with 512, 31.9 with 256, 29.4 with 768; 4096 x 8192 52.0 with 256, 50.4 with 512,
 // but 1000 x 16384 31.0, 37.5.
 int backward_groups(int rows, int dim) {
-  const int teams = dim <= 1024 ? (rows + 3) / 4 : rows;
-  const int most = dim <= 512 ? 1024 : dim > 4096 ? 256 : dim > 1024 && dim <= 2048 && rows >= 4096 ? 768 : 512;
+  const int teams = dim <= 256 ? (rows + 15) / 16 : dim <= 1024 ? (rows + 3) / 4 : rows;
+  const int most = dim <= 256 ? 512 : dim <= 512 ? 1024 : dim > 4096 ? 256 : dim > 1024 && dim <= 2048 && rows >= 4096 ? 768 : 512;
   return teams < most ? teams : most;
 }
 
@@ -311,7 +320,9 @@ hipError_t rmsnorm_backward_of(const NormBackArgs& a, hipStream_t s) {
   const int groups = backward_groups(a.rows, a.dim);
   const bool alone = groups == 1 && a.dim <= kOnePass;          // its sums are the gradient
   float* partials = alone ? a.dgamma : a.work;
-  if (a.dim <= 512) rmsnorm_backward_kernel<T, 1, 1, true><<<groups, 256, 0, s>>>(a, partials);
+  if (a.dim <= 128) rmsnorm_backward_kernel<T, 1, 1, true, 16><<<groups, 256, 0, s>>>(a, partials);
+  else if (a.dim <= 256) rmsnorm_backward_kernel<T, 1, 2, true, 16><<<groups, 256, 0, s>>>(a, partials);
+  else if (a.dim <= 512) rmsnorm_backward_kernel<T, 1, 1, true><<<groups, 256, 0, s>>>(a, partials);
   else if (a.dim <= 1024) rmsnorm_backward_kernel<T, 1, 2, true><<<groups, 256, 0, s>>>(a, partials);
   else if (a.dim <= 2048) rmsnorm_backward_kernel<T, 4, 1, true><<<groups, 256, 0, s>>>(a, partials);
   else if (a.dim <= 4096) rmsnorm_backward_kernel<T, 4, 2, true><<<groups, 256, 0, s>>>(a, partials);

@@ -483,7 +483,8 @@ def test_rmsnorm_backward_of_few_rows(rows, dim):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
-@pytest.mark.parametrize("rows,dim", [(1100, 1500), (4100, 1030), (600, 9001), (3, 12288), (520, 12289), (2, 13000)])
+@pytest.mark.parametrize("rows,dim", [(1100, 1500), (4100, 1030), (600, 9001), (3, 12288), (520, 12289), (2, 13000), (33000, 24), (9000, 100), (4100, 200), (17, 256),
+                                      (4099, 257)])
 def test_rmsnorm_where_workgroups_take_several_rows(rows, dim, dtype):
     test_rmsnorm(rows, dim, dtype)
     test_rmsnorm_backward(rows, dim, dtype)
