@@ -235,10 +235,11 @@ def quantize(x, block=1, rows=True, transposed=False, mask=None, column_sums=Fal
     return QuantizeResult(Quantized(q, s, block) if rows else None, Quantized(qt, st, block) if transposed else None, sums)
 
 
-def product(a, b, bias=None, relu=False, dtype=BF16, out=None):
+def product(a, b, bias=None, relu=False, dtype=BF16, out=None, float32_sums=False):
     """slp_product: act(a b^T + bias) of two Quantized matrices with the same number of columns, as a matrix of `dtype` (or into
-    `out`, whose type decides then)."""
-    return _outputs(_binding().product(a[0], a[1], a[2], b[0], b[1], b[2], bias, relu, dtype, out, _stream()))
+    `out`, whose type decides then).  Sums for a bf16 output of many rows lose what is 2^-13 below the largest of 8 neighbouring products
+    (some 2e-5 of the result, where nothing cancels); `float32_sums` adds them in float32, as for a float32 output, at half the rate."""
+    return _outputs(_binding().product(a[0], a[1], a[2], b[0], b[1], b[2], bias, relu, dtype, out, float32_sums, _stream()))
 
 
 def rmsnorm(x, gamma=None, residual=None, eps=1e-6, normed=False, quantized=True):

@@ -188,7 +188,7 @@ PyObject* quantize(PyObject* const* a) {
   return rc ? code(rc) : tuple({r.q, r.scales, t.q, t.scales, sums});
 }
 
-// a's values, scales, block, b's, bias, relu, dtype, out, stream
+// a's values, scales, block, b's, bias, relu, dtype, out, float32_sums, stream
 PyObject* product(PyObject* const* a) {
   const int64_t cols = tensor(a[0]).size(-1);
   const int64_t ablock = integer(a[2]), bblock = integer(a[5]);
@@ -210,7 +210,7 @@ PyObject* product(PyObject* const* a) {
   }
   const at::Tensor work = room.bytes(size);
   const int rc = slp_product(x.at, x.ld, x.scales_at, x.lds, (int)ablock, y.at, y.ld, y.scales_at, y.lds, (int)bblock, vector(a[6], n, x.q), truth(a[7]), side(m), side(n),
-                             side(cols), out.data_ptr(), ldo, dt, address(work), size, PyLong_AsVoidPtr(a[10]));
+                             side(cols), out.data_ptr(), ldo, truth(a[10]) ? dt | SLP_FLOAT32_SUMS : dt, address(work), size, PyLong_AsVoidPtr(a[11]));
   if (rc) return code(rc);
   return wrapped(out);
 }
@@ -338,7 +338,7 @@ PyMethodDef method(const char* name) {
   return {name, (PyCFunction)(void (*)())entry<F, N>, METH_FASTCALL, nullptr};
 }
 
-PyMethodDef methods[] = {method<quantize, 7>("quantize"),           method<product, 11>("product"), method<rmsnorm, 7>("rmsnorm"), method<rmsnorm_backward, 7>("rmsnorm_backward"),
+PyMethodDef methods[] = {method<quantize, 7>("quantize"),           method<product, 12>("product"), method<rmsnorm, 7>("rmsnorm"), method<rmsnorm_backward, 7>("rmsnorm_backward"),
                          method<gradient_norm, 2>("gradient_norm"), method<clip_gradients, 4>("clip_gradients"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -61,6 +61,7 @@ struct ProductArgs {
   void* out;                // [M][ldo]
   int64_t ldo;
   int out_dtype;
+  bool exact;               // float32 sums for a bf16 output, too
   float* work;              // product_floats(M, N, K)
 };
 size_t product_floats(int M, int N, int K);

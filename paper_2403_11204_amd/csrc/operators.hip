@@ -155,6 +155,8 @@ int slp_product(const void* a, int64_t lda, const void* a_scales, int64_t ldsa, 
                 int64_t ldsb, int b_block, const float* bias, int relu, int M, int N, int K, void* out, int64_t ldo, int dt, void* workspace,
                 size_t workspace_bytes, slp_stream stream) {
   const char* const who = "slp_product";
+  const bool exact = dt >= 0 && (dt & SLP_FLOAT32_SUMS) != 0;
+  if (exact) dt &= ~SLP_FLOAT32_SUMS;
   if (!known(dt)) return fail(SLP_ERR_ARG, "%s: unknown dtype %d", who, dt);
   if ((a_block != 1 && a_block != kScaleBlock) || (b_block != 1 && b_block != kScaleBlock))
     return fail(SLP_ERR_ARG, "%s: blocks of 1 or %d rows (got %d, %d)", who, kScaleBlock, a_block, b_block);
@@ -172,7 +174,7 @@ int slp_product(const void* a, int64_t lda, const void* a_scales, int64_t ldsa, 
   if (bias && off(bias, 4)) return fail(SLP_ERR_ALLOC, "%s: bias is not on an element's boundary", who);
   SLP_CHECK(check_work(who, workspace, workspace_bytes, slp_product_workspace_bytes(M, N, K)));
   const ProductArgs g{(const uint8_t*)a, (const uint8_t*)a_scales, (const uint8_t*)b, (const uint8_t*)b_scales, lda, ldsa, ldb, ldsb,
-                      a_block == 1 ? 0 : 7, b_block == 1 ? 0 : 7, M, N, K, bias, relu, out, ldo, dt, (float*)workspace};
+                      a_block == 1 ? 0 : 7, b_block == 1 ? 0 : 7, M, N, K, bias, relu, out, ldo, dt, exact, (float*)workspace};
   HIP_TRY(launch_product(g, (hipStream_t)stream));
   return SLP_OK;
 }
