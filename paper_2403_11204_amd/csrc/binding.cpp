@@ -267,8 +267,10 @@ PyObject* rmsnorm_backward(PyObject* const* a) {
   return rc ? code(rc) : tuple({dx, dgamma});
 }
 
-// A list of tensors as the library takes it.
+// Several tensors as the library takes them.  They are held until the call is queued: what an iterator makes has no other owner, and its memory would be
+// given to the outputs and the workspace.
 struct Tensors {
+  std::vector<at::Tensor> held;
   std::vector<void*> at;
   std::vector<int64_t> counts;
   std::vector<int> dts;
@@ -286,6 +288,7 @@ Tensors tensors(PyObject* list, const Tensors* as) {
     require(t.is_cuda() && t.is_contiguous(), "contiguous tensors on the device are wanted");
     if (i == 0) all.device = t.device();
     require(t.device() == all.device, "tensors on one device are wanted");
+    all.held.push_back(t);
     all.at.push_back(t.data_ptr());
     all.counts.push_back(t.numel());
     all.dts.push_back(dtype_of(t));
