@@ -231,7 +231,7 @@ def quantize(x, block=1, rows=True, transposed=False, mask=None, column_sums=Fal
     """slp_quantize: x in 8 bits, row-major (`rows`) and transposed as asked, with a scale for each 128 elements of a row of the
     result (block=1) or each 128 x 128 block (block=128).  Elements whose `mask` is not positive count as zero; column_sums: also
     the sums of x's (masked) columns."""
-    q, s, qt, st, sums = _outputs(_binding().quantize(x, block, rows, transposed, mask, column_sums, _stream()))
+    q, s, qt, st, sums = _outputs(_binding().quantize(x, block, rows, transposed, mask, column_sums))
     return QuantizeResult(Quantized(q, s, block) if rows else None, Quantized(qt, st, block) if transposed else None, sums)
 
 
@@ -239,29 +239,29 @@ def product(a, b, bias=None, relu=False, dtype=BF16, out=None, float32_sums=Fals
     """slp_product: act(a b^T + bias) of two Quantized matrices with the same number of columns, as a matrix of `dtype` (or into
     `out`, whose type decides then).  Sums for a bf16 output of many rows lose what is 2^-13 below the largest of 8 neighbouring products
     (some 2e-5 of the result, where nothing cancels); `float32_sums` adds them in float32, as for a float32 output, at half the rate."""
-    return _outputs(_binding().product(a[0], a[1], a[2], b[0], b[1], b[2], bias, relu, dtype, out, float32_sums, _stream()))
+    return _outputs(_binding().product(a[0], a[1], a[2], b[0], b[1], b[2], bias, relu, dtype, out, float32_sums))
 
 
 def rmsnorm(x, gamma=None, residual=None, eps=1e-6, normed=False, quantized=True):
     """slp_rmsnorm: h = x + residual (x itself without one), rstd, the norm y in x's type if `normed`, and y8 in 8 bits if `quantized`."""
-    h, rstd, y, q, s = _outputs(_binding().rmsnorm(x, gamma, residual, eps, normed, quantized, _stream()))
+    h, rstd, y, q, s = _outputs(_binding().rmsnorm(x, gamma, residual, eps, normed, quantized))
     return NormResult(h, rstd, y, Quantized(q, s, 1) if quantized else None)
 
 
 def rmsnorm_backward(dy, h, gamma, rstd, dh=None, gamma_grad=True):
     """slp_rmsnorm_backward: (the gradient of x and of the residual, the gradient of gamma or None)."""
-    return _outputs(_binding().rmsnorm_backward(dy, h, gamma, rstd, dh, gamma_grad, _stream()))
+    return _outputs(_binding().rmsnorm_backward(dy, h, gamma, rstd, dh, gamma_grad))
 
 
 def gradient_norm(tensors):
     """slp_gradient_norm: the norm of all tensors' values together, as a device scalar."""
-    return _outputs(_binding().gradient_norm(tensors, _stream()))
+    return _outputs(_binding().gradient_norm(tensors))
 
 
 def clip_gradients(tensors, max_norm, out=None):
     """slp_clip_gradients: scales the tensors together to a norm of at most max_norm, in place or into `out` (tensors of the same
     sizes and types).  Returns the norm before, a device scalar; where it is not finite the values are left as they are."""
-    return _outputs(_binding().clip_gradients(tensors, max_norm, out, _stream()))
+    return _outputs(_binding().clip_gradients(tensors, max_norm, out))
 
 
 class Segment:

@@ -83,8 +83,8 @@ def _compile_binding(verbose):
     from torch.utils import cpp_extension
     obj = os.path.join(BUILD, "binding.o")
     cmd = ["g++", "-std=c++17", "-O2", "-fPIC", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
-           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"]]
-    for path in cpp_extension.include_paths():
+           "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"]]
+    for path in cpp_extension.include_paths("cuda"):         # (torch's name for HIP, too)
         cmd += ["-isystem", path]
     _run(cmd + ["-c", os.path.join(CSRC, "binding.cpp"), "-o", obj], "g++ on binding.cpp", verbose)
     return obj
@@ -93,7 +93,7 @@ def _compile_binding(verbose):
 def _link_binding(obj, verbose):
     from torch.utils import cpp_extension
     libs = [a for path in cpp_extension.library_paths() for a in ("-L", path)]
-    _run(["g++", "-shared", "-o", BINDING, obj, "-L", HERE, "-l:libslp.so", "-Wl,-rpath,$ORIGIN"] + libs + ["-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"], "linking _binding.so", verbose)
+    _run(["g++", "-shared", "-o", BINDING, obj, "-L", HERE, "-l:libslp.so", "-Wl,-rpath,$ORIGIN"] + libs + ["-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip"], "linking _binding.so", verbose)
 
 
 def build(verbose=True):

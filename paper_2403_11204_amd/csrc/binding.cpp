@@ -1,9 +1,12 @@
 // The operators' way from Python tensors to the C ABI (include/slp.h): argument checks, room for the outputs and workspaces from torch's
 // allocator, the call.  An operator on a few rows takes the device 3 to 5 us; written in Python these steps took the host 10 to 17 us
-// a call, here 5 with one launch, 8 to 12 with two.  Each function returns its outputs, or the library's error code as an integer.  `stream` is a hipStream_t as an integer.
+// a call, here 5 with one launch, 8 to 12 with two.  Each function returns its outputs, or the library's error code as an integer.  A call runs on the device
+// that its tensors are on, whichever is current, and on torch's current stream of that device.
 #include <Python.h>
 
 #include <ATen/Functions.h>
+#include <c10/core/DeviceGuard.h>
+#include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
@@ -71,6 +74,17 @@ const float* vector(PyObject* o, int64_t n, const at::Tensor& x) {
   require(t.device() == x.device() && t.scalar_type() == at::kFloat && t.is_contiguous() && t.numel() == n, "a contiguous float32 vector on the same device is wanted");
   return (const float*)t.data_ptr();
 }
+
+// The tensors' device, current as long as this lives, and torch's current stream of it.
+class On {
+ public:
+  explicit On(const at::Device& device) : guard_(device), stream_(c10::hip::getCurrentHIPStream(device.index()).stream()) {}
+  slp_stream stream() const { return stream_; }
+
+ private:
+  c10::DeviceGuard guard_;
+  slp_stream stream_;
+};
 
 // Room for a call's outputs and workspace.  Each allocation takes the host 0.6 us: where all of them come to 256 KB at most (a request's
 // rows: the device is done before the host) they are parts of one, on 256-byte boundaries.
@@ -162,7 +176,7 @@ PyObject* tuple(std::initializer_list<at::Tensor> outputs) {
 }
 PyObject* code(int c) { return PyLong_FromLong(c); }
 
-// x, block, rows, transposed, mask, column_sums, stream
+// x, block, rows, transposed, mask, column_sums
 PyObject* quantize(PyObject* const* a) {
   const at::Tensor& x = tensor(a[0]);
   const int64_t block = integer(a[1]), ldx = leading(x), m = x.size(0), n = x.size(1);
@@ -176,6 +190,7 @@ PyObject* quantize(PyObject* const* a) {
   }
   const bool rows = truth(a[2]), transposed = truth(a[3]), column_sums = truth(a[5]);
   const size_t size = column_sums ? slp_quantize_workspace_bytes(side(m), side(n)) : 0;
+  const On on(x.device());
   Room room(x.device(), (rows ? eight_bytes(m, n, block) : 0) + (transposed ? eight_bytes(n, m, block) : 0) + (column_sums ? Room::padded(4 * n) : 0) + Room::padded(size));
   Eight r, t;
   if (rows) r = eight_room(m, n, block, room);
@@ -184,11 +199,11 @@ PyObject* quantize(PyObject* const* a) {
   if (column_sums) sums = room.take({n}, at::kFloat);
   const at::Tensor work = room.bytes(size);
   const int rc = slp_quantize(x.data_ptr(), ldx, mask, ldmask, dt, side(m), side(n), (int)block, r.at, r.ld, r.scales_at, r.lds, t.at, t.ld, t.scales_at, t.lds,
-                              (float*)address(sums), address(work), size, PyLong_AsVoidPtr(a[6]));
+                              (float*)address(sums), address(work), size, on.stream());
   return rc ? code(rc) : tuple({r.q, r.scales, t.q, t.scales, sums});
 }
 
-// a's values, scales, block, b's, bias, relu, dtype, out, float32_sums, stream
+// a's values, scales, block, b's, bias, relu, dtype, out, float32_sums
 PyObject* product(PyObject* const* a) {
   const int64_t cols = tensor(a[0]).size(-1);
   const int64_t ablock = integer(a[2]), bblock = integer(a[5]);
@@ -199,6 +214,7 @@ PyObject* product(PyObject* const* a) {
   at::Tensor out;
   int dt = (int)integer(a[8]);
   int64_t ldo = n;
+  const On on(x.q.device());
   Room room(x.q.device(), Room::padded(size) + (given(a[9]) ? 0 : Room::padded((size_t)(m * n) * (dt == SLP_BF16 ? 2 : 4))));
   if (given(a[9])) {
     out = tensor(a[9]);
@@ -210,12 +226,12 @@ PyObject* product(PyObject* const* a) {
   }
   const at::Tensor work = room.bytes(size);
   const int rc = slp_product(x.at, x.ld, x.scales_at, x.lds, (int)ablock, y.at, y.ld, y.scales_at, y.lds, (int)bblock, vector(a[6], n, x.q), truth(a[7]), side(m), side(n),
-                             side(cols), out.data_ptr(), ldo, truth(a[10]) ? dt | SLP_FLOAT32_SUMS : dt, address(work), size, PyLong_AsVoidPtr(a[11]));
+                             side(cols), out.data_ptr(), ldo, truth(a[10]) ? dt | SLP_FLOAT32_SUMS : dt, address(work), size, on.stream());
   if (rc) return code(rc);
   return wrapped(out);
 }
 
-// x, gamma, residual, eps, normed, quantized, stream
+// x, gamma, residual, eps, normed, quantized
 PyObject* rmsnorm(PyObject* const* a) {
   const at::Tensor& x = tensor(a[0]);
   const int64_t ldx = leading(x), m = x.size(0), n = x.size(1);
@@ -223,6 +239,7 @@ PyObject* rmsnorm(PyObject* const* a) {
   const float* gamma = vector(a[1], n, x);
   const bool normed = truth(a[4]), quantized = truth(a[5]);
   const size_t matrix = Room::padded((size_t)(m * n) * (dt == SLP_BF16 ? 2 : 4));
+  const On on(x.device());
   Room room(x.device(), (given(a[2]) ? matrix : 0) + (normed ? matrix : 0) + (quantized ? eight_bytes(m, n, 1) : 0) + Room::padded(4 * m));
   at::Tensor h = x, y;
   const void* r = nullptr;
@@ -239,11 +256,11 @@ PyObject* rmsnorm(PyObject* const* a) {
   if (quantized) e = eight_room(m, n, 1, room);
   const at::Tensor rstd = room.take({m}, at::kFloat);
   const int rc = slp_rmsnorm(x.data_ptr(), ldx, r, ldr, gamma, (float)number(a[3]), dt, side(m), side(n), to, n, address(y), n, e.at, e.ld, e.scales_at, e.lds,
-                             (float*)rstd.data_ptr(), PyLong_AsVoidPtr(a[6]));
+                             (float*)rstd.data_ptr(), on.stream());
   return rc ? code(rc) : tuple({h, rstd, y, e.q, e.scales});
 }
 
-// dy, h, gamma, rstd, dh, gamma_grad, stream
+// dy, h, gamma, rstd, dh, gamma_grad
 PyObject* rmsnorm_backward(PyObject* const* a) {
   const at::Tensor &dy = tensor(a[0]), &h = tensor(a[1]);
   const int64_t ldh = leading(h), lddy = like(dy, h), m = h.size(0), n = h.size(1);
@@ -257,13 +274,14 @@ PyObject* rmsnorm_backward(PyObject* const* a) {
   require(given(a[3]), "rstd of the forward pass is wanted");
   const float *gamma = vector(a[2], n, h), *rstd = vector(a[3], m, h);
   const size_t size = slp_rmsnorm_backward_workspace_bytes(side(m), side(n));
+  const On on(h.device());
   Room room(h.device(), Room::padded((size_t)(m * n) * (dt == SLP_BF16 ? 2 : 4)) + Room::padded(4 * n) + Room::padded(size));
   const at::Tensor dx = room.take({m, n}, h.scalar_type());
   at::Tensor dgamma;
   if (truth(a[5])) dgamma = room.take({n}, at::kFloat);
   const at::Tensor work = room.bytes(size);
   const int rc = slp_rmsnorm_backward(dy.data_ptr(), lddy, h.data_ptr(), ldh, gamma, rstd, dh, lddh, dt, side(m), side(n), dx.data_ptr(), n, (float*)address(dgamma),
-                                      address(work), size, PyLong_AsVoidPtr(a[6]));
+                                      address(work), size, on.stream());
   return rc ? code(rc) : tuple({dx, dgamma});
 }
 
@@ -297,29 +315,31 @@ Tensors tensors(PyObject* list, const Tensors* as) {
   return all;
 }
 
-// tensors, stream
+// tensors
 PyObject* gradient_norm(PyObject* const* a) {
   const Tensors in = tensors(a[0], nullptr);
   const int n = (int)in.at.size();
   const size_t size = slp_gradient_norm_workspace_bytes(n);
+  const On on(in.device);
   Room room(in.device, Room::padded(4) + Room::padded(size));
   const at::Tensor norm = room.take({}, at::kFloat), work = room.bytes(size);
-  const int rc = slp_gradient_norm(in.at.data(), in.counts.data(), in.dts.data(), n, (float*)norm.data_ptr(), address(work), size, PyLong_AsVoidPtr(a[1]));
+  const int rc = slp_gradient_norm(in.at.data(), in.counts.data(), in.dts.data(), n, (float*)norm.data_ptr(), address(work), size, on.stream());
   if (rc) return code(rc);
   return wrapped(norm);
 }
 
-// tensors, max_norm, out, stream
+// tensors, max_norm, out
 PyObject* clip_gradients(PyObject* const* a) {
   const Tensors in = tensors(a[0], nullptr);
   const int n = (int)in.at.size();
   Tensors out;
   if (given(a[2])) out = tensors(a[2], &in);
   const size_t size = slp_gradient_norm_workspace_bytes(n);
+  const On on(in.device);
   Room room(in.device, Room::padded(4) + Room::padded(size));
   const at::Tensor norm = room.take({}, at::kFloat), work = room.bytes(size);
   const int rc = slp_clip_gradients(in.at.data(), given(a[2]) ? out.at.data() : nullptr, in.counts.data(), in.dts.data(), n, (float)number(a[1]), (float*)norm.data_ptr(),
-                                    address(work), size, PyLong_AsVoidPtr(a[3]));
+                                    address(work), size, on.stream());
   if (rc) return code(rc);
   return wrapped(norm);
 }
@@ -341,8 +361,8 @@ PyMethodDef method(const char* name) {
   return {name, (PyCFunction)(void (*)())entry<F, N>, METH_FASTCALL, nullptr};
 }
 
-PyMethodDef methods[] = {method<quantize, 7>("quantize"),           method<product, 12>("product"), method<rmsnorm, 7>("rmsnorm"), method<rmsnorm_backward, 7>("rmsnorm_backward"),
-                         method<gradient_norm, 2>("gradient_norm"), method<clip_gradients, 4>("clip_gradients"), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {method<quantize, 6>("quantize"),           method<product, 11>("product"), method<rmsnorm, 6>("rmsnorm"), method<rmsnorm_backward, 6>("rmsnorm_backward"),
+                         method<gradient_norm, 1>("gradient_norm"), method<clip_gradients, 3>("clip_gradients"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

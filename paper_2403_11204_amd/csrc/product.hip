@@ -21,7 +21,7 @@
 // columns of one row of the output.
 #include "eightbit_device.h"
 
-#include <mutex>
+#include <atomic>
 #include <type_traits>
 #include <utility>
 
@@ -761,17 +761,28 @@ int parts_of(Shape shape, int M, int N, int K) {
   return t < most ? (int)t : most;
 }
 
+// Lets a kernel have that much LDS, once on each device (bit of `done`); host threads that launch first together both do.
+hipError_t allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = (uint64_t)1 << (device & 63);
+  if (device < 64 && (done.load(std::memory_order_acquire) & bit)) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess && device < 64) done.fetch_or(bit, std::memory_order_release);
+  return e;
+}
+
 template <int BM, int BN, int NS, int NG, bool EXACT>
 hipError_t launch_tile(const ProductArgs& g, int wanted, hipStream_t s) {
   constexpr int smem = NG * (NS * (BM + BN) * 128 + 2048);
   static_assert(smem >= (NG - 1) * BM * BN * 4, "room for the groups' sums");
-  static std::once_flag once;          // one attribute call per instantiation, also when two host threads launch first together
-  static hipError_t result = hipSuccess;
-  std::call_once(once, [] { result = hipFuncSetAttribute((const void*)product_tile_kernel<BM, BN, NS, NG, EXACT>, hipFuncAttributeMaxDynamicSharedMemorySize, smem); });
-  if (result != hipSuccess) return result;
+  static std::atomic<uint64_t> done{0};
+  hipError_t e = allow_lds((const void*)product_tile_kernel<BM, BN, NS, NG, EXACT>, smem, done);
+  if (e != hipSuccess) return e;
   const int nk = (g.K + 127) / 128, all = wanted * NG, kper = all > 1 ? ((nk + all - 1) / all + 3) & ~3 : nk, parts = wanted > 1 ? (nk + NG * kper - 1) / (NG * kper) : 1;
   hipLaunchKernelGGL((product_tile_kernel<BM, BN, NS, NG, EXACT>), dim3((unsigned)tiles_of(g.M, g.N, BM, BN), parts), dim3(256 * NG), smem, s, g, kper);
-  hipError_t e = hipGetLastError();
+  e = hipGetLastError();
   if (e != hipSuccess || parts == 1) return e;
   const int64_t quads = (int64_t)g.M * ((g.N + 3) / 4);
   join_kernel<<<(unsigned)((quads + 255) / 256), 256, 0, s>>>(g, parts);
@@ -780,10 +791,9 @@ hipError_t launch_tile(const ProductArgs& g, int wanted, hipStream_t s) {
 
 template <bool EXACT>
 hipError_t launch_long(const ProductArgs& g, hipStream_t s) {
-  static std::once_flag once;
-  static hipError_t result = hipSuccess;
-  std::call_once(once, [] { result = hipFuncSetAttribute((const void*)product_long_kernel<EXACT>, hipFuncAttributeMaxDynamicSharedMemorySize, kBigSmem); });
-  if (result != hipSuccess) return result;
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = allow_lds((const void*)product_long_kernel<EXACT>, kBigSmem, done);
+  if (e != hipSuccess) return e;
   product_long_kernel<EXACT><<<(unsigned)tiles_of(g.M, g.N, 256, 256), 256, kBigSmem, s>>>(g);
   return hipGetLastError();
 }

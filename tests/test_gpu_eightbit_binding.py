@@ -20,3 +20,59 @@ def test_tensors_that_only_the_call_holds():
         out = [torch.empty(h.shape, device=DEV) for h in halves]
         norm = api.clip_gradients((h.float() for h in halves), ref / 2, out=iter(out))
         assert abs(float(norm) - ref) <= 1e-6 * ref and all(bool(((o - 0.25).abs() <= 1e-6).all()) for o in out)
+
+
+def calls(device):
+    """Every operator on small tensors of `device`, and what they give."""
+    g = torch.Generator().manual_seed(3)
+    x, r, dy, w = (torch.randn(s, generator=g).to(device) for s in ((40, 200), (40, 200), (40, 200), (300, 200)))
+    gamma = torch.ones(200, device=device)
+
+    def run():
+        n = api.rmsnorm(x, gamma, residual=r, normed=True)
+        w8 = api.quantize(w, block=128, transposed=True)
+        z = api.product(n.y8, w8.rows, relu=True, dtype=api.F32)
+        q = api.quantize(x, transposed=True, mask=r, column_sums=True)
+        dx, dgamma = api.rmsnorm_backward(dy, n.h, gamma, n.rstd)
+        norm = api.gradient_norm([dx, dgamma])
+        out = [torch.empty_like(dx), torch.empty_like(dgamma)]
+        return [n.h, n.y, z, q.column_sums, dx, dgamma, norm, api.clip_gradients([dx, dgamma], 0.1, out=out)] + out
+
+    return x, run
+
+
+def test_the_stream_is_the_current_one_of_the_tensors_device(monkeypatch):
+    x, run = calls(DEV)
+    ref = [t.clone() for t in run()]
+    start = x.clone()
+
+    def not_asked():
+        raise AssertionError("the current device's stream was looked up, whatever device the tensors are on")
+
+    monkeypatch.setattr(api, "_stream", not_asked)
+    assert all(torch.equal(a, b) for a, b in zip(run(), ref))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            x.zero_()
+            torch.cuda._sleep(2_000_000)           # what another stream queues meanwhile would read zeros
+            x.copy_(start)
+            got = run()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, ref))
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two devices")
+def test_tensors_on_a_device_that_is_not_the_current_one():
+    ref = [t.cpu() for t in calls("cuda:0")[1]()]
+    with torch.cuda.device(0):
+        x, run = calls("cuda:1")
+        for _ in range(3):
+            with torch.cuda.device(1):
+                torch.cuda._sleep(2_000_000)
+            got = run()
+        assert torch.cuda.current_device() == 0 and all(t.device == x.device for t in got)
+        assert all(torch.equal(a.cpu(), b) for a, b in zip(got, ref))
+    big = [api.quantize(torch.randn(4096, 512, device="cuda:1")).rows for _ in range(2)]      # kernels that take more than the usual LDS
+    assert api.product(*big).device.index == 1 and api.product(*big, dtype=api.F32).device.index == 1
