@@ -286,7 +286,8 @@ int slp_count_correct_static(const void* logits /*device*/, const int32_t* targe
 /* ---- segments in 8 bits ----------------------------------------------------------------
  * Products of 8-bit matrices run at twice the bf16 rate and read half the bytes.  An 8-bit matrix here is two device buffers:
  *   q       [rows][ldq]   e4m3 values (OCP: 4 exponent and 3 fraction bits, largest 448, no infinity), one byte each; q on a 16-byte boundary,
- *                         ldq a multiple of 16, the bytes from the last column up to the next multiple of 16 zero;
+ *                         ldq a multiple of 16; the bytes from the last column up to the next multiple of 16 are read with
+ *                         it but not interpreted (so the matrix may be the first columns of a wider one), and written as zeros;
  *   scales  [rows / block, rounded up][lds]   one byte e for each 128 consecutive columns (and, block = 128, each 128 rows): the values
  *                         stand for q * 2^(e - 127); 255 is NaN.  On a 4-byte boundary, lds a multiple of 4 and at least the number of
  *                         blocks of a row; bytes past that number are not interpreted.

@@ -187,8 +187,8 @@ def mean_loss(losses, out=None):
 
 # ---- segments in 8 bits -----------------------------------------------------------------------------------------
 # A matrix in 8 bits: q [rows, cols] (float8_e4m3fn, rows on 16-byte boundaries), scales [rows / block, cols / 128] (both rounded up,
-# float8_e8m0fnu, rows on 4-byte boundaries), block 1 or 128 rows that share a scale.  Between the last column and the next multiple of 16 the
-# values in memory are zeros: a slice of whole columns ends at a multiple of 128, or where the matrix does.
+# float8_e8m0fnu, rows on 4-byte boundaries), block 1 or 128 rows that share a scale.  What lies in memory between the last column and the
+# next multiple of 16 is not interpreted: slices of rows (of whole blocks) and of columns from a multiple of 512 on are matrices like any other.
 Quantized = collections.namedtuple("Quantized", "q scales block")
 QuantizeResult = collections.namedtuple("QuantizeResult", "rows transposed column_sums")
 NormResult = collections.namedtuple("NormResult", "h rstd y y8")
@@ -216,8 +216,8 @@ def _outputs(r):
 
 
 def empty_quantized(rows, cols, block=1, device="cuda"):
-    """Room for a matrix in 8 bits: rows on 128-byte boundaries and, where there are many, not a multiple of 4 KB apart (they are read
-    faster then)."""
+    """Room for a matrix in 8 bits, not initialised: rows on 128-byte boundaries and, where there are many, not a multiple of 4 KB apart
+    (they are read faster then)."""
     ld, blocks, srows = (cols + 127) & -128, (cols + 127) >> 7, -(-rows // block)
     if ld % 4096 == 0 and rows > 16:
         ld += 128

@@ -67,6 +67,28 @@ __device__ __forceinline__ f32x4 mma(const Fragment<true>& b, const Fragment<tru
   return acc;
 }
 
+// What lies between a row's last column and the next multiple of 16 is whatever the memory holds (the columns that follow, where the matrix is part of a
+// wider one).  It is read with the last piece of the row, and cut off with this: ones over the first n of 16 bytes.
+__device__ __forceinline__ u32x4 first_bytes(int n) {
+  u32x4 mask;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int m = n - 4 * i;
+    mask[i] = m >= 4 ? ~0u : m <= 0 ? 0u : (1u << (8 * m)) - 1u;
+  }
+  return mask;
+}
+// The same for a lane's two pieces of a k-tile of which `left` columns exist; what begins past them is zero already.
+__device__ __forceinline__ void cut_off(i32x8& v, int left, int lgrp) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int n = left - 64 * h - 16 * lgrp;
+    const u32x4 mask = first_bytes(n);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[4 * h + j] &= (int)mask[j];
+  }
+}
+
 // Four consecutive columns n .. n + 3 of row m.
 __device__ __forceinline__ void store4(const ProductArgs& g, int m, int n, f32x4 v) {
   if (m >= g.M || n >= g.N) return;
@@ -177,23 +199,16 @@ __global__ __launch_bounds__(256 * NG) void product_tile_kernel(const ProductArg
 #pragma unroll
     for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-#pragma unroll
-  for (int s = 0; s < NS - 1; ++s) load(k0 + s, s);
-  for (int kt = k0; kt < (NG > 1 ? k0 + kper : k1); ++kt) {
-    // this wavefront's part of k-tile kt has landed and its reads of the last one are done; behind the barrier, everybody's
-    __builtin_amdgcn_s_waitcnt(SLP_VMCNT_LGKM0((NS - 2) * NLD));
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    const int step = kt - k0;
-    load(kt + NS - 1, (step + NS - 1) % NS);
-    if (NG > 1 && kt >= k1) continue;            // (a shorter part takes the others' barriers)
-    const unsigned char* const st = smem + step % NS * STAGE;
+  // a k-tile that everybody's loads have filled
+  auto multiply = [&](int kt, auto ragged) {
+    const unsigned char* const st = smem + (kt - k0) % NS * STAGE;
     const unsigned char* const sc = smem + (kt & 4) * 256 + (kt & 3);
     Fragment<EXACT> a[MI], b[NI];
     auto fragment = [&](uint32_t at) {
       const u32x4 lo = *(const u32x4*)(st + at + x0), hi = *(const u32x4*)(st + at + x1);
-      return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+      i32x8 v = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+      if constexpr (ragged) cut_off(v, g.K & 127, lgrp);
+      return v;
     };
 #pragma unroll
     for (int j = 0; j < NI; ++j) b[j].set(fragment(fragB + j * 2048), sc[scaleB + j * 64]);
@@ -203,6 +218,29 @@ __global__ __launch_bounds__(256 * NG) void product_tile_kernel(const ProductArg
     for (int i = 0; i < MI; ++i)
 #pragma unroll
       for (int j = 0; j < NI; ++j) acc[i][j] = mma(b[j], a[i], acc[i][j]);
+  };
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s) load(k0 + s, s);
+  // The last k-tile has a copy of its own behind the loop where it ends inside 16 bytes: 0.2 to 0.3 us of such a product (1000 x 3001 x 1500 in float32 16.9 / 17.2, its
+  // sums then leave nothing to the memory behind a row's end).  Asked inside the loop, every product would take 0.2 us longer.
+  const int end = NG > 1 ? k0 + kper : k1, whole = (g.K & 15) && k0 < nk && end >= nk ? nk - 1 : end;
+  for (int kt = k0; kt < whole; ++kt) {
+    // this wavefront's part of k-tile kt has landed and its reads of the last one are done; behind the barrier, everybody's
+    __builtin_amdgcn_s_waitcnt(SLP_VMCNT_LGKM0((NS - 2) * NLD));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    load(kt + NS - 1, (kt - k0 + NS - 1) % NS);
+    if (NG > 1 && kt >= k1) continue;            // (a shorter part takes the others' barriers)
+    multiply(kt, std::false_type{});
+  }
+  if (whole < end) {
+    __builtin_amdgcn_s_waitcnt(SLP_VMCNT_LGKM0((NS - 2) * NLD));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    multiply(nk - 1, std::true_type{});
+    for (int kt = nk; kt < end; ++kt) __builtin_amdgcn_s_barrier();
   }
   __builtin_amdgcn_s_waitcnt(SLP_VMCNT(0));      // no load into LDS may outlive the workgroup
   if constexpr (NG > 1) {
@@ -279,7 +317,7 @@ __global__ __launch_bounds__(1024) void product_rows_kernel(const ProductArgs g)
   auto scale = [&](__amdgpu_buffer_rsrc_t r, uint32_t row, int kt) {        // (past the end: the last one, for zeros)
     return (int)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, row + (uint32_t)(kt < nk ? kt : nk - 1), 0, 0);
   };
-  for (int k0 = w * STEP; k0 < nk; k0 += waves * STEP) {
+  auto turn = [&](int k0, auto ragged) {
     i32x8 vb[STEP], va[STEP][MF];
     int sb[STEP], sa[STEP][MF];
 #pragma unroll
@@ -295,14 +333,20 @@ __global__ __launch_bounds__(1024) void product_rows_kernel(const ProductArgs g)
 #pragma unroll
     for (int s = 0; s < STEP; ++s) {
       Fragment<true> b, a;
+      if constexpr (ragged) cut_off(vb[s], g.K - (k0 + s) * 128, lgrp);
       b.set(vb[s], sb[s]);
 #pragma unroll
       for (int i = 0; i < MF; ++i) {
+        if constexpr (ragged) cut_off(va[s][i], g.K - (k0 + s) * 128, lgrp);
         a.set(va[s][i], sa[s][i]);
         acc[i] = mma(b, a, acc[i]);
       }
     }
-  }
+  };
+  // a copy of its own for the turn that ends inside 16 bytes: the question alone takes 0.2 us of every call
+  int k0 = w * STEP;
+  for (const int end = g.K & 15 ? nk - STEP : nk; k0 < end; k0 += waves * STEP) turn(k0, std::false_type{});
+  if (k0 < nk) turn(k0, std::true_type{});
   f32x4* const part = (f32x4*)smem;
 #pragma unroll
   for (int i = 0; i < MF; ++i) part[(i * waves + w) * 64 + lane] = acc[i];
@@ -445,6 +489,24 @@ __global__ __launch_bounds__(256) void product_long_kernel(const ProductArgs g) 
     __builtin_amdgcn_s_barrier();                                   \
     asm volatile("" ::: "memory");                                  \
   } while (0)
+  // The k-tile whose last piece ends inside 16 bytes: a lane cuts off what it has loaded itself, `wait` having seen it land, before the barrier behind which
+  // others read it.  Only the last k-tiles' copy of the loop asks: the question in the loop itself takes 1 %.
+  const int ragged = g.K & 15 ? nk - 1 : -1;
+#define SLP_CUT(kt, wait)                                                                                           \
+  do {                                                                                                              \
+    if ((kt) == ragged) {                                                                                           \
+      __builtin_amdgcn_s_waitcnt(wait);                                                                             \
+      asm volatile("" ::: "memory");                                                                                \
+      if (chunk == (g.K >> 4 & 7)) {                                                                                \
+        const u32x4 mask = first_bytes(g.K & 15);                                                                   \
+        u32x4* const p = (u32x4*)(smem + ((kt) & 1) * STAGE + w * 1024 + lane * 16);                                \
+        _Pragma("unroll 4") for (int i = 0; i < 16; ++i) p[i * 256] &= mask;                                        \
+      }                                                                                                             \
+      asm volatile("" ::: "memory");                                                                                \
+      __builtin_amdgcn_s_waitcnt(0xC07F);                                                                           \
+    }                                                                                                               \
+  } while (0)
+  const int whole = ragged < 0 ? nk : nk < 2 ? 0 : nk - 2;       // k-tiles in front of the last two
   const int rowW = m0 + wm * 128, colW = n0 + wn * 128;
   f32x4 bias[8];
 #pragma unroll
@@ -505,23 +567,28 @@ __global__ __launch_bounds__(256) void product_long_kernel(const ProductArgs g) 
   constexpr std::integral_constant<int, 2> s2{};
   constexpr std::integral_constant<int, 3> s3{};
 
+  SLP_CUT(0, SLP_VMCNT(12));
   SLP_BARRIER(SLP_VMCNT(12));
 #pragma unroll
   for (int f = 0; f < 5; ++f) read_b(0, f);
   read_a(0, 0);
   read_a(0, 1);
   strip(s0, 0, 1);
-  for (int kt = 0; kt < nk; ++kt) {
+  auto ktile = [&](int kt, auto last) {
     SLP_BARRIER(0xC07F);                                   // X: every LDS read so far has returned
     clip(kt + 2);
     if ((kt & 3) == 0) load_scales(kt / 4 + 1);
     SLP_FENCE();
     strip(s1, kt, kt + 2);
     strip(s2, kt, kt + 2);
+    if constexpr (last) SLP_CUT(kt + 1, SLP_VMCNT(8));
     SLP_BARRIER(SLP_VMCNT_LGKM0(8));                       // Y
     strip(s3, kt, kt + 2);
     strip(s0, kt + 1, kt + 2);                             // (of k-tile nk, too: all zeros)
-  }
+  };
+  int kt = 0;
+  for (; kt < whole; ++kt) ktile(kt, std::false_type{});
+  for (; kt < nk; ++kt) ktile(kt, std::true_type{});
 #undef SLP_MFMA
 #undef SLP_MFMA_ARGS
   } else {
@@ -552,13 +619,16 @@ __global__ __launch_bounds__(256) void product_long_kernel(const ProductArgs g) 
                  : [acc] "+a"(acc[i][j]) : SLP_MFMA_ARGS(kk, i, j, q), SLP_LOAD_ARGS(l, base, koff) : "memory", "scc", "m0");
   };
   // Sub-step KK of k-tile kt.  MFMA p: pair p / 2, 32 k p % 2.
-  auto substep = [&](auto kc, int kt) {
+  auto substep = [&](auto kc, int kt, auto last) {
     constexpr int KK = decltype(kc)::value;
     const int kn = KK ? kt + 1 : kt;               // k-tile of the next sub-step
     const uint32_t base0 = lds_wave + ((kt & 1) ^ 1) * STAGE, koff0 = koff_of(kt + 1), base1 = lds_wave + (kt & 1) * STAGE, koff1 = koff_of(kt + 2);
     static_for<128>([&](auto pc) {
       constexpr int p = decltype(pc)::value, i = row_of(p / 2), j = col_of(p / 2), q = p % 2, S = p / 32;
-      if constexpr (KK == 1 && p == 0) SLP_BARRIER(SLP_VMCNT_LGKM0(0));            // Z
+      if constexpr (KK == 1 && p == 0) {
+        if constexpr (last) SLP_CUT(kt + 1, SLP_VMCNT(0));
+        SLP_BARRIER(SLP_VMCNT_LGKM0(0));                                           // Z
+      }
       if constexpr (KK == 1 && p == 2) clip(kt + 2);
       if constexpr (KK == 1 && p == 72) SLP_BARRIER(0xC07F);                       // X
       // bytes: B's of the next sub-step, A's of the strip after the next (14 MFMAs ahead of the conversions)
@@ -587,6 +657,7 @@ __global__ __launch_bounds__(256) void product_long_kernel(const ProductArgs g) 
   constexpr std::integral_constant<int, 0> k0{};
   constexpr std::integral_constant<int, 1> k1{};
   static_for<7>([&](auto i) { load(i, lds_wave + STAGE, koff_of(1)); });
+  SLP_CUT(0, SLP_VMCNT(15));
   SLP_BARRIER(SLP_VMCNT(15));
   // what a sub-step finds: B's fragments but the last one's conversions, the first strip of A's, the bytes of the fragment behind each
   static_for<7>([&](auto f) {
@@ -601,12 +672,15 @@ __global__ __launch_bounds__(256) void product_long_kernel(const ProductArgs g) 
   });
   read_a(0, 0, 2);
   SLP_FENCE();
-  for (int kt = 0; kt < nk; ++kt) {
+  auto ktile = [&](int kt, auto last) {
     if ((kt & 3) == 0) load_scales(kt / 4 + 1);
     SLP_FENCE();
-    substep(k0, kt);
-    substep(k1, kt);
-  }
+    substep(k0, kt, last);
+    substep(k1, kt, last);
+  };
+  int kt = 0;
+  for (; kt < whole; ++kt) ktile(kt, std::false_type{});
+  for (; kt < nk; ++kt) ktile(kt, std::true_type{});
   }
   // the last zero fills have landed, and the matrix pipe is done with the accumulators (the compiler does not see MFMAs in assembly)
   __builtin_amdgcn_s_waitcnt(SLP_VMCNT_LGKM0(0));
@@ -615,6 +689,7 @@ __global__ __launch_bounds__(256) void product_long_kernel(const ProductArgs g) 
   for (int i = 0; i < 64; ++i) asm volatile("" : "+a"(acc[i / 8][i % 8]));
 #undef SLP_FENCE
 #undef SLP_BARRIER
+#undef SLP_CUT
 #undef SLP_LOAD_ARGS
 #undef SLP_MFMA
 #undef SLP_MFMA_ARGS
