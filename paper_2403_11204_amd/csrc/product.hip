@@ -13,7 +13,8 @@
 //     beside one of 65536 is lost, and at most 7 times 2^-13 of the largest product of each 8 is.  On normal values that is 1.4e-5 of the result's norm, 6e-5 on
 //     values spread over e^1.5, whatever the length, where rounding the output to bf16 costs 1.7e-3.  A register-only loop of it runs at 3700-4400 TFLOP/s.
 //   * float32 outputs (gradients of weights above all), bf16 ones whose caller asks for float32 sums, and products of few rows: the values are turned
-//     into bf16, scale and all, which is exact (4 of 8 bits are used), and
+//     into bf16, scale and all, which is exact between 2^-126 and 1.75 2^127 (4 of 8 bits are used; scales from 2^-117 to 2^119 keep every value there.  Above, a value
+//     becomes infinite, which 256 2^120 is in float32 as well; below, it loses bits and ends as zero under 2^-133), and
 //     v_mfma_f32_16x16x32_bf16 adds the exact products in float32: 1.7e-8 and 7e-8 on the same values, at 2100-2200 TFLOP/s.
 //
 // A lane feeds either form 32 bytes of one row, as two 16-byte pieces of the row's 128: both operands take the same two pieces, so which k an

@@ -56,3 +56,21 @@ def test_what_lies_past_a_long_contraction(m, n, k):
     ref = a64 @ b64.t().contiguous()
     assert torch.equal(api.product(a, b, dtype=api.F32).double(), ref)
     assert torch.equal(api.product(a, b, dtype=api.F32, out=torch.empty(m, n + 5, device=DEV)[:, 2:n + 2]).double(), ref)
+
+
+SHAPES = [(1, 40), (3, 5000), (30, 64), (40, 100), (300, 260), (1000, 1000), (4000, 4200)]
+
+
+@pytest.mark.parametrize("m,n", SHAPES)
+@pytest.mark.parametrize("ea,eb", [(246, 10), (10, 246), (227, 27), (27, 227), (127, 127)])
+def test_scales_far_apart(m, n, ea, eb):
+    """Values at 2^119 and 2^-117, between which both forms are exact: their products are integers."""
+    for k in (90, 400):
+        (a, a64), (b, b64) = integers(m, k, 1, m, 0x7F), integers(n, k, 128, n, 0x7F)
+        a64, b64 = a.q.float().double(), b.q.float().double()
+        a.scales.view(torch.uint8).fill_(ea)
+        b.scales.view(torch.uint8).fill_(eb)
+        ref = a64 @ b64.t().contiguous() * 2.0 ** (ea + eb - 254)
+        assert torch.equal(api.product(a, b, dtype=api.F32).double(), ref)
+        assert torch.equal(api.product(a, b).double(), ref.to(torch.bfloat16).double())
+        assert torch.equal(api.product(a, b, float32_sums=True).double(), ref.to(torch.bfloat16).double())
