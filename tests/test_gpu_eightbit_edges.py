@@ -74,3 +74,41 @@ def test_scales_far_apart(m, n, ea, eb):
         assert torch.equal(api.product(a, b, dtype=api.F32).double(), ref)
         assert torch.equal(api.product(a, b).double(), ref.to(torch.bfloat16).double())
         assert torch.equal(api.product(a, b, float32_sums=True).double(), ref.to(torch.bfloat16).double())
+
+
+@pytest.mark.parametrize("m,n", SHAPES)
+@pytest.mark.parametrize("k", [100, 400])
+def test_what_is_not_finite_stays_in_its_row_and_block_in_both_forms(m, n, k):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(m)
+    x, w = torch.randn(m, k, device=DEV, generator=g), torch.randn(n, k, device=DEV, generator=g)
+    x[m // 2, k - 1] = float("inf")
+    w[n - 1, 3] = float("nan")                   # a block of up to 128 rows of weights
+    x8, w8, first = api.quantize(x).rows, api.quantize(w, block=128).rows, (n - 1) // 128 * 128
+    for dtype, sums in ((api.F32, False), (api.BF16, False), (api.BF16, True)):
+        for relu in (False, True):
+            bad = api.product(x8, w8, dtype=dtype, float32_sums=sums, relu=relu).isnan()
+            assert bool(bad[m // 2].all()) and bool(bad[:, first:].all())
+            bad[m // 2] = False
+            assert not bool(bad[:, :first].any())
+
+
+@pytest.mark.parametrize("m,n,k", [(4000, 4200, 300), (4093, 4099, 277), (3111, 5003, 1291)])
+def test_large_ragged_products_into_a_wider_matrix(m, n, k):
+    (a, a64), (b, b64) = integers(m, k, 1, m, 0), integers(n, k, 128, n, 0)
+    bias = torch.arange(n, device=DEV).float() % 7 - 3
+    ref = (a64 @ b64.t().contiguous() + bias.double()).clamp(min=0)
+    for dtype in (torch.float32, torch.bfloat16):
+        room = torch.full((m + 2, n + 9), 7.0, dtype=dtype, device=DEV)
+        for first in (0, 1, 8):
+            api.product(a, b, bias=bias, relu=True, out=room[1:m + 1, first:first + n])
+            assert torch.equal(room[1:m + 1, first:first + n].double(), ref.to(dtype).double())
+            room[1:m + 1, first:first + n] = 7.0
+            assert bool((room == 7.0).all())
+
+
+def test_shapes_and_sums_of_empty_matrices():
+    for shape in ((0, 5), (5, 0), (0, 0)):
+        r = api.quantize(torch.empty(shape, device=DEV), transposed=True, column_sums=True)
+        assert tuple(r.rows.q.shape) == shape and tuple(r.transposed.q.shape) == shape[::-1]
+        assert r.column_sums.tolist() == [0.0] * shape[1]
