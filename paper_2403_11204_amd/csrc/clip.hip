@@ -90,12 +90,13 @@ __global__ __launch_bounds__(256) void norm_of_kernel(const double* __restrict__
   if (threadIdx.x == 0) *norm = (float)sqrt(x);
 }
 
+// The factor as m 2^e, m in [0.5, 1]: it may lie below float32's range where the values scaled by it do not.
 template <typename T>
-__device__ __forceinline__ void scaled(const T* in, T* out, int64_t count, int c, float by) {
+__device__ __forceinline__ void scaled(const T* in, T* out, int64_t count, int c, float m, int e) {
   each_eight(in, count, c, [&](int64_t k, int n, const Raw<T>& v) {
     float o[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = item(v, j) * by;
+    for (int j = 0; j < 8; ++j) o[j] = ldexpf(item(v, j) * m, e);
     store8(out + k, n, o);
   });
 }
@@ -104,11 +105,12 @@ __global__ __launch_bounds__(256) void scale_kernel(const ClipTable t, const dou
   const double x = sqrt(total(partials, n));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)x;
   const double ratio = (double)max_norm / (x + 1e-6);
-  const float by = x < INFINITY && ratio < 1.0 ? (float)ratio : 1.0f;
+  int e = 0;
+  const float m = x < INFINITY && ratio < 1.0 ? (float)frexp(ratio, &e) : 1.0f;
   each_chunk(t, [&](int i, int c) {
-    if (by == 1.0f && t.in[i] == t.out[i]) return;
-    if ((t.bf16 >> i) & 1) scaled((const bf16*)t.in[i], (bf16*)t.out[i], t.count[i], c, by);
-    else scaled((const float*)t.in[i], (float*)t.out[i], t.count[i], c, by);
+    if (m == 1.0f && e == 0 && t.in[i] == t.out[i]) return;
+    if ((t.bf16 >> i) & 1) scaled((const bf16*)t.in[i], (bf16*)t.out[i], t.count[i], c, m, e);
+    else scaled((const float*)t.in[i], (float*)t.out[i], t.count[i], c, m, e);
   });
 }
 
