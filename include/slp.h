@@ -346,7 +346,7 @@ int slp_rmsnorm_backward(const void* dy /*device*/, int64_t lddy, const void* h,
  * tensors[i] (device) holds counts[i] contiguous elements of dtype dts[i]; the three arrays are host memory and are not kept.
  * slp_gradient_norm: *norm_out = sqrt of the sum of all squares (float32; squares and sums are float64, in a fixed order).
  * slp_clip_gradients: out[i] = c tensors[i] with c = min(1, max_norm / (norm + 1e-6)); out[i] may be tensors[i] (out NULL: all of them), where c = 1 costs
- * nothing.  A norm that is not finite leaves the values as they are: look at *norm_out and skip the update.  norm_out may be NULL.
+ * nothing.  A norm that is not finite (in float32, as norm_out holds it) leaves the values as they are: look at *norm_out and skip the update.  norm_out may be NULL.
  * Workspace: 256-byte aligned.  Errors: SLP_ERR_ARG (null array or tensor, negative count, unknown dtype, max_norm not > 0), SLP_ERR_ALLOC, SLP_ERR_DEVICE. */
 size_t slp_gradient_norm_workspace_bytes(int n);
 int slp_gradient_norm(const void* const* tensors /*host*/, const int64_t* counts /*host*/, const int* dts /*host*/, int n, float* norm_out /*device*/,

@@ -4,7 +4,7 @@
 //
 // Squares and their sums are float64, in which no float32 value's square overflows or underflows; every workgroup adds up its own elements
 // in a fixed order and stores one partial sum, and whoever needs the total adds up all partial sums in the same order: no atomics, the same
-// bits every time.  A norm that is not finite leaves the gradients as they are (c = 1): it is the caller's to see and to skip the update.
+// bits every time.  A norm that is not finite in float32, as the caller sees it, leaves the gradients as they are (c = 1): it is the caller's to skip the update.
 #include "eightbit_device.h"
 
 namespace slp {
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(256) void scale_kernel(const ClipTable t, const dou
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)x;
   const double ratio = (double)max_norm / (x + 1e-6);
   int e = 0;
-  const float m = x < INFINITY && ratio < 1.0 ? (float)frexp(ratio, &e) : 1.0f;
+  const float m = (float)x < INFINITY && ratio < 1.0 ? (float)frexp(ratio, &e) : 1.0f;
   each_chunk(t, [&](int i, int c) {
     if (m == 1.0f && e == 0 && t.in[i] == t.out[i]) return;
     if ((t.bf16 >> i) & 1) scaled((const bf16*)t.in[i], (bf16*)t.out[i], t.count[i], c, m, e);

@@ -29,3 +29,17 @@ def test_a_factor_below_the_range_of_float32(values, max_norm, dtype):
     assert np.all(np.abs(f64(out[0]) - ref) <= (3 * U + (2.0 ** -8 if dtype is torch.bfloat16 else 0)) * np.abs(ref) + 2.0 ** (-149 if dtype is torch.float32 else -133)), (f64(out[0]), ref)
     api.clip_gradients([t], max_norm)
     assert torch.equal(t, out[0])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_norm_that_float32_does_not_hold_leaves_the_values(dtype):
+    """What the caller is given is infinite: that the step is to be skipped, and that nothing has been scaled."""
+    t = [torch.tensor([3e38, -3e38, 5.0]).to(dtype).to(DEV), torch.arange(7.0).to(dtype).to(DEV)]
+    before, out = [x.clone() for x in t], [torch.empty_like(x) for x in t]
+    assert float(api.gradient_norm(t)) == float("inf") == float(api.clip_gradients(t, 1.0, out=out))
+    assert all(torch.equal(a, b) for a, b in zip(out, before))
+    assert float(api.clip_gradients(t, 1.0)) == float("inf") and all(torch.equal(a, b) for a, b in zip(t, before))
+    # the largest norm that it holds
+    big = torch.tensor([3.4e38], device=DEV)
+    norm = float(api.clip_gradients([big], 2.0))
+    assert np.isfinite(norm) and abs(float(big) - 2.0) <= 4 * U * 2.0
