@@ -331,7 +331,7 @@ int slp_product(const void* a /*device*/, int64_t lda, const void* a_scales, int
  *   h = x + residual (added in float32, rounded to dt; h = x where residual is NULL);  n = 1 / sqrt(mean over the row of h^2 + eps);  y = h n gamma
  * x, residual, h, y: [rows][dim] of dtype dt; gamma float32 [dim], NULL for ones; rstd float32 [rows] receives n.  h must be given where
  * residual is, and may be x or residual; y, rstd and the 8-bit output (q and scales together, block 1) may be NULL.  The norm and the 8-bit values
- * are of h as stored. */
+ * are of h as stored.  The squares are float32: a row that holds a value beyond 1.8e19 has an infinite mean, n = 0; with eps = 0 a row of zeros, or below 1e-23, has n infinite. */
 int slp_rmsnorm(const void* x /*device*/, int64_t ldx, const void* residual /*device, may be NULL*/, int64_t ldr, const float* gamma, float eps, int dt,
                 int rows, int dim, void* h, int64_t ldh, void* y, int64_t ldy, void* q, int64_t ldq, void* scales, int64_t lds, float* rstd, slp_stream stream);
 

@@ -4,7 +4,8 @@
 //   h = x + r (rounded to the type: the norm is of what is stored);  n = 1 / sqrt(mean(h^2) + eps);  y = h n gamma
 //   dx_j = dh_j + n (gamma_j dy_j - h_j n^2 mean(gamma dy h));  dgamma_j = sum over the rows of dy_j h_j n
 //
-// Sums and everything between the loads and the stores are float32.
+// Sums and everything between the loads and the stores are float32.  The backward pass takes h as h n, which is of the size of one, in every product: dy h, n^2 and n^3 may
+// leave float32's range where dx and dgamma do not.
 #include "eightbit_device.h"
 
 namespace slp {
@@ -195,9 +196,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_backwar
     for (int i = 0; i < CH; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float yx = item(y[i], j) * item(x[i], j);
-        dot += g[i][j] * yx;
-        acc[i][j] += yx * n;
+        const float xn = item(x[i], j) * n;
+        dot += g[i][j] * item(y[i], j) * xn;
+        acc[i][j] += item(y[i], j) * xn;
       }
     Raw<T> y2[CH], x2[CH], d2[CH];
     if (AHEAD && row + step < a.rows) fetch(row + step, y2, x2, d2);
@@ -209,14 +210,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_backwar
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) dot += part[turn][w];
     }
-    const float k = dot * over * n * n * n;          // (in this order nothing leaves the range that the result stays in)
+    const float k = dot * over;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const int c = 8 * (i * TEAM + t);
       float o[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        o[j] = n * (g[i][j] * item(y[i], j)) - item(x[i], j) * k;
+        o[j] = n * (g[i][j] * item(y[i], j) - item(x[i], j) * n * k);
         if (a.dh) o[j] += item(d[i], j);
       }
       store8((T*)a.dx + row * a.lddx + c, D - c, o);
@@ -258,6 +259,7 @@ __global__ __launch_bounds__(256) void rmsnorm_dots_kernel(const NormBackArgs a,
   __shared__ float part[4];
   const int64_t row = blockIdx.x;
   const T *dy = (const T*)a.dy + row * a.lddy, *h = (const T*)a.h + row * a.ldh;
+  const float n = a.rstd[row];
   float dot = 0.0f;
   for (int c = threadIdx.x; 8 * c < a.dim; c += 256) {
     float y[8], x[8], g[8];
@@ -265,15 +267,12 @@ __global__ __launch_bounds__(256) void rmsnorm_dots_kernel(const NormBackArgs a,
     load8(h + 8 * c, a.dim - 8 * c, x);
     if (a.gamma) load8(a.gamma + 8 * c, a.dim - 8 * c, g);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) dot += (a.gamma ? g[j] : 1.0f) * y[j] * x[j];
+    for (int j = 0; j < 8; ++j) dot += (a.gamma ? g[j] : 1.0f) * y[j] * (x[j] * n);
   }
   dot = sum_of_64(dot);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = dot;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    const float n = a.rstd[row];
-    dots[row] = n * n * ((part[0] + part[1]) + (part[2] + part[3])) / (float)a.dim;
-  }
+  if (threadIdx.x == 0) dots[row] = ((part[0] + part[1]) + (part[2] + part[3])) / (float)a.dim;
 }
 
 template <typename T>
@@ -297,8 +296,8 @@ __global__ __launch_bounds__(256) void rmsnorm_columns_kernel(const NormBackArgs
     if (a.dh) load8((const T*)a.dh + row * a.lddh + c, left, d);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      acc[j] += y[j] * x[j] * n;
-      d[j] += n * (g[j] * y[j] - x[j] * k);
+      acc[j] += y[j] * (x[j] * n);
+      d[j] += n * (g[j] * y[j] - x[j] * n * k);
     }
     store8((T*)a.dx + row * a.lddx + c, left, d);
   }
