@@ -192,6 +192,8 @@ def mean_loss(losses, out=None):
 Quantized = collections.namedtuple("Quantized", "q scales block")
 QuantizeResult = collections.namedtuple("QuantizeResult", "rows transposed column_sums")
 NormResult = collections.namedtuple("NormResult", "h rstd y y8")
+# Outputs of a call that come to 256 KB at most are parts of one allocation: one that is kept keeps all of them, and torch.save writes
+# all of them.  clone() what is to stand alone.
 
 
 _native = None

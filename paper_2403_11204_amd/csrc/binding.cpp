@@ -87,10 +87,11 @@ class On {
 };
 
 // Room for a call's outputs and workspace.  Each allocation takes the host 0.6 us: where all of them come to 256 KB at most (a request's
-// rows: the device is done before the host) they are parts of one, on 256-byte boundaries.
+// rows: the device is done before the host) they are parts of one, on 256-byte boundaries.  A workspace only up to 4 KB: whatever output is kept keeps the block.
 class Room {
  public:
-  Room(const at::Device& device, size_t all) : device_(device) {
+  Room(const at::Device& device, size_t outputs, size_t workspace) : device_(device), apart_(workspace > 4096) {
+    const size_t all = outputs + (apart_ ? 0 : padded(workspace));
     if (all <= (256u << 10)) block_ = at::empty({(int64_t)all}, at::TensorOptions().dtype(at::kByte).device(device));
   }
   static size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
@@ -104,10 +105,14 @@ class Room {
     require(used_ <= block_.nbytes(), "room counted too small");
     return t;
   }
-  at::Tensor bytes(size_t n) { return n ? take({(int64_t)n}, at::kByte) : at::Tensor(); }
+  at::Tensor work(size_t n) {
+    if (!n) return at::Tensor();
+    return apart_ ? at::empty({(int64_t)n}, at::TensorOptions().dtype(at::kByte).device(device_)) : take({(int64_t)n}, at::kByte);
+  }
 
  private:
   at::Device device_;
+  bool apart_;
   at::Tensor block_;
   size_t used_ = 0;
 };
@@ -191,13 +196,13 @@ PyObject* quantize(PyObject* const* a) {
   const bool rows = truth(a[2]), transposed = truth(a[3]), column_sums = truth(a[5]);
   const size_t size = column_sums ? slp_quantize_workspace_bytes(side(m), side(n)) : 0;
   const On on(x.device());
-  Room room(x.device(), (rows ? eight_bytes(m, n, block) : 0) + (transposed ? eight_bytes(n, m, block) : 0) + (column_sums ? Room::padded(4 * n) : 0) + Room::padded(size));
+  Room room(x.device(), (rows ? eight_bytes(m, n, block) : 0) + (transposed ? eight_bytes(n, m, block) : 0) + (column_sums ? Room::padded(4 * n) : 0), size);
   Eight r, t;
   if (rows) r = eight_room(m, n, block, room);
   if (transposed) t = eight_room(n, m, block, room);
   at::Tensor sums;
   if (column_sums) sums = room.take({n}, at::kFloat);
-  const at::Tensor work = room.bytes(size);
+  const at::Tensor work = room.work(size);
   const int rc = slp_quantize(x.data_ptr(), ldx, mask, ldmask, dt, side(m), side(n), (int)block, r.at, r.ld, r.scales_at, r.lds, t.at, t.ld, t.scales_at, t.lds,
                               (float*)address(sums), address(work), size, on.stream());
   return rc ? code(rc) : tuple({r.q, r.scales, t.q, t.scales, sums});
@@ -215,7 +220,7 @@ PyObject* product(PyObject* const* a) {
   int dt = (int)integer(a[8]);
   int64_t ldo = n;
   const On on(x.q.device());
-  Room room(x.q.device(), Room::padded(size) + (given(a[9]) ? 0 : Room::padded((size_t)(m * n) * (dt == SLP_BF16 ? 2 : 4))));
+  Room room(x.q.device(), given(a[9]) ? 0 : Room::padded((size_t)(m * n) * (dt == SLP_BF16 ? 2 : 4)), size);
   if (given(a[9])) {
     out = tensor(a[9]);
     require(out.dim() == 2 && out.size(0) == m && out.size(1) == n && out.device() == x.q.device(), "an output of the product's shape is wanted");
@@ -224,7 +229,7 @@ PyObject* product(PyObject* const* a) {
   } else {
     out = room.take({m, n}, dt == SLP_BF16 ? at::kBFloat16 : at::kFloat);
   }
-  const at::Tensor work = room.bytes(size);
+  const at::Tensor work = room.work(size);
   const int rc = slp_product(x.at, x.ld, x.scales_at, x.lds, (int)ablock, y.at, y.ld, y.scales_at, y.lds, (int)bblock, vector(a[6], n, x.q), truth(a[7]), side(m), side(n),
                              side(cols), out.data_ptr(), ldo, truth(a[10]) ? dt | SLP_FLOAT32_SUMS : dt, address(work), size, on.stream());
   if (rc) return code(rc);
@@ -240,7 +245,7 @@ PyObject* rmsnorm(PyObject* const* a) {
   const bool normed = truth(a[4]), quantized = truth(a[5]);
   const size_t matrix = Room::padded((size_t)(m * n) * (dt == SLP_BF16 ? 2 : 4));
   const On on(x.device());
-  Room room(x.device(), (given(a[2]) ? matrix : 0) + (normed ? matrix : 0) + (quantized ? eight_bytes(m, n, 1) : 0) + Room::padded(4 * m));
+  Room room(x.device(), (given(a[2]) ? matrix : 0) + (normed ? matrix : 0) + (quantized ? eight_bytes(m, n, 1) : 0) + Room::padded(4 * m), 0);
   at::Tensor h = x, y;
   const void* r = nullptr;
   void* to = nullptr;
@@ -275,11 +280,11 @@ PyObject* rmsnorm_backward(PyObject* const* a) {
   const float *gamma = vector(a[2], n, h), *rstd = vector(a[3], m, h);
   const size_t size = slp_rmsnorm_backward_workspace_bytes(side(m), side(n));
   const On on(h.device());
-  Room room(h.device(), Room::padded((size_t)(m * n) * (dt == SLP_BF16 ? 2 : 4)) + Room::padded(4 * n) + Room::padded(size));
+  Room room(h.device(), Room::padded((size_t)(m * n) * (dt == SLP_BF16 ? 2 : 4)) + Room::padded(4 * n), size);
   const at::Tensor dx = room.take({m, n}, h.scalar_type());
   at::Tensor dgamma;
   if (truth(a[5])) dgamma = room.take({n}, at::kFloat);
-  const at::Tensor work = room.bytes(size);
+  const at::Tensor work = room.work(size);
   const int rc = slp_rmsnorm_backward(dy.data_ptr(), lddy, h.data_ptr(), ldh, gamma, rstd, dh, lddh, dt, side(m), side(n), dx.data_ptr(), n, (float*)address(dgamma),
                                       address(work), size, on.stream());
   return rc ? code(rc) : tuple({dx, dgamma});
@@ -321,8 +326,8 @@ PyObject* gradient_norm(PyObject* const* a) {
   const int n = (int)in.at.size();
   const size_t size = slp_gradient_norm_workspace_bytes(n);
   const On on(in.device);
-  Room room(in.device, Room::padded(4) + Room::padded(size));
-  const at::Tensor norm = room.take({}, at::kFloat), work = room.bytes(size);
+  Room room(in.device, Room::padded(4), size);
+  const at::Tensor norm = room.take({}, at::kFloat), work = room.work(size);
   const int rc = slp_gradient_norm(in.at.data(), in.counts.data(), in.dts.data(), n, (float*)norm.data_ptr(), address(work), size, on.stream());
   if (rc) return code(rc);
   return wrapped(norm);
@@ -336,8 +341,8 @@ PyObject* clip_gradients(PyObject* const* a) {
   if (given(a[2])) out = tensors(a[2], &in);
   const size_t size = slp_gradient_norm_workspace_bytes(n);
   const On on(in.device);
-  Room room(in.device, Room::padded(4) + Room::padded(size));
-  const at::Tensor norm = room.take({}, at::kFloat), work = room.bytes(size);
+  Room room(in.device, Room::padded(4), size);
+  const at::Tensor norm = room.take({}, at::kFloat), work = room.work(size);
   const int rc = slp_clip_gradients(in.at.data(), given(a[2]) ? out.at.data() : nullptr, in.counts.data(), in.dts.data(), n, (float)number(a[1]), (float*)norm.data_ptr(),
                                     address(work), size, on.stream());
   if (rc) return code(rc);

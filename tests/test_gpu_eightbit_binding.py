@@ -76,3 +76,11 @@ def test_tensors_on_a_device_that_is_not_the_current_one():
         assert all(torch.equal(a.cpu(), b) for a, b in zip(got, ref))
     big = [api.quantize(torch.randn(4096, 512, device="cuda:1")).rows for _ in range(2)]      # kernels that take more than the usual LDS
     assert api.product(*big).device.index == 1 and api.product(*big, dtype=api.F32).device.index == 1
+
+
+@pytest.mark.parametrize("n", [1, 48, 49, 1000])
+def test_a_kept_norm_holds_no_large_workspace(n):
+    t = [torch.ones(1 + i % 5, device=DEV) for i in range(n)]
+    norms = [api.gradient_norm(t), api.clip_gradients(t, 1e9)]
+    assert all(abs(float(x) - sum(y.numel() for y in t) ** 0.5) < 1e-3 for x in norms)
+    assert all(x.untyped_storage().nbytes() <= 4096 + 256 for x in norms)
