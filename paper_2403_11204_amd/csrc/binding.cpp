@@ -159,8 +159,9 @@ Eight eight_given(PyObject* q, PyObject* scales, int64_t block, int64_t cols) {
   require((e.q.stride(1) == 1 || cols <= 1) && (e.scales.stride(1) == 1 || cols <= 128), "rows must be contiguous");
   e.at = e.q.data_ptr();
   e.scales_at = e.scales.data_ptr();
-  e.ld = e.q.stride(0);
-  e.lds = e.scales.stride(0);
+  // (a single row may have any stride; what it is read with beyond its end lies in the same 16 or 4 bytes)
+  e.ld = e.q.size(0) <= 1 ? (cols + 15) / 16 * 16 : e.q.stride(0);
+  e.lds = e.scales.size(0) <= 1 ? ((cols + 127) / 128 + 3) / 4 * 4 : e.scales.stride(0);
   return e;
 }
 

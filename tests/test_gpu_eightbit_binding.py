@@ -84,3 +84,19 @@ def test_a_kept_norm_holds_no_large_workspace(n):
     norms = [api.gradient_norm(t), api.clip_gradients(t, 1e9)]
     assert all(abs(float(x) - sum(y.numel() for y in t) ** 0.5) < 1e-3 for x in norms)
     assert all(x.untyped_storage().nbytes() <= 4096 + 256 for x in norms)
+
+
+@pytest.mark.parametrize("k", [100, 128, 300, 1024])
+def test_a_single_row_of_any_stride(k):
+    """One row of values, one row of scales: whatever stride torch has for them means nothing."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(k)
+    x, w = torch.randn(1, k, device=DEV, generator=g), torch.randn(90, k, device=DEV, generator=g)
+    x8, w8 = api.quantize(x).rows, api.quantize(w, block=128).rows
+    ref = api.product(x8, w8, dtype=api.F32)
+    q = x8.q.view(torch.uint8).contiguous().view(k, 1).t().view(torch.float8_e4m3fn)
+    s = x8.scales.view(torch.uint8).contiguous().view(-1, 1).t().view(torch.float8_e8m0fnu)
+    assert q.shape == (1, k) and q.stride(0) == 1 and s.stride(0) == 1
+    ws = w8.scales.view(torch.uint8).clone().view(-1, 1).t().view(torch.float8_e8m0fnu)      # one block of 90 rows
+    assert torch.equal(api.product(api.Quantized(q, s, 1), api.Quantized(w8.q, ws, 128), dtype=api.F32), ref)
+    assert torch.equal(api.product(api.Quantized(w8.q, ws, 128), api.Quantized(q, s, 1), dtype=api.F32), api.product(w8, x8, dtype=api.F32))
