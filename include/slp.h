@@ -297,7 +297,7 @@ int slp_count_correct_static(const void* logits /*device*/, const int32_t* targe
  * that holds an infinity or a NaN gets the scale 255, so that whatever is computed from it is NaN.
  * Rows that are not a multiple of 4096 bytes apart are read faster (fewer of them share a memory channel).
  * The calls take the leading dimensions of every matrix in elements, 64 bits wide; float32 and bf16 matrices may start at any element.  An
- * empty matrix (0 rows) is a call without effect.  Common errors: SLP_ERR_ARG (null pointer, negative size, unknown dtype or block),
+ * empty matrix (0 rows) is a call without effect but for sums over its rows, which become zeros.  Common errors: SLP_ERR_ARG (null pointer, negative size, unknown dtype or block),
  * SLP_ERR_SHAPE (a leading dimension below the row, rows or columns above 2^24, more than 2^34 elements, an 8-bit row above 2^22 bytes), SLP_ERR_ALLOC (alignment, workspace),
  * SLP_ERR_DEVICE. */
 

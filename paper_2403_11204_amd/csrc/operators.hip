@@ -126,6 +126,7 @@ int slp_quantize(const void* x, int64_t ldx, const void* mask, int64_t ldmask, i
   if (!known(dt)) return fail(SLP_ERR_ARG, "%s: unknown dtype %d", who, dt);
   if (block != 1 && block != kScaleBlock) return fail(SLP_ERR_ARG, "%s: blocks of 1 or %d rows (got %d)", who, kScaleBlock, block);
   SLP_CHECK(check_sides(who, rows, cols));
+  if (off(column_sums, 4)) return fail(SLP_ERR_ALLOC, "%s: the sums are not on an element's boundary", who);
   if (rows == 0 && cols > 0 && column_sums) {       // sums of nothing
     HIP_TRY(launch_sum_rows(nullptr, 0, cols, column_sums, (hipStream_t)stream));
     return SLP_OK;
@@ -137,10 +138,7 @@ int slp_quantize(const void* x, int64_t ldx, const void* mask, int64_t ldmask, i
   if (!x) return fail(SLP_ERR_ARG, "%s: null pointer", who);
   SLP_CHECK(check_dense(who, "x", x, ldx, cols, dt));
   if (mask) SLP_CHECK(check_dense(who, "mask", mask, ldmask, cols, dt));
-  if (column_sums) {
-    if (off(column_sums, 4)) return fail(SLP_ERR_ALLOC, "%s: the sums are not on an element's boundary", who);
-    SLP_CHECK(check_work(who, workspace, workspace_bytes, slp_quantize_workspace_bytes(rows, cols)));
-  }
+  if (column_sums) SLP_CHECK(check_work(who, workspace, workspace_bytes, slp_quantize_workspace_bytes(rows, cols)));
   const QuantizeArgs a{x, mask, (uint8_t*)q, (uint8_t*)scales, (uint8_t*)qt, (uint8_t*)scales_t, column_sums, (float*)workspace, ldx, ldmask, ldq, lds,
                        ldqt, ldst, rows, cols, block};
   HIP_TRY(launch_quantize(dt, a, (hipStream_t)stream));
