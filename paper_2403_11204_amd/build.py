@@ -101,9 +101,8 @@ def build(verbose=True):
     with ThreadPoolExecutor(max_workers=4) as ex:
         binding = ex.submit(_compile_binding, verbose)
         objs = list(ex.map(lambda kv: _compile(kv[0], kv[1], verbose), UNITS.items()))
-        binding = binding.result()
     _run([hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", OUT] + objs, "linking libslp.so", verbose)
-    _link_binding(binding, verbose)
+    _link_binding(binding.result(), verbose)         # (the library stands without it)
     return OUT
 
 
