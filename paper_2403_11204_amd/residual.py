@@ -5,8 +5,9 @@ weight matrices and every gradient that enters a product are 8-bit matrices (api
 blocks and the outputs of products are bf16, weights and their gradients float32.  Gradients are clipped together by
 their norm before the update, which is torch's SGD on the float32 weights.
 
-The class has the calls of api.Segment that pipeline.py makes of a left partition, so it can be trained through a frozen
-right one (Sec. 5 of the paper, pipeline.recovery_epochs) and joined with it (pipeline.joined_forward, pipeline.accuracy):
+Of api.Segment's calls the class has forward and step_external, so it can be trained through a frozen right partition (Sec. 5
+of the paper, pipeline.recovery_epochs), joined with it (pipeline.joined_forward, pipeline.accuracy) and its response stored
+(pipeline.store_response).  It has no step against labels, which pipeline.train_epochs, train_partitioned and train_simultaneous call:
 
     left = ResidualSegment(width=512, hidden=2048, blocks=2)
     right = api.Segment([512, 1024, 47], api.RELU_HIDDEN_IDENTITY_LAST, api.SOFTMAX_XENT, max_batch=256, dtype=api.BF16, input_grad=True)
