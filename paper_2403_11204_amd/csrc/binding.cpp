@@ -6,6 +6,7 @@
 
 #include <ATen/Functions.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -75,15 +76,20 @@ const float* vector(PyObject* o, int64_t n, const at::Tensor& x) {
   return (const float*)t.data_ptr();
 }
 
-// The tensors' device, current as long as this lives, and torch's current stream of it.
+// The tensors' device, current as long as this lives, and torch's current stream of it.  (A guard, and what a stream asks to find its handle, take the host
+// half a microsecond each: not where the device is the current one already, the stream the default one, whose handle is null.)
 class On {
  public:
-  explicit On(const at::Device& device) : guard_(device), stream_(c10::hip::getCurrentHIPStream(device.index()).stream()) {}
+  explicit On(const at::Device& device) {
+    if (c10::hip::current_device() != device.index()) guard_.reset_device(device);
+    const c10::hip::HIPStream s = c10::hip::getCurrentHIPStream(device.index());
+    stream_ = s == c10::hip::getDefaultHIPStream(device.index()) ? nullptr : s.stream();
+  }
   slp_stream stream() const { return stream_; }
 
  private:
-  c10::DeviceGuard guard_;
-  slp_stream stream_;
+  c10::OptionalDeviceGuard guard_;
+  slp_stream stream_ = nullptr;
 };
 
 // Room for a call's outputs and workspace.  Each allocation takes the host 0.6 us: where all of them come to 256 KB at most (a request's
@@ -294,25 +300,27 @@ PyObject* rmsnorm_backward(PyObject* const* a) {
 // Several tensors as the library takes them.  They are held until the call is queued: what an iterator makes has no other owner, and its memory would be
 // given to the outputs and the workspace.
 struct Tensors {
-  std::vector<at::Tensor> held;
+  THPObjectPtr held;
   std::vector<void*> at;
   std::vector<int64_t> counts;
   std::vector<int> dts;
   at::Device device = at::kCPU;
 };
 Tensors tensors(PyObject* list, const Tensors* as) {
-  THPObjectPtr fast(PySequence_Fast(list, "a list of tensors is wanted"));
-  if (!fast) throw python_error();
-  const Py_ssize_t n = PySequence_Fast_GET_SIZE(fast.get());
+  Tensors all;
+  all.held = THPObjectPtr(PySequence_Tuple(list));
+  if (!all.held) throw python_error();
+  const Py_ssize_t n = PyTuple_GET_SIZE(all.held.get());
   require(n > 0, "at least one tensor is wanted");
   require(!as || as->at.size() == (size_t)n, "as many outputs as tensors are wanted");
-  Tensors all;
+  all.at.reserve((size_t)n);
+  all.counts.reserve((size_t)n);
+  all.dts.reserve((size_t)n);
   for (Py_ssize_t i = 0; i < n; ++i) {
-    const at::Tensor& t = tensor(PySequence_Fast_GET_ITEM(fast.get(), i));
+    const at::Tensor& t = tensor(PyTuple_GET_ITEM(all.held.get(), i));
     require(t.is_cuda() && t.is_contiguous(), "contiguous tensors on the device are wanted");
     if (i == 0) all.device = t.device();
     require(t.device() == all.device, "tensors on one device are wanted");
-    all.held.push_back(t);
     all.at.push_back(t.data_ptr());
     all.counts.push_back(t.numel());
     all.dts.push_back(dtype_of(t));
