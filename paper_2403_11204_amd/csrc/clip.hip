@@ -29,7 +29,8 @@ __device__ __forceinline__ double total(const double* __restrict__ partials, int
 
 // f(tensor, its chunk) for each chunk of this workgroup.  Chunks are dealt out in turns, to one workgroup for each compute unit, so that all of
 // them read and write within 8 MB at a time: 549 million float32 values, norm / clipping 334 / 1141 us (6.5 TB/s / 5.8 for 6.6 GB) against 349 / 1172
-// with two workgroups each and 375 / 1201 with four; 455 / 1357 with chunks of 16 KB, 355 / 1187 with 64 KB.
+// with two workgroups each and 375 / 1201 with four; 455 / 1357 with chunks of 16 KB, 355 / 1187 with 64 KB.  These are repeated calls; behind other work the squares take 371, between
+// two clippings 386 (5.7 TB/s).
 template <typename F>
 __device__ __forceinline__ void each_chunk(const ClipTable& t, F f) {
   int i = 0;

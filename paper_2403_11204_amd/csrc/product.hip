@@ -130,7 +130,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, int64_t
 
 // BM x BN tile, 4 wavefronts in a 2 x 2 grid, NS LDS stages of a k-tile of 128 each, one barrier a k-tile.  NG such groups of wavefronts
 // take a part of the contraction each (kper k-tiles) and are added up in order at the end.  blockIdx.y: part of the contraction of a whole workgroup;
-// several parts leave float32 partial products for join_kernel.  1000 x 3001 x 1500, 752 tiles of 64x64: bf16 11.2 us, float32 16.2 (560 TFLOP/s): operands
+// several parts leave float32 partial products for join_kernel.  1000 x 3001 x 1500, 752 tiles of 64x64: bf16 11.7 us, float32 17.2 (520 TFLOP/s; contractions of 1504 16.1): operands
 // into LDS 5.6 us of it, conversions and matrix instructions 4.5 each, 2.5 the launch.  1024 x 4096 x 4096 on 128x64: bf16 24.8 (1.39 PFLOP/s), float32 40.3.
 template <int BM, int BN, int NS, int NG, bool EXACT>
 __global__ __launch_bounds__(256 * NG) void product_tile_kernel(const ProductArgs g, int kper) {

@@ -94,8 +94,9 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs a
 // Everything else, a 128 x 128 tile a workgroup of 8 wavefronts: a thread holds 4 rows of 8 columns.  The transposed bytes go through LDS, a row
 // of 128 bytes for each column of the tile; the 16-byte piece p of column c sits at p ^ (c / 8 mod 8), so that the lanes of a wavefront, which
 // write 16 columns 8 apart, spread over the banks.  8 wavefronts: with 4, which hold twice as much each, a 4096 x 8192 bf16 gradient took 73 us, not 57.
-// Bound by memory where there are many tiles, to both layouts: 8192 x 8192 float32 76 us (405 MB, 5.3 TB/s) with either kind of blocks, 4096 x 8192 bf16
-// with a mask and sums 39 us (203 MB, 5.2 TB/s); by the steps of one tile, 1.5 us behind the 2.5 of an empty launch, where there are few.
+// Bound by memory where there are many tiles, to both layouts: 8192 x 8192 float32 75 us (405 MB, 5.4 TB/s) with either kind of blocks.  4096 x 8192 bf16
+// with a mask and sums (203 MB) takes 33 us in repeated calls, whose inputs the last cache holds, but 47 to 56 behind other work (3.6 to 4.3 TB/s): a workgroup loads, exchanges
+// and stores its one tile in turns.  By the steps of one tile, 1.5 us behind the 2.5 of an empty launch, where there are few.
 template <typename T, int BLOCK>
 __global__ __launch_bounds__(512) void quantize_tile_kernel(const QuantizeArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t turned[128 * 128];
