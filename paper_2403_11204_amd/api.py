@@ -3,7 +3,8 @@
 Every function here packs its arguments, calls the library entry point of the
 same name and raises ``SlpError`` on a non-zero status.  Tensors are torch CUDA
 tensors used as raw device memory; the stream passed to the library is torch's
-current stream, so ordinary torch stream semantics apply.
+current stream, so ordinary torch stream semantics apply.  It is the current
+device's; the operators in 8 bits and clipping take that of their tensors' device.
 """
 
 import collections
