@@ -85,6 +85,9 @@ def lib():
         "slp_rmsnorm_backward": (i32, [vp, i64, vp, i64, vp, vp, vp, i64, i32, i32, i32, vp, i64, vp, vp, sz, vp]),
         "slp_gradient_norm_workspace_bytes": (sz, [i32]),
         "slp_gradient_norm": (i32, [ctypes.POINTER(vp), ctypes.POINTER(i64), ctypes.POINTER(i32), i32, vp, vp, sz, vp]),
+        "slp_linear_loss_workspace_bytes": (sz, [vp, i64, vp, i64, i32, i32, i32, i32, i32, i32]),
+        "slp_linear_cross_entropy": (i32, [vp, i64, vp, i64, vp, i32, i32, i32, i32, vp, i32, f32, vp, vp, vp, vp, i64, vp, i64, i32, vp, vp, sz, vp]),
+        "slp_linear_distillation": (i32, [vp, i64, vp, i64, vp, i32, i32, i32, i32, vp, i64, i32, vp, i64, i32, i32, f32, f32, vp, vp, vp, vp, i64, vp, i64, i32, vp, vp, sz, vp]),
         "slp_clip_gradients": (i32, [ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.POINTER(i64), ctypes.POINTER(i32), i32, f32, vp, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
@@ -104,7 +107,8 @@ EXPORTS = ["slp_last_error", "slp_make_synthetic_labels", "slp_make_segment_inpu
            "slp_count_correct_static", "slp_segment_set_fused_update", "slp_segment_target_errors",
            "slp_segment_graph_stats", "slp_quantize_workspace_bytes", "slp_quantize", "slp_product_workspace_bytes",
            "slp_product", "slp_rmsnorm", "slp_rmsnorm_backward_workspace_bytes", "slp_rmsnorm_backward",
-           "slp_gradient_norm_workspace_bytes", "slp_gradient_norm", "slp_clip_gradients"]
+           "slp_gradient_norm_workspace_bytes", "slp_gradient_norm", "slp_clip_gradients", "slp_linear_loss_workspace_bytes", "slp_linear_cross_entropy",
+           "slp_linear_distillation"]
 
 
 def _check(code):
@@ -265,6 +269,24 @@ def clip_gradients(tensors, max_norm, out=None):
     """slp_clip_gradients: scales the tensors together to a norm of at most max_norm, in place or into `out` (tensors of the same
     sizes and types).  Returns the norm before, a device scalar; where it is not finite the values are left as they are."""
     return _outputs(_binding().clip_gradients(tensors, max_norm, out))
+
+
+# ---- a last layer over many classes -----------------------------------------------------------------------------
+LossResult = collections.namedtuple("LossResult", "loss losses lse dx dw dbias")
+
+
+def linear_cross_entropy(x, w, targets, bias=None, gradients=True, weight_gradients=True, scale=1.0, dtype=None):
+    """slp_linear_cross_entropy: the softmax cross-entropy of logits x w^T + bias, which are never kept as a whole, against a class id a row (int32 or
+    int64; one outside [0, classes) leaves its row out).  loss: the mean over the rows that count, a device scalar; losses and lse (log-sum-exp): each
+    row's; with `gradients` dx, with `weight_gradients` as well dw (of `dtype`, w's own by default) and, where there is a bias, dbias: those of scale * loss."""
+    return LossResult(*_outputs(_binding().linear_cross_entropy(x, w, targets, bias, gradients, weight_gradients, scale, dtype)))
+
+
+def linear_distillation(x, w, top, classes, bias=None, temperature=1.0, gradients=True, weight_gradients=True, scale=1.0, dtype=None):
+    """slp_linear_distillation: the same from a teacher's logits `top` [rows, k] of the classes named beside them (as torch.topk gives them; an id outside
+    [0, classes) or a logit of -inf leaves its entry out, a row without entries counts as nothing): temperature^2 KL(softmax(top / temperature) ||
+    softmax((x w^T + bias) / temperature)).  lse is that of the logits over the temperature."""
+    return LossResult(*_outputs(_binding().linear_distillation(x, w, top, classes, bias, temperature, gradients, weight_gradients, scale, dtype)))
 
 
 class Segment:

@@ -42,6 +42,9 @@ UNITS = {
     "quantize.hip": [],
     "product.hip": [],
     "clip.hip": [],
+    "losses.hip": [],
+    "class_loss.hip": [],
+    "class_products.hip": [],
 }
 
 

@@ -297,6 +297,75 @@ PyObject* rmsnorm_backward(PyObject* const* a) {
   return rc ? code(rc) : tuple({dx, dgamma});
 }
 
+// What the two losses over a linear layer's classes share: the operands, the outputs and the workspace.
+struct LossCall {
+  const at::Tensor &x, &w;
+  int64_t ldx, ldw, rows, dim, classes;
+  int dt, dw_dt = 0;
+  const float* bias;
+  bool gradients, weight_gradients;
+  at::Tensor loss, losses, lse, dx, dw, dbias, work;
+  size_t size = 0;
+  LossCall(PyObject* px, PyObject* pw, PyObject* pbias, bool grads, bool weight_grads)
+      : x(tensor(px)), w(tensor(pw)), ldx(leading(x)), ldw(leading(w)), rows(x.size(0)), dim(x.size(1)), classes(w.size(0)), dt(dtype_of(x)), gradients(grads), weight_gradients(grads && weight_grads) {
+    require(w.scalar_type() == x.scalar_type() && w.device() == x.device() && w.size(1) == dim, "weights of the rows' width, type and device are wanted");
+    bias = vector(pbias, classes, x);
+  }
+  // top: entries of a distillation, 0 without.  dtype of the weights' gradient: SLP_F32, SLP_BF16, or None for the weights' own.
+  void room(int64_t top, PyObject* dtype) {
+    dw_dt = given(dtype) ? (int)integer(dtype) : dt;
+    require(dw_dt == SLP_F32 || dw_dt == SLP_BF16, "float32 or bfloat16 is wanted");
+    const bool b = weight_gradients && bias;
+    size = slp_linear_loss_workspace_bytes(x.data_ptr(), ldx, w.data_ptr(), ldw, dt, side(rows), side(classes), side(dim), side(top),
+                                           (gradients ? SLP_LOSS_DX : 0) | (weight_gradients ? SLP_LOSS_DW : 0) | (b ? SLP_LOSS_DBIAS : 0));
+    const at::ScalarType type = dw_dt == SLP_BF16 ? at::kBFloat16 : at::kFloat;
+    const size_t es = dt == SLP_BF16 ? 2 : 4;
+    Room r(x.device(), 3 * Room::padded(4 * rows + 4) + (gradients ? Room::padded((size_t)(rows * dim) * es) : 0) +
+                           (weight_gradients ? Room::padded((size_t)(classes * dim) * (dw_dt == SLP_BF16 ? 2 : 4)) : 0) + (b ? Room::padded(4 * classes) : 0), size);
+    loss = r.take({}, at::kFloat);
+    losses = r.take({rows}, at::kFloat);
+    lse = r.take({rows}, at::kFloat);
+    if (gradients) dx = r.take({rows, dim}, x.scalar_type());
+    if (weight_gradients) dw = r.take({classes, dim}, type);
+    if (b) dbias = r.take({classes}, at::kFloat);
+    work = r.work(size);
+  }
+  PyObject* results() const { return tuple({loss, losses, lse, dx, dw, dbias}); }
+};
+int id_bytes(const at::Tensor& t, const at::Tensor& x) {
+  require(t.device() == x.device() && (t.scalar_type() == at::kInt || t.scalar_type() == at::kLong), "class ids of int32 or int64 on the same device are wanted");
+  return t.scalar_type() == at::kLong ? 8 : 4;
+}
+
+// x, w, targets, bias, gradients, weight_gradients, scale, dtype
+PyObject* linear_cross_entropy(PyObject* const* a) {
+  LossCall c(a[0], a[1], a[3], truth(a[4]), truth(a[5]));
+  const at::Tensor& y = tensor(a[2]);
+  const int bytes = id_bytes(y, c.x);
+  require(y.is_contiguous() && y.dim() == 1 && y.numel() == c.rows, "a contiguous vector of one class id a row is wanted");
+  const On on(c.x.device());
+  c.room(0, a[7]);
+  const int rc = slp_linear_cross_entropy(c.x.data_ptr(), c.ldx, c.w.data_ptr(), c.ldw, c.bias, c.dt, side(c.rows), side(c.classes), side(c.dim), y.data_ptr(), bytes, (float)number(a[6]),
+                                          (float*)address(c.loss), (float*)address(c.losses), (float*)address(c.lse), address(c.dx), c.dim, address(c.dw), c.dim, c.dw_dt,
+                                          (float*)address(c.dbias), address(c.work), c.size, on.stream());
+  return rc ? code(rc) : c.results();
+}
+
+// x, w, top, classes, bias, temperature, gradients, weight_gradients, scale, dtype
+PyObject* linear_distillation(PyObject* const* a) {
+  LossCall c(a[0], a[1], a[4], truth(a[6]), truth(a[7]));
+  const at::Tensor &top = tensor(a[2]), &ids = tensor(a[3]);
+  const int64_t ldtop = leading(top), ldids = leading(ids), k = top.size(1);
+  const int bytes = id_bytes(ids, c.x), top_dt = dtype_of(top);
+  require(top.device() == c.x.device() && top.size(0) == c.rows && ids.sizes() == top.sizes(), "the teacher's logits and their classes, as many a row, are wanted");
+  const On on(c.x.device());
+  c.room(k, a[9]);
+  const int rc = slp_linear_distillation(c.x.data_ptr(), c.ldx, c.w.data_ptr(), c.ldw, c.bias, c.dt, side(c.rows), side(c.classes), side(c.dim), top.data_ptr(), ldtop, top_dt, ids.data_ptr(),
+                                         ldids, bytes, side(k), (float)number(a[5]), (float)number(a[8]), (float*)address(c.loss), (float*)address(c.losses), (float*)address(c.lse),
+                                         address(c.dx), c.dim, address(c.dw), c.dim, c.dw_dt, (float*)address(c.dbias), address(c.work), c.size, on.stream());
+  return rc ? code(rc) : c.results();
+}
+
 // Several tensors as the library takes them.  They are held until the call is queued: what an iterator makes has no other owner, and its memory would be
 // given to the outputs and the workspace.
 struct Tensors {
@@ -376,7 +445,8 @@ PyMethodDef method(const char* name) {
 }
 
 PyMethodDef methods[] = {method<quantize, 6>("quantize"),           method<product, 11>("product"), method<rmsnorm, 6>("rmsnorm"), method<rmsnorm_backward, 6>("rmsnorm_backward"),
-                         method<gradient_norm, 1>("gradient_norm"), method<clip_gradients, 3>("clip_gradients"), {nullptr, nullptr, 0, nullptr}};
+                         method<gradient_norm, 1>("gradient_norm"), method<clip_gradients, 3>("clip_gradients"),
+                         method<linear_cross_entropy, 8>("linear_cross_entropy"), method<linear_distillation, 10>("linear_distillation"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

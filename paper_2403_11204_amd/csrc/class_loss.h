@@ -1,0 +1,110 @@
+// Internal launch interface of the losses over the classes of a linear layer (class_loss.hip: what is done for each row and entry,
+// class_products.hip: the matrix products); the C ABI's host code for them is in losses.hip.  dtype: 0 = float32, 1 = bf16.  Leading dimensions are in
+// elements.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace slp {
+
+// C[m][n] = sum over k of A[m][k] B[n][k], both operands of one type, rows on 16-byte boundaries and zero from K up to the next 16 bytes.  What becomes of
+// the sums s:
+//   PRODUCT_STATS  rows of x against classes: z = (s + bias[n]) times per_t; for each row and span of columns the largest z and sum of exp(z - it)
+//   PRODUCT_PROB   the same z: p = exp(z - norm[m].x) norm[m].y to P, row-major, and, if wanted, transposed; if wanted the sums of P's columns over parts of the rows
+//   PRODUCT_OUT    alpha s to a matrix of either type, or s to (or added to) partial sums, one matrix for each part of the contraction
+enum { PRODUCT_STATS = 0, PRODUCT_PROB = 1, PRODUCT_OUT = 2 };
+struct ClassProduct {
+  const void *a, *b;
+  int64_t lda, ldb;
+  int M, N, K;
+  // STATS and PROB
+  const float* bias;        // [N], may be null
+  float per_t;
+  float2* stats;            // [stats_spans(M, N)][M]: (largest, sum)
+  const float2* norm;       // [M]: the row's largest z (+infinity: the row does not count, its P is zero), 1 / its sum of exp(z - that)
+  const int32_t* labels;    // [M], may be null: class whose P is zero and is left out of the sums (the caller writes it)
+  int label0;               // column 0's class
+  void *p, *pt;             // [M][ldp]; [N][ldpt], may be null; both up to the next 8 columns
+  int64_t ldp, ldpt;
+  float* sums;              // [sum_parts(M, N)][N], may be null
+  // OUT
+  void* out;                // [M][ldo] of out_dtype, any alignment
+  int64_t ldo;
+  int out_dtype;
+  const float* alpha;       // device
+  float* work;              // not null: partial sums instead, [parts][M][N rounded up to 4]
+  int parts;                // of the contraction (1 where work is null)
+  bool add;                 // to what work holds
+};
+int stats_spans(int dtype, int M, int N);
+int sum_parts(int dtype, int M, int N);
+hipError_t launch_class_product(int dtype, int kind, const ClassProduct& g, hipStream_t s);
+
+// The rows' targets: class ids (a class id outside [0, classes) is none), and for a distillation the teacher's logits of them.
+struct Targets {
+  const void* ids;          // [rows][ldids], int32 or int64
+  int64_t ldids;
+  int ids64;
+  const void* top;          // [rows][ldtop] of top_dtype; null: one class for each row, with probability 1
+  int64_t ldtop;
+  int top_dtype;
+  int k;
+  float per_t;              // 1 / temperature
+};
+// zt[row][j] = (x[row] . w[ids[row][j]] + bias) per_t; 0 where the id is none
+struct TargetLogits {
+  const void *x, *w;
+  int64_t ldx, ldw;
+  const float* bias;
+  int rows, classes, dim;
+  Targets t;
+  float* zt;                // [rows][k]
+};
+hipError_t launch_target_logits(int dtype, const TargetLogits& a, hipStream_t s);
+
+// From the spans' statistics to each row's log-sum-exp, its loss, what its gradient needs.
+struct RowLoss {
+  const float2* stats;      // [spans][rows]
+  int spans;
+  int rows, classes;
+  Targets t;
+  const float* zt;
+  float square_t;           // temperature squared
+  float *lse, *losses;      // [rows]
+  float2* norm;             // [rows]: see ClassProduct
+  float* p;                 // [rows][k], may be null where t.top is: the teacher's probabilities, 0 for entries that do not count
+  int32_t* labels;          // [rows], may be null: the row's class or -1
+};
+hipError_t launch_row_loss(const RowLoss& a, hipStream_t s);
+// *loss = mean of the rows that count (0 where none does), *alpha = scale / their number (0)
+hipError_t launch_mean(const float* losses, const float2* norm, int rows, float scale, float* loss, float* alpha, hipStream_t s);
+
+// P at the targets: softmax - (the probability of all the row's entries of that class), in classes [first, first + columns)
+struct TargetFix {
+  Targets t;
+  int rows, classes, dtype;
+  const float *zt, *p;
+  const float2* norm;
+  int first, columns;
+  void *P, *PT;             // PT may be null
+  int64_t ldp, ldpt;
+  unsigned long long* fixed;      // [columns], may be null: what the targets add to the sums of P's columns, in units of 2^-40 ...
+  float* sums;                    // ... and the sums, where that is NaN (the first part's)
+};
+hipError_t launch_target_fix(const TargetFix& a, hipStream_t s);
+
+// dbias[c] = alpha (sum over the parts of sums[part][c] + fixed[c] 2^-40)
+hipError_t launch_bias_gradient(const float* sums, int parts, const unsigned long long* fixed, int columns, const float* alpha, float* dbias, hipStream_t s);
+hipError_t launch_clear(unsigned long long* p, int n, hipStream_t s);
+
+// out[c][r] = in[r][c], zero from rows up to the next multiple of 8; rows that do not count by norm (which may be null) are zeros
+hipError_t launch_transpose(int dtype, const void* in, int64_t ldin, int rows, int cols, const float2* norm, void* out, int64_t ldo, hipStream_t s);
+// out[r][c] = in[r][c], zero from cols up to the next multiple of 8
+hipError_t launch_pad_rows(int dtype, const void* in, int64_t ldin, int rows, int cols, void* out, int64_t ldo, hipStream_t s);
+hipError_t launch_zero(int dtype, void* out, int64_t ldo, int rows, int cols, hipStream_t s);
+// out = alpha * sum over the parts, rounded to the type
+hipError_t launch_join_parts(int dtype, const float* work, int parts, int rows, int cols, const float* alpha, void* out, int64_t ldo, hipStream_t s);
+
+}  // namespace slp

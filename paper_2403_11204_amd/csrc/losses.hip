@@ -1,0 +1,332 @@
+// C ABI of the losses over the classes of a linear layer (see include/slp.h for the contract).  Host code only: every argument is checked
+// before anything is queued.
+#include "../../include/slp.h"
+
+#include "class_loss.h"
+#include "operator_checks.h"
+
+using namespace slp;
+
+namespace {
+
+constexpr int kMaxRows = 1 << 20, kMaxDim = 1 << 20, kMaxTop = 1024;
+// P of a piece of the classes takes this much at most, its transpose as much again.
+constexpr int64_t kPieceBytes = 256 << 20;
+// A tile of 256 rows is addressed with 32-bit offsets: rows of x, W and P lie at most this many elements apart.
+constexpr int kMaxPiece = 1 << 20;
+// Grids have fewer than 2^32 threads.
+constexpr int64_t kMaxWeights = (int64_t)1 << 33, kMaxLogits = (int64_t)1 << 36, kMaxTargets = (int64_t)1 << 25;
+
+// Rows of `width` elements on 128-byte boundaries, not a multiple of 4 KB apart where that many rows share few memory channels.
+int64_t row_ld(int64_t width, int64_t es) {
+  int64_t ld = (width * es + 127) / 128 * 128;
+  if (ld % 4096 == 0) ld += 128;
+  return ld / es;
+}
+
+struct Call {
+  const void* x;
+  int64_t ldx;
+  const void* w;
+  int64_t ldw;
+  const float* bias;
+  Targets t;
+  int dt, rows, classes, dim;
+  float temperature, scale;
+  float *loss, *losses, *lse;
+  void* dx;
+  int64_t lddx;
+  void* dw;
+  int64_t lddw;
+  int dw_dt;
+  float* dbias;
+};
+
+// Where everything lies in the workspace, and in which pieces the classes are taken.
+struct Plan {
+  int64_t es, ldk, ldp, ldr;            // operands' element size; leading dimensions of copies of x and W, of P and W^T, of P^T and x^T
+  bool copy_x, copy_w;
+  int piece;                            // classes
+  int dx_parts, dw_parts, spans;
+  size_t zt, p, labels, norm, alpha, stats, xc, wc, xt, wt, P, PT, dx_work, dw_work, sums, fixed, bytes;
+};
+
+int parts_of(int dt, int M, int N, int K) {
+  const int64_t tiles = (int64_t)((M + 63) / 64) * ((N + 63) / 64);
+  const int nk = (K + (dt == SLP_BF16 ? 63 : 31)) / (dt == SLP_BF16 ? 64 : 32);
+  const int64_t want = 512 / tiles, most = nk / 4;
+  const int64_t parts = want < most ? want : most;
+  return parts < 1 ? 1 : (int)parts;
+}
+
+// Whether the products can read a matrix in place.
+bool in_place(const void* p, int64_t ld, int rows, int dim, int64_t es) { return !off(p, 16) && (rows == 1 || ld * es % 16 == 0) && dim * es % 16 == 0; }
+
+Plan plan_of(const Call& c) {
+  Plan a{};
+  const bool grads = c.dx || c.dw || c.dbias;
+  a.es = (int64_t)size_of(c.dt);
+  a.ldk = row_ld(c.dim, a.es);
+  a.copy_x = !in_place(c.x, c.ldx, c.rows, c.dim, a.es);
+  a.copy_w = !in_place(c.w, c.ldw, c.classes, c.dim, a.es);
+  int64_t most = kPieceBytes / ((int64_t)c.rows * a.es) / 256 * 256;
+  if (most < 256) most = 256;
+  if (most > kMaxPiece) most = kMaxPiece;
+  const int wanted = (int)((c.classes + most - 1) / most);
+  a.piece = wanted == 1 ? c.classes : ((c.classes + wanted - 1) / wanted + 255) / 256 * 256;
+  const int pieces = (c.classes + a.piece - 1) / a.piece;
+  a.ldp = row_ld(a.piece, a.es);
+  a.ldr = row_ld(c.rows, a.es);
+  a.dx_parts = parts_of(c.dt, c.rows, c.dim, a.piece);
+  a.dw_parts = parts_of(c.dt, a.piece, c.dim, c.rows);
+  for (int first = 0; first < c.classes; first += a.copy_w ? a.piece : c.classes)
+    a.spans += stats_spans(c.dt, c.rows, a.copy_w && c.classes - first > a.piece ? a.piece : c.classes - first);
+  size_t at = 0;
+  auto take = [&](bool wanted, int64_t bytes) {
+    const size_t here = at;
+    if (wanted) at += ((size_t)bytes + 255) & ~(size_t)255;
+    return here;
+  };
+  const int64_t targets = (int64_t)c.rows * c.t.k, r = c.rows, d = c.dim, dq = (c.dim + 3) / 4 * 4;
+  a.zt = take(true, targets * 4);
+  a.p = take(c.t.top, targets * 4);
+  a.labels = take(!c.t.top, r * 4);
+  a.norm = take(true, r * 8);
+  a.alpha = take(true, 4);
+  a.stats = take(true, (int64_t)a.spans * r * 8);
+  a.xc = take(a.copy_x, r * a.ldk * a.es);
+  a.wc = take(a.copy_w, (int64_t)a.piece * a.ldk * a.es);
+  a.xt = take(c.dw, d * a.ldr * a.es);
+  a.wt = take(c.dx, d * a.ldp * a.es);
+  a.P = take(grads, r * a.ldp * a.es);
+  a.PT = take(c.dw, (int64_t)a.piece * a.ldr * a.es);
+  a.dx_work = take(c.dx && (pieces > 1 || a.dx_parts > 1), (int64_t)a.dx_parts * r * dq * 4);
+  a.dw_work = take(c.dw && a.dw_parts > 1, (int64_t)a.dw_parts * a.piece * dq * 4);
+  const int64_t rest = c.classes - (int64_t)(pieces - 1) * a.piece, most_sums = (int64_t)sum_parts(c.dt, c.rows, a.piece) * a.piece;
+  const int64_t rest_sums = rest > 0 ? sum_parts(c.dt, c.rows, (int)rest) * rest : 0;      // (smaller tiles, more parts)
+  a.sums = take(c.dbias, (most_sums > rest_sums ? most_sums : rest_sums) * 4);
+  a.fixed = take(c.dbias, (int64_t)a.piece * 8);
+  a.bytes = at;
+  return a;
+}
+
+int run(const Call& c, void* workspace, hipStream_t s) {
+  const Plan a = plan_of(c);
+  char* const base = (char*)workspace;
+  auto at = [&](size_t offset) { return base + offset; };
+  float *const zt = (float*)at(a.zt), *const p = (float*)at(a.p), *const alpha = (float*)at(a.alpha);
+  float2* const norm = (float2*)at(a.norm);
+  const float per_t = 1.0f / c.temperature;
+  const bool grads = c.dx || c.dw || c.dbias;
+
+  const void* x = c.x;
+  int64_t ldx = c.rows == 1 ? a.ldk : c.ldx;       // (a single row may have any)
+  if (a.copy_x) {
+    HIP_TRY(launch_pad_rows(c.dt, c.x, c.ldx, c.rows, c.dim, at(a.xc), a.ldk, s));
+    x = at(a.xc);
+    ldx = a.ldk;
+  }
+  // W's rows from class `first` on, where the products can read them
+  auto weights = [&](int first, int columns, const void*& w, int64_t& ldw) -> int {
+    w = (const char*)c.w + (int64_t)first * c.ldw * a.es;
+    ldw = c.classes == 1 ? a.ldk : c.ldw;
+    if (a.copy_w) {
+      HIP_TRY(launch_pad_rows(c.dt, w, c.ldw, columns, c.dim, at(a.wc), a.ldk, s));
+      w = at(a.wc);
+      ldw = a.ldk;
+    }
+    return SLP_OK;
+  };
+  HIP_TRY(launch_target_logits(c.dt, TargetLogits{c.x, c.w, c.ldx, c.ldw, c.bias, c.rows, c.classes, c.dim, c.t, zt}, s));
+  float2* stats = (float2*)at(a.stats);
+  for (int first = 0; first < c.classes; first += a.copy_w ? a.piece : c.classes) {
+    const int left = c.classes - first, columns = a.copy_w && left > a.piece ? a.piece : left;
+    ClassProduct g{};
+    SLP_CHECK(weights(first, columns, g.b, g.ldb));
+    g.a = x;
+    g.lda = ldx;
+    g.M = c.rows;
+    g.N = columns;
+    g.K = c.dim;
+    g.bias = c.bias ? c.bias + first : nullptr;
+    g.per_t = per_t;
+    g.stats = stats;
+    g.parts = 1;
+    HIP_TRY(launch_class_product(c.dt, PRODUCT_STATS, g, s));
+    stats += (int64_t)stats_spans(c.dt, c.rows, columns) * c.rows;
+  }
+  int32_t* const labels = c.t.top ? nullptr : (int32_t*)at(a.labels);
+  HIP_TRY(launch_row_loss(RowLoss{(const float2*)at(a.stats), a.spans, c.rows, c.classes, c.t, zt, c.temperature * c.temperature, c.lse, c.losses, norm, p, labels}, s));
+  HIP_TRY(launch_mean(c.losses, norm, c.rows, c.scale * c.temperature, c.loss, alpha, s));
+  if (!grads) return SLP_OK;
+
+  if (c.dw) HIP_TRY(launch_transpose(c.dt, x, ldx, c.rows, c.dim, norm, at(a.xt), a.ldr, s));
+  for (int first = 0; first < c.classes; first += a.piece) {
+    const int columns = c.classes - first < a.piece ? c.classes - first : a.piece;
+    const bool last = first + columns == c.classes;
+    ClassProduct g{};
+    SLP_CHECK(weights(first, columns, g.b, g.ldb));
+    const void* const w = g.b;
+    const int64_t ldw = g.ldb;
+    g.a = x;
+    g.lda = ldx;
+    g.M = c.rows;
+    g.N = columns;
+    g.K = c.dim;
+    g.bias = c.bias ? c.bias + first : nullptr;
+    g.per_t = per_t;
+    g.norm = norm;
+    g.labels = labels;
+    g.label0 = first;
+    g.p = at(a.P);
+    g.ldp = a.ldp;
+    g.pt = c.dw ? at(a.PT) : nullptr;
+    g.ldpt = a.ldr;
+    g.sums = c.dbias ? (float*)at(a.sums) : nullptr;
+    g.parts = 1;
+    HIP_TRY(launch_class_product(c.dt, PRODUCT_PROB, g, s));
+    unsigned long long* const fixed = c.dbias ? (unsigned long long*)at(a.fixed) : nullptr;
+    if (fixed) HIP_TRY(launch_clear(fixed, columns, s));
+    HIP_TRY(launch_target_fix(TargetFix{c.t, c.rows, c.classes, c.dt, zt, p, norm, first, columns, g.p, g.pt, a.ldp, a.ldr, fixed, g.sums}, s));
+    if (c.dbias) HIP_TRY(launch_bias_gradient(g.sums, sum_parts(c.dt, c.rows, columns), fixed, columns, alpha, c.dbias + first, s));
+    if (c.dx) {
+      HIP_TRY(launch_transpose(c.dt, w, ldw, columns, c.dim, nullptr, at(a.wt), a.ldp, s));
+      ClassProduct o{};
+      o.a = at(a.P);
+      o.lda = a.ldp;
+      o.b = at(a.wt);
+      o.ldb = a.ldp;
+      o.M = c.rows;
+      o.N = c.dim;
+      o.K = columns;
+      o.alpha = alpha;
+      o.parts = a.dx_parts;
+      if (a.dx_parts > 1 || a.piece < c.classes) {
+        o.work = (float*)at(a.dx_work);
+        o.add = first > 0;
+      } else {
+        o.out = c.dx;
+        o.ldo = c.lddx;
+        o.out_dtype = c.dt;
+      }
+      HIP_TRY(launch_class_product(c.dt, PRODUCT_OUT, o, s));
+      if (o.work && last) HIP_TRY(launch_join_parts(c.dt, o.work, o.parts, c.rows, c.dim, alpha, c.dx, c.lddx, s));
+    }
+    if (c.dw) {
+      char* const dw = (char*)c.dw + (int64_t)first * c.lddw * (int64_t)size_of(c.dw_dt);
+      ClassProduct o{};
+      o.a = at(a.PT);
+      o.lda = a.ldr;
+      o.b = at(a.xt);
+      o.ldb = a.ldr;
+      o.M = columns;
+      o.N = c.dim;
+      o.K = c.rows;
+      o.alpha = alpha;
+      o.parts = a.dw_parts;
+      if (a.dw_parts > 1) {
+        o.work = (float*)at(a.dw_work);
+      } else {
+        o.out = dw;
+        o.ldo = c.lddw;
+        o.out_dtype = c.dw_dt;
+      }
+      HIP_TRY(launch_class_product(c.dt, PRODUCT_OUT, o, s));
+      if (o.work) HIP_TRY(launch_join_parts(c.dw_dt, o.work, o.parts, columns, c.dim, alpha, dw, c.lddw, s));
+    }
+  }
+  return SLP_OK;
+}
+
+int check_call(const char* who, const Call& c) {
+  if (!known(c.dt) || (c.dw && !known(c.dw_dt))) return fail(SLP_ERR_ARG, "%s: unknown dtype %d", who, known(c.dt) ? c.dw_dt : c.dt);
+  if (c.rows < 0 || c.classes <= 0 || c.dim <= 0) return fail(SLP_ERR_ARG, "%s: rows %d, classes %d, dim %d", who, c.rows, c.classes, c.dim);
+  if (c.rows > kMaxRows || c.classes > kMaxSide || c.dim > kMaxDim)
+    return fail(SLP_ERR_SHAPE, "%s: up to %d rows, %d classes and a width of %d (got %d, %d, %d)", who, kMaxRows, kMaxSide, kMaxDim, c.rows, c.classes, c.dim);
+  if ((int64_t)c.classes * c.dim > kMaxWeights || (int64_t)c.rows * c.dim > kMaxWeights || (int64_t)c.rows * c.classes > kMaxLogits || (int64_t)c.rows * c.t.k > kMaxTargets)
+    return fail(SLP_ERR_SHAPE, "%s: %d rows of %d and %d classes, %d targets a row", who, c.rows, c.dim, c.classes, c.t.k);
+  if (!(c.scale == c.scale) || c.scale - c.scale != 0.0f) return fail(SLP_ERR_ARG, "%s: the gradients' scale must be finite", who);
+  if (!c.loss) return fail(SLP_ERR_ARG, "%s: null pointer", who);
+  if (off(c.loss, 4) || off(c.losses, 4) || off(c.lse, 4) || off(c.bias, 4) || off(c.dbias, 4))
+    return fail(SLP_ERR_ALLOC, "%s: a float32 vector is not on an element's boundary", who);
+  if (c.dw) SLP_CHECK(check_dense(who, "dw", c.dw, c.lddw, c.dim, c.dw_dt));
+  if (c.rows == 0) return SLP_OK;
+  if (!c.x || !c.w || !c.t.ids || !c.losses || !c.lse) return fail(SLP_ERR_ARG, "%s: null pointer", who);
+  SLP_CHECK(check_dense(who, "x", c.x, c.ldx, c.dim, c.dt));
+  SLP_CHECK(check_dense(who, "w", c.w, c.ldw, c.dim, c.dt));
+  if (c.dx) SLP_CHECK(check_dense(who, "dx", c.dx, c.lddx, c.dim, c.dt));
+  if ((c.rows > 1 && c.ldx > kMaxPiece) || (c.classes > 1 && c.ldw > kMaxPiece)) return fail(SLP_ERR_SHAPE, "%s: rows of x and w lie at most %d elements apart", who, kMaxPiece);
+  if (off(c.t.ids, c.t.ids64 ? 8 : 4)) return fail(SLP_ERR_ALLOC, "%s: class ids are not on an element's boundary", who);
+  return SLP_OK;
+}
+
+// What no rows leave: a loss of zero, gradients of zero.
+int nothing(const Call& c, hipStream_t s) {
+  HIP_TRY(launch_zero(SLP_F32, c.loss, 1, 1, 1, s));
+  if (c.dbias) HIP_TRY(launch_zero(SLP_F32, c.dbias, c.classes, 1, c.classes, s));
+  if (c.dw) HIP_TRY(launch_zero(c.dw_dt, c.dw, c.lddw, c.classes, c.dim, s));
+  return SLP_OK;
+}
+
+int loss_call(const char* who, const Call& c, void* workspace, size_t workspace_bytes, hipStream_t s) {
+  if (c.rows == 0) return nothing(c, s);
+  SLP_CHECK(check_work(who, workspace, workspace_bytes, plan_of(c).bytes));
+  return run(c, workspace, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t slp_linear_loss_workspace_bytes(const void* x, int64_t ldx, const void* w, int64_t ldw, int dt, int rows, int classes, int dim, int top, int outputs) {
+  if (!known(dt) || rows <= 0 || classes <= 0 || dim <= 0 || rows > kMaxRows || classes > kMaxSide || dim > kMaxDim || top < 0 || top > kMaxTop) return 0;
+  static char given;
+  Call c{};
+  c.x = x;
+  c.ldx = ldx;
+  c.w = w;
+  c.ldw = ldw;
+  c.dt = dt;
+  c.rows = rows;
+  c.classes = classes;
+  c.dim = dim;
+  c.t.k = top ? top : 1;
+  c.t.top = top ? &given : nullptr;
+  c.dx = outputs & SLP_LOSS_DX ? &given : nullptr;
+  c.dw = outputs & SLP_LOSS_DW ? &given : nullptr;
+  c.dbias = outputs & SLP_LOSS_DBIAS ? (float*)&given : nullptr;
+  return plan_of(c).bytes;
+}
+
+int slp_linear_cross_entropy(const void* x, int64_t ldx, const void* w, int64_t ldw, const float* bias, int dt, int rows, int classes, int dim, const void* targets,
+                             int target_bytes, float scale, float* loss, float* losses, float* lse, void* dx, int64_t lddx, void* dw, int64_t lddw, int dw_dt,
+                             float* dbias, void* workspace, size_t workspace_bytes, slp_stream stream) {
+  const char* const who = "slp_linear_cross_entropy";
+  if (target_bytes != 4 && target_bytes != 8) return fail(SLP_ERR_ARG, "%s: class ids of 4 or 8 bytes (got %d)", who, target_bytes);
+  const Targets t{targets, 1, target_bytes == 8, nullptr, 0, 0, 1, 1.0f};
+  const Call c{x, ldx, w, ldw, bias, t, dt, rows, classes, dim, 1.0f, scale, loss, losses, lse, dx, lddx, dw, lddw, dw_dt, dbias};
+  SLP_CHECK(check_call(who, c));
+  return loss_call(who, c, workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+int slp_linear_distillation(const void* x, int64_t ldx, const void* w, int64_t ldw, const float* bias, int dt, int rows, int classes, int dim, const void* top, int64_t ldtop,
+                            int top_dt, const void* top_classes, int64_t ldclasses, int class_bytes, int k, float temperature, float scale, float* loss, float* losses,
+                            float* lse, void* dx, int64_t lddx, void* dw, int64_t lddw, int dw_dt, float* dbias, void* workspace, size_t workspace_bytes,
+                            slp_stream stream) {
+  const char* const who = "slp_linear_distillation";
+  if (class_bytes != 4 && class_bytes != 8) return fail(SLP_ERR_ARG, "%s: class ids of 4 or 8 bytes (got %d)", who, class_bytes);
+  if (!known(top_dt)) return fail(SLP_ERR_ARG, "%s: unknown dtype %d", who, top_dt);
+  if (k <= 0 || k > kMaxTop) return fail(SLP_ERR_ARG, "%s: 1 to %d of the teacher's logits a row (got %d)", who, kMaxTop, k);
+  if (!(temperature >= 1e-3f && temperature <= 1e3f)) return fail(SLP_ERR_ARG, "%s: a temperature between 0.001 and 1000 (got %g)", who, (double)temperature);
+  const Targets t{top_classes, ldclasses, class_bytes == 8, top, ldtop, top_dt, k, 1.0f / temperature};
+  const Call c{x, ldx, w, ldw, bias, t, dt, rows, classes, dim, temperature, scale, loss, losses, lse, dx, lddx, dw, lddw, dw_dt, dbias};
+  SLP_CHECK(check_call(who, c));
+  if (rows > 0) {
+    if (!top) return fail(SLP_ERR_ARG, "%s: null pointer", who);
+    SLP_CHECK(check_dense(who, "top", top, ldtop, k, top_dt));
+    if (ldclasses < k || ldclasses > kMaxLd) return fail(SLP_ERR_SHAPE, "%s: leading dimension %lld of the classes, rows of %d", who, (long long)ldclasses, k);
+  }
+  return loss_call(who, c, workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+}  // extern "C"

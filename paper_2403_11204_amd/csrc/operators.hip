@@ -3,32 +3,19 @@
 #include "../../include/slp.h"
 
 #include "eightbit.h"
-#include "host_errors.h"
+#include "operator_checks.h"
 
 using namespace slp;
 
 namespace {
 
-constexpr int kMaxSide = 1 << 24;
 constexpr int64_t kMaxRow8 = 1 << 22;      // bytes of an 8-bit row: a tile of 256 rows is addressed with 32-bit offsets
-constexpr int64_t kMaxLd = (int64_t)1 << 40;
 constexpr int64_t kMaxElements = (int64_t)1 << 34;      // of a matrix: a grid has fewer than 2^32 threads
-
-bool known(int dt) { return dt == SLP_F32 || dt == SLP_BF16; }
-size_t size_of(int dt) { return dt == SLP_BF16 ? 2 : 4; }
-bool off(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
 int check_sides(const char* who, int rows, int cols) {
   if (rows < 0 || cols < 0) return fail(SLP_ERR_ARG, "%s: negative size (%d, %d)", who, rows, cols);
   if (rows > kMaxSide || cols > kMaxSide) return fail(SLP_ERR_SHAPE, "%s: sizes up to %d (got %d, %d)", who, kMaxSide, rows, cols);
   if ((int64_t)rows * cols > kMaxElements) return fail(SLP_ERR_SHAPE, "%s: a matrix of %d x %d", who, rows, cols);
-  return SLP_OK;
-}
-
-// A float32 or bf16 matrix with rows of `cols` elements.
-int check_dense(const char* who, const char* what, const void* p, int64_t ld, int cols, int dt) {
-  if (ld < cols || ld > kMaxLd) return fail(SLP_ERR_SHAPE, "%s: leading dimension %lld of %s, rows of %d", who, (long long)ld, what, cols);
-  if (off(p, size_of(dt))) return fail(SLP_ERR_ALLOC, "%s: %s is not on an element's boundary", who, what);
   return SLP_OK;
 }
 
@@ -42,18 +29,6 @@ int check_eight(const char* who, const char* what, const void* q, int64_t ldq, c
   if (off(scales, 4) || lds % 4) return fail(SLP_ERR_ALLOC, "%s: rows of the scales of %s must start on 4-byte boundaries", who, what);
   return SLP_OK;
 }
-
-int check_work(const char* who, const void* p, size_t bytes, size_t need) {
-  if (need && (!p || bytes < need || off(p, 256)))
-    return fail(SLP_ERR_ALLOC, "%s: workspace of %zu bytes (256-byte aligned) needed, %zu given", who, need, p ? bytes : (size_t)0);
-  return SLP_OK;
-}
-
-#define SLP_CHECK(expr)         \
-  do {                          \
-    const int rc__ = (expr);    \
-    if (rc__) return rc__;      \
-  } while (0)
 
 int chunk_groups(int64_t chunks) { return (int)(chunks < 1 ? 1 : chunks < kClipMaxGroups ? chunks : kClipMaxGroups); }
 int64_t chunks_of(int64_t count, int dt) { return (count * (int64_t)size_of(dt) + kClipChunk - 1) / kClipChunk; }

@@ -21,8 +21,8 @@
 // instruction pairs with which lane does not matter.  The operands are passed in the order B, A: a lane then holds 4 consecutive
 // columns of one row of the output.
 #include "eightbit_device.h"
+#include "gemm_launch.h"
 
-#include <atomic>
 #include <type_traits>
 #include <utility>
 
@@ -835,18 +835,6 @@ int parts_of(Shape shape, int M, int N, int K) {
   const int64_t t = shape == kSplit ? 512 / tiles_of(M, N, 64, 64) : 256 / tiles_of(M, N, 32, 32);
   const int most = shape == kSplit ? nk / 8 : nk / 16;
   return t < most ? (int)t : most;
-}
-
-// Lets a kernel have that much LDS, once on each device (bit of `done`); host threads that launch first together both do.
-hipError_t allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
-  int device = 0;
-  hipError_t e = hipGetDevice(&device);
-  if (e != hipSuccess) return e;
-  const uint64_t bit = (uint64_t)1 << (device & 63);
-  if (device < 64 && (done.load(std::memory_order_acquire) & bit)) return hipSuccess;
-  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == hipSuccess && device < 64) done.fetch_or(bit, std::memory_order_release);
-  return e;
 }
 
 template <int BM, int BN, int NS, int NG, bool EXACT>
