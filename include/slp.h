@@ -327,6 +327,19 @@ int slp_product(const void* a /*device*/, int64_t lda, const void* a_scales, int
                 const void* b_scales, int64_t ldsb, int b_block, const float* bias /*device, may be NULL*/, int relu, int M, int N, int K,
                 void* out /*device*/, int64_t ldo, int dt, void* workspace /*device*/, size_t workspace_bytes, slp_stream stream);
 
+/* ---- 8-bit integers with a scale for each row ----
+ * A matrix of integers is q [rows][ldq] (signed bytes, alignment and reading past the last column as for 8-bit matrices above) and float32 scales [rows], one for a token of the
+ * activations, one for an output channel of the weights: the values are q * scale.
+ * slp_quantize_integers: q = round(127 x / max|x|) over each row, ties to even, of the real quotient; scale = max|x| / 127.  A row of zeros has the scale 0, one that holds an
+ * infinity or a NaN zeros and the scale NaN.  Written up to the next multiple of 16 columns.
+ * slp_product_integers: out[M][N] = act(a_scales[m] b_scales[n] sum over k of A[m][k] B[n][k] + bias[n]), out of dtype dt; the sums are exact, K up to 131071 (any signed byte may stand
+ * in A and B); scales, bias and ReLU (where relu is not 0; a NaN stays one) in float32.  The workspace holds parts of a contraction that is split over the chip; 256-byte aligned, 0 for most large products.
+ * Limits and errors as for 8-bit matrices; SLP_ERR_SHAPE also for a longer contraction. */
+int slp_quantize_integers(const void* x /*device*/, int64_t ldx, int dt, int rows, int cols, void* q /*device*/, int64_t ldq, float* scales /*device*/, slp_stream stream);
+size_t slp_product_integers_workspace_bytes(int M, int N, int K);
+int slp_product_integers(const void* a /*device*/, int64_t lda, const float* a_scales, const void* b /*device*/, int64_t ldb, const float* b_scales, const float* bias /*device, may be NULL*/,
+                         int relu, int M, int N, int K, void* out /*device*/, int64_t ldo, int dt, void* workspace /*device*/, size_t workspace_bytes, slp_stream stream);
+
 /* Root-mean-square norm of x + residual:
  *   h = x + residual (added in float32, rounded to dt; h = x where residual is NULL);  n = 1 / sqrt(mean over the row of h^2 + eps);  y = h n gamma
  * x, residual, h, y: [rows][dim] of dtype dt; gamma float32 [dim], NULL for ones; rstd float32 [rows] receives n.  h must be given where

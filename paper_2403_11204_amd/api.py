@@ -85,6 +85,9 @@ def lib():
         "slp_rmsnorm_backward": (i32, [vp, i64, vp, i64, vp, vp, vp, i64, i32, i32, i32, vp, i64, vp, vp, sz, vp]),
         "slp_gradient_norm_workspace_bytes": (sz, [i32]),
         "slp_gradient_norm": (i32, [ctypes.POINTER(vp), ctypes.POINTER(i64), ctypes.POINTER(i32), i32, vp, vp, sz, vp]),
+        "slp_quantize_integers": (i32, [vp, i64, i32, i32, i32, vp, i64, vp, vp]),
+        "slp_product_integers_workspace_bytes": (sz, [i32, i32, i32]),
+        "slp_product_integers": (i32, [vp, i64, vp, vp, i64, vp, vp, i32, i32, i32, i32, vp, i64, i32, vp, sz, vp]),
         "slp_linear_loss_workspace_bytes": (sz, [vp, i64, vp, i64, i32, i32, i32, i32, i32, i32]),
         "slp_linear_cross_entropy": (i32, [vp, i64, vp, i64, vp, i32, i32, i32, i32, vp, i32, f32, vp, vp, vp, vp, i64, vp, i64, i32, vp, vp, sz, vp]),
         "slp_linear_distillation": (i32, [vp, i64, vp, i64, vp, i32, i32, i32, i32, vp, i64, i32, vp, i64, i32, i32, f32, f32, vp, vp, vp, vp, i64, vp, i64, i32, vp, vp, sz, vp]),
@@ -108,7 +111,7 @@ EXPORTS = ["slp_last_error", "slp_make_synthetic_labels", "slp_make_segment_inpu
            "slp_segment_graph_stats", "slp_quantize_workspace_bytes", "slp_quantize", "slp_product_workspace_bytes",
            "slp_product", "slp_rmsnorm", "slp_rmsnorm_backward_workspace_bytes", "slp_rmsnorm_backward",
            "slp_gradient_norm_workspace_bytes", "slp_gradient_norm", "slp_clip_gradients", "slp_linear_loss_workspace_bytes", "slp_linear_cross_entropy",
-           "slp_linear_distillation"]
+           "slp_linear_distillation", "slp_quantize_integers", "slp_product_integers_workspace_bytes", "slp_product_integers"]
 
 
 def _check(code):
@@ -247,6 +250,22 @@ def product(a, b, bias=None, relu=False, dtype=BF16, out=None, float32_sums=Fals
     `out`, whose type decides then).  Sums for a bf16 output of many rows lose what is 2^-13 below the largest of 8 neighbouring products
     (some 2e-5 of the result, where nothing cancels); `float32_sums` adds them in float32, as for a float32 output, at half the rate."""
     return _outputs(_binding().product(a[0], a[1], a[2], b[0], b[1], b[2], bias, relu, dtype, out, float32_sums))
+
+
+# A matrix of 8-bit integers: q [rows, cols] (int8, rows on 16-byte boundaries), scales [rows] (float32); the values are q * scale.  What lies between the last
+# column and the next multiple of 16 is not interpreted, as for Quantized.
+Integers = collections.namedtuple("Integers", "q scales")
+
+
+def quantize_integers(x):
+    """slp_quantize_integers: the rows of x (tokens, or the output channels of a weight matrix) as integers from -127 to 127, each with its own scale."""
+    return Integers(*_outputs(_binding().quantize_integers(x)))
+
+
+def product_integers(a, b, bias=None, relu=False, dtype=BF16, out=None):
+    """slp_product_integers: act(a b^T + bias) of two Integers matrices with the same number of columns (131071 at most; the sums are exact), as a matrix of `dtype`
+    (or into `out`, whose type decides then)."""
+    return _outputs(_binding().product_integers(a[0], a[1], b[0], b[1], bias, relu, dtype, out))
 
 
 def rmsnorm(x, gamma=None, residual=None, eps=1e-6, normed=False, quantized=True):

@@ -42,6 +42,7 @@ UNITS = {
     "quantize.hip": [],
     "product.hip": [],
     "clip.hip": [],
+    "integers.hip": [],
     "losses.hip": [],
     "class_loss.hip": [],
     "class_products.hip": [],

@@ -243,6 +243,58 @@ PyObject* product(PyObject* const* a) {
   return wrapped(out);
 }
 
+// x
+PyObject* quantize_integers(PyObject* const* a) {
+  const at::Tensor& x = tensor(a[0]);
+  const int64_t ldx = leading(x), m = x.size(0), n = x.size(1), ld = eight_ld(m, n);
+  const int dt = dtype_of(x);
+  const On on(x.device());
+  Room room(x.device(), Room::padded((size_t)(m * ld)) + Room::padded(4 * m), 0);
+  const at::Tensor q = room.take({m, ld}, at::kChar), scales = room.take({m}, at::kFloat);
+  if (ld != n) q.unsafeGetTensorImpl()->set_sizes_and_strides(at::IntArrayRef({m, n}), at::IntArrayRef({ld, 1}));
+  const int rc = slp_quantize_integers(x.data_ptr(), ldx, dt, side(m), side(n), q.data_ptr(), ld, (float*)scales.data_ptr(), on.stream());
+  return rc ? code(rc) : tuple({q, scales});
+}
+
+// A matrix of integers: its leading dimension and scales.
+const float* integers_given(PyObject* q, PyObject* scales, int64_t cols, int64_t& ld) {
+  const at::Tensor& t = tensor(q);
+  require(t.is_cuda() && t.dim() == 2 && t.scalar_type() == at::kChar && t.size(1) == cols, "values of int8 with as many columns are wanted");
+  require(t.stride(1) == 1 || cols <= 1, "rows must be contiguous");
+  ld = t.size(0) <= 1 ? (cols + 15) / 16 * 16 : t.stride(0);
+  require(given(scales), "scales of float32, one a row, are wanted");
+  return vector(scales, t.size(0), t);
+}
+
+// a's values, scales, b's, bias, relu, dtype, out
+PyObject* product_integers(PyObject* const* a) {
+  const at::Tensor &x = tensor(a[0]), &y = tensor(a[2]);
+  const int64_t cols = x.size(-1);
+  int64_t lda, ldb;
+  const float *const sa = integers_given(a[0], a[1], cols, lda), *const sb = integers_given(a[2], a[3], cols, ldb);
+  require(x.device() == y.device(), "matrices on one device are wanted");
+  const int64_t m = x.size(0), n = y.size(0);
+  const size_t size = slp_product_integers_workspace_bytes(side(m), side(n), side(cols));
+  at::Tensor out;
+  int dt = (int)integer(a[6]);
+  int64_t ldo = n;
+  const On on(x.device());
+  Room room(x.device(), given(a[7]) ? 0 : Room::padded((size_t)(m * n) * (dt == SLP_BF16 ? 2 : 4)), size);
+  if (given(a[7])) {
+    out = tensor(a[7]);
+    require(out.dim() == 2 && out.size(0) == m && out.size(1) == n && out.device() == x.device(), "an output of the product's shape is wanted");
+    ldo = leading(out);
+    dt = dtype_of(out);
+  } else {
+    out = room.take({m, n}, dt == SLP_BF16 ? at::kBFloat16 : at::kFloat);
+  }
+  const at::Tensor work = room.work(size);
+  const int rc = slp_product_integers(x.data_ptr(), lda, sa, y.data_ptr(), ldb, sb, vector(a[4], n, x), truth(a[5]), side(m), side(n), side(cols), out.data_ptr(), ldo, dt,
+                                      address(work), size, on.stream());
+  if (rc) return code(rc);
+  return wrapped(out);
+}
+
 // x, gamma, residual, eps, normed, quantized
 PyObject* rmsnorm(PyObject* const* a) {
   const at::Tensor& x = tensor(a[0]);
@@ -446,6 +498,7 @@ PyMethodDef method(const char* name) {
 
 PyMethodDef methods[] = {method<quantize, 6>("quantize"),           method<product, 11>("product"), method<rmsnorm, 6>("rmsnorm"), method<rmsnorm_backward, 6>("rmsnorm_backward"),
                          method<gradient_norm, 1>("gradient_norm"), method<clip_gradients, 3>("clip_gradients"),
+                         method<quantize_integers, 1>("quantize_integers"), method<product_integers, 8>("product_integers"),
                          method<linear_cross_entropy, 8>("linear_cross_entropy"), method<linear_distillation, 10>("linear_distillation"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -67,6 +67,30 @@ struct ProductArgs {
 size_t product_floats(int M, int N, int K);
 hipError_t launch_product(const ProductArgs& a, hipStream_t s);
 
+// Integers: rows of x to q = round(127 x / max|x|), ties to even, and scale = max|x| / 127.
+struct IntegersArgs {
+  const void* x;
+  int8_t* q;
+  float* scales;            // [rows]
+  int64_t ldx, ldq;
+  int rows, cols;
+};
+hipError_t launch_quantize_integers(int dtype, const IntegersArgs& a, hipStream_t s);
+struct IntegerProductArgs {
+  const int8_t *a, *b;
+  const float *sa, *sb;     // of the rows
+  int64_t lda, ldb;
+  int M, N, K;
+  const float* bias;        // [N], may be null
+  int relu;
+  void* out;                // [M][ldo]
+  int64_t ldo;
+  int out_dtype;
+  int32_t* work;            // integer_product_words(M, N, K)
+};
+size_t integer_product_words(int M, int N, int K);
+hipError_t launch_integer_product(const IntegerProductArgs& g, hipStream_t s);
+
 constexpr int kClipTensors = 48;      // a launch takes (kernel arguments)
 struct ClipTable {
   const void* in[kClipTensors];

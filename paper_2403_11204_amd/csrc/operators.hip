@@ -10,6 +10,7 @@ using namespace slp;
 namespace {
 
 constexpr int64_t kMaxRow8 = 1 << 22;      // bytes of an 8-bit row: a tile of 256 rows is addressed with 32-bit offsets
+constexpr int kMaxIntegerK = 131071;       // 131071 * 128^2 < 2^31
 constexpr int64_t kMaxElements = (int64_t)1 << 34;      // of a matrix: a grid has fewer than 2^32 threads
 
 int check_sides(const char* who, int rows, int cols) {
@@ -27,6 +28,14 @@ int check_eight(const char* who, const char* what, const void* q, int64_t ldq, c
     return fail(SLP_ERR_SHAPE, "%s: leading dimension %lld of the scales of %s, rows of %d", who, (long long)lds, what, cols);
   if (off(q, 16) || ldq % 16) return fail(SLP_ERR_ALLOC, "%s: rows of %s must start on 16-byte boundaries", who, what);
   if (off(scales, 4) || lds % 4) return fail(SLP_ERR_ALLOC, "%s: rows of the scales of %s must start on 4-byte boundaries", who, what);
+  return SLP_OK;
+}
+
+// A matrix of integers with rows of `cols` elements and a scale each.
+int check_integers(const char* who, const char* what, const void* q, int64_t ldq, const float* scales, int cols) {
+  if (ldq < cols || ldq > kMaxRow8) return fail(SLP_ERR_SHAPE, "%s: leading dimension %lld of %s, rows of %d, at most %lld", who, (long long)ldq, what, cols, (long long)kMaxRow8);
+  if (off(q, 16) || ldq % 16) return fail(SLP_ERR_ALLOC, "%s: rows of %s must start on 16-byte boundaries", who, what);
+  if (off(scales, 4)) return fail(SLP_ERR_ALLOC, "%s: the scales of %s are not on an element's boundary", who, what);
   return SLP_OK;
 }
 
@@ -149,6 +158,43 @@ int slp_product(const void* a, int64_t lda, const void* a_scales, int64_t ldsa, 
   const ProductArgs g{(const uint8_t*)a, (const uint8_t*)a_scales, (const uint8_t*)b, (const uint8_t*)b_scales, lda, ldsa, ldb, ldsb,
                       a_block == 1 ? 0 : 7, b_block == 1 ? 0 : 7, M, N, K, bias, relu, out, ldo, dt, exact, (float*)workspace};
   HIP_TRY(launch_product(g, (hipStream_t)stream));
+  return SLP_OK;
+}
+
+int slp_quantize_integers(const void* x, int64_t ldx, int dt, int rows, int cols, void* q, int64_t ldq, float* scales, slp_stream stream) {
+  const char* const who = "slp_quantize_integers";
+  if (!known(dt)) return fail(SLP_ERR_ARG, "%s: unknown dtype %d", who, dt);
+  SLP_CHECK(check_sides(who, rows, cols));
+  if (rows == 0) return SLP_OK;
+  if (!scales || (cols > 0 && (!x || !q))) return fail(SLP_ERR_ARG, "%s: null pointer", who);
+  SLP_CHECK(check_integers(who, "q", q, ldq, scales, cols));
+  SLP_CHECK(check_dense(who, "x", x, ldx, cols, dt));
+  const IntegersArgs a{x, (int8_t*)q, scales, ldx, ldq, rows, cols};
+  HIP_TRY(launch_quantize_integers(dt, a, (hipStream_t)stream));
+  return SLP_OK;
+}
+
+size_t slp_product_integers_workspace_bytes(int M, int N, int K) {
+  return M > 0 && N > 0 && K >= 0 && M <= kMaxSide && N <= kMaxSide && K <= kMaxIntegerK ? integer_product_words(M, N, K) * sizeof(int32_t) : 0;
+}
+
+int slp_product_integers(const void* a, int64_t lda, const float* a_scales, const void* b, int64_t ldb, const float* b_scales, const float* bias, int relu, int M, int N, int K,
+                         void* out, int64_t ldo, int dt, void* workspace, size_t workspace_bytes, slp_stream stream) {
+  const char* const who = "slp_product_integers";
+  if (!known(dt)) return fail(SLP_ERR_ARG, "%s: unknown dtype %d", who, dt);
+  SLP_CHECK(check_sides(who, M, N));
+  if (K < 0) return fail(SLP_ERR_ARG, "%s: negative size %d", who, K);
+  if (K > kMaxIntegerK) return fail(SLP_ERR_SHAPE, "%s: contractions of up to %d, whose sums fit 32 bits (got %d)", who, kMaxIntegerK, K);
+  if (M == 0 || N == 0) return SLP_OK;
+  if (!out || !a_scales || !b_scales || (K > 0 && (!a || !b))) return fail(SLP_ERR_ARG, "%s: null pointer", who);
+  SLP_CHECK(check_dense(who, "out", out, ldo, N, dt));
+  if (K == 0) lda = ldb = 0;             // (the kernels' bounds are made of them)
+  SLP_CHECK(check_integers(who, "a", a, lda, a_scales, K));
+  SLP_CHECK(check_integers(who, "b", b, ldb, b_scales, K));
+  if (off(bias, 4)) return fail(SLP_ERR_ALLOC, "%s: bias is not on an element's boundary", who);
+  SLP_CHECK(check_work(who, workspace, workspace_bytes, slp_product_integers_workspace_bytes(M, N, K)));
+  const IntegerProductArgs g{(const int8_t*)a, (const int8_t*)b, a_scales, b_scales, lda, ldb, M, N, K, bias, relu, out, ldo, dt, (int32_t*)workspace};
+  HIP_TRY(launch_integer_product(g, (hipStream_t)stream));
   return SLP_OK;
 }
 
