@@ -10,16 +10,13 @@
 #include "class_loss.h"
 #include "eightbit_device.h"
 #include "gemm_launch.h"
-
-#include <type_traits>
+#include "long_tile.h"
 
 namespace slp {
 namespace {
 
 constexpr int kXcds = 8;
 constexpr uint32_t kOutOfRange = 0x80000000u;     // byte offset past the end of every tile
-#define SLP_VMCNT(n) ((((n) & 15) | 0x0F70 | (((n) >> 4) << 14)))
-#define SLP_VMCNT_LGKM0(n) (SLP_VMCNT(n) & 0xF0FF)
 constexpr float kLog2e = 1.44269504088896340736f;
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, int64_t bytes) {
@@ -298,14 +295,208 @@ __global__ __launch_bounds__(256) void class_tile_kernel(const ClassProduct g, i
 #endif
 }
 
+// Large bf16 products (long_tile.h).  What the epilogues of the tiles above do, with the accumulators taken out of the AGPRs a block at a time, and stores of whole
+// row segments: a wavefront stages its 128 x 128 outputs in a 32 KB of the stages that is its own, rows of 256 bytes whose 16-byte piece c sits at c ^ swz(row), and takes
+// them out row by row and, through transposing LDS reads (a group of 16 lanes reads 4 rows of 16 columns, lane l gets the 4 values of column l), column by column.
+// 16 rows in a row lie on 16 pieces, the 8 rows that half a wavefront reads transposed on disjoint ones.
+template <int KIND>
+__global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, int kper) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef __attribute__((ext_vector_type(4))) short i16x4;
+  typedef __attribute__((address_space(3))) i16x4* lds_i16x4;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  int tm, tn;
+  big_tile(g.M, g.N, tm, tn);
+  const int m0 = tm * 256, n0 = tn * 256;
+  f32x4 acc[8][8];
+  {
+    const int64_t lda = g.lda * 2, ldb = g.ldb * 2, from = (int64_t)blockIdx.y * kper * 128, all = (int64_t)g.K * 2 - from, part = (int64_t)kper * 128;
+    const int K = all <= 0 ? 0 : (int)(all < part ? all : part);
+    const int64_t at = all <= 0 ? 0 : from;
+    long_tile<f32x4, false>(acc, smem, (const char*)g.a + m0 * lda + at, (const char*)g.b + n0 * ldb + at, lda, ldb, g.M - m0 < 256 ? g.M - m0 : 256, g.N - n0 < 256 ? g.N - n0 : 256, K);
+  }
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, wm = w & 1, wn = w >> 1, lgrp = lane >> 4, lrow = lane & 15;
+  const int rowW = m0 + wm * 128, colW = n0 + wn * 128;
+  if constexpr (KIND == PRODUCT_STATS) {
+    // z log2(e), so that the exponentials take one addition
+    f32x4 bias[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int n = colW + 16 * j + 4 * lgrp + e;
+        bias[j][e] = n >= g.N ? -INFINITY : g.bias ? g.bias[n] : 0.0f;
+      }
+    const int span = colW / 128;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      f32x4 z[8];
+      float most = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        asm volatile("" : "+a"(acc[i][j]));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          z[j][e] = (acc[i][j][e] + bias[j][e]) * g.per_t;
+          most = fmaxf(most, z[j][e]);
+        }
+      }
+      most = fmax_of_rows(most);
+      const float from = most == -INFINITY ? 0.0f : most;
+      float sum = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((z[j][e] - from) * kLog2e);
+      sum = sum_of_rows(sum);
+      const int m = rowW + 16 * i + lrow;
+      if (lgrp == 0 && m < g.M) g.stats[(int64_t)span * g.M + m] = float2{most, sum};
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    return;
+  }
+  auto swz = [](int r) { return ((r & 3) << 1) | (r & 8) | ((r >> 2) & 1); };
+  __syncthreads();                       // nobody reads the stages any more
+  unsigned char* const st = smem + w * 32768;
+  unsigned char* const wbase = st + lrow * 256 + (lgrp & 1) * 8;
+  const int wsw = (lgrp >> 1) ^ swz(lrow);
+  auto stage = [&](int i, int j, const f32x4& v) {
+    const bf16x4 o = {(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+    *(u32x2*)(wbase + i * 4096 + ((wsw ^ (2 * j)) << 4)) = __builtin_bit_cast(u32x2, o);
+  };
+  // 16-byte pieces of whole rows, 8 at a time: their LDS reads are under way together
+  auto rows_out = [&](auto put) {
+    const int r0 = lane >> 4, c = lane & 15;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      u32x4 val[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int r = (8 * b + q) * 4 + r0;
+        val[q] = *(const u32x4*)(st + r * 256 + ((c ^ swz(r & 15)) << 4));
+      }
+#pragma unroll
+      for (int q = 0; q < 8; ++q) put((8 * b + q) * 4 + r0, c * 8, val[q]);
+    }
+  };
+  if constexpr (KIND == PRODUCT_OUT) {
+    const float alpha = g.work ? 1.0f : *g.alpha;
+    if (g.work || g.out_dtype == 0) {    // float32, straight from the accumulators: 64-byte segments
+      const int64_t ld = g.work ? (g.N + 3) & ~3 : g.ldo;
+      float* const out = g.work ? g.work + (int64_t)blockIdx.y * g.M * ld : (float*)g.out;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int n = colW + 16 * j + 4 * lgrp;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          asm volatile("" : "+a"(acc[i][j]));
+          const int m = rowW + 16 * i + lrow;
+          if (m < g.M && n < g.N) {
+            float* const to = out + m * ld + n;
+            f32x4 v = acc[i][j] * alpha;
+            if (g.work) {
+              if (g.add) v += *(const f32x4*)to;
+              *(f32x4*)to = v;
+            } else {
+              store4(to, g.N - n, v);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        asm volatile("" : "+a"(acc[i][j]));
+        stage(i, j, acc[i][j] * alpha);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    rows_out([&](int r, int c, const u32x4& v) {
+      const int m = rowW + r, n = colW + c;
+      if (m < g.M && n < g.N) {
+        bf16* const to = (bf16*)g.out + m * g.ldo + n;
+        const bf16x8 o = __builtin_bit_cast(bf16x8, v);
+        if (n + 8 <= g.N) ((AnyBf16x8*)to)->v = o;
+        else
+          for (int e = 0; e < g.N - n; ++e) to[e] = o[e];
+      }
+    });
+  } else if constexpr (KIND == PRODUCT_PROB) {
+    float2 norm[8];
+    int label[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int m = rowW + 16 * i + lrow;
+      norm[i] = m < g.M ? g.norm[m] : float2{INFINITY, 0.0f};
+      label[i] = g.labels && m < g.M ? g.labels[m] - g.label0 : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int n = colW + 16 * j + 4 * lgrp;
+      f32x4 bias, sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) bias[e] = n + e >= g.N ? -INFINITY : g.bias ? g.bias[n + e] : 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        asm volatile("" : "+a"(acc[i][j]));
+        f32x4 p;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float z = (acc[i][j][e] + bias[e]) * g.per_t;
+          p[e] = __builtin_amdgcn_exp2f((z - norm[i].x) * kLog2e) * norm[i].y;
+          if (norm[i].x == INFINITY || n + e == label[i] || n + e >= g.N) p[e] = 0.0f;       // (also where the row holds NaN)
+        }
+        sum += p;
+        stage(i, j, p);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (g.sums) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float all = sum_of_16(sum[e]);
+          if (lrow == 0 && n + e < g.N) g.sums[(int64_t)(rowW / 128) * g.N + n + e] = all;
+        }
+      }
+    }
+    rows_out([&](int r, int c, const u32x4& v) {
+      if (rowW + r < g.M && colW + c < g.N) *(u32x4*)((bf16*)g.p + (int64_t)(rowW + r) * g.ldp + colW + c) = v;
+    });
+    if (g.pt) {
+      const int gq = lane >> 4, jj = lane & 15, r0 = gq * 8 + (jj >> 2);        // staged row of the first of the two reads
+      const uint32_t base = (uint32_t)(r0 * 256 + ((((jj & 3) >> 1) ^ swz(r0 & 15)) << 4) + (jj & 1) * 8);
+#pragma unroll
+      for (int b = 0; b < 8; b += 2) {
+        u32x2 val[8][2];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const uint32_t o1 = (base ^ ((b + q / 4) << 5)) + q % 4 * 8192;
+          val[q][0] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(st + o1)));
+          val[q][1] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(st + ((o1 ^ 16) + 1024))));
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int n = colW + jj + (b + q / 4) * 16, m = rowW + gq * 8 + q % 4 * 32;
+          if (n < g.N && m < g.M) *(u32x4*)((bf16*)g.pt + (int64_t)n * g.ldpt + m) = u32x4{val[q][0][0], val[q][0][1], val[q][1][0], val[q][1][1]};
+        }
+      }
+    }
+  }
+#endif
+}
+
 // ---- host side -------------------------------------------------------------------------------
 int64_t tiles_of(int M, int N, int BM, int BN) { return (int64_t)((M + BM - 1) / BM) * ((N + BN - 1) / BN); }
 
-enum Shape { k128, k64 };
+enum Shape { kLong, k128, k64 };
 Shape shape_of(int dtype, int M, int N) {
-  (void)dtype;
+  if (dtype == 1 && tiles_of(M, N, 256, 256) >= 200) return kLong;
   return tiles_of(M, N, 128, 128) >= 200 ? k128 : k64;
 }
+// Rows, or columns, of a wavefront's part of a tile.
+int span_of(Shape s) { return s == kLong ? 128 : s == k128 ? 64 : 32; }
 
 template <typename T, int KIND, int BM, int BN, int NS>
 hipError_t launch_tile(const ClassProduct& g, hipStream_t s) {
@@ -318,9 +509,20 @@ hipError_t launch_tile(const ClassProduct& g, hipStream_t s) {
   hipLaunchKernelGGL((class_tile_kernel<T, KIND, BM, BN, NS>), dim3((unsigned)tiles_of(g.M, g.N, BM, BN), parts), dim3(256), smem, s, g, kper);
   return hipGetLastError();
 }
+template <int KIND>
+hipError_t launch_long(const ClassProduct& g, hipStream_t s) {
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = allow_lds((const void*)class_long_kernel<KIND>, kLongSmem, done);
+  if (e != hipSuccess) return e;
+  const int nk = (g.K + 63) / 64, parts = g.work ? g.parts : 1, kper = (nk + parts - 1) / parts;
+  class_long_kernel<KIND><<<dim3((unsigned)tiles_of(g.M, g.N, 256, 256), parts), 256, kLongSmem, s>>>(g, kper);
+  return hipGetLastError();
+}
 template <typename T, int KIND>
 hipError_t launch_kind(int dtype, const ClassProduct& g, hipStream_t s) {
   switch (shape_of(dtype, g.M, g.N)) {
+    case kLong:
+      if constexpr (sizeof(T) == 2) return launch_long<KIND>(g, s);
     case k128: return launch_tile<T, KIND, 128, 128, 2>(g, s);
     default: return launch_tile<T, KIND, 64, 64, 2>(g, s);
   }
@@ -337,11 +539,11 @@ hipError_t launch_type(int dtype, int kind, const ClassProduct& g, hipStream_t s
 }  // namespace
 
 int stats_spans(int dtype, int M, int N) {
-  const int w = shape_of(dtype, M, N) == k128 ? 64 : 32;
+  const int w = span_of(shape_of(dtype, M, N));
   return (N + 2 * w - 1) / (2 * w) * 2;
 }
 int sum_parts(int dtype, int M, int N) {
-  const int w = shape_of(dtype, M, N) == k128 ? 64 : 32;
+  const int w = span_of(shape_of(dtype, M, N));
   return (M + 2 * w - 1) / (2 * w) * 2;
 }
 

@@ -1,0 +1,63 @@
+"""Losses over a linear layer's classes at sizes whose products run on 256x256 tiles, whole and ragged, against 64 bits on the device."""
+
+import pytest
+import torch
+
+from paper_2403_11204_amd import api
+
+pytestmark = pytest.mark.gpu
+DT = {"fp32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.mark.parametrize("rows,classes,dim,k,bias,dtype", [(2048, 8192, 512, 0, False, "bf16"), (2001, 8201, 520, 3, True, "bf16"), (300, 33001, 72, 0, True, "bf16"), (4100, 4099, 264, 5, True, "bf16"),
+                                                           (5000, 3001, 4104, 0, True, "bf16"), (3, 60000, 256, 2, True, "bf16"), (1030, 2100, 700, 2, True, "fp32"), (3000, 500, 2056, 0, True, "bf16")])
+def test_large(rows, classes, dim, k, bias, dtype):
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn(rows, dim, device="cuda", generator=g).to(DT[dtype])
+    w = (torch.randn(classes, dim, device="cuda", generator=g) * (2.5 / dim ** 0.5)).to(DT[dtype])
+    b = torch.randn(classes, device="cuda", generator=g) if bias else None
+    ids = torch.randint(-classes // 8, classes, (rows, max(k, 1)), device="cuda", generator=g)
+    top = 2 * torch.randn(rows, k, device="cuda", generator=g) if k else None
+    T = 2.0 if k else 1.0
+    r = api.linear_distillation(x, w, top, ids, bias=b, temperature=T) if k else api.linear_cross_entropy(x, w, ids[:, 0].contiguous(), bias=b)
+    X, W = x.double(), w.double()
+    z = X @ W.t()
+    if bias:
+        z += b.double()
+    z /= T
+    lse = torch.logsumexp(z, 1)
+    live = ids >= 0
+    counts = live.any(1)
+    n = int(counts.sum())
+    t = (top.double() / T if k else torch.zeros_like(ids, dtype=torch.float64)).masked_fill(~live, -float("inf"))
+    p = torch.where(counts[:, None], torch.softmax(torch.where(counts[:, None], t, torch.zeros_like(t)), 1), torch.zeros_like(t))
+    at = ids.clamp(min=0)
+    losses = T * T * (p * torch.where(p > 0, p.log() + lse[:, None] - z.gather(1, at), torch.zeros_like(p))).sum(1)
+    soft = torch.exp(z - lse[:, None])
+    # A logit: dim additions that each round by 2^-24 of a partial sum, which stays below |z| + 3 * 2.5 (the products' squares add up to 2.5^2), 6 standard deviations of
+    # their sum; log-sum-exp and losses twice that and 2^-21 of their size
+    dz = 6 * dim ** 0.5 * 2.0 ** -24 * (float(z.abs().max()) + 7.5)
+    assert (r.lse.double() - lse).abs().max() <= 2 * dz + 2.0 ** -21 * float(lse.abs().max())
+    far = T * T * (2 * dz + 2.0 ** -20 * (float(lse.abs().max()) + float(losses.max())))
+    assert (r.losses.double() - losses).abs().max() <= far and abs(float(r.loss) - float(losses.sum()) / n) <= far
+    target = torch.zeros_like(soft).scatter_add_(1, at, p)
+    G = (soft - target) * (counts[:, None] * (T / n))
+    # P: relative 2 dz + 2^-22, of the teacher's probabilities 2^-19, half a step of bf16 behind; products: sqrt(terms) additions; outputs: half a step
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    P = (soft * (2 * dz + 2.0 ** -22) + target * 2.0 ** -19) * (counts[:, None] * (T / n)) + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) * G.abs()
+
+    def check(got, want, err, size, terms):
+        off = (got.double() - want).abs() - (err + 6 * terms ** 0.5 * 2.0 ** -24 * size + 1.01 * half * want.abs() + 1e-30)
+        assert off.max() <= 0, (float(off.max()), int(off.argmax()))
+
+    check(r.dx, G @ W, P @ W.abs(), G.abs() @ W.abs(), classes)
+    Gt, Pt = G.t().contiguous(), P.t().contiguous()
+    check(r.dw, Gt @ X, Pt @ X.abs(), Gt.abs() @ X.abs(), rows)
+    if bias:
+        off = (r.dbias.double() - G.sum(0)).abs()
+        # sums in float32 over up to 256 rows, then in 64 bits; integers of 2^-40 for the targets
+        assert (off <= (P - (2.0 ** -8 * G.abs() if dtype == "bf16" else 0)).sum(0) + 2.0 ** -20 * (soft * counts[:, None]).sum(0) * (T / n) + 2.0 ** -22 * G.sum(0).abs() + T * 2.0 ** -40).all()
+    # an output of another type: the same sums
+    if not k:
+        other = api.linear_cross_entropy(x, w, ids[:, 0].contiguous(), bias=b, dtype=api.F32 if dtype == "bf16" else api.BF16)
+        assert torch.equal(other.dw.bfloat16(), r.dw.bfloat16())
