@@ -12,9 +12,12 @@ namespace slp {
 // C[m][n] = sum over k of A[m][k] B[n][k], both operands of one type, rows on 16-byte boundaries and zero from K up to the next 16 bytes.  What becomes of
 // the sums s:
 //   PRODUCT_STATS  rows of x against classes: z = (s + bias[n]) times per_t; for each row and span of columns the largest z and sum of exp(z - it)
-//   PRODUCT_PROB   the same z: p = exp(z - norm[m].x) norm[m].y to P, row-major, and, if wanted, transposed; if wanted the sums of P's columns over parts of the rows
-//   PRODUCT_OUT    alpha s to a matrix of either type, or s to (or added to) partial sums, one matrix for each part of the contraction
-enum { PRODUCT_STATS = 0, PRODUCT_PROB = 1, PRODUCT_OUT = 2 };
+//   PRODUCT_PROB   the same z: p = exp(z - norm[m].x) norm[m].y to P; if wanted the sums of P's columns over parts of the rows
+//   PRODUCT_DX     P W: B lies the other way, as [K][ldb]
+//   PRODUCT_DW     P^T x: both do, A as [K][lda], B as [K][ldb]; either: alpha s to a matrix of either type, or s to (or added to) partial sums, one matrix for each
+//                  part of the contraction
+// An operand that lies the other way has its columns' last 16 bytes to itself, and is smaller than 2 GiB.
+enum { PRODUCT_STATS = 0, PRODUCT_PROB = 1, PRODUCT_DX = 2, PRODUCT_DW = 3 };
 struct ClassProduct {
   const void *a, *b;
   int64_t lda, ldb;
@@ -26,10 +29,10 @@ struct ClassProduct {
   const float2* norm;       // [M]: the row's largest z (+infinity: the row does not count, its P is zero), 1 / its sum of exp(z - that)
   const int32_t* labels;    // [M], may be null: class whose P is zero and is left out of the sums (the caller writes it)
   int label0;               // column 0's class
-  void *p, *pt;             // [M][ldp]; [N][ldpt], may be null; both up to the next 8 columns
-  int64_t ldp, ldpt;
+  void* p;                  // [M][ldp], written up to the next 8 columns
+  int64_t ldp;
   float* sums;              // [sum_parts(M, N)][N], may be null
-  // OUT
+  // DX and DW
   void* out;                // [M][ldo] of out_dtype, any alignment
   int64_t ldo;
   int out_dtype;
@@ -38,6 +41,8 @@ struct ClassProduct {
   int parts;                // of the contraction (1 where work is null)
   bool add;                 // to what work holds
 };
+// parts of a product's contraction that fill the chip: for PRODUCT_DX and PRODUCT_DW
+int class_parts(int dtype, int M, int N, int K);
 int stats_spans(int dtype, int M, int N);
 int sum_parts(int dtype, int M, int N);
 hipError_t launch_class_product(int dtype, int kind, const ClassProduct& g, hipStream_t s);
@@ -88,8 +93,8 @@ struct TargetFix {
   const float *zt, *p;
   const float2* norm;
   int first, columns;
-  void *P, *PT;             // PT may be null
-  int64_t ldp, ldpt;
+  void* P;
+  int64_t ldp;
   unsigned long long* fixed;      // [columns], may be null: what the targets add to the sums of P's columns, in units of 2^-40 ...
   float* sums;                    // ... and the sums, where that is NaN (the first part's)
 };
@@ -99,10 +104,8 @@ hipError_t launch_target_fix(const TargetFix& a, hipStream_t s);
 hipError_t launch_bias_gradient(const float* sums, int parts, const unsigned long long* fixed, int columns, const float* alpha, float* dbias, hipStream_t s);
 hipError_t launch_clear(unsigned long long* p, int n, hipStream_t s);
 
-// out[c][r] = in[r][c], zero from rows up to the next multiple of 8; rows that do not count by norm (which may be null) are zeros
-hipError_t launch_transpose(int dtype, const void* in, int64_t ldin, int rows, int cols, const float2* norm, void* out, int64_t ldo, hipStream_t s);
-// out[r][c] = in[r][c], zero from cols up to the next multiple of 8
-hipError_t launch_pad_rows(int dtype, const void* in, int64_t ldin, int rows, int cols, void* out, int64_t ldo, hipStream_t s);
+// out[r][c] = in[r][c], zero from cols up to the next multiple of 8; rows that do not count by norm (which may be null) are zeros
+hipError_t launch_pad_rows(int dtype, const void* in, int64_t ldin, int rows, int cols, const float2* norm, void* out, int64_t ldo, hipStream_t s);
 hipError_t launch_zero(int dtype, void* out, int64_t ldo, int rows, int cols, hipStream_t s);
 // out = alpha * sum over the parts, rounded to the type
 hipError_t launch_join_parts(int dtype, const float* work, int parts, int rows, int cols, const float* alpha, void* out, int64_t ldo, hipStream_t s);

@@ -167,10 +167,8 @@ __global__ __launch_bounds__(256) void target_fix_kernel(const TargetFix a) {
   const float d = a.zt[at] - norm.x, v = given > 0.5f ? expm1f(d + logf(norm.y)) + (1.0f - given) : expf(d) * norm.y - given;
   if (a.dtype == 1) {
     ((bf16*)a.P)[row * a.ldp + col] = (bf16)v;
-    if (a.PT) ((bf16*)a.PT)[col * a.ldpt + row] = (bf16)v;
   } else {
     ((float*)a.P)[row * a.ldp + col] = v;
-    if (a.PT) ((float*)a.PT)[col * a.ldpt + row] = v;
   }
   // (integers: the order of the additions does not matter.  One class: the column's sum has left the target out, otherwise it holds the probability.)
   if (a.fixed) {
@@ -193,34 +191,14 @@ __global__ __launch_bounds__(256) void clear_kernel(unsigned long long* p, int n
   if (i < n) p[i] = 0;
 }
 
-// 64 x 64 elements a workgroup, through LDS.
 template <typename T>
-__global__ __launch_bounds__(256) void transpose_kernel(const T* in, int64_t ldin, int rows, int cols, const float2* norm, T* out, int64_t ldo) {
-  __shared__ T tile[64][65];
-  const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64, t = threadIdx.x;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int r = r0 + i * 4 + (t >> 6), c = c0 + (t & 63);
-    T v = (T)0.0f;
-    if (r < rows && c < cols && !(norm && norm[r].x == INFINITY)) v = in[(int64_t)r * ldin + c];
-    tile[i * 4 + (t >> 6)][t & 63] = v;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int c = c0 + i * 4 + (t >> 6), r = r0 + (t & 63);
-    if (c < cols && r < ((rows + 7) & ~7)) out[(int64_t)c * ldo + r] = tile[t & 63][i * 4 + (t >> 6)];
-  }
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void pad_rows_kernel(const T* in, int64_t ldin, int rows, int cols, T* out, int64_t ldo) {
+__global__ __launch_bounds__(256) void pad_rows_kernel(const T* in, int64_t ldin, int rows, int cols, const float2* norm, T* out, int64_t ldo) {
   const int eights = (cols + 7) / 8;
   const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / eights;
   const int c = (int)(at % eights) * 8;
   if (row >= rows) return;
   float v[8];
-  load8(in + row * ldin + c, cols - c, v);
+  load8(in + row * ldin + c, norm && norm[row].x == INFINITY ? 0 : cols - c, v);
   store8(out + row * ldo + c, 8, v);
 }
 
@@ -291,17 +269,10 @@ hipError_t launch_zero(int dtype, void* out, int64_t ldo, int rows, int cols, hi
   return hipGetLastError();
 }
 
-hipError_t launch_transpose(int dtype, const void* in, int64_t ldin, int rows, int cols, const float2* norm, void* out, int64_t ldo, hipStream_t s) {
-  const dim3 grid(blocks(rows, 64), blocks(cols, 64));
-  if (dtype == 1) transpose_kernel<bf16><<<grid, 256, 0, s>>>((const bf16*)in, ldin, rows, cols, norm, (bf16*)out, ldo);
-  else transpose_kernel<float><<<grid, 256, 0, s>>>((const float*)in, ldin, rows, cols, norm, (float*)out, ldo);
-  return hipGetLastError();
-}
-
-hipError_t launch_pad_rows(int dtype, const void* in, int64_t ldin, int rows, int cols, void* out, int64_t ldo, hipStream_t s) {
+hipError_t launch_pad_rows(int dtype, const void* in, int64_t ldin, int rows, int cols, const float2* norm, void* out, int64_t ldo, hipStream_t s) {
   const unsigned n = blocks((int64_t)rows * ((cols + 7) / 8), 256);
-  if (dtype == 1) pad_rows_kernel<bf16><<<n, 256, 0, s>>>((const bf16*)in, ldin, rows, cols, (bf16*)out, ldo);
-  else pad_rows_kernel<float><<<n, 256, 0, s>>>((const float*)in, ldin, rows, cols, (float*)out, ldo);
+  if (dtype == 1) pad_rows_kernel<bf16><<<n, 256, 0, s>>>((const bf16*)in, ldin, rows, cols, norm, (bf16*)out, ldo);
+  else pad_rows_kernel<float><<<n, 256, 0, s>>>((const float*)in, ldin, rows, cols, norm, (float*)out, ldo);
   return hipGetLastError();
 }
 

@@ -2,7 +2,10 @@
 //
 //   STATS  z = (x W^T + b) / T, tile by tile; a row's largest z and sum of exp(z - largest) over each wavefront's columns leave the chip, nothing else
 //   PROB   z again, p = softmax(z) for a piece of the classes, row-major and transposed
-//   OUT    dx = P W (a long contraction, split over the chip where there are few tiles), dW = P^T x
+//   DX     P W, a contraction over the piece's classes, split over the chip where there are few tiles
+//   DW     P^T x, over the rows
+// W lies in DX, and both operands in DW, with a row for each step of the contraction: their tiles are read transposed from LDS, so that nothing has to be
+// written twice.
 //
 // Float32 operands go through the bf16 matrix unit, which does 16 times the float32 one's work: each value is the sum of three bf16 values (8 bits of its 24
 // each, exact above 2^-110), and of the nine products of two values' parts the six largest are added in float32; the three left out are below 2^-26 of the product,
@@ -61,20 +64,6 @@ __device__ __forceinline__ f32x4 mma(const Fragment<float>& b, const Fragment<fl
   return mfma(b.v[0], a.v[0], acc);
 }
 
-// 4x4 transpose across the 4 lanes of a quad: on return, lane i holds in v[j] what lane j held in v[i].
-__device__ __forceinline__ float quad_swap(float x, bool by_two) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, x);
-  return __builtin_bit_cast(float, by_two ? dpp<kSwap2>(u) : dpp<kSwap1>(u));
-}
-__device__ __forceinline__ void quad_transpose(f32x4& v, int lane) {
-  const bool b0 = lane & 1, b1 = lane & 2;
-  float r;
-  r = quad_swap(b0 ? v[0] : v[1], false); if (b0) v[0] = r; else v[1] = r;
-  r = quad_swap(b0 ? v[2] : v[3], false); if (b0) v[2] = r; else v[3] = r;
-  r = quad_swap(b1 ? v[0] : v[2], true);  if (b1) v[0] = r; else v[2] = r;
-  r = quad_swap(b1 ? v[1] : v[3], true);  if (b1) v[1] = r; else v[3] = r;
-}
-
 // Four consecutive elements, rounded to the type; `left` of them exist.
 __device__ __forceinline__ void store4(bf16* out, int left, const f32x4& v) {
   const bf16x4 o = {(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
@@ -105,7 +94,7 @@ __device__ __forceinline__ float fmax_of_rows(float x) {
 template <typename T, int KIND, int MI, int NI>
 __device__ __forceinline__ void finish(const ClassProduct& g, f32x4 (&acc)[MI][NI], int m0, int n0, int lane) {
   const int lgrp = lane >> 4, lrow = lane & 15;
-  if constexpr (KIND == PRODUCT_OUT) {
+  if constexpr (KIND >= PRODUCT_DX) {
     if (g.work) {
       const int64_t ldw = (g.N + 3) & ~3;
 #pragma unroll
@@ -169,7 +158,7 @@ __device__ __forceinline__ void finish(const ClassProduct& g, f32x4 (&acc)[MI][N
         if (lgrp == 0 && m < g.M) g.stats[(int64_t)span * g.M + m] = float2{most, sum};
       }
     } else {
-      const int last_n = (g.N + 7) & ~7, last_m = (g.M + 7) & ~7;
+      const int last_n = (g.N + 7) & ~7;
       float2 norm[MI];
       int label[MI];
 #pragma unroll
@@ -197,11 +186,6 @@ __device__ __forceinline__ void finish(const ClassProduct& g, f32x4 (&acc)[MI][N
             T* const to = (T*)g.p + (int64_t)m * g.ldp + n;
             store4(to, 4, p);
           }
-          if (g.pt) {
-            quad_transpose(p, lane);      // now 4 rows of column n + lane % 4
-            const int c = n + (lane & 3), r = m - (lane & 3);
-            if (c < g.N && r < last_m) store4((T*)g.pt + (int64_t)c * g.ldpt + r, 4, p);
-          }
         }
         if (g.sums) {
 #pragma unroll
@@ -225,46 +209,108 @@ __device__ __forceinline__ void tile_of(int tilesM, int tilesN, int& tm, int& tn
   tn = tid % width / rows;
 }
 
+// One operand of a tile in LDS: ROWS rows (columns of a matrix that lies the other way) by 128 bytes of the contraction.
+//   rows by contraction: a load of the workgroup fills 32 rows, lane l of wavefront w the 16-byte piece l % 8 of row 8 w + l / 8; piece c of a row sits at c ^ (row / 2
+//   mod 8), which spreads the 16 rows of a fragment over all LDS banks
+//   KM, the other way: BK rows of ROWS columns; piece c of row k sits at c ^ key(k), so that what half a wavefront reads of 8 rows (bf16, transposing reads) or a wavefront of 4
+//   (float32) lies on all banks.
+template <typename T, int ROWS, bool KM>
+struct Side {
+  static constexpr int ES = sizeof(T), BK = 128 / ES, LOADS = ROWS / 32, PIECES = ROWS * ES / 16;     // loads of a k-tile; KM: pieces of a row
+  __amdgpu_buffer_rsrc_t rsrc;
+  uint32_t voff[LOADS];
+  uint32_t step;            // bytes from a k-tile to the next
+  int k[LOADS], K;          // KM: rows of the loads in a k-tile, the contraction's length; otherwise k[0]: first byte of the piece, K: bytes
+  static __device__ __forceinline__ int key(int k) {
+    if constexpr (ES == 4) return ((k >> 2) & 3) << 2;
+    else if constexpr (PIECES >= 16) return ((k & 3) | ((k >> 1) & 4)) << 1;
+    else return (((k >> 1) & 1) | ((k >> 2) & 2)) << 1;
+  }
+  // rows (columns) [first, first + n) exist, n <= ROWS
+  __device__ __forceinline__ void init(const void* p, int64_t ld, int first, int n, int K_, int t) {
+    const int64_t bytes = ld * ES;
+    if constexpr (!KM) {
+      const int prow = t >> 3, chunk = (t & 7) ^ ((prow >> 1) & 7);
+      K = (K_ * ES + 15) & ~15;
+      rsrc = rsrc_of((const char*)p + first * bytes, (n - 1) * bytes + K);
+      k[0] = chunk * 16;
+      step = 128;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) voff[i] = prow + 32 * i < n ? (uint32_t)((prow + 32 * i) * bytes + chunk * 16) : kOutOfRange;
+    } else {
+      const int width = (n * ES + 15) & ~15;
+      K = K_;
+      rsrc = rsrc_of((const char*)p + (int64_t)first * ES, (K - 1) * bytes + width);
+      step = (uint32_t)(BK * bytes);
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        k[i] = (t + 256 * i) / PIECES;
+        const int c = (t % PIECES) ^ key(k[i]);
+        voff[i] = c * 16 < width ? (uint32_t)(k[i] * bytes + c * 16) : kOutOfRange;
+      }
+    }
+  }
+  __device__ __forceinline__ void load(unsigned char* to, int kt, bool in) const {
+    typedef __attribute__((address_space(3))) void* lds_ptr_t;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const bool exists = in && voff[i] != kOutOfRange && (KM ? kt * BK + k[i] < K : kt * 128 + k[0] < K);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr_t)(to + i * 4096), 16, exists ? voff[i] + (uint32_t)kt * step : kOutOfRange, 0, 0, 0);
+    }
+  }
+  // 32 bytes of the contraction for row (column) r0 + lane % 16, those that the other operand's fragment takes
+  __device__ __forceinline__ Fragment<T> fragment(const unsigned char* st, int r0, int lane) const {
+    const int lgrp = lane >> 4, lrow = lane & 15;
+    Fragment<T> f;
+    if constexpr (!KM) {
+      const unsigned char* const row = st + (r0 + lrow) * 128;
+      const int x0 = (lgrp ^ ((lane >> 1) & 7)) << 4;
+      f.set(*(const u32x4*)(row + x0), *(const u32x4*)(row + (x0 ^ 64)));
+    } else if constexpr (ES == 2) {
+      typedef __attribute__((ext_vector_type(4))) short i16x4;
+      typedef __attribute__((address_space(3))) i16x4* lds_i16x4;
+      const int row = lgrp * 8 + (lrow >> 2), c = (r0 >> 3) + ((lrow & 3) >> 1);
+      const unsigned char* const at = st + row * (ROWS * 2) + ((c ^ key(row)) << 4) + (lrow & 1) * 8;
+      u32x2 v[4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) v[h] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(at + ((h >> 1) * 32 + (h & 1) * 4) * (ROWS * 2))));
+      f.set(u32x4{v[0][0], v[0][1], v[1][0], v[1][1]}, u32x4{v[2][0], v[2][1], v[3][0], v[3][1]});
+    } else {
+      const int c = (r0 + lrow) >> 2;
+      u32x4 v[2];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int row = (e >> 2) * 16 + lgrp * 4 + (e & 3);
+        v[e >> 2][e & 3] = *(const uint32_t*)(st + row * (ROWS * 4) + ((c ^ key(row)) << 4) + (lrow & 3) * 4);
+      }
+      f.set(v[0], v[1]);
+    }
+    return f;
+  }
+};
+
 // BM x BN tile, 4 wavefronts in a 2 x 2 grid, NS LDS stages of a k-tile of 128 bytes each, one barrier a k-tile.  blockIdx.y: part of the contraction, kper
 // k-tiles long.
 template <typename T, int KIND, int BM, int BN, int NS>
 __global__ __launch_bounds__(256) void class_tile_kernel(const ClassProduct g, int kper) {
 #if defined(__HIP_DEVICE_COMPILE__)
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  constexpr int ES = sizeof(T), BK = 128 / ES, CH = 16 / ES;
-  constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128;
-  constexpr int LA = BM / 32, LB = BN / 32, NLD = LA + LB, MI = BM / 32, NI = BN / 32;
+  constexpr int BK = 128 / (int)sizeof(T), A_BYTES = BM * 128, STAGE = (BM + BN) * 128, NLD = (BM + BN) / 32, MI = BM / 32, NI = BN / 32;
   int tm, tn;
   tile_of((g.M + BM - 1) / BM, (g.N + BN - 1) / BN, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6, wm = w & 1, wn = w >> 1, lgrp = lane >> 4, lrow = lane & 15;
-  const int64_t lda = g.lda * ES, ldb = g.ldb * ES;
-  const int nk = (g.K + BK - 1) / BK, Kr = (g.K + CH - 1) / CH * 16;       // bytes of a row, to the end of its last 16
-  const int k0 = blockIdx.y * kper, k1 = k0 + kper < nk ? k0 + kper : nk;
-  const int ra = g.M - m0 < BM ? g.M - m0 : BM, rb = g.N - n0 < BN ? g.N - n0 : BN;        // rows of the tile that exist
-  const __amdgpu_buffer_rsrc_t rsrcA = rsrc_of((const char*)g.a + (int64_t)m0 * lda, (ra - 1) * lda + Kr);
-  const __amdgpu_buffer_rsrc_t rsrcB = rsrc_of((const char*)g.b + (int64_t)n0 * ldb, (rb - 1) * ldb + Kr);
-  // a load of the workgroup fills 32 rows, lane l of wavefront w the 16-byte piece l % 8 of row 8 w + l / 8; piece c of a row is chunk
-  // c ^ (row / 2 mod 8), which spreads the 16 rows of a fragment over all LDS banks
-  const int prow = w * 8 + (lane >> 3), chunk = (lane & 7) ^ ((prow >> 1) & 7);
-  uint32_t voff[NLD];
-#pragma unroll
-  for (int i = 0; i < LA; ++i) voff[i] = prow + 32 * i < ra ? (uint32_t)((prow + 32 * i) * lda + chunk * 16) : kOutOfRange;
-#pragma unroll
-  for (int i = 0; i < LB; ++i) voff[LA + i] = prow + 32 * i < rb ? (uint32_t)((prow + 32 * i) * ldb + chunk * 16) : kOutOfRange;
-  typedef __attribute__((address_space(3))) void* lds_ptr_t;
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, wm = w & 1, wn = w >> 1;
+  const int nk = (g.K + BK - 1) / BK, k0 = blockIdx.y * kper, k1 = k0 + kper < nk ? k0 + kper : nk;
+  Side<T, BM, KIND == PRODUCT_DW> A;
+  Side<T, BN, KIND >= PRODUCT_DX> B;
+  A.init(g.a, g.lda, m0, g.M - m0 < BM ? g.M - m0 : BM, g.K, t);
+  B.init(g.b, g.ldb, n0, g.N - n0 < BN ? g.N - n0 : BN, g.K, t);
   const int lds_wave = __builtin_amdgcn_readfirstlane(w * 1024);
   auto load = [&](int kt, int stage) {
-    unsigned char* const st = smem + stage * STAGE;
-    const bool in = kt < k1 && kt * 128 + chunk * 16 < Kr;
-    const uint32_t koff = (uint32_t)kt * 128u;
-#pragma unroll
-    for (int i = 0; i < NLD; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(i < LA ? rsrcA : rsrcB, (lds_ptr_t)(st + lds_wave + i * 4096), 16,
-                                               in && voff[i] != kOutOfRange ? voff[i] + koff : kOutOfRange, 0, 0, 0);
+    unsigned char* const st = smem + stage * STAGE + lds_wave;
+    A.load(st, kt, kt < k1);
+    B.load(st + A_BYTES, kt, kt < k1);
   };
-  const uint32_t fragA = (uint32_t)((wm * (BM / 2) + lrow) * 128), fragB = (uint32_t)(A_BYTES + (wn * (BN / 2) + lrow) * 128);
-  const uint32_t x0 = (uint32_t)((lgrp ^ ((lane >> 1) & 7)) << 4), x1 = x0 ^ 64;
   f32x4 acc[MI][NI];
 #pragma unroll
   for (int i = 0; i < MI; ++i)
@@ -282,9 +328,9 @@ __global__ __launch_bounds__(256) void class_tile_kernel(const ClassProduct g, i
     const unsigned char* const st = smem + (kt - k0) % NS * STAGE;
     Fragment<T> a[MI], b[NI];
 #pragma unroll
-    for (int j = 0; j < NI; ++j) b[j].set(*(const u32x4*)(st + fragB + j * 2048 + x0), *(const u32x4*)(st + fragB + j * 2048 + x1));
+    for (int j = 0; j < NI; ++j) b[j] = B.fragment(st + A_BYTES, wn * (BN / 2) + 16 * j, lane);
 #pragma unroll
-    for (int i = 0; i < MI; ++i) a[i].set(*(const u32x4*)(st + fragA + i * 2048 + x0), *(const u32x4*)(st + fragA + i * 2048 + x1));
+    for (int i = 0; i < MI; ++i) a[i] = A.fragment(st, wm * (BM / 2) + 16 * i, lane);
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -295,15 +341,11 @@ __global__ __launch_bounds__(256) void class_tile_kernel(const ClassProduct g, i
 #endif
 }
 
-// Large bf16 products (long_tile.h).  What the epilogues of the tiles above do, with the accumulators taken out of the AGPRs a block at a time, and stores of whole
-// row segments: a wavefront stages its 128 x 128 outputs in a 32 KB of the stages that is its own, rows of 256 bytes whose 16-byte piece c sits at c ^ swz(row), and takes
-// them out row by row and, through transposing LDS reads (a group of 16 lanes reads 4 rows of 16 columns, lane l gets the 4 values of column l), column by column.
-// 16 rows in a row lie on 16 pieces, the 8 rows that half a wavefront reads transposed on disjoint ones.
+// Large bf16 products (long_tile.h).  What the epilogues of the tiles above do, with the accumulators taken out of the AGPRs a block at a time; bf16 outputs leave as whole
+// row segments, staged by each wavefront in a 32 KB of the stages that is its own, rows of 256 bytes whose 16-byte piece c sits at c ^ (row mod 16).
 template <int KIND>
 __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, int kper) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  typedef __attribute__((ext_vector_type(4))) short i16x4;
-  typedef __attribute__((address_space(3))) i16x4* lds_i16x4;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   int tm, tn;
   big_tile(g.M, g.N, tm, tn);
@@ -313,7 +355,8 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
     const int64_t lda = g.lda * 2, ldb = g.ldb * 2, from = (int64_t)blockIdx.y * kper * 128, all = (int64_t)g.K * 2 - from, part = (int64_t)kper * 128;
     const int K = all <= 0 ? 0 : (int)(all < part ? all : part);
     const int64_t at = all <= 0 ? 0 : from;
-    long_tile<f32x4, false>(acc, smem, (const char*)g.a + m0 * lda + at, (const char*)g.b + n0 * ldb + at, lda, ldb, g.M - m0 < 256 ? g.M - m0 : 256, g.N - n0 < 256 ? g.N - n0 : 256, K);
+    constexpr bool KMA = KIND == PRODUCT_DW, KMB = KIND >= PRODUCT_DX;
+    long_tile<f32x4, false, KMA, KMB>(acc, smem, (const char*)g.a + (KMA ? at / 2 * lda + m0 * 2 : m0 * lda + at), (const char*)g.b + (KMB ? at / 2 * ldb + n0 * 2 : n0 * ldb + at), lda, ldb, g.M - m0 < 256 ? g.M - m0 : 256, g.N - n0 < 256 ? g.N - n0 : 256, K);
   }
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, wm = w & 1, wn = w >> 1, lgrp = lane >> 4, lrow = lane & 15;
   const int rowW = m0 + wm * 128, colW = n0 + wn * 128;
@@ -355,11 +398,10 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
     }
     return;
   }
-  auto swz = [](int r) { return ((r & 3) << 1) | (r & 8) | ((r >> 2) & 1); };
   __syncthreads();                       // nobody reads the stages any more
   unsigned char* const st = smem + w * 32768;
   unsigned char* const wbase = st + lrow * 256 + (lgrp & 1) * 8;
-  const int wsw = (lgrp >> 1) ^ swz(lrow);
+  const int wsw = (lgrp >> 1) ^ lrow;
   auto stage = [&](int i, int j, const f32x4& v) {
     const bf16x4 o = {(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
     *(u32x2*)(wbase + i * 4096 + ((wsw ^ (2 * j)) << 4)) = __builtin_bit_cast(u32x2, o);
@@ -373,13 +415,13 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
         const int r = (8 * b + q) * 4 + r0;
-        val[q] = *(const u32x4*)(st + r * 256 + ((c ^ swz(r & 15)) << 4));
+        val[q] = *(const u32x4*)(st + r * 256 + ((c ^ (r & 15)) << 4));
       }
 #pragma unroll
       for (int q = 0; q < 8; ++q) put((8 * b + q) * 4 + r0, c * 8, val[q]);
     }
   };
-  if constexpr (KIND == PRODUCT_OUT) {
+  if constexpr (KIND >= PRODUCT_DX) {
     const float alpha = g.work ? 1.0f : *g.alpha;
     if (g.work || g.out_dtype == 0) {    // float32, straight from the accumulators: 64-byte segments
       const int64_t ld = g.work ? (g.N + 3) & ~3 : g.ldo;
@@ -464,25 +506,6 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
     rows_out([&](int r, int c, const u32x4& v) {
       if (rowW + r < g.M && colW + c < g.N) *(u32x4*)((bf16*)g.p + (int64_t)(rowW + r) * g.ldp + colW + c) = v;
     });
-    if (g.pt) {
-      const int gq = lane >> 4, jj = lane & 15, r0 = gq * 8 + (jj >> 2);        // staged row of the first of the two reads
-      const uint32_t base = (uint32_t)(r0 * 256 + ((((jj & 3) >> 1) ^ swz(r0 & 15)) << 4) + (jj & 1) * 8);
-#pragma unroll
-      for (int b = 0; b < 8; b += 2) {
-        u32x2 val[8][2];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          const uint32_t o1 = (base ^ ((b + q / 4) << 5)) + q % 4 * 8192;
-          val[q][0] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(st + o1)));
-          val[q][1] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(st + ((o1 ^ 16) + 1024))));
-        }
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          const int n = colW + jj + (b + q / 4) * 16, m = rowW + gq * 8 + q % 4 * 32;
-          if (n < g.N && m < g.M) *(u32x4*)((bf16*)g.pt + (int64_t)n * g.ldpt + m) = u32x4{val[q][0][0], val[q][0][1], val[q][1][0], val[q][1][1]};
-        }
-      }
-    }
   }
 #endif
 }
@@ -491,9 +514,10 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
 int64_t tiles_of(int M, int N, int BM, int BN) { return (int64_t)((M + BM - 1) / BM) * ((N + BN - 1) / BN); }
 
 enum Shape { kLong, k128, k64 };
-Shape shape_of(int dtype, int M, int N) {
-  if (dtype == 1 && tiles_of(M, N, 256, 256) >= 200) return kLong;
-  return tiles_of(M, N, 128, 128) >= 200 ? k128 : k64;
+// parts: of the contraction, which share the chip
+Shape shape_of(int dtype, int M, int N, int parts = 1) {
+  if (dtype == 1 && tiles_of(M, N, 256, 256) * parts >= 200) return kLong;
+  return tiles_of(M, N, 128, 128) * parts >= 200 ? k128 : k64;
 }
 // Rows, or columns, of a wavefront's part of a tile.
 int span_of(Shape s) { return s == kLong ? 128 : s == k128 ? 64 : 32; }
@@ -520,7 +544,7 @@ hipError_t launch_long(const ClassProduct& g, hipStream_t s) {
 }
 template <typename T, int KIND>
 hipError_t launch_kind(int dtype, const ClassProduct& g, hipStream_t s) {
-  switch (shape_of(dtype, g.M, g.N)) {
+  switch (shape_of(dtype, g.M, g.N, g.work ? g.parts : 1)) {
     case kLong:
       if constexpr (sizeof(T) == 2) return launch_long<KIND>(g, s);
     case k128: return launch_tile<T, KIND, 128, 128, 2>(g, s);
@@ -532,11 +556,27 @@ hipError_t launch_type(int dtype, int kind, const ClassProduct& g, hipStream_t s
   switch (kind) {
     case PRODUCT_STATS: return launch_kind<T, PRODUCT_STATS>(dtype, g, s);
     case PRODUCT_PROB: return launch_kind<T, PRODUCT_PROB>(dtype, g, s);
-    default: return launch_kind<T, PRODUCT_OUT>(dtype, g, s);
+    case PRODUCT_DX: return launch_kind<T, PRODUCT_DX>(dtype, g, s);
+    default: return launch_kind<T, PRODUCT_DW>(dtype, g, s);
   }
 }
 
 }  // namespace
+
+// As many parts as make one round of the largest tiles that then have 16 k-tiles each.
+int class_parts(int dtype, int M, int N, int K) {
+  const int64_t nk = (K + (dtype == 1 ? 63 : 31)) / (dtype == 1 ? 64 : 32);
+  auto parts = [&](int tile, int round, int least) {
+    const int64_t want = round / tiles_of(M, N, tile, tile), most = nk / least;
+    return (int)(want < most ? want : most);
+  };
+  if (dtype == 1 && tiles_of(M, N, 256, 256) * (nk / 16) >= 200) {
+    const int p = parts(256, 256, 16);
+    return p < 1 ? 1 : p;
+  }
+  const int p = tiles_of(M, N, 128, 128) * (nk / 8) >= 200 ? parts(128, 512, 8) : parts(64, 512, 4);
+  return p < 1 ? 1 : p;
+}
 
 int stats_spans(int dtype, int M, int N) {
   const int w = span_of(shape_of(dtype, M, N));
@@ -549,8 +589,9 @@ int sum_parts(int dtype, int M, int N) {
 
 hipError_t launch_class_product(int dtype, int kind, const ClassProduct& g, hipStream_t s) {
   const int64_t es = dtype == 1 ? 2 : 4;
-  // a tile's rows are addressed with 32-bit offsets
-  if (g.M <= 0 || g.N <= 0 || g.K <= 0 || 256 * g.lda * es >= 0x7FFFFF00 || 256 * g.ldb * es >= 0x7FFFFF00) return hipErrorInvalidValue;
+  // a tile's rows, or an operand that lies the other way, are addressed with 32-bit offsets
+  const int64_t rows_a = kind == PRODUCT_DW ? g.K : 256, rows_b = kind >= PRODUCT_DX ? g.K : 256;
+  if (g.M <= 0 || g.N <= 0 || g.K <= 0 || rows_a * g.lda * es >= 0x7FFFFF00 || rows_b * g.ldb * es >= 0x7FFFFF00) return hipErrorInvalidValue;
   if ((((uintptr_t)g.a | (uintptr_t)g.b) & 15) || g.lda * es % 16 || g.ldb * es % 16) return hipErrorInvalidValue;
   return dtype == 1 ? launch_type<bf16>(dtype, kind, g, s) : launch_type<float>(dtype, kind, g, s);
 }

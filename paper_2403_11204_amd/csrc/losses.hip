@@ -10,10 +10,11 @@ using namespace slp;
 namespace {
 
 constexpr int kMaxRows = 1 << 20, kMaxDim = 1 << 20, kMaxTop = 1024;
-// P of a piece of the classes takes this much at most, its transpose as much again.
+// P of a piece of the classes takes this much at most.
 constexpr int64_t kPieceBytes = 256 << 20;
 // A tile of 256 rows is addressed with 32-bit offsets: rows of x, W and P lie at most this many elements apart.
 constexpr int kMaxPiece = 1 << 20;
+constexpr int64_t kAcross = 0x7FFFFF00;
 // Grids have fewer than 2^32 threads.
 constexpr int64_t kMaxWeights = (int64_t)1 << 33, kMaxLogits = (int64_t)1 << 36, kMaxTargets = (int64_t)1 << 25;
 
@@ -44,20 +45,12 @@ struct Call {
 
 // Where everything lies in the workspace, and in which pieces the classes are taken.
 struct Plan {
-  int64_t es, ldk, ldp, ldr;            // operands' element size; leading dimensions of copies of x and W, of P and W^T, of P^T and x^T
+  int64_t es, ldk, ldp;                 // operands' element size; leading dimensions of copies of x and W, of P
   bool copy_x, copy_w;
   int piece;                            // classes
   int dx_parts, dw_parts, spans;
-  size_t zt, p, labels, norm, alpha, stats, xc, wc, xt, wt, P, PT, dx_work, dw_work, sums, fixed, bytes;
+  size_t zt, p, labels, norm, alpha, stats, xc, wc, xz, P, dx_work, dw_work, sums, fixed, bytes;
 };
-
-int parts_of(int dt, int M, int N, int K) {
-  const int64_t tiles = (int64_t)((M + 63) / 64) * ((N + 63) / 64);
-  const int nk = (K + (dt == SLP_BF16 ? 63 : 31)) / (dt == SLP_BF16 ? 64 : 32);
-  const int64_t want = 512 / tiles, most = nk / 4;
-  const int64_t parts = want < most ? want : most;
-  return parts < 1 ? 1 : (int)parts;
-}
 
 // Whether the products can read a matrix in place.
 bool in_place(const void* p, int64_t ld, int rows, int dim, int64_t es) { return !off(p, 16) && (rows == 1 || ld * es % 16 == 0) && dim * es % 16 == 0; }
@@ -72,13 +65,15 @@ Plan plan_of(const Call& c) {
   int64_t most = kPieceBytes / ((int64_t)c.rows * a.es) / 256 * 256;
   if (most < 256) most = 256;
   if (most > kMaxPiece) most = kMaxPiece;
+  // W's piece and x are addressed with 32-bit offsets where they lie the other way (see class_loss.h)
+  const int64_t across = kAcross / ((a.copy_w ? a.ldk : c.ldw) * a.es) / 256 * 256;
+  if (c.classes > 1 && most > across) most = across;
   const int wanted = (int)((c.classes + most - 1) / most);
   a.piece = wanted == 1 ? c.classes : ((c.classes + wanted - 1) / wanted + 255) / 256 * 256;
   const int pieces = (c.classes + a.piece - 1) / a.piece;
   a.ldp = row_ld(a.piece, a.es);
-  a.ldr = row_ld(c.rows, a.es);
-  a.dx_parts = parts_of(c.dt, c.rows, c.dim, a.piece);
-  a.dw_parts = parts_of(c.dt, a.piece, c.dim, c.rows);
+  a.dx_parts = class_parts(c.dt, c.rows, c.dim, a.piece);
+  a.dw_parts = class_parts(c.dt, a.piece, c.dim, c.rows);
   for (int first = 0; first < c.classes; first += a.copy_w ? a.piece : c.classes)
     a.spans += stats_spans(c.dt, c.rows, a.copy_w && c.classes - first > a.piece ? a.piece : c.classes - first);
   size_t at = 0;
@@ -87,7 +82,7 @@ Plan plan_of(const Call& c) {
     if (wanted) at += ((size_t)bytes + 255) & ~(size_t)255;
     return here;
   };
-  const int64_t targets = (int64_t)c.rows * c.t.k, r = c.rows, d = c.dim, dq = (c.dim + 3) / 4 * 4;
+  const int64_t targets = (int64_t)c.rows * c.t.k, r = c.rows, dq = (c.dim + 3) / 4 * 4;
   a.zt = take(true, targets * 4);
   a.p = take(c.t.top, targets * 4);
   a.labels = take(!c.t.top, r * 4);
@@ -96,10 +91,8 @@ Plan plan_of(const Call& c) {
   a.stats = take(true, (int64_t)a.spans * r * 8);
   a.xc = take(a.copy_x, r * a.ldk * a.es);
   a.wc = take(a.copy_w, (int64_t)a.piece * a.ldk * a.es);
-  a.xt = take(c.dw, d * a.ldr * a.es);
-  a.wt = take(c.dx, d * a.ldp * a.es);
+  a.xz = take(c.dw, r * a.ldk * a.es);
   a.P = take(grads, r * a.ldp * a.es);
-  a.PT = take(c.dw, (int64_t)a.piece * a.ldr * a.es);
   a.dx_work = take(c.dx && (pieces > 1 || a.dx_parts > 1), (int64_t)a.dx_parts * r * dq * 4);
   a.dw_work = take(c.dw && a.dw_parts > 1, (int64_t)a.dw_parts * a.piece * dq * 4);
   const int64_t rest = c.classes - (int64_t)(pieces - 1) * a.piece, most_sums = (int64_t)sum_parts(c.dt, c.rows, a.piece) * a.piece;
@@ -122,7 +115,7 @@ int run(const Call& c, void* workspace, hipStream_t s) {
   const void* x = c.x;
   int64_t ldx = c.rows == 1 ? a.ldk : c.ldx;       // (a single row may have any)
   if (a.copy_x) {
-    HIP_TRY(launch_pad_rows(c.dt, c.x, c.ldx, c.rows, c.dim, at(a.xc), a.ldk, s));
+    HIP_TRY(launch_pad_rows(c.dt, c.x, c.ldx, c.rows, c.dim, nullptr, at(a.xc), a.ldk, s));
     x = at(a.xc);
     ldx = a.ldk;
   }
@@ -131,7 +124,7 @@ int run(const Call& c, void* workspace, hipStream_t s) {
     w = (const char*)c.w + (int64_t)first * c.ldw * a.es;
     ldw = c.classes == 1 ? a.ldk : c.ldw;
     if (a.copy_w) {
-      HIP_TRY(launch_pad_rows(c.dt, w, c.ldw, columns, c.dim, at(a.wc), a.ldk, s));
+      HIP_TRY(launch_pad_rows(c.dt, w, c.ldw, columns, c.dim, nullptr, at(a.wc), a.ldk, s));
       w = at(a.wc);
       ldw = a.ldk;
     }
@@ -160,7 +153,8 @@ int run(const Call& c, void* workspace, hipStream_t s) {
   HIP_TRY(launch_mean(c.losses, norm, c.rows, c.scale * c.temperature, c.loss, alpha, s));
   if (!grads) return SLP_OK;
 
-  if (c.dw) HIP_TRY(launch_transpose(c.dt, x, ldx, c.rows, c.dim, norm, at(a.xt), a.ldr, s));
+  // the rows that count: 0 times what others hold may be NaN
+  if (c.dw) HIP_TRY(launch_pad_rows(c.dt, c.x, c.ldx, c.rows, c.dim, norm, at(a.xz), a.ldk, s));
   for (int first = 0; first < c.classes; first += a.piece) {
     const int columns = c.classes - first < a.piece ? c.classes - first : a.piece;
     const bool last = first + columns == c.classes;
@@ -180,22 +174,19 @@ int run(const Call& c, void* workspace, hipStream_t s) {
     g.label0 = first;
     g.p = at(a.P);
     g.ldp = a.ldp;
-    g.pt = c.dw ? at(a.PT) : nullptr;
-    g.ldpt = a.ldr;
     g.sums = c.dbias ? (float*)at(a.sums) : nullptr;
     g.parts = 1;
     HIP_TRY(launch_class_product(c.dt, PRODUCT_PROB, g, s));
     unsigned long long* const fixed = c.dbias ? (unsigned long long*)at(a.fixed) : nullptr;
     if (fixed) HIP_TRY(launch_clear(fixed, columns, s));
-    HIP_TRY(launch_target_fix(TargetFix{c.t, c.rows, c.classes, c.dt, zt, p, norm, first, columns, g.p, g.pt, a.ldp, a.ldr, fixed, g.sums}, s));
+    HIP_TRY(launch_target_fix(TargetFix{c.t, c.rows, c.classes, c.dt, zt, p, norm, first, columns, g.p, a.ldp, fixed, g.sums}, s));
     if (c.dbias) HIP_TRY(launch_bias_gradient(g.sums, sum_parts(c.dt, c.rows, columns), fixed, columns, alpha, c.dbias + first, s));
     if (c.dx) {
-      HIP_TRY(launch_transpose(c.dt, w, ldw, columns, c.dim, nullptr, at(a.wt), a.ldp, s));
       ClassProduct o{};
       o.a = at(a.P);
       o.lda = a.ldp;
-      o.b = at(a.wt);
-      o.ldb = a.ldp;
+      o.b = w;
+      o.ldb = ldw;
       o.M = c.rows;
       o.N = c.dim;
       o.K = columns;
@@ -209,16 +200,16 @@ int run(const Call& c, void* workspace, hipStream_t s) {
         o.ldo = c.lddx;
         o.out_dtype = c.dt;
       }
-      HIP_TRY(launch_class_product(c.dt, PRODUCT_OUT, o, s));
+      HIP_TRY(launch_class_product(c.dt, PRODUCT_DX, o, s));
       if (o.work && last) HIP_TRY(launch_join_parts(c.dt, o.work, o.parts, c.rows, c.dim, alpha, c.dx, c.lddx, s));
     }
     if (c.dw) {
       char* const dw = (char*)c.dw + (int64_t)first * c.lddw * (int64_t)size_of(c.dw_dt);
       ClassProduct o{};
-      o.a = at(a.PT);
-      o.lda = a.ldr;
-      o.b = at(a.xt);
-      o.ldb = a.ldr;
+      o.a = at(a.P);
+      o.lda = a.ldp;
+      o.b = at(a.xz);
+      o.ldb = a.ldk;
       o.M = columns;
       o.N = c.dim;
       o.K = c.rows;
@@ -231,7 +222,7 @@ int run(const Call& c, void* workspace, hipStream_t s) {
         o.ldo = c.lddw;
         o.out_dtype = c.dw_dt;
       }
-      HIP_TRY(launch_class_product(c.dt, PRODUCT_OUT, o, s));
+      HIP_TRY(launch_class_product(c.dt, PRODUCT_DW, o, s));
       if (o.work) HIP_TRY(launch_join_parts(c.dw_dt, o.work, o.parts, columns, c.dim, alpha, dw, c.lddw, s));
     }
   }
@@ -255,6 +246,7 @@ int check_call(const char* who, const Call& c) {
   SLP_CHECK(check_dense(who, "x", c.x, c.ldx, c.dim, c.dt));
   SLP_CHECK(check_dense(who, "w", c.w, c.ldw, c.dim, c.dt));
   if (c.dx) SLP_CHECK(check_dense(who, "dx", c.dx, c.lddx, c.dim, c.dt));
+  if (c.dw && c.rows * row_ld(c.dim, (int64_t)size_of(c.dt)) * (int64_t)size_of(c.dt) >= kAcross) return fail(SLP_ERR_SHAPE, "%s: %d rows of %d come to 2 GiB", who, c.rows, c.dim);
   if ((c.rows > 1 && c.ldx > kMaxPiece) || (c.classes > 1 && c.ldw > kMaxPiece)) return fail(SLP_ERR_SHAPE, "%s: rows of x and w lie at most %d elements apart", who, kMaxPiece);
   if (off(c.t.ids, c.t.ids64 ? 8 : 4)) return fail(SLP_ERR_ALLOC, "%s: class ids are not on an element's boundary", who);
   return SLP_OK;
