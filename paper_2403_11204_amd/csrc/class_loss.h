@@ -26,6 +26,9 @@ struct ClassProduct {
   const float* bias;        // [N], may be null
   float per_t;
   float2* stats;            // [stats_spans(M, N)][M]: (largest, sum)
+  float* z;                 // [M][ldz], may be null: z itself of the first zcols columns
+  int64_t ldz;
+  int zcols;
   const float2* norm;       // [M]: the row's largest z (+infinity: the row does not count, its P is zero), 1 / its sum of exp(z - that)
   const int32_t* labels;    // [M], may be null: class whose P is zero and is left out of the sums (the caller writes it)
   int label0;               // column 0's class
@@ -58,12 +61,12 @@ struct Targets {
   int k;
   float per_t;              // 1 / temperature
 };
-// zt[row][j] = (x[row] . w[ids[row][j]] + bias) per_t; 0 where the id is none
+// zt[row][j] = (x[row] . w[ids[row][j]] + bias) per_t, for classes from `kept` on (the others' logits are kept)
 struct TargetLogits {
   const void *x, *w;
   int64_t ldx, ldw;
   const float* bias;
-  int rows, classes, dim;
+  int rows, classes, dim, kept;
   Targets t;
   float* zt;                // [rows][k]
 };
@@ -75,16 +78,33 @@ struct RowLoss {
   int spans;
   int rows, classes;
   Targets t;
-  const float* zt;
+  const float* z;           // [rows][ldz]: the logits of classes below `kept`
+  int64_t ldz;
+  int kept;
+  float* zt;                // [rows][k]: of the others; written where kept
   float square_t;           // temperature squared
   float *lse, *losses;      // [rows]
   float2* norm;             // [rows]: see ClassProduct
-  float* p;                 // [rows][k], may be null where t.top is: the teacher's probabilities, 0 for entries that do not count
+  float* p;                 // [rows][k], may be null where t.top is: the teacher's probabilities, of all the row's entries of that class
+                            // together at the first of them, -1 at the others; 0 where none counts
   int32_t* labels;          // [rows], may be null: the row's class or -1
 };
 hipError_t launch_row_loss(const RowLoss& a, hipStream_t s);
-// *loss = mean of the rows that count (0 where none does), *alpha = scale / their number (0)
-hipError_t launch_mean(const float* losses, const float2* norm, int rows, float scale, float* loss, float* alpha, hipStream_t s);
+// What follows from all rows: *loss = mean of those that count (0 where none does), *alpha = scale / their number (0); xz = the rows of x, zeros for those that do not
+// count and up to the next multiple of 8 columns (may be null); fixed[0 .. classes) = 0 (may be null)
+struct AllRows {
+  const float* losses;
+  const float2* norm;
+  int rows, classes, dim;
+  float scale;
+  float *loss, *alpha;
+  const void* x;
+  int64_t ldx;
+  void* xz;
+  int64_t ldxz;
+  unsigned long long* fixed;
+};
+hipError_t launch_all_rows(int dtype, const AllRows& a, hipStream_t s);
 
 // P at the targets: softmax - (the probability of all the row's entries of that class), in classes [first, first + columns)
 struct TargetFix {
@@ -96,16 +116,18 @@ struct TargetFix {
   void* P;
   int64_t ldp;
   unsigned long long* fixed;      // [columns], may be null: what the targets add to the sums of P's columns, in units of 2^-40 ...
-  float* sums;                    // ... and the sums, where that is NaN (the first part's)
+  float* sums;                    // ... and the sums, where that is NaN
 };
 hipError_t launch_target_fix(const TargetFix& a, hipStream_t s);
+// P of a piece whose logits are kept, targets and all: rows [rows][ldz] of z from the piece's first class on; sums: as PRODUCT_PROB's, kept_sum_parts(rows) of them
+hipError_t launch_kept_prob(const TargetFix& a, const float* z, int64_t ldz, const int32_t* labels, hipStream_t s);
+int kept_sum_parts(int rows);
 
 // dbias[c] = alpha (sum over the parts of sums[part][c] + fixed[c] 2^-40)
 hipError_t launch_bias_gradient(const float* sums, int parts, const unsigned long long* fixed, int columns, const float* alpha, float* dbias, hipStream_t s);
-hipError_t launch_clear(unsigned long long* p, int n, hipStream_t s);
 
-// out[r][c] = in[r][c], zero from cols up to the next multiple of 8; rows that do not count by norm (which may be null) are zeros
-hipError_t launch_pad_rows(int dtype, const void* in, int64_t ldin, int rows, int cols, const float2* norm, void* out, int64_t ldo, hipStream_t s);
+// out[r][c] = in[r][c], zero from cols up to the next multiple of 8
+hipError_t launch_pad_rows(int dtype, const void* in, int64_t ldin, int rows, int cols, void* out, int64_t ldo, hipStream_t s);
 hipError_t launch_zero(int dtype, void* out, int64_t ldo, int rows, int cols, hipStream_t s);
 // out = alpha * sum over the parts, rounded to the type
 hipError_t launch_join_parts(int dtype, const float* work, int parts, int rows, int cols, const float* alpha, void* out, int64_t ldo, hipStream_t s);

@@ -35,10 +35,7 @@ __global__ __launch_bounds__(256) void target_logits_kernel(const TargetLogits a
   if (at >= (int64_t)a.rows * a.t.k) return;
   const int64_t row = at / a.t.k;
   const int c = class_of(a.t, row, (int)(at % a.t.k), a.classes);
-  if (c < 0) {
-    if (lane == 0) a.zt[at] = 0.0f;
-    return;
-  }
+  if (c < a.kept) return;                // (none, or kept)
   const T* const x = (const T*)a.x + row * a.ldx;
   const T* const w = (const T*)a.w + (int64_t)c * a.ldw;
   float sum = 0.0f;
@@ -59,57 +56,95 @@ __device__ __forceinline__ float2 joined(float2 a, float2 b) {
   return float2{most, (a.x == most ? a.y : a.y * expf(a.x - most)) + (b.x == most ? b.y : b.y * expf(b.x - most))};
 }
 
-// 16 rows a workgroup, 16 threads each.
+// TEAM threads a row: 16, or all 256 of a workgroup where there are few rows (1 x 131072 classes, 1024 spans: 35 us on 16 threads).
+template <int TEAM>
 __global__ __launch_bounds__(256) void row_loss_kernel(const RowLoss a) {
-  __shared__ float2 part[16][16];
-  const int r = threadIdx.x & 15, s = threadIdx.x >> 4;
-  const int64_t row = (int64_t)blockIdx.x * 16 + r;
+  constexpr int ROWS = 256 / TEAM;
+  __shared__ float2 part[TEAM][ROWS];
+  extern __shared__ float2 entries[];          // of a distillation: class and probability of each row's entries
+  const int r = threadIdx.x % ROWS, s = threadIdx.x / ROWS;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + r;
   const bool in = row < a.rows;
-  auto all = [&](float2 mine) {           // of the row's 16 threads, in their order
+  // of the row's threads, halves of them at a time: the same order every time
+  auto all = [&](float2 mine) {
     __syncthreads();
     part[s][r] = mine;
+    for (int step = TEAM / 2; step > 0; step >>= 1) {
+      __syncthreads();
+      if (s < step) part[s][r] = joined(part[s][r], part[s + step][r]);
+    }
     __syncthreads();
-    float2 sum = part[0][r];
-    for (int i = 1; i < 16; ++i) sum = joined(sum, part[i][r]);
-    return sum;
+    return part[0][r];
   };
   auto total = [&](float mine) {
     __syncthreads();
     part[s][r].x = mine;
+    for (int step = TEAM / 2; step > 0; step >>= 1) {
+      __syncthreads();
+      if (s < step) part[s][r].x += part[s + step][r].x;
+    }
     __syncthreads();
-    float sum = part[0][r].x;
-    for (int i = 1; i < 16; ++i) sum += part[i][r].x;
-    return sum;
+    return part[0][r].x;
   };
   float2 mine = {-INFINITY, 0.0f};
-  if (in)
-    for (int i = s; i < a.spans; i += 16) mine = joined(mine, a.stats[(int64_t)i * a.rows + row]);
+  if (in) {
+    int i = s;
+    for (; i + 3 * TEAM < a.spans; i += 4 * TEAM) {        // four loads under way
+      float2 v[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = a.stats[(int64_t)(i + q * TEAM) * a.rows + row];
+      mine = joined(mine, joined(joined(v[0], v[1]), joined(v[2], v[3])));
+    }
+    for (; i < a.spans; i += TEAM) mine = joined(mine, a.stats[(int64_t)i * a.rows + row]);
+  }
   mine = all(mine);
   const float log_all = logf(mine.y), lse = mine.x + log_all;         // (apart where the logits are so large that their sum is the largest)
+  auto logit = [&](int j, int c) {       // of the row's entry j, class c
+    const int64_t at = row * a.t.k + j;
+    if (c >= a.kept) return a.zt[at];
+    const float z = a.z[row * a.ldz + c];
+    a.zt[at] = z;
+    return z;
+  };
   float loss = 0.0f;
   bool counts = false;
   if (!a.t.top) {
     const int c = in ? class_of(a.t, row, 0, a.classes) : -1;
     counts = c >= 0;
-    if (counts && s == 0) loss = log_all + (mine.x - a.zt[row]);
+    if (counts && s == 0) loss = log_all + (mine.x - logit(0, c));
     if (in && s == 0 && a.labels) a.labels[row] = c;
   } else {
     const int k = in ? a.t.k : 0;
     float2 top = {-INFINITY, 0.0f};
-    for (int j = s; j < k; j += 16) {
+    for (int j = s; j < k; j += TEAM) {
       const float t = teacher(a.t, row, j, a.classes);
       if (t != -INFINITY) top = joined(top, float2{t, 1.0f});
     }
     top = all(top);
     counts = top.y != 0.0f;               // (a NaN counts)
     const float log_sum = logf(top.y);
-    for (int j = s; j < k; j += 16) {
-      const float t = teacher(a.t, row, j, a.classes);
+    for (int j = s; j < k; j += TEAM) {
+      const int c = class_of(a.t, row, j, a.classes);
+      const float t = teacher(a.t, row, j, a.classes), z = c >= 0 ? logit(j, c) : 0.0f;
       const float logp = t - top.x - log_sum, p = counts && t != -INFINITY ? expf(t - top.x) / top.y : 0.0f;
-      a.p[row * k + j] = p;
-      if (p != 0.0f) loss += p * (logp + log_all + (mine.x - a.zt[row * k + j]));
+      entries[r * (k | 1) + j] = float2{__builtin_bit_cast(float, c), p};
+      if (p != 0.0f) loss += p * (logp + log_all + (mine.x - z));
     }
     loss = total(loss) * a.square_t;
+    // what the entries of one class add up to, at the first of them
+    for (int j = s; j < k; j += TEAM) {
+      const int c = __builtin_bit_cast(int, entries[r * (k | 1) + j].x);
+      float sum = 0.0f;
+      bool first = true;
+      for (int i = 0; i < k; ++i) {
+        const float2 e = entries[r * (k | 1) + i];
+        if (__builtin_bit_cast(int, e.x) == c) {
+          sum += e.y;
+          first &= i >= j;
+        }
+      }
+      a.p[row * k + j] = first ? sum : -1.0f;
+    }
   }
   if (in && s == 0) {
     a.lse[row] = lse;
@@ -118,64 +153,126 @@ __global__ __launch_bounds__(256) void row_loss_kernel(const RowLoss a) {
   }
 }
 
-__global__ __launch_bounds__(1024) void mean_kernel(const float* losses, const float2* norm, int rows, float scale, float* loss, float* alpha) {
-  __shared__ double sums[1024];
-  __shared__ int counts[1024];
+// Workgroup 0: the mean.  The others: 2048 elements each of xz's rows, then of `fixed`.
+template <typename T>
+__global__ __launch_bounds__(256) void all_rows_kernel(const AllRows a, int pads) {
   const int t = threadIdx.x;
-  double sum = 0.0;
-  int n = 0;
-  for (int i = t; i < rows; i += 1024)
-    if (norm[i].x != INFINITY) {
-      sum += (double)losses[i];
-      ++n;
+  if (blockIdx.x == 0) {
+    __shared__ double sums[256];
+    __shared__ int counts[256];
+    double sum = 0.0;
+    int n = 0;
+    for (int i0 = t; i0 < a.rows; i0 += 2048) {         // eight loads under way
+      float loss[8], peak[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int i = i0 + 256 * q;
+        loss[q] = i < a.rows ? a.losses[i] : 0.0f;
+        peak[q] = i < a.rows ? a.norm[i].x : INFINITY;
+      }
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (peak[q] != INFINITY) {
+          sum += (double)loss[q];
+          ++n;
+        }
     }
-  sums[t] = sum;
-  counts[t] = n;
-  for (int step = 512; step > 0; step >>= 1) {
-    __syncthreads();
-    if (t < step) {
-      sums[t] += sums[t + step];
-      counts[t] += counts[t + step];
+    sums[t] = sum;
+    counts[t] = n;
+    for (int step = 128; step > 0; step >>= 1) {
+      __syncthreads();
+      if (t < step) {
+        sums[t] += sums[t + step];
+        counts[t] += counts[t + step];
+      }
     }
+    if (t == 0) {
+      *a.loss = counts[0] ? (float)(sums[0] / counts[0]) : 0.0f;
+      *a.alpha = counts[0] ? a.scale / (float)counts[0] : 0.0f;
+    }
+    return;
   }
-  if (t == 0) {
-    *loss = counts[0] ? (float)(sums[0] / counts[0]) : 0.0f;
-    *alpha = counts[0] ? scale / (float)counts[0] : 0.0f;
+  const int64_t at = (int64_t)(blockIdx.x - 1) * 256 + t;
+  if ((int)blockIdx.x <= pads) {
+    const int eights = (a.dim + 7) / 8;
+    const int64_t row = at / eights;
+    const int c = (int)(at % eights) * 8;
+    if (row >= a.rows) return;
+    float v[8];
+    load8((const T*)a.x + row * a.ldx + c, a.norm[row].x == INFINITY ? 0 : a.dim - c, v);
+    store8((T*)a.xz + row * a.ldxz + c, 8, v);
+    return;
   }
+  const int64_t i = (at - (int64_t)pads * 256) * 8;
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (i + e < a.classes) a.fixed[i + e] = 0;
 }
 
-// The first entry of a class in its row writes what all of that class add up to.
-__global__ __launch_bounds__(256) void target_fix_kernel(const TargetFix a) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= (int64_t)a.rows * a.t.k) return;
-  const int64_t row = at / a.t.k;
-  const int j = (int)(at % a.t.k), c = class_of(a.t, row, j, a.classes), col = c - a.first;
-  if (c < 0 || col < 0 || col >= a.columns) return;
+// Entry j of a row, the first of its class, where that is one of the columns [col0, col1).
+// sums: a part of the columns' sums that is there already.
+__device__ __forceinline__ void fix_target(const TargetFix& a, int64_t row, int j, int col0, int col1, float* sums) {
+  const int c = class_of(a.t, row, j, a.classes), col = c - a.first;
+  if (c < 0 || col < col0 || col >= col1) return;
   const float2 norm = a.norm[row];
   if (norm.x == INFINITY) return;
-  float given = 1.0f;
-  if (a.t.top) {
-    const float* const p = a.p + row * a.t.k;
-    given = 0.0f;
-    for (int i = 0; i < a.t.k; ++i)
-      if (class_of(a.t, row, i, a.classes) == c) {
-        if (i < j) return;
-        given += p[i];
-      }
-  }
+  const float given = a.t.top ? a.p[row * a.t.k + j] : 1.0f;
+  if (given < 0.0f) return;
   // the probability less what is given, to a step of the larger one; of the result where both are near 1
-  const float d = a.zt[at] - norm.x, v = given > 0.5f ? expm1f(d + logf(norm.y)) + (1.0f - given) : expf(d) * norm.y - given;
-  if (a.dtype == 1) {
-    ((bf16*)a.P)[row * a.ldp + col] = (bf16)v;
-  } else {
-    ((float*)a.P)[row * a.ldp + col] = v;
-  }
+  const float d = a.zt[row * a.t.k + j] - norm.x, v = given > 0.5f ? expm1f(d + logf(norm.y)) + (1.0f - given) : expf(d) * norm.y - given;
+  if (a.dtype == 1) ((bf16*)a.P)[row * a.ldp + col] = (bf16)v;
+  else ((float*)a.P)[row * a.ldp + col] = v;
   // (integers: the order of the additions does not matter.  One class: the column's sum has left the target out, otherwise it holds the probability.)
   if (a.fixed) {
     const float add = a.t.top ? -given : v;
-    if (add != add) a.sums[col] = NAN;
+    if (add != add) sums[col] = NAN;
     else atomicAdd(a.fixed + col, (unsigned long long)(long long)rint((double)add * 1099511627776.0));
   }
+}
+
+__global__ __launch_bounds__(256) void target_fix_kernel(const TargetFix a) {
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at < (int64_t)a.rows * a.t.k) fix_target(a, at / a.t.k, (int)(at % a.t.k), 0, a.columns, a.sums);
+}
+
+// 512 columns by 4 EACH rows a workgroup, a lane 8 columns of EACH rows; then, where fix is set, the targets among them.  Bound by memory: 4 bytes in, 2 or 4 out.
+template <typename T, int EACH>
+__global__ __launch_bounds__(256) void kept_prob_kernel(const TargetFix a, const float* z, int64_t ldz, const int32_t* labels, bool fix) {
+  constexpr float kLog2e = 1.44269504088896340736f;
+  __shared__ float sums[4][512];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, col0 = blockIdx.x * 512, c = col0 + lane * 8, row0 = blockIdx.y * 4 * EACH;
+  float sum[8] = {};
+  if (c < a.columns) {
+#pragma unroll 4
+    for (int i = 0; i < EACH; ++i) {
+      const int row = row0 + w * EACH + i;
+      if (row >= a.rows) break;
+      const f32x4 u[2] = {*(const f32x4*)(z + row * ldz + c), *(const f32x4*)(z + row * ldz + c + 4)};
+      const float2 norm = a.norm[row];
+      const int label = labels ? labels[row] - a.first : -1;
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = __builtin_amdgcn_exp2f((u[e / 4][e % 4] - norm.x) * kLog2e) * norm.y;
+        if (norm.x == INFINITY || c + e == label || c + e >= a.columns) p[e] = 0.0f;       // (also where the row holds NaN)
+        sum[e] += p[e];
+      }
+      store8((T*)a.P + (int64_t)row * a.ldp + c, 8, p);
+    }
+  }
+  if (a.sums) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[w][lane * 8 + e] = sum[e];
+  }
+  __syncthreads();                       // (what this workgroup has written is in order from here on)
+  if (a.sums) {
+    for (int i = t; i < 512; i += 256)
+      if (col0 + i < a.columns) a.sums[(int64_t)blockIdx.y * a.columns + col0 + i] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+    __syncthreads();
+  }
+  if (!fix) return;
+  const int rows = a.rows - row0 < 4 * EACH ? a.rows - row0 : 4 * EACH, col1 = col0 + 512 < a.columns ? col0 + 512 : a.columns;
+  for (int i = t; i < rows * a.t.k; i += 256) fix_target(a, row0 + i / a.t.k, i % a.t.k, col0, col1, a.sums + (int64_t)blockIdx.y * a.columns);
 }
 
 __global__ __launch_bounds__(256) void bias_gradient_kernel(const float* sums, int parts, const unsigned long long* fixed, int columns, const float* alpha, float* dbias) {
@@ -186,19 +283,14 @@ __global__ __launch_bounds__(256) void bias_gradient_kernel(const float* sums, i
   dbias[c] = (float)(sum * (double)*alpha);
 }
 
-__global__ __launch_bounds__(256) void clear_kernel(unsigned long long* p, int n) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i < n) p[i] = 0;
-}
-
 template <typename T>
-__global__ __launch_bounds__(256) void pad_rows_kernel(const T* in, int64_t ldin, int rows, int cols, const float2* norm, T* out, int64_t ldo) {
+__global__ __launch_bounds__(256) void pad_rows_kernel(const T* in, int64_t ldin, int rows, int cols, T* out, int64_t ldo) {
   const int eights = (cols + 7) / 8;
   const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / eights;
   const int c = (int)(at % eights) * 8;
   if (row >= rows) return;
   float v[8];
-  load8(in + row * ldin + c, norm && norm[row].x == INFINITY ? 0 : cols - c, v);
+  load8(in + row * ldin + c, cols - c, v);
   store8(out + row * ldo + c, 8, v);
 }
 
@@ -238,13 +330,35 @@ hipError_t launch_target_logits(int dtype, const TargetLogits& a, hipStream_t s)
 }
 
 hipError_t launch_row_loss(const RowLoss& a, hipStream_t s) {
-  row_loss_kernel<<<blocks(a.rows, 16), 256, 0, s>>>(a);
+  const int entries = a.t.top ? (a.t.k | 1) * (int)sizeof(float2) : 0;
+  if (a.rows <= 256 || a.t.k > 256) row_loss_kernel<256><<<a.rows, 256, entries, s>>>(a);
+  else row_loss_kernel<16><<<blocks(a.rows, 16), 256, 16 * entries, s>>>(a);
   return hipGetLastError();
 }
 
-hipError_t launch_mean(const float* losses, const float2* norm, int rows, float scale, float* loss, float* alpha, hipStream_t s) {
-  mean_kernel<<<1, 1024, 0, s>>>(losses, norm, rows, scale, loss, alpha);
+hipError_t launch_all_rows(int dtype, const AllRows& a, hipStream_t s) {
+  const unsigned pads = a.xz ? blocks((int64_t)a.rows * ((a.dim + 7) / 8), 256) : 0, clears = a.fixed ? blocks(a.classes, 2048) : 0;
+  if (dtype == 1) all_rows_kernel<bf16><<<1 + pads + clears, 256, 0, s>>>(a, (int)pads);
+  else all_rows_kernel<float><<<1 + pads + clears, 256, 0, s>>>(a, (int)pads);
   return hipGetLastError();
+}
+
+// Rows of a workgroup of kept_prob_kernel: few where there are few, so that there are workgroups.
+int kept_sum_parts(int rows) { return (int)blocks(rows, rows >= 1024 ? 64 : 16); }
+
+hipError_t launch_kept_prob(const TargetFix& a, const float* z, int64_t ldz, const int32_t* labels, hipStream_t s) {
+  // each workgroup looks through its rows' targets: a few of them
+  const bool fix = a.t.k <= 16;
+  const dim3 grid(blocks(a.columns, 512), kept_sum_parts(a.rows));
+  if (a.rows >= 1024) {
+    if (a.dtype == 1) kept_prob_kernel<bf16, 16><<<grid, 256, 0, s>>>(a, z, ldz, labels, fix);
+    else kept_prob_kernel<float, 16><<<grid, 256, 0, s>>>(a, z, ldz, labels, fix);
+  } else {
+    if (a.dtype == 1) kept_prob_kernel<bf16, 4><<<grid, 256, 0, s>>>(a, z, ldz, labels, fix);
+    else kept_prob_kernel<float, 4><<<grid, 256, 0, s>>>(a, z, ldz, labels, fix);
+  }
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || fix ? e : launch_target_fix(a, s);
 }
 
 hipError_t launch_target_fix(const TargetFix& a, hipStream_t s) {
@@ -257,11 +371,6 @@ hipError_t launch_bias_gradient(const float* sums, int parts, const unsigned lon
   return hipGetLastError();
 }
 
-hipError_t launch_clear(unsigned long long* p, int n, hipStream_t s) {
-  clear_kernel<<<blocks(n, 256), 256, 0, s>>>(p, n);
-  return hipGetLastError();
-}
-
 hipError_t launch_zero(int dtype, void* out, int64_t ldo, int rows, int cols, hipStream_t s) {
   const unsigned n = blocks((int64_t)rows * ((cols + 7) / 8), 256);
   if (dtype == 1) zero_kernel<bf16><<<n, 256, 0, s>>>((bf16*)out, ldo, rows, cols);
@@ -269,10 +378,10 @@ hipError_t launch_zero(int dtype, void* out, int64_t ldo, int rows, int cols, hi
   return hipGetLastError();
 }
 
-hipError_t launch_pad_rows(int dtype, const void* in, int64_t ldin, int rows, int cols, const float2* norm, void* out, int64_t ldo, hipStream_t s) {
+hipError_t launch_pad_rows(int dtype, const void* in, int64_t ldin, int rows, int cols, void* out, int64_t ldo, hipStream_t s) {
   const unsigned n = blocks((int64_t)rows * ((cols + 7) / 8), 256);
-  if (dtype == 1) pad_rows_kernel<bf16><<<n, 256, 0, s>>>((const bf16*)in, ldin, rows, cols, norm, (bf16*)out, ldo);
-  else pad_rows_kernel<float><<<n, 256, 0, s>>>((const float*)in, ldin, rows, cols, norm, (float*)out, ldo);
+  if (dtype == 1) pad_rows_kernel<bf16><<<n, 256, 0, s>>>((const bf16*)in, ldin, rows, cols, (bf16*)out, ldo);
+  else pad_rows_kernel<float><<<n, 256, 0, s>>>((const float*)in, ldin, rows, cols, (float*)out, ldo);
   return hipGetLastError();
 }
 

@@ -1,6 +1,6 @@
 // Matrix products of the losses over the classes of a linear layer: logits that never go to memory as a whole, and what their gradient is multiplied with.
 //
-//   STATS  z = (x W^T + b) / T, tile by tile; a row's largest z and sum of exp(z - largest) over each wavefront's columns leave the chip, nothing else
+//   STATS  z = (x W^T + b) / T, tile by tile; a row's largest z and sum of exp(z - largest) over each wavefront's columns leave the chip, and z where it is kept
 //   PROB   z again, p = softmax(z) for a piece of the classes, row-major and transposed
 //   DX     P W, a contraction over the piece's classes, split over the chip where there are few tiles
 //   DW     P^T x, over the rows
@@ -155,6 +155,13 @@ __device__ __forceinline__ void finish(const ClassProduct& g, f32x4 (&acc)[MI][N
           for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((acc[i][j][e] - from) * kLog2e);
         sum = sum_of_rows(sum);
         const int m = m0 + 16 * i + lrow;
+        if (g.z && m < g.M) {
+#pragma unroll
+          for (int j = 0; j < NI; ++j) {
+            const int n = n0 + 16 * j + 4 * lgrp;
+            if (n < g.zcols) *(f32x4*)(g.z + (int64_t)m * g.ldz + n) = acc[i][j];
+          }
+        }
         if (lgrp == 0 && m < g.M) g.stats[(int64_t)span * g.M + m] = float2{most, sum};
       }
     } else {
@@ -361,7 +368,6 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, wm = w & 1, wn = w >> 1, lgrp = lane >> 4, lrow = lane & 15;
   const int rowW = m0 + wm * 128, colW = n0 + wn * 128;
   if constexpr (KIND == PRODUCT_STATS) {
-    // z log2(e), so that the exponentials take one addition
     f32x4 bias[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -393,6 +399,13 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
         for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((z[j][e] - from) * kLog2e);
       sum = sum_of_rows(sum);
       const int m = rowW + 16 * i + lrow;
+      if (g.z && m < g.M) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int n = colW + 16 * j + 4 * lgrp;
+          if (n < g.zcols) *(f32x4*)(g.z + (int64_t)m * g.ldz + n) = z[j];
+        }
+      }
       if (lgrp == 0 && m < g.M) g.stats[(int64_t)span * g.M + m] = float2{most, sum};
       __builtin_amdgcn_sched_barrier(0);
     }

@@ -12,6 +12,9 @@ namespace {
 constexpr int kMaxRows = 1 << 20, kMaxDim = 1 << 20, kMaxTop = 1024;
 // P of a piece of the classes takes this much at most.
 constexpr int64_t kPieceBytes = 256 << 20;
+// Logits that are kept in float32 between the loss and the gradient, where they are wanted: what fits here.  A piece of others is computed twice, which takes the third of three products
+// again.
+constexpr int64_t kKeptBytes = (int64_t)1 << 30;
 // A tile of 256 rows is addressed with 32-bit offsets: rows of x, W and P lie at most this many elements apart.
 constexpr int kMaxPiece = 1 << 20;
 constexpr int64_t kAcross = 0x7FFFFF00;
@@ -47,9 +50,10 @@ struct Call {
 struct Plan {
   int64_t es, ldk, ldp;                 // operands' element size; leading dimensions of copies of x and W, of P
   bool copy_x, copy_w;
-  int piece;                            // classes
+  int piece, kept;                      // classes of a piece; those whose logits are kept, whole pieces
+  int64_t ldz;
   int dx_parts, dw_parts, spans;
-  size_t zt, p, labels, norm, alpha, stats, xc, wc, xz, P, dx_work, dw_work, sums, fixed, bytes;
+  size_t zt, p, labels, norm, alpha, stats, xc, wc, xz, z, P, dx_work, dw_work, sums, fixed, bytes;
 };
 
 // Whether the products can read a matrix in place.
@@ -72,6 +76,11 @@ Plan plan_of(const Call& c) {
   a.piece = wanted == 1 ? c.classes : ((c.classes + wanted - 1) / wanted + 255) / 256 * 256;
   const int pieces = (c.classes + a.piece - 1) / a.piece;
   a.ldp = row_ld(a.piece, a.es);
+  if (grads) {
+    const int64_t fit = kKeptBytes / ((int64_t)c.rows * 4);
+    a.kept = fit >= c.classes ? c.classes : (int)(fit / a.piece) * a.piece;
+    a.ldz = row_ld(a.kept, 4);
+  }
   a.dx_parts = class_parts(c.dt, c.rows, c.dim, a.piece);
   a.dw_parts = class_parts(c.dt, a.piece, c.dim, c.rows);
   for (int first = 0; first < c.classes; first += a.copy_w ? a.piece : c.classes)
@@ -92,13 +101,16 @@ Plan plan_of(const Call& c) {
   a.xc = take(a.copy_x, r * a.ldk * a.es);
   a.wc = take(a.copy_w, (int64_t)a.piece * a.ldk * a.es);
   a.xz = take(c.dw, r * a.ldk * a.es);
+  a.z = take(a.kept > 0, r * a.ldz * 4);
   a.P = take(grads, r * a.ldp * a.es);
   a.dx_work = take(c.dx && (pieces > 1 || a.dx_parts > 1), (int64_t)a.dx_parts * r * dq * 4);
   a.dw_work = take(c.dw && a.dw_parts > 1, (int64_t)a.dw_parts * a.piece * dq * 4);
+  // sums of a piece's columns, over as many parts of the rows as the widest kernel makes
   const int64_t rest = c.classes - (int64_t)(pieces - 1) * a.piece, most_sums = (int64_t)sum_parts(c.dt, c.rows, a.piece) * a.piece;
   const int64_t rest_sums = rest > 0 ? sum_parts(c.dt, c.rows, (int)rest) * rest : 0;      // (smaller tiles, more parts)
-  a.sums = take(c.dbias, (most_sums > rest_sums ? most_sums : rest_sums) * 4);
-  a.fixed = take(c.dbias, (int64_t)a.piece * 8);
+  const int64_t kept_sums = (int64_t)kept_sum_parts(c.rows) * a.piece, gemm_sums = most_sums > rest_sums ? most_sums : rest_sums;
+  a.sums = take(c.dbias, (kept_sums > gemm_sums ? kept_sums : gemm_sums) * 4);
+  a.fixed = take(c.dbias, (int64_t)c.classes * 8);
   a.bytes = at;
   return a;
 }
@@ -115,22 +127,25 @@ int run(const Call& c, void* workspace, hipStream_t s) {
   const void* x = c.x;
   int64_t ldx = c.rows == 1 ? a.ldk : c.ldx;       // (a single row may have any)
   if (a.copy_x) {
-    HIP_TRY(launch_pad_rows(c.dt, c.x, c.ldx, c.rows, c.dim, nullptr, at(a.xc), a.ldk, s));
+    HIP_TRY(launch_pad_rows(c.dt, c.x, c.ldx, c.rows, c.dim, at(a.xc), a.ldk, s));
     x = at(a.xc);
     ldx = a.ldk;
   }
   // W's rows from class `first` on, where the products can read them
+  int copied = -1;                       // what the copy holds
   auto weights = [&](int first, int columns, const void*& w, int64_t& ldw) -> int {
     w = (const char*)c.w + (int64_t)first * c.ldw * a.es;
     ldw = c.classes == 1 ? a.ldk : c.ldw;
     if (a.copy_w) {
-      HIP_TRY(launch_pad_rows(c.dt, w, c.ldw, columns, c.dim, nullptr, at(a.wc), a.ldk, s));
+      if (copied != first) HIP_TRY(launch_pad_rows(c.dt, w, c.ldw, columns, c.dim, at(a.wc), a.ldk, s));
+      copied = first;
       w = at(a.wc);
       ldw = a.ldk;
     }
     return SLP_OK;
   };
-  HIP_TRY(launch_target_logits(c.dt, TargetLogits{c.x, c.w, c.ldx, c.ldw, c.bias, c.rows, c.classes, c.dim, c.t, zt}, s));
+  if (a.kept < c.classes) HIP_TRY(launch_target_logits(c.dt, TargetLogits{c.x, c.w, c.ldx, c.ldw, c.bias, c.rows, c.classes, c.dim, a.kept, c.t, zt}, s));
+  float* const z = a.kept ? (float*)at(a.z) : nullptr;
   float2* stats = (float2*)at(a.stats);
   for (int first = 0; first < c.classes; first += a.copy_w ? a.piece : c.classes) {
     const int left = c.classes - first, columns = a.copy_w && left > a.piece ? a.piece : left;
@@ -144,43 +159,56 @@ int run(const Call& c, void* workspace, hipStream_t s) {
     g.bias = c.bias ? c.bias + first : nullptr;
     g.per_t = per_t;
     g.stats = stats;
+    if (first < a.kept) {
+      g.z = z + first;
+      g.ldz = a.ldz;
+      g.zcols = a.kept - first < columns ? a.kept - first : columns;
+    }
     g.parts = 1;
     HIP_TRY(launch_class_product(c.dt, PRODUCT_STATS, g, s));
     stats += (int64_t)stats_spans(c.dt, c.rows, columns) * c.rows;
   }
   int32_t* const labels = c.t.top ? nullptr : (int32_t*)at(a.labels);
-  HIP_TRY(launch_row_loss(RowLoss{(const float2*)at(a.stats), a.spans, c.rows, c.classes, c.t, zt, c.temperature * c.temperature, c.lse, c.losses, norm, p, labels}, s));
-  HIP_TRY(launch_mean(c.losses, norm, c.rows, c.scale * c.temperature, c.loss, alpha, s));
+  HIP_TRY(launch_row_loss(RowLoss{(const float2*)at(a.stats), a.spans, c.rows, c.classes, c.t, z, a.ldz, a.kept, zt, c.temperature * c.temperature, c.lse, c.losses, norm, p, labels}, s));
+  // (xz: the rows that count; 0 times what others hold may be NaN)
+  unsigned long long* const all_fixed = c.dbias ? (unsigned long long*)at(a.fixed) : nullptr;
+  HIP_TRY(launch_all_rows(c.dt, AllRows{c.losses, norm, c.rows, c.classes, c.dim, c.scale * c.temperature, c.loss, alpha, c.x, c.ldx, c.dw ? at(a.xz) : nullptr, a.ldk, all_fixed}, s));
   if (!grads) return SLP_OK;
 
-  // the rows that count: 0 times what others hold may be NaN
-  if (c.dw) HIP_TRY(launch_pad_rows(c.dt, c.x, c.ldx, c.rows, c.dim, norm, at(a.xz), a.ldk, s));
   for (int first = 0; first < c.classes; first += a.piece) {
     const int columns = c.classes - first < a.piece ? c.classes - first : a.piece;
     const bool last = first + columns == c.classes;
-    ClassProduct g{};
-    SLP_CHECK(weights(first, columns, g.b, g.ldb));
-    const void* const w = g.b;
-    const int64_t ldw = g.ldb;
-    g.a = x;
-    g.lda = ldx;
-    g.M = c.rows;
-    g.N = columns;
-    g.K = c.dim;
-    g.bias = c.bias ? c.bias + first : nullptr;
-    g.per_t = per_t;
-    g.norm = norm;
-    g.labels = labels;
-    g.label0 = first;
-    g.p = at(a.P);
-    g.ldp = a.ldp;
-    g.sums = c.dbias ? (float*)at(a.sums) : nullptr;
-    g.parts = 1;
-    HIP_TRY(launch_class_product(c.dt, PRODUCT_PROB, g, s));
-    unsigned long long* const fixed = c.dbias ? (unsigned long long*)at(a.fixed) : nullptr;
-    if (fixed) HIP_TRY(launch_clear(fixed, columns, s));
-    HIP_TRY(launch_target_fix(TargetFix{c.t, c.rows, c.classes, c.dt, zt, p, norm, first, columns, g.p, a.ldp, fixed, g.sums}, s));
-    if (c.dbias) HIP_TRY(launch_bias_gradient(g.sums, sum_parts(c.dt, c.rows, columns), fixed, columns, alpha, c.dbias + first, s));
+    const bool kept = first < a.kept;
+    const void* w = nullptr;
+    int64_t ldw = 0;
+    if (!kept || c.dx) SLP_CHECK(weights(first, columns, w, ldw));
+    float* const sums = c.dbias ? (float*)at(a.sums) : nullptr;
+    unsigned long long* const fixed = c.dbias ? all_fixed + first : nullptr;
+    const TargetFix fix{c.t, c.rows, c.classes, c.dt, zt, p, norm, first, columns, at(a.P), a.ldp, fixed, sums};
+    if (kept) {
+      HIP_TRY(launch_kept_prob(fix, z + first, a.ldz, labels, s));
+    } else {
+      ClassProduct g{};
+      g.a = x;
+      g.lda = ldx;
+      g.b = w;
+      g.ldb = ldw;
+      g.M = c.rows;
+      g.N = columns;
+      g.K = c.dim;
+      g.bias = c.bias ? c.bias + first : nullptr;
+      g.per_t = per_t;
+      g.norm = norm;
+      g.labels = labels;
+      g.label0 = first;
+      g.p = at(a.P);
+      g.ldp = a.ldp;
+      g.sums = sums;
+      g.parts = 1;
+      HIP_TRY(launch_class_product(c.dt, PRODUCT_PROB, g, s));
+      HIP_TRY(launch_target_fix(fix, s));
+    }
+    if (c.dbias) HIP_TRY(launch_bias_gradient(sums, kept ? kept_sum_parts(c.rows) : sum_parts(c.dt, c.rows, columns), fixed, columns, alpha, c.dbias + first, s));
     if (c.dx) {
       ClassProduct o{};
       o.a = at(a.P);

@@ -85,5 +85,7 @@ def test_workspace():
     a = (P, 4096, P, 4096, 1, 8192, 131072, 4096, 0)
     assert size(*a, 0) < size(*a, 1) < size(*a, 3) < size(*a, 7)
     assert size(*a, 7) < 8192 * 131072 * 2                       # less than the logits alone in 16 bits
+    b = (P, 4096, P, 4096, 1, 65536, 131072, 4096, 0)
+    assert size(*b, 7) < size(*a, 7) + 65536 * 4096 * (4 + 2) + (2 << 30)     # what grows with the rows: x's gradient, its copy, statistics
     assert size(P + 2, *a[1:], 0) > size(*a, 0)                  # a copy of what cannot be read in place
     assert size(P, 64, P, 64, 9, 10, 300, 64, 0, 7) == 0 and size(P, 64, P, 64, 0, 0, 300, 64, 0, 7) == 0 and size(P, 64, P, 64, 0, 10, 300, 64, 1025, 7) == 0
