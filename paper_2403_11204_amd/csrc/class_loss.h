@@ -25,7 +25,7 @@ struct ClassProduct {
   // STATS and PROB
   const float* bias;        // [N], may be null
   float per_t;
-  float2* stats;            // [stats_spans(M, N)][M]: (largest, sum)
+  float2* stats;            // [stats_spans(M, N, K)][M]: (largest, sum)
   float* z;                 // [M][ldz], may be null: z itself of the first zcols columns
   int64_t ldz;
   int zcols;
@@ -34,7 +34,7 @@ struct ClassProduct {
   int label0;               // column 0's class
   void* p;                  // [M][ldp], written up to the next 8 columns
   int64_t ldp;
-  float* sums;              // [sum_parts(M, N)][N], may be null
+  float* sums;              // [sum_parts(M, N, K)][N], may be null
   // DX and DW
   void* out;                // [M][ldo] of out_dtype, any alignment
   int64_t ldo;
@@ -46,8 +46,8 @@ struct ClassProduct {
 };
 // parts of a product's contraction that fill the chip: for PRODUCT_DX and PRODUCT_DW
 int class_parts(int dtype, int M, int N, int K);
-int stats_spans(int dtype, int M, int N);
-int sum_parts(int dtype, int M, int N);
+int stats_spans(int dtype, int M, int N, int K);
+int sum_parts(int dtype, int M, int N, int K);
 hipError_t launch_class_product(int dtype, int kind, const ClassProduct& g, hipStream_t s);
 
 // The rows' targets: class ids (a class id outside [0, classes) is none), and for a distillation the teacher's logits of them.

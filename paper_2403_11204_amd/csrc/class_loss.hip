@@ -275,11 +275,26 @@ __global__ __launch_bounds__(256) void kept_prob_kernel(const TargetFix a, const
   for (int i = t; i < rows * a.t.k; i += 256) fix_target(a, row0 + i / a.t.k, i % a.t.k, col0, col1, a.sums + (int64_t)blockIdx.y * a.columns);
 }
 
+// 32 columns a workgroup, 8 strands of parts each, four loads under way.
 __global__ __launch_bounds__(256) void bias_gradient_kernel(const float* sums, int parts, const unsigned long long* fixed, int columns, const float* alpha, float* dbias) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= columns) return;
-  double sum = (double)(long long)fixed[c] * (1.0 / 1099511627776.0);
-  for (int i = 0; i < parts; ++i) sum += (double)sums[(int64_t)i * columns + c];
+  __shared__ double strand[8][32];
+  const int t = threadIdx.x, l = t & 31, s = t >> 5, c = blockIdx.x * 32 + l;
+  double sum = 0.0;
+  if (c < columns) {
+    int i = s;
+    for (; i + 24 < parts; i += 32) {
+      float v[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = sums[(int64_t)(i + 8 * q) * columns + c];
+      sum += ((double)v[0] + (double)v[1]) + ((double)v[2] + (double)v[3]);
+    }
+    for (; i < parts; i += 8) sum += (double)sums[(int64_t)i * columns + c];
+  }
+  strand[s][l] = sum;
+  __syncthreads();
+  if (s > 0 || c >= columns) return;
+  sum = (double)(long long)fixed[c] * (1.0 / 1099511627776.0);
+  for (int i = 0; i < 8; ++i) sum += strand[i][l];
   dbias[c] = (float)(sum * (double)*alpha);
 }
 
@@ -367,7 +382,7 @@ hipError_t launch_target_fix(const TargetFix& a, hipStream_t s) {
 }
 
 hipError_t launch_bias_gradient(const float* sums, int parts, const unsigned long long* fixed, int columns, const float* alpha, float* dbias, hipStream_t s) {
-  bias_gradient_kernel<<<blocks(columns, 256), 256, 0, s>>>(sums, parts, fixed, columns, alpha, dbias);
+  bias_gradient_kernel<<<blocks(columns, 32), 256, 0, s>>>(sums, parts, fixed, columns, alpha, dbias);
   return hipGetLastError();
 }
 

@@ -26,6 +26,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, int64_t
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00020000);
 }
 
+typedef __attribute__((ext_vector_type(2))) float f32x2;
 // What a lane feeds the matrix unit with from 32 bytes of a row, two of the 16-byte pieces of its 128: 2 x 8 bf16, or 8 float32 in three parts.
 template <typename T> struct Fragment;
 template <> struct Fragment<bf16> {
@@ -37,31 +38,38 @@ template <> struct Fragment<bf16> {
 };
 template <> struct Fragment<float> {
   bf16x8 v[3];
+  // (pairs: one conversion, two values back to float32 and two subtractions make the next part's)
   __device__ __forceinline__ void set(const u32x4& lo, const u32x4& hi) {
+    u32x4 part[3];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t bits = e < 4 ? lo[e & 3] : hi[e & 3];
-      const float x = __builtin_bit_cast(float, bits);
-      v[0][e] = (bf16)x;
-      const float r = x - (float)v[0][e];
-      v[1][e] = (bf16)r;
-      v[2][e] = (bf16)(r - (float)v[1][e]);
+    for (int e = 0; e < 4; ++e) {
+      f32x2 x = e < 2 ? f32x2{__builtin_bit_cast(float, (uint32_t)lo[2 * (e & 1)]), __builtin_bit_cast(float, (uint32_t)lo[2 * (e & 1) + 1])}
+                      : f32x2{__builtin_bit_cast(float, (uint32_t)hi[2 * (e & 1)]), __builtin_bit_cast(float, (uint32_t)hi[2 * (e & 1) + 1])};
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+        part[q][e] = u;
+        x[0] -= __builtin_bit_cast(float, u << 16);
+        x[1] -= __builtin_bit_cast(float, u & 0xFFFF0000u);
+      }
     }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) v[q] = __builtin_bit_cast(bf16x8, part[q]);
   }
 };
-__device__ __forceinline__ f32x4 mfma(const bf16x8& b, const bf16x8& a, const f32x4& acc) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, acc, 0, 0, 0); }
-// (operands in the order B, A: a lane then holds 4 consecutive columns of one row of the output)
-__device__ __forceinline__ f32x4 mma(const Fragment<bf16>& b, const Fragment<bf16>& a, f32x4 acc) {
-  acc = mfma(b.v[0], a.v[0], acc);
-  return mfma(b.v[1], a.v[1], acc);
-}
-__device__ __forceinline__ f32x4 mma(const Fragment<float>& b, const Fragment<float>& a, f32x4 acc) {
-  acc = mfma(b.v[2], a.v[0], acc);
-  acc = mfma(b.v[0], a.v[2], acc);
-  acc = mfma(b.v[1], a.v[1], acc);
-  acc = mfma(b.v[1], a.v[0], acc);
-  acc = mfma(b.v[0], a.v[1], acc);
-  return mfma(b.v[0], a.v[0], acc);
+// All fragments of A against all of B, a product of parts at a time: one on the same accumulator comes MI NI instructions later.  (operands in the order B, A: a lane then
+// holds 4 consecutive columns of one row of the output)
+template <typename T, int MI, int NI>
+__device__ __forceinline__ void mma(f32x4 (&acc)[MI][NI], const Fragment<T> (&a)[MI], const Fragment<T> (&b)[NI]) {
+  constexpr int N = sizeof(T) == 2 ? 2 : 6;
+  constexpr int pa[6] = {0, 2, 1, 1, 0, 0}, pb[6] = {2, 0, 1, 0, 1, 0};        // (the smallest first)
+#pragma unroll
+  for (int q = 0; q < N; ++q)
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j].v[N == 2 ? q : pb[q]], a[i].v[N == 2 ? q : pa[q]], acc[i][j], 0, 0, 0);
 }
 
 // Four consecutive elements, rounded to the type; `left` of them exist.
@@ -95,14 +103,18 @@ template <typename T, int KIND, int MI, int NI>
 __device__ __forceinline__ void finish(const ClassProduct& g, f32x4 (&acc)[MI][NI], int m0, int n0, int lane) {
   const int lgrp = lane >> 4, lrow = lane & 15;
   if constexpr (KIND >= PRODUCT_DX) {
+    // (float32, see Side::fragments: rows that lie the other way are dealt out one by one, columns 4 NI side by side to a lane)
+    constexpr bool AROUND = sizeof(T) == 4 && KIND == PRODUCT_DW, BROUND = sizeof(T) == 4;
+    auto row = [&](int i) { return AROUND ? m0 + MI * lrow + i : m0 + 16 * i + lrow; };
+    auto col = [&](int j) { return BROUND ? n0 + 4 * NI * lgrp + 4 * j : n0 + 16 * j + 4 * lgrp; };
     if (g.work) {
       const int64_t ldw = (g.N + 3) & ~3;
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
-        const int n = n0 + 16 * j + 4 * lgrp;
+        const int n = col(j);
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
-          const int m = m0 + 16 * i + lrow;
+          const int m = row(i);
           if (m < g.M && n < g.N) {
             f32x4* const to = (f32x4*)(g.work + ((int64_t)blockIdx.y * g.M + m) * ldw + n);
             *to = g.add ? *to + acc[i][j] : acc[i][j];
@@ -113,10 +125,10 @@ __device__ __forceinline__ void finish(const ClassProduct& g, f32x4 (&acc)[MI][N
       const float alpha = *g.alpha;
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
-        const int n = n0 + 16 * j + 4 * lgrp;
+        const int n = col(j);
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
-          const int m = m0 + 16 * i + lrow;
+          const int m = row(i);
           if (m < g.M && n < g.N) {
             const int64_t at = (int64_t)m * g.ldo + n;
             if (g.out_dtype == 1) store4((bf16*)g.out + at, g.N - n, acc[i][j] * alpha);
@@ -219,8 +231,7 @@ __device__ __forceinline__ void tile_of(int tilesM, int tilesN, int& tm, int& tn
 // One operand of a tile in LDS: ROWS rows (columns of a matrix that lies the other way) by 128 bytes of the contraction.
 //   rows by contraction: a load of the workgroup fills 32 rows, lane l of wavefront w the 16-byte piece l % 8 of row 8 w + l / 8; piece c of a row sits at c ^ (row / 2
 //   mod 8), which spreads the 16 rows of a fragment over all LDS banks
-//   KM, the other way: BK rows of ROWS columns; piece c of row k sits at c ^ key(k), so that what half a wavefront reads of 8 rows (bf16, transposing reads) or a wavefront of 4
-//   (float32) lies on all banks.
+//   KM, the other way: BK rows of ROWS columns; piece c of row k sits at c ^ key(k), so that what half a wavefront reads of 8 rows (bf16, transposing reads) or of 2 (float32) lies on all banks.
 template <typename T, int ROWS, bool KM>
 struct Side {
   static constexpr int ES = sizeof(T), BK = 128 / ES, LOADS = ROWS / 32, PIECES = ROWS * ES / 16;     // loads of a k-tile; KM: pieces of a row
@@ -229,9 +240,10 @@ struct Side {
   uint32_t step;            // bytes from a k-tile to the next
   int k[LOADS], K;          // KM: rows of the loads in a k-tile, the contraction's length; otherwise k[0]: first byte of the piece, K: bytes
   static __device__ __forceinline__ int key(int k) {
-    if constexpr (ES == 4) return ((k >> 2) & 3) << 2;
+    if constexpr (ES == 4) return PIECES == 32 ? 0 : PIECES == 16 ? (k & 4) << 1 : k & 4;
     else if constexpr (PIECES >= 16) return ((k & 3) | ((k >> 1) & 4)) << 1;
-    else return (((k >> 1) & 1) | ((k >> 2) & 2)) << 1;
+    else if constexpr (PIECES == 8) return (((k >> 1) & 1) | ((k >> 2) & 2)) << 1;
+    else return (k >> 2) & 2;
   }
   // rows (columns) [first, first + n) exist, n <= ROWS
   __device__ __forceinline__ void init(const void* p, int64_t ld, int first, int n, int K_, int t) {
@@ -265,51 +277,72 @@ struct Side {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr_t)(to + i * 4096), 16, exists ? voff[i] + (uint32_t)kt * step : kOutOfRange, 0, 0, 0);
     }
   }
-  // 32 bytes of the contraction for row (column) r0 + lane % 16, those that the other operand's fragment takes
-  __device__ __forceinline__ Fragment<T> fragment(const unsigned char* st, int r0, int lane) const {
+  // 32 bytes of the contraction for each of the wavefront's 16 N rows (columns) from r0 on, those that the other operand's fragments take.  Fragment i's row is r0 + 16 i + lane % 16,
+  // but of float32 that lies the other way r0 + N (lane % 16) + i: one read then brings N columns of a step of the contraction.
+  template <int N>
+  __device__ __forceinline__ void fragments(const unsigned char* st, int r0, int lane, Fragment<T> (&f)[N]) const {
     const int lgrp = lane >> 4, lrow = lane & 15;
-    Fragment<T> f;
     if constexpr (!KM) {
       const unsigned char* const row = st + (r0 + lrow) * 128;
       const int x0 = (lgrp ^ ((lane >> 1) & 7)) << 4;
-      f.set(*(const u32x4*)(row + x0), *(const u32x4*)(row + (x0 ^ 64)));
+#pragma unroll
+      for (int i = 0; i < N; ++i) f[i].set(*(const u32x4*)(row + i * 2048 + x0), *(const u32x4*)(row + i * 2048 + (x0 ^ 64)));
     } else if constexpr (ES == 2) {
       typedef __attribute__((ext_vector_type(4))) short i16x4;
       typedef __attribute__((address_space(3))) i16x4* lds_i16x4;
-      const int row = lgrp * 8 + (lrow >> 2), c = (r0 >> 3) + ((lrow & 3) >> 1);
-      const unsigned char* const at = st + row * (ROWS * 2) + ((c ^ key(row)) << 4) + (lrow & 1) * 8;
-      u32x2 v[4];
+      const int row = lgrp * 8 + (lrow >> 2);
 #pragma unroll
-      for (int h = 0; h < 4; ++h) v[h] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(at + ((h >> 1) * 32 + (h & 1) * 4) * (ROWS * 2))));
-      f.set(u32x4{v[0][0], v[0][1], v[1][0], v[1][1]}, u32x4{v[2][0], v[2][1], v[3][0], v[3][1]});
+      for (int i = 0; i < N; ++i) {
+        const int c = ((r0 + 16 * i) >> 3) + ((lrow & 3) >> 1);
+        const unsigned char* const at = st + row * (ROWS * 2) + ((c ^ key(row)) << 4) + (lrow & 1) * 8;
+        u32x2 v[4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) v[h] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(at + ((h >> 1) * 32 + (h & 1) * 4) * (ROWS * 2))));
+        f[i].set(u32x4{v[0][0], v[0][1], v[1][0], v[1][1]}, u32x4{v[2][0], v[2][1], v[3][0], v[3][1]});
+      }
     } else {
-      const int c = (r0 + lrow) >> 2;
-      u32x4 v[2];
+      const int c = r0 + N * lrow;
+      uint32_t v[8][N];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int row = (e >> 2) * 16 + lgrp * 4 + (e & 3);
-        v[e >> 2][e & 3] = *(const uint32_t*)(st + row * (ROWS * 4) + ((c ^ key(row)) << 4) + (lrow & 3) * 4);
+        const unsigned char* const at = st + row * (ROWS * 4) + (((c >> 2) ^ key(row)) << 4) + (c & 3) * 4;
+        if constexpr (N == 4) {
+          const u32x4 w = *(const u32x4*)at;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[e][i] = w[i];
+        } else if constexpr (N == 2) {
+          const u32x2 w = *(const u32x2*)at;
+          v[e][0] = w[0];
+          v[e][1] = w[1];
+        } else {
+#pragma unroll
+          for (int i = 0; i < N; ++i) v[e][i] = ((const uint32_t*)at)[i];
+        }
       }
-      f.set(v[0], v[1]);
+#pragma unroll
+      for (int i = 0; i < N; ++i) f[i].set(u32x4{v[0][i], v[1][i], v[2][i], v[3][i]}, u32x4{v[4][i], v[5][i], v[6][i], v[7][i]});
     }
-    return f;
   }
 };
 
-// BM x BN tile, 4 wavefronts in a 2 x 2 grid, NS LDS stages of a k-tile of 128 bytes each, one barrier a k-tile.  blockIdx.y: part of the contraction, kper
-// k-tiles long.
-template <typename T, int KIND, int BM, int BN, int NS>
-__global__ __launch_bounds__(256) void class_tile_kernel(const ClassProduct g, int kper) {
+// BM x BN tile, 4 wavefronts in a 2 x 2 grid, NS LDS stages of a k-tile of 128 bytes each, one barrier a k-tile.  NG such groups of wavefronts take a part of the
+// contraction each (kper k-tiles) and are added up in order at the end.  blockIdx.y: part of the contraction of a whole workgroup.
+template <typename T, int KIND, int BM, int BN, int NS, int NG>
+__global__ __launch_bounds__(256 * NG) void class_tile_kernel(const ClassProduct g, int kper) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  extern __shared__ __attribute__((aligned(16))) unsigned char all_smem[];
   constexpr int BK = 128 / (int)sizeof(T), A_BYTES = BM * 128, STAGE = (BM + BN) * 128, NLD = (BM + BN) / 32, MI = BM / 32, NI = BN / 32;
+  constexpr bool KMA = KIND == PRODUCT_DW, KMB = KIND >= PRODUCT_DX;
+  const int group = NG > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
+  unsigned char* const smem = all_smem + group * (NS * STAGE);
   int tm, tn;
   tile_of((g.M + BM - 1) / BM, (g.N + BN - 1) / BN, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6, wm = w & 1, wn = w >> 1;
-  const int nk = (g.K + BK - 1) / BK, k0 = blockIdx.y * kper, k1 = k0 + kper < nk ? k0 + kper : nk;
-  Side<T, BM, KIND == PRODUCT_DW> A;
-  Side<T, BN, KIND >= PRODUCT_DX> B;
+  const int t = threadIdx.x & 255, lane = t & 63, w = t >> 6, wm = w & 1, wn = w >> 1;
+  const int nk = (g.K + BK - 1) / BK, k0 = (blockIdx.y * NG + group) * kper, k1 = k0 + kper < nk ? k0 + kper : nk;
+  Side<T, BM, KMA> A;
+  Side<T, BN, KMB> B;
   A.init(g.a, g.lda, m0, g.M - m0 < BM ? g.M - m0 : BM, g.K, t);
   B.init(g.b, g.ldb, n0, g.N - n0 < BN ? g.N - n0 : BN, g.K, t);
   const int lds_wave = __builtin_amdgcn_readfirstlane(w * 1024);
@@ -325,25 +358,49 @@ __global__ __launch_bounds__(256) void class_tile_kernel(const ClassProduct g, i
     for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s) load(k0 + s, s);
-  for (int kt = k0; kt < k1; ++kt) {
+  for (int kt = k0; kt < (NG > 1 ? k0 + kper : k1); ++kt) {
     // this wavefront's part of k-tile kt has landed and its reads of the last one are done; behind the barrier, everybody's
     __builtin_amdgcn_s_waitcnt(SLP_VMCNT_LGKM0((NS - 2) * NLD));
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     load(kt + NS - 1, (kt - k0 + NS - 1) % NS);
+    if (NG > 1 && kt >= k1) continue;            // (a shorter part takes the others' barriers)
     const unsigned char* const st = smem + (kt - k0) % NS * STAGE;
     Fragment<T> a[MI], b[NI];
-#pragma unroll
-    for (int j = 0; j < NI; ++j) b[j] = B.fragment(st + A_BYTES, wn * (BN / 2) + 16 * j, lane);
-#pragma unroll
-    for (int i = 0; i < MI; ++i) a[i] = A.fragment(st, wm * (BM / 2) + 16 * i, lane);
-#pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-      for (int j = 0; j < NI; ++j) acc[i][j] = mma(b[j], a[i], acc[i][j]);
+    B.fragments(st + A_BYTES, wn * (BN / 2), lane, b);
+    A.fragments(st, wm * (BM / 2), lane, a);
+    mma<T, MI, NI>(acc, a, b);
   }
   __builtin_amdgcn_s_waitcnt(SLP_VMCNT(0));      // no load into LDS may outlive the workgroup
+  if constexpr (NG > 1) {
+    // the other groups' sums, 16 bytes of each lane side by side
+    __syncthreads();
+    f32x4* const sums = (f32x4*)all_smem + t;
+    if (group > 0) {
+#pragma unroll
+      for (int i = 0; i < MI * NI; ++i) sums[((group - 1) * MI * NI + i) * 256] = acc[i / NI][i % NI];
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int v = 0; v < NG - 1; ++v)
+#pragma unroll
+      for (int i = 0; i < MI * NI; ++i) acc[i / NI][i % NI] += sums[(v * MI * NI + i) * 256];
+  }
+  if constexpr (sizeof(T) == 4 && KMB) {
+    // the columns that a lane holds lie side by side: 4 NI of them, element e of fragment j the (NI e + j)-th
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      f32x4 v[NI];
+#pragma unroll
+      for (int q = 0; q < NI; ++q)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[q][r] = acc[i][(4 * q + r) % NI][(4 * q + r) / NI];
+#pragma unroll
+      for (int q = 0; q < NI; ++q) acc[i][q] = v[q];
+    }
+  }
   finish<T, KIND, MI, NI>(g, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), lane);
 #endif
 }
@@ -526,24 +583,33 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
 // ---- host side -------------------------------------------------------------------------------
 int64_t tiles_of(int M, int N, int BM, int BN) { return (int64_t)((M + BM - 1) / BM) * ((N + BN - 1) / BN); }
 
-enum Shape { kLong, k128, k64 };
+enum Tile { kLong, k128, k128x64, k64, k64by2, k32x64, k32x64by2, k32, k32by4 };
 // parts: of the contraction, which share the chip
-Shape shape_of(int dtype, int M, int N, int parts = 1) {
-  if (dtype == 1 && tiles_of(M, N, 256, 256) * parts >= 200) return kLong;
-  return tiles_of(M, N, 128, 128) * parts >= 200 ? k128 : k64;
+Tile shape_of(int dtype, int M, int N, int K, int parts = 1) {
+  const int64_t nk = ((int64_t)K * (dtype == 1 ? 2 : 4) + 127) / 128 / parts;
+  const int64_t t256 = tiles_of(M, N, 256, 256) * parts, t128 = tiles_of(M, N, 128, 128) * parts, t64 = tiles_of(M, N, 64, 64) * parts;
+  if (dtype == 1 && t256 >= 200) return kLong;
+  if (t128 >= 384) return k128;
+  if (tiles_of(M, N, 128, 64) * parts >= 480) return k128x64;
+  if (tiles_of(M, N, 32, 32) * parts <= 256) return nk >= 11 ? k32by4 : k32;
+  if (tiles_of(M, N, 32, 64) * parts <= 256) return nk >= 7 ? k32x64by2 : k32x64;
+  if (nk >= 7 && t64 <= (nk >= 32 ? 512 : nk >= 16 ? 384 : 256)) return k64by2;
+  return k64;
 }
-// Rows, or columns, of a wavefront's part of a tile.
-int span_of(Shape s) { return s == kLong ? 128 : s == k128 ? 64 : 32; }
+// Rows and columns of a wavefront's part of a tile.
+int span_rows(Tile s) { return s == kLong ? 128 : s <= k128x64 ? 64 : s <= k64by2 ? 32 : 16; }
+int span_columns(Tile s) { return s == kLong ? 128 : s == k128 ? 64 : s <= k32x64by2 ? 32 : 16; }
 
-template <typename T, int KIND, int BM, int BN, int NS>
+template <typename T, int KIND, int BM, int BN, int NS, int NG>
 hipError_t launch_tile(const ClassProduct& g, hipStream_t s) {
-  constexpr int smem = NS * (BM + BN) * 128;
+  constexpr int smem = NG * NS * (BM + BN) * 128;
+  static_assert(smem >= (NG - 1) * BM * BN * 4, "room for the groups' sums");
   static std::atomic<uint64_t> done{0};
-  hipError_t e = allow_lds((const void*)class_tile_kernel<T, KIND, BM, BN, NS>, smem, done);
+  hipError_t e = allow_lds((const void*)class_tile_kernel<T, KIND, BM, BN, NS, NG>, smem, done);
   if (e != hipSuccess) return e;
   constexpr int BK = 128 / (int)sizeof(T);
-  const int nk = (g.K + BK - 1) / BK, parts = g.work ? g.parts : 1, kper = (nk + parts - 1) / parts;
-  hipLaunchKernelGGL((class_tile_kernel<T, KIND, BM, BN, NS>), dim3((unsigned)tiles_of(g.M, g.N, BM, BN), parts), dim3(256), smem, s, g, kper);
+  const int nk = (g.K + BK - 1) / BK, parts = g.work ? g.parts : 1, kper = (nk + parts * NG - 1) / (parts * NG);
+  hipLaunchKernelGGL((class_tile_kernel<T, KIND, BM, BN, NS, NG>), dim3((unsigned)tiles_of(g.M, g.N, BM, BN), parts), dim3(256 * NG), smem, s, g, kper);
   return hipGetLastError();
 }
 template <int KIND>
@@ -557,11 +623,17 @@ hipError_t launch_long(const ClassProduct& g, hipStream_t s) {
 }
 template <typename T, int KIND>
 hipError_t launch_kind(int dtype, const ClassProduct& g, hipStream_t s) {
-  switch (shape_of(dtype, g.M, g.N, g.work ? g.parts : 1)) {
+  switch (shape_of(dtype, g.M, g.N, g.K, g.work ? g.parts : 1)) {
     case kLong:
       if constexpr (sizeof(T) == 2) return launch_long<KIND>(g, s);
-    case k128: return launch_tile<T, KIND, 128, 128, 2>(g, s);
-    default: return launch_tile<T, KIND, 64, 64, 2>(g, s);
+    case k128: return launch_tile<T, KIND, 128, 128, 2, 1>(g, s);
+    case k128x64: return launch_tile<T, KIND, 128, 64, 2, 1>(g, s);
+    case k64: return launch_tile<T, KIND, 64, 64, 2, 1>(g, s);
+    case k64by2: return launch_tile<T, KIND, 64, 64, 2, 2>(g, s);
+    case k32x64: return launch_tile<T, KIND, 32, 64, 3, 1>(g, s);
+    case k32x64by2: return launch_tile<T, KIND, 32, 64, 3, 2>(g, s);
+    case k32: return launch_tile<T, KIND, 32, 32, 4, 1>(g, s);
+    default: return launch_tile<T, KIND, 32, 32, 2, 4>(g, s);
   }
 }
 template <typename T>
@@ -591,12 +663,12 @@ int class_parts(int dtype, int M, int N, int K) {
   return p < 1 ? 1 : p;
 }
 
-int stats_spans(int dtype, int M, int N) {
-  const int w = span_of(shape_of(dtype, M, N));
+int stats_spans(int dtype, int M, int N, int K) {
+  const int w = span_columns(shape_of(dtype, M, N, K));
   return (N + 2 * w - 1) / (2 * w) * 2;
 }
-int sum_parts(int dtype, int M, int N) {
-  const int w = span_of(shape_of(dtype, M, N));
+int sum_parts(int dtype, int M, int N, int K) {
+  const int w = span_rows(shape_of(dtype, M, N, K));
   return (M + 2 * w - 1) / (2 * w) * 2;
 }
 

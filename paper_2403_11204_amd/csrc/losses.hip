@@ -84,7 +84,7 @@ Plan plan_of(const Call& c) {
   a.dx_parts = class_parts(c.dt, c.rows, c.dim, a.piece);
   a.dw_parts = class_parts(c.dt, a.piece, c.dim, c.rows);
   for (int first = 0; first < c.classes; first += a.copy_w ? a.piece : c.classes)
-    a.spans += stats_spans(c.dt, c.rows, a.copy_w && c.classes - first > a.piece ? a.piece : c.classes - first);
+    a.spans += stats_spans(c.dt, c.rows, a.copy_w && c.classes - first > a.piece ? a.piece : c.classes - first, c.dim);
   size_t at = 0;
   auto take = [&](bool wanted, int64_t bytes) {
     const size_t here = at;
@@ -106,8 +106,8 @@ Plan plan_of(const Call& c) {
   a.dx_work = take(c.dx && (pieces > 1 || a.dx_parts > 1), (int64_t)a.dx_parts * r * dq * 4);
   a.dw_work = take(c.dw && a.dw_parts > 1, (int64_t)a.dw_parts * a.piece * dq * 4);
   // sums of a piece's columns, over as many parts of the rows as the widest kernel makes
-  const int64_t rest = c.classes - (int64_t)(pieces - 1) * a.piece, most_sums = (int64_t)sum_parts(c.dt, c.rows, a.piece) * a.piece;
-  const int64_t rest_sums = rest > 0 ? sum_parts(c.dt, c.rows, (int)rest) * rest : 0;      // (smaller tiles, more parts)
+  const int64_t rest = c.classes - (int64_t)(pieces - 1) * a.piece, most_sums = (int64_t)sum_parts(c.dt, c.rows, a.piece, c.dim) * a.piece;
+  const int64_t rest_sums = rest > 0 ? sum_parts(c.dt, c.rows, (int)rest, c.dim) * rest : 0;      // (smaller tiles, more parts)
   const int64_t kept_sums = (int64_t)kept_sum_parts(c.rows) * a.piece, gemm_sums = most_sums > rest_sums ? most_sums : rest_sums;
   a.sums = take(c.dbias, (kept_sums > gemm_sums ? kept_sums : gemm_sums) * 4);
   a.fixed = take(c.dbias, (int64_t)c.classes * 8);
@@ -166,7 +166,7 @@ int run(const Call& c, void* workspace, hipStream_t s) {
     }
     g.parts = 1;
     HIP_TRY(launch_class_product(c.dt, PRODUCT_STATS, g, s));
-    stats += (int64_t)stats_spans(c.dt, c.rows, columns) * c.rows;
+    stats += (int64_t)stats_spans(c.dt, c.rows, columns, c.dim) * c.rows;
   }
   int32_t* const labels = c.t.top ? nullptr : (int32_t*)at(a.labels);
   HIP_TRY(launch_row_loss(RowLoss{(const float2*)at(a.stats), a.spans, c.rows, c.classes, c.t, z, a.ldz, a.kept, zt, c.temperature * c.temperature, c.lse, c.losses, norm, p, labels}, s));
@@ -208,7 +208,7 @@ int run(const Call& c, void* workspace, hipStream_t s) {
       HIP_TRY(launch_class_product(c.dt, PRODUCT_PROB, g, s));
       HIP_TRY(launch_target_fix(fix, s));
     }
-    if (c.dbias) HIP_TRY(launch_bias_gradient(sums, kept ? kept_sum_parts(c.rows) : sum_parts(c.dt, c.rows, columns), fixed, columns, alpha, c.dbias + first, s));
+    if (c.dbias) HIP_TRY(launch_bias_gradient(sums, kept ? kept_sum_parts(c.rows) : sum_parts(c.dt, c.rows, columns, c.dim), fixed, columns, alpha, c.dbias + first, s));
     if (c.dx) {
       ClassProduct o{};
       o.a = at(a.P);
