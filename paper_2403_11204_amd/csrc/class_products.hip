@@ -629,11 +629,11 @@ hipError_t launch_kind(int dtype, const ClassProduct& g, hipStream_t s) {
     case k128: return launch_tile<T, KIND, 128, 128, 2, 1>(g, s);
     case k128x64: return launch_tile<T, KIND, 128, 64, 2, 1>(g, s);
     case k64: return launch_tile<T, KIND, 64, 64, 2, 1>(g, s);
-    case k64by2: return launch_tile<T, KIND, 64, 64, 2, 2>(g, s);
+    case k64by2: return tiles_of(g.M, g.N, 64, 64) * (g.work ? g.parts : 1) <= 256 ? launch_tile<T, KIND, 64, 64, 3, 2>(g, s) : launch_tile<T, KIND, 64, 64, 2, 2>(g, s);
     case k32x64: return launch_tile<T, KIND, 32, 64, 3, 1>(g, s);
     case k32x64by2: return launch_tile<T, KIND, 32, 64, 3, 2>(g, s);
     case k32: return launch_tile<T, KIND, 32, 32, 4, 1>(g, s);
-    default: return launch_tile<T, KIND, 32, 32, 2, 4>(g, s);
+    default: return launch_tile<T, KIND, 32, 32, 3, 4>(g, s);
   }
 }
 template <typename T>
