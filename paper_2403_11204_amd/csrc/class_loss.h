@@ -88,21 +88,21 @@ struct RowLoss {
   float* p;                 // [rows][k], may be null where t.top is: the teacher's probabilities, of all the row's entries of that class
                             // together at the first of them, -1 at the others; 0 where none counts
   int32_t* labels;          // [rows], may be null: the row's class or -1
+  unsigned long long* fixed;      // [classes], may be null: cleared on the way
 };
 hipError_t launch_row_loss(const RowLoss& a, hipStream_t s);
 // What follows from all rows: *loss = mean of those that count (0 where none does), *alpha = scale / their number (0); xz = the rows of x, zeros for those that do not
-// count and up to the next multiple of 8 columns (may be null); fixed[0 .. classes) = 0 (may be null)
+// count and up to the next multiple of 8 columns (may be null)
 struct AllRows {
   const float* losses;
   const float2* norm;
-  int rows, classes, dim;
+  int rows, dim;
   float scale;
   float *loss, *alpha;
   const void* x;
   int64_t ldx;
   void* xz;
   int64_t ldxz;
-  unsigned long long* fixed;
 };
 hipError_t launch_all_rows(int dtype, const AllRows& a, hipStream_t s);
 
@@ -119,17 +119,23 @@ struct TargetFix {
   float* sums;                    // ... and the sums, where that is NaN
 };
 hipError_t launch_target_fix(const TargetFix& a, hipStream_t s);
-// P of a piece whose logits are kept, targets and all: rows [rows][ldz] of z from the piece's first class on; sums: as PRODUCT_PROB's, kept_sum_parts(rows) of them
-hipError_t launch_kept_prob(const TargetFix& a, const float* z, int64_t ldz, const int32_t* labels, hipStream_t s);
+// P of a piece whose logits are kept, targets and all, and (all may be null) launch_all_rows on the way: rows [rows][ldz] of z from the piece's first class on; sums: as PRODUCT_PROB's, kept_sum_parts(rows) of them
+hipError_t launch_kept_prob(const TargetFix& a, const float* z, int64_t ldz, const int32_t* labels, const AllRows* all, hipStream_t s);
 int kept_sum_parts(int rows);
 
 // dbias[c] = alpha (sum over the parts of sums[part][c] + fixed[c] 2^-40)
-hipError_t launch_bias_gradient(const float* sums, int parts, const unsigned long long* fixed, int columns, const float* alpha, float* dbias, hipStream_t s);
+struct BiasGradient {
+  const float* sums;        // [parts][columns]
+  int parts, columns;
+  const unsigned long long* fixed;
+  const float* alpha;
+  float* dbias;
+};
 
 // out[r][c] = in[r][c], zero from cols up to the next multiple of 8
 hipError_t launch_pad_rows(int dtype, const void* in, int64_t ldin, int rows, int cols, void* out, int64_t ldo, hipStream_t s);
 hipError_t launch_zero(int dtype, void* out, int64_t ldo, int rows, int cols, hipStream_t s);
-// out = alpha * sum over the parts, rounded to the type
-hipError_t launch_join_parts(int dtype, const float* work, int parts, int rows, int cols, const float* alpha, void* out, int64_t ldo, hipStream_t s);
+// out = alpha * sum over the parts, rounded to the type (no rows: nothing of it), and (bias may be null) a bias's gradient on the way
+hipError_t launch_join_parts(int dtype, const float* work, int parts, int rows, int cols, const float* alpha, void* out, int64_t ldo, const BiasGradient* bias, hipStream_t s);
 
 }  // namespace slp

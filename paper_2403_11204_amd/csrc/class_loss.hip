@@ -7,6 +7,8 @@
 #include "class_loss.h"
 #include "eightbit_device.h"
 
+#include <type_traits>
+
 namespace slp {
 namespace {
 
@@ -56,35 +58,71 @@ __device__ __forceinline__ float2 joined(float2 a, float2 b) {
   return float2{most, (a.x == most ? a.y : a.y * expf(a.x - most)) + (b.x == most ? b.y : b.y * expf(b.x - most))};
 }
 
-// TEAM threads a row: 16, or all 256 of a workgroup where there are few rows (1 x 131072 classes, 1024 spans: 35 us on 16 threads).
+// Over the lanes of a wavefront.
+__device__ __forceinline__ float fmax_of_64(float x) {
+  auto step = [&](auto ctrl) { x = fmaxf(x, __builtin_bit_cast(float, dpp<decltype(ctrl)::value>(__builtin_bit_cast(uint32_t, x)))); };
+  step(std::integral_constant<int, kSwap1>{});
+  step(std::integral_constant<int, kSwap2>{});
+  step(std::integral_constant<int, kHalfMirror>{});
+  step(std::integral_constant<int, kMirror>{});
+  uint32_t u = __builtin_bit_cast(uint32_t, x);
+  u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(u, u, false, false));
+  uint32_t a = r[0], b = r[1];
+  u = __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
+  r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(u, u, false, false));
+  a = r[0];
+  b = r[1];
+  return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+
+// TEAM threads a row: 16; a wavefront where there are few rows; all 256 of a workgroup where there are many spans as well (1 x 131072 classes, 1024 spans: 35 us on 16 threads,
+// 5 on 256; 64 x 1000 with 8 entries 8 on 256).  Workgroups behind the rows' clear `fixed`.
 template <int TEAM>
 __global__ __launch_bounds__(256) void row_loss_kernel(const RowLoss a) {
   constexpr int ROWS = 256 / TEAM;
-  __shared__ float2 part[TEAM][ROWS];
+  __shared__ float2 part[TEAM == 64 ? 1 : 16][TEAM == 16 ? 16 : 1];
   extern __shared__ float2 entries[];          // of a distillation: class and probability of each row's entries
-  const int r = threadIdx.x % ROWS, s = threadIdx.x / ROWS;
+  const int t = threadIdx.x, r = TEAM == 16 ? t % 16 : t / TEAM, s = TEAM == 16 ? t / 16 : t % TEAM, groups = (a.rows + ROWS - 1) / ROWS;
+  if ((int)blockIdx.x >= groups) {
+    const int64_t i = ((int64_t)(blockIdx.x - groups) * 256 + t) * 8;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (i + e < a.classes) a.fixed[i + e] = 0;
+    return;
+  }
   const int64_t row = (int64_t)blockIdx.x * ROWS + r;
   const bool in = row < a.rows;
-  // of the row's threads, halves of them at a time: the same order every time
+  // of the row's threads, in the same order every time
   auto all = [&](float2 mine) {
-    __syncthreads();
-    part[s][r] = mine;
-    for (int step = TEAM / 2; step > 0; step >>= 1) {
-      __syncthreads();
-      if (s < step) part[s][r] = joined(part[s][r], part[s + step][r]);
+    if constexpr (TEAM > 16) {
+      const float most = fmax_of_64(mine.x);
+      mine = float2{most, sum_of_64(mine.x == most ? mine.y : mine.y * expf(mine.x - most))};
     }
-    __syncthreads();
-    return part[0][r];
+    if constexpr (TEAM != 64) {
+      constexpr int N = TEAM == 16 ? 16 : 4;
+      const int c = TEAM == 16 ? r : 0, at = TEAM == 16 ? s : s >> 6;
+      __syncthreads();
+      part[at][c] = mine;
+      __syncthreads();
+      mine = part[0][c];
+#pragma unroll
+      for (int i = 1; i < N; ++i) mine = joined(mine, part[i][c]);
+    }
+    return mine;
   };
   auto total = [&](float mine) {
-    __syncthreads();
-    part[s][r].x = mine;
-    for (int step = TEAM / 2; step > 0; step >>= 1) {
+    if constexpr (TEAM > 16) mine = sum_of_64(mine);
+    if constexpr (TEAM != 64) {
+      constexpr int N = TEAM == 16 ? 16 : 4;
+      const int c = TEAM == 16 ? r : 0, at = TEAM == 16 ? s : s >> 6;
       __syncthreads();
-      if (s < step) part[s][r].x += part[s + step][r].x;
+      part[at][c].x = mine;
+      __syncthreads();
+      mine = part[0][c].x;
+#pragma unroll
+      for (int i = 1; i < N; ++i) mine += part[i][c].x;
     }
-    __syncthreads();
-    return part[0][r].x;
+    return mine;
   };
   float2 mine = {-INFINITY, 0.0f};
   if (in) {
@@ -132,6 +170,7 @@ __global__ __launch_bounds__(256) void row_loss_kernel(const RowLoss a) {
     }
     loss = total(loss) * a.square_t;
     // what the entries of one class add up to, at the first of them
+    __syncthreads();
     for (int j = s; j < k; j += TEAM) {
       const int c = __builtin_bit_cast(int, entries[r * (k | 1) + j].x);
       float sum = 0.0f;
@@ -153,13 +192,13 @@ __global__ __launch_bounds__(256) void row_loss_kernel(const RowLoss a) {
   }
 }
 
-// Workgroup 0: the mean.  The others: 2048 elements each of xz's rows, then of `fixed`.
+// Block 0: the mean.  The others: 2048 elements each of xz's rows.
 template <typename T>
-__global__ __launch_bounds__(256) void all_rows_kernel(const AllRows a, int pads) {
+__device__ __forceinline__ void all_rows_block(const AllRows& a, int block) {
   const int t = threadIdx.x;
-  if (blockIdx.x == 0) {
-    __shared__ double sums[256];
-    __shared__ int counts[256];
+  if (block == 0) {
+    __shared__ double sums[4];
+    __shared__ int counts[4];
     double sum = 0.0;
     int n = 0;
     for (int i0 = t; i0 < a.rows; i0 += 2048) {         // eight loads under way
@@ -177,36 +216,34 @@ __global__ __launch_bounds__(256) void all_rows_kernel(const AllRows a, int pads
           ++n;
         }
     }
-    sums[t] = sum;
-    counts[t] = n;
-    for (int step = 128; step > 0; step >>= 1) {
-      __syncthreads();
-      if (t < step) {
-        sums[t] += sums[t + step];
-        counts[t] += counts[t + step];
-      }
+    for (int step = 32; step > 0; step >>= 1) {
+      sum += __shfl_xor(sum, step);
+      n += __shfl_xor(n, step);
     }
+    if ((t & 63) == 0) {
+      sums[t >> 6] = sum;
+      counts[t >> 6] = n;
+    }
+    __syncthreads();
     if (t == 0) {
-      *a.loss = counts[0] ? (float)(sums[0] / counts[0]) : 0.0f;
-      *a.alpha = counts[0] ? a.scale / (float)counts[0] : 0.0f;
+      sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+      n = counts[0] + counts[1] + counts[2] + counts[3];
+      *a.loss = n ? (float)(sum / n) : 0.0f;
+      *a.alpha = n ? a.scale / (float)n : 0.0f;
     }
     return;
   }
-  const int64_t at = (int64_t)(blockIdx.x - 1) * 256 + t;
-  if ((int)blockIdx.x <= pads) {
-    const int eights = (a.dim + 7) / 8;
-    const int64_t row = at / eights;
-    const int c = (int)(at % eights) * 8;
-    if (row >= a.rows) return;
-    float v[8];
-    load8((const T*)a.x + row * a.ldx + c, a.norm[row].x == INFINITY ? 0 : a.dim - c, v);
-    store8((T*)a.xz + row * a.ldxz + c, 8, v);
-    return;
-  }
-  const int64_t i = (at - (int64_t)pads * 256) * 8;
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (i + e < a.classes) a.fixed[i + e] = 0;
+  const int eights = (a.dim + 7) / 8;
+  const int64_t at = (int64_t)(block - 1) * 256 + t, row = at / eights;
+  const int c = (int)(at % eights) * 8;
+  if (row >= a.rows) return;
+  float v[8];
+  load8((const T*)a.x + row * a.ldx + c, a.norm[row].x == INFINITY ? 0 : a.dim - c, v);
+  store8((T*)a.xz + row * a.ldxz + c, 8, v);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void all_rows_kernel(const AllRows a) {
+  all_rows_block<T>(a, blockIdx.x);
 }
 
 // Entry j of a row, the first of its class, where that is one of the columns [col0, col1).
@@ -235,12 +272,17 @@ __global__ __launch_bounds__(256) void target_fix_kernel(const TargetFix a) {
   if (at < (int64_t)a.rows * a.t.k) fix_target(a, at / a.t.k, (int)(at % a.t.k), 0, a.columns, a.sums);
 }
 
-// 512 columns by 4 EACH rows a workgroup, a lane 8 columns of EACH rows; then, where fix is set, the targets among them.  Bound by memory: 4 bytes in, 2 or 4 out.
+// 512 columns by 4 EACH rows a workgroup, a lane 8 columns of EACH rows; then, where fix is set, the targets among them.  Workgroups behind those: all_rows_block.  Bound by memory: 4 bytes in, 2 or 4 out.
 template <typename T, int EACH>
-__global__ __launch_bounds__(256) void kept_prob_kernel(const TargetFix a, const float* z, int64_t ldz, const int32_t* labels, bool fix) {
+__global__ __launch_bounds__(256) void kept_prob_kernel(const TargetFix a, const float* z, int64_t ldz, const int32_t* labels, bool fix, const AllRows all) {
   constexpr float kLog2e = 1.44269504088896340736f;
   __shared__ float sums[4][512];
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6, col0 = blockIdx.x * 512, c = col0 + lane * 8, row0 = blockIdx.y * 4 * EACH;
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, wide = (a.columns + 511) / 512, high = (a.rows + 4 * EACH - 1) / (4 * EACH);
+  if ((int)blockIdx.x >= wide * high) {
+    all_rows_block<T>(all, blockIdx.x - wide * high);
+    return;
+  }
+  const int bx = blockIdx.x % wide, by = blockIdx.x / wide, col0 = bx * 512, c = col0 + lane * 8, row0 = by * 4 * EACH;
   float sum[8] = {};
   if (c < a.columns) {
 #pragma unroll 4
@@ -267,35 +309,12 @@ __global__ __launch_bounds__(256) void kept_prob_kernel(const TargetFix a, const
   __syncthreads();                       // (what this workgroup has written is in order from here on)
   if (a.sums) {
     for (int i = t; i < 512; i += 256)
-      if (col0 + i < a.columns) a.sums[(int64_t)blockIdx.y * a.columns + col0 + i] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+      if (col0 + i < a.columns) a.sums[(int64_t)by * a.columns + col0 + i] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
     __syncthreads();
   }
   if (!fix) return;
   const int rows = a.rows - row0 < 4 * EACH ? a.rows - row0 : 4 * EACH, col1 = col0 + 512 < a.columns ? col0 + 512 : a.columns;
-  for (int i = t; i < rows * a.t.k; i += 256) fix_target(a, row0 + i / a.t.k, i % a.t.k, col0, col1, a.sums + (int64_t)blockIdx.y * a.columns);
-}
-
-// 32 columns a workgroup, 8 strands of parts each, four loads under way.
-__global__ __launch_bounds__(256) void bias_gradient_kernel(const float* sums, int parts, const unsigned long long* fixed, int columns, const float* alpha, float* dbias) {
-  __shared__ double strand[8][32];
-  const int t = threadIdx.x, l = t & 31, s = t >> 5, c = blockIdx.x * 32 + l;
-  double sum = 0.0;
-  if (c < columns) {
-    int i = s;
-    for (; i + 24 < parts; i += 32) {
-      float v[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = sums[(int64_t)(i + 8 * q) * columns + c];
-      sum += ((double)v[0] + (double)v[1]) + ((double)v[2] + (double)v[3]);
-    }
-    for (; i < parts; i += 8) sum += (double)sums[(int64_t)i * columns + c];
-  }
-  strand[s][l] = sum;
-  __syncthreads();
-  if (s > 0 || c >= columns) return;
-  sum = (double)(long long)fixed[c] * (1.0 / 1099511627776.0);
-  for (int i = 0; i < 8; ++i) sum += strand[i][l];
-  dbias[c] = (float)(sum * (double)*alpha);
+  for (int i = t; i < rows * a.t.k; i += 256) fix_target(a, row0 + i / a.t.k, i % a.t.k, col0, col1, a.sums + (int64_t)by * a.columns);
 }
 
 template <typename T>
@@ -309,13 +328,42 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const T* in, int64_t ldin
   store8(out + row * ldo + c, 8, v);
 }
 
+// 32 columns a workgroup, 8 strands of parts each, four loads under way.
+__device__ __forceinline__ void bias_block(const BiasGradient& a, int block) {
+  __shared__ double strand[8][32];
+  const int t = threadIdx.x, l = t & 31, s = t >> 5, c = block * 32 + l;
+  double sum = 0.0;
+  if (c < a.columns) {
+    int i = s;
+    for (; i + 24 < a.parts; i += 32) {
+      float v[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = a.sums[(int64_t)(i + 8 * q) * a.columns + c];
+      sum += ((double)v[0] + (double)v[1]) + ((double)v[2] + (double)v[3]);
+    }
+    for (; i < a.parts; i += 8) sum += (double)a.sums[(int64_t)i * a.columns + c];
+  }
+  strand[s][l] = sum;
+  __syncthreads();
+  if (s > 0 || c >= a.columns) return;
+  sum = (double)(long long)a.fixed[c] * (1.0 / 1099511627776.0);
+  for (int i = 0; i < 8; ++i) sum += strand[i][l];
+  a.dbias[c] = (float)(sum * (double)*a.alpha);
+}
+
+// Workgroups behind the joining ones: bias_block.
 template <typename T>
-__global__ __launch_bounds__(256) void join_parts_kernel(const float* work, int parts, int rows, int cols, const float* alpha, T* out, int64_t ldo) {
+__global__ __launch_bounds__(256) void join_parts_kernel(const float* work, int parts, int rows, int cols, const float* alpha, T* out, int64_t ldo, unsigned joins, const BiasGradient bias) {
+  if (blockIdx.x >= joins) {
+    bias_block(bias, blockIdx.x - joins);
+    return;
+  }
   const int quads = (cols + 3) / 4;
   const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / quads, ldw = (int64_t)quads * 4;
   const int c = (int)(at % quads) * 4;
   if (row >= rows) return;
   f32x4 sum = *(const f32x4*)(work + row * ldw + c);
+#pragma unroll 4
   for (int p = 1; p < parts; ++p) sum += *(const f32x4*)(work + ((int64_t)p * rows + row) * ldw + c);
   sum *= *alpha;
   T* const to = out + row * ldo + c;
@@ -346,43 +394,42 @@ hipError_t launch_target_logits(int dtype, const TargetLogits& a, hipStream_t s)
 
 hipError_t launch_row_loss(const RowLoss& a, hipStream_t s) {
   const int entries = a.t.top ? (a.t.k | 1) * (int)sizeof(float2) : 0;
-  if (a.rows <= 256 || a.t.k > 256) row_loss_kernel<256><<<a.rows, 256, entries, s>>>(a);
-  else row_loss_kernel<16><<<blocks(a.rows, 16), 256, 16 * entries, s>>>(a);
+  const unsigned clears = a.fixed ? blocks(a.classes, 2048) : 0;
+  if (a.rows <= 256 ? a.spans > 512 : a.t.k > 256) row_loss_kernel<256><<<a.rows + clears, 256, entries, s>>>(a);
+  else if (a.rows <= 256) row_loss_kernel<64><<<blocks(a.rows, 4) + clears, 256, 4 * entries, s>>>(a);
+  else row_loss_kernel<16><<<blocks(a.rows, 16) + clears, 256, 16 * entries, s>>>(a);
   return hipGetLastError();
 }
 
+static unsigned all_rows_blocks(const AllRows& a) { return 1 + (a.xz ? blocks((int64_t)a.rows * ((a.dim + 7) / 8), 256) : 0); }
 hipError_t launch_all_rows(int dtype, const AllRows& a, hipStream_t s) {
-  const unsigned pads = a.xz ? blocks((int64_t)a.rows * ((a.dim + 7) / 8), 256) : 0, clears = a.fixed ? blocks(a.classes, 2048) : 0;
-  if (dtype == 1) all_rows_kernel<bf16><<<1 + pads + clears, 256, 0, s>>>(a, (int)pads);
-  else all_rows_kernel<float><<<1 + pads + clears, 256, 0, s>>>(a, (int)pads);
+  if (dtype == 1) all_rows_kernel<bf16><<<all_rows_blocks(a), 256, 0, s>>>(a);
+  else all_rows_kernel<float><<<all_rows_blocks(a), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
 // Rows of a workgroup of kept_prob_kernel: few where there are few, so that there are workgroups.
-int kept_sum_parts(int rows) { return (int)blocks(rows, rows >= 1024 ? 64 : 16); }
+int kept_sum_parts(int rows) { return (int)blocks(rows, rows >= 1024 ? 64 : rows >= 128 ? 16 : 4); }
 
-hipError_t launch_kept_prob(const TargetFix& a, const float* z, int64_t ldz, const int32_t* labels, hipStream_t s) {
+hipError_t launch_kept_prob(const TargetFix& a, const float* z, int64_t ldz, const int32_t* labels, const AllRows* all, hipStream_t s) {
   // each workgroup looks through its rows' targets: a few of them
   const bool fix = a.t.k <= 16;
-  const dim3 grid(blocks(a.columns, 512), kept_sum_parts(a.rows));
-  if (a.rows >= 1024) {
-    if (a.dtype == 1) kept_prob_kernel<bf16, 16><<<grid, 256, 0, s>>>(a, z, ldz, labels, fix);
-    else kept_prob_kernel<float, 16><<<grid, 256, 0, s>>>(a, z, ldz, labels, fix);
-  } else {
-    if (a.dtype == 1) kept_prob_kernel<bf16, 4><<<grid, 256, 0, s>>>(a, z, ldz, labels, fix);
-    else kept_prob_kernel<float, 4><<<grid, 256, 0, s>>>(a, z, ldz, labels, fix);
-  }
+  const unsigned grid = blocks(a.columns, 512) * (unsigned)kept_sum_parts(a.rows) + (all ? all_rows_blocks(*all) : 0);
+  const AllRows more = all ? *all : AllRows{};
+  auto launch = [&](auto type, auto each) { kept_prob_kernel<decltype(type), decltype(each)::value><<<grid, 256, 0, s>>>(a, z, ldz, labels, fix, more); };
+  auto rows_of = [&](auto type) {
+    if (a.rows >= 1024) launch(type, std::integral_constant<int, 16>{});
+    else if (a.rows >= 128) launch(type, std::integral_constant<int, 4>{});
+    else launch(type, std::integral_constant<int, 1>{});
+  };
+  if (a.dtype == 1) rows_of(bf16{});
+  else rows_of(0.0f);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess || fix ? e : launch_target_fix(a, s);
 }
 
 hipError_t launch_target_fix(const TargetFix& a, hipStream_t s) {
   target_fix_kernel<<<blocks((int64_t)a.rows * a.t.k, 256), 256, 0, s>>>(a);
-  return hipGetLastError();
-}
-
-hipError_t launch_bias_gradient(const float* sums, int parts, const unsigned long long* fixed, int columns, const float* alpha, float* dbias, hipStream_t s) {
-  bias_gradient_kernel<<<blocks(columns, 32), 256, 0, s>>>(sums, parts, fixed, columns, alpha, dbias);
   return hipGetLastError();
 }
 
@@ -400,10 +447,11 @@ hipError_t launch_pad_rows(int dtype, const void* in, int64_t ldin, int rows, in
   return hipGetLastError();
 }
 
-hipError_t launch_join_parts(int dtype, const float* work, int parts, int rows, int cols, const float* alpha, void* out, int64_t ldo, hipStream_t s) {
-  const unsigned n = blocks((int64_t)rows * ((cols + 3) / 4), 256);
-  if (dtype == 1) join_parts_kernel<bf16><<<n, 256, 0, s>>>(work, parts, rows, cols, alpha, (bf16*)out, ldo);
-  else join_parts_kernel<float><<<n, 256, 0, s>>>(work, parts, rows, cols, alpha, (float*)out, ldo);
+hipError_t launch_join_parts(int dtype, const float* work, int parts, int rows, int cols, const float* alpha, void* out, int64_t ldo, const BiasGradient* bias, hipStream_t s) {
+  const unsigned n = blocks((int64_t)rows * ((cols + 3) / 4), 256), more = bias ? blocks(bias->columns, 32) : 0;
+  const BiasGradient b = bias ? *bias : BiasGradient{};
+  if (dtype == 1) join_parts_kernel<bf16><<<n + more, 256, 0, s>>>(work, parts, rows, cols, alpha, (bf16*)out, ldo, n, b);
+  else join_parts_kernel<float><<<n + more, 256, 0, s>>>(work, parts, rows, cols, alpha, (float*)out, ldo, n, b);
   return hipGetLastError();
 }
 

@@ -168,11 +168,12 @@ int run(const Call& c, void* workspace, hipStream_t s) {
     HIP_TRY(launch_class_product(c.dt, PRODUCT_STATS, g, s));
     stats += (int64_t)stats_spans(c.dt, c.rows, columns, c.dim) * c.rows;
   }
-  int32_t* const labels = c.t.top ? nullptr : (int32_t*)at(a.labels);
-  HIP_TRY(launch_row_loss(RowLoss{(const float2*)at(a.stats), a.spans, c.rows, c.classes, c.t, z, a.ldz, a.kept, zt, c.temperature * c.temperature, c.lse, c.losses, norm, p, labels}, s));
-  // (xz: the rows that count; 0 times what others hold may be NaN)
   unsigned long long* const all_fixed = c.dbias ? (unsigned long long*)at(a.fixed) : nullptr;
-  HIP_TRY(launch_all_rows(c.dt, AllRows{c.losses, norm, c.rows, c.classes, c.dim, c.scale * c.temperature, c.loss, alpha, c.x, c.ldx, c.dw ? at(a.xz) : nullptr, a.ldk, all_fixed}, s));
+  int32_t* const labels = c.t.top ? nullptr : (int32_t*)at(a.labels);
+  HIP_TRY(launch_row_loss(RowLoss{(const float2*)at(a.stats), a.spans, c.rows, c.classes, c.t, z, a.ldz, a.kept, zt, c.temperature * c.temperature, c.lse, c.losses, norm, p, labels, all_fixed}, s));
+  // (xz: the rows that count; 0 times what others hold may be NaN)
+  const AllRows all{c.losses, norm, c.rows, c.dim, c.scale * c.temperature, c.loss, alpha, c.x, c.ldx, c.dw ? at(a.xz) : nullptr, a.ldk};
+  if (!a.kept) HIP_TRY(launch_all_rows(c.dt, all, s));
   if (!grads) return SLP_OK;
 
   for (int first = 0; first < c.classes; first += a.piece) {
@@ -186,7 +187,7 @@ int run(const Call& c, void* workspace, hipStream_t s) {
     unsigned long long* const fixed = c.dbias ? all_fixed + first : nullptr;
     const TargetFix fix{c.t, c.rows, c.classes, c.dt, zt, p, norm, first, columns, at(a.P), a.ldp, fixed, sums};
     if (kept) {
-      HIP_TRY(launch_kept_prob(fix, z + first, a.ldz, labels, s));
+      HIP_TRY(launch_kept_prob(fix, z + first, a.ldz, labels, first == 0 ? &all : nullptr, s));
     } else {
       ClassProduct g{};
       g.a = x;
@@ -208,7 +209,13 @@ int run(const Call& c, void* workspace, hipStream_t s) {
       HIP_TRY(launch_class_product(c.dt, PRODUCT_PROB, g, s));
       HIP_TRY(launch_target_fix(fix, s));
     }
-    if (c.dbias) HIP_TRY(launch_bias_gradient(sums, kept ? kept_sum_parts(c.rows) : sum_parts(c.dt, c.rows, columns, c.dim), fixed, columns, alpha, c.dbias + first, s));
+    const BiasGradient bias{sums, kept ? kept_sum_parts(c.rows) : sum_parts(c.dt, c.rows, columns, c.dim), columns, fixed, alpha, c.dbias + first};
+    bool bias_left = c.dbias;              // (goes along with the first joining of parts)
+    auto join = [&](int dt, const float* work, int parts, int rows, void* out, int64_t ldo) -> int {
+      HIP_TRY(launch_join_parts(dt, work, parts, rows, c.dim, alpha, out, ldo, bias_left ? &bias : nullptr, s));
+      bias_left = false;
+      return SLP_OK;
+    };
     if (c.dx) {
       ClassProduct o{};
       o.a = at(a.P);
@@ -229,7 +236,7 @@ int run(const Call& c, void* workspace, hipStream_t s) {
         o.out_dtype = c.dt;
       }
       HIP_TRY(launch_class_product(c.dt, PRODUCT_DX, o, s));
-      if (o.work && last) HIP_TRY(launch_join_parts(c.dt, o.work, o.parts, c.rows, c.dim, alpha, c.dx, c.lddx, s));
+      if (o.work && last) SLP_CHECK(join(c.dt, o.work, o.parts, c.rows, c.dx, c.lddx));
     }
     if (c.dw) {
       char* const dw = (char*)c.dw + (int64_t)first * c.lddw * (int64_t)size_of(c.dw_dt);
@@ -251,8 +258,9 @@ int run(const Call& c, void* workspace, hipStream_t s) {
         o.out_dtype = c.dw_dt;
       }
       HIP_TRY(launch_class_product(c.dt, PRODUCT_DW, o, s));
-      if (o.work) HIP_TRY(launch_join_parts(c.dw_dt, o.work, o.parts, columns, c.dim, alpha, dw, c.lddw, s));
+      if (o.work) SLP_CHECK(join(c.dw_dt, o.work, o.parts, columns, dw, c.lddw));
     }
+    if (bias_left) SLP_CHECK(join(c.dt, nullptr, 0, 0, nullptr, 0));
   }
   return SLP_OK;
 }
