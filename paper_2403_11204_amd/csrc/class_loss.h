@@ -17,7 +17,8 @@ namespace slp {
 //   PRODUCT_DW     P^T x: both do, A as [K][lda], B as [K][ldb]; either: alpha s to a matrix of either type, or s to (or added to) partial sums, one matrix for each
 //                  part of the contraction
 // An operand that lies the other way has its columns' last 16 bytes to itself, and is smaller than 2 GiB.
-enum { PRODUCT_STATS = 0, PRODUCT_PROB = 1, PRODUCT_DX = 2, PRODUCT_DW = 3 };
+//   PRODUCT_Z      partial sums of rows of x against classes, of few tiles with a long contraction
+enum { PRODUCT_STATS = 0, PRODUCT_PROB = 1, PRODUCT_DX = 2, PRODUCT_DW = 3, PRODUCT_Z = 4 };
 struct ClassProduct {
   const void *a, *b;
   int64_t lda, ldb;
@@ -35,7 +36,7 @@ struct ClassProduct {
   void* p;                  // [M][ldp], written up to the next 8 columns
   int64_t ldp;
   float* sums;              // [sum_parts(M, N, K)][N], may be null
-  // DX and DW
+  // DX, DW and Z
   void* out;                // [M][ldo] of out_dtype, any alignment
   int64_t ldo;
   int out_dtype;
@@ -46,6 +47,7 @@ struct ClassProduct {
 };
 // parts of a product's contraction that fill the chip: for PRODUCT_DX and PRODUCT_DW
 int class_parts(int dtype, int M, int N, int K);
+int z_parts(int dtype, int M, int N, int K);      // 0: PRODUCT_STATS
 int stats_spans(int dtype, int M, int N, int K);
 int sum_parts(int dtype, int M, int N, int K);
 hipError_t launch_class_product(int dtype, int kind, const ClassProduct& g, hipStream_t s);
@@ -72,13 +74,16 @@ struct TargetLogits {
 };
 hipError_t launch_target_logits(int dtype, const TargetLogits& a, hipStream_t s);
 
-// From the spans' statistics to each row's log-sum-exp, its loss, what its gradient needs.
+// From the spans' statistics, or from partial sums of the logits, to each row's log-sum-exp, its loss, what its gradient needs.
 struct RowLoss {
   const float2* stats;      // [spans][rows]
   int spans;
+  const float* work;        // not null: [parts][rows][classes rounded up to 4], the logits without bias; z, of all classes, is then written from them
+  int parts;
+  const float* bias;
   int rows, classes;
   Targets t;
-  const float* z;           // [rows][ldz]: the logits of classes below `kept`
+  float* z;                 // [rows][ldz]: the logits of classes below `kept`
   int64_t ldz;
   int kept;
   float* zt;                // [rows][k]: of the others; written where kept
@@ -89,12 +94,15 @@ struct RowLoss {
                             // together at the first of them, -1 at the others; 0 where none counts
   int32_t* labels;          // [rows], may be null: the row's class or -1
   unsigned long long* fixed;      // [classes], may be null: cleared on the way
+  double2* means;           // [row_groups(this)]: sum of the losses and number of the rows that count, of a group of rows
 };
 hipError_t launch_row_loss(const RowLoss& a, hipStream_t s);
+int row_groups(const RowLoss& a);
 // What follows from all rows: *loss = mean of those that count (0 where none does), *alpha = scale / their number (0); xz = the rows of x, zeros for those that do not
-// count and up to the next multiple of 8 columns (may be null)
+// count and up to the next multiple of 8 columns (may be null; x null: it holds the others already)
 struct AllRows {
-  const float* losses;
+  const double2* means;     // of `groups` groups of rows
+  int groups;
   const float2* norm;
   int rows, dim;
   float scale;
@@ -121,7 +129,7 @@ struct TargetFix {
 hipError_t launch_target_fix(const TargetFix& a, hipStream_t s);
 // P of a piece whose logits are kept, targets and all, and (all may be null) launch_all_rows on the way: rows [rows][ldz] of z from the piece's first class on; sums: as PRODUCT_PROB's, kept_sum_parts(rows) of them
 hipError_t launch_kept_prob(const TargetFix& a, const float* z, int64_t ldz, const int32_t* labels, const AllRows* all, hipStream_t s);
-int kept_sum_parts(int rows);
+int kept_sum_parts(int rows, int columns);
 
 // dbias[c] = alpha (sum over the parts of sums[part][c] + fixed[c] 2^-40)
 struct BiasGradient {

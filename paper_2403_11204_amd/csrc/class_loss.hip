@@ -125,7 +125,32 @@ __global__ __launch_bounds__(256) void row_loss_kernel(const RowLoss a) {
     return mine;
   };
   float2 mine = {-INFINITY, 0.0f};
-  if (in) {
+  if (a.work) {
+    // four classes at a time; then once more, from what this thread has written itself
+    const int64_t ldw = (a.classes + 3) & ~3;
+    const float* const work = a.work + row * ldw;
+    float* const z = a.z + row * a.ldz;
+    if (in)
+      for (int c = 4 * s; c < a.classes; c += 4 * TEAM) {
+        f32x4 v = *(const f32x4*)(work + c);
+#pragma unroll 8
+        for (int p = 1; p < a.parts; ++p) v += *(const f32x4*)(work + p * a.rows * ldw + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = c + e < a.classes ? (v[e] + (a.bias ? a.bias[c + e] : 0.0f)) * a.t.per_t : -INFINITY;
+          mine.x = fmaxf(mine.x, v[e]);
+        }
+        *(f32x4*)(z + c) = v;
+      }
+    const float most = all(mine).x, from = most == -INFINITY ? 0.0f : most;
+    mine.x = most;
+    if (in)
+      for (int c = 4 * s; c < a.classes; c += 4 * TEAM) {
+        const f32x4 v = *(const f32x4*)(z + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine.y += expf(v[e] - from);
+      }
+  } else if (in) {
     int i = s;
     for (; i + 3 * TEAM < a.spans; i += 4 * TEAM) {        // four loads under way
       float2 v[4];
@@ -190,6 +215,18 @@ __global__ __launch_bounds__(256) void row_loss_kernel(const RowLoss a) {
     a.losses[row] = counts ? loss : 0.0f;
     a.norm[row] = float2{!counts ? INFINITY : mine.x == INFINITY ? NAN : mine.x, 1.0f / mine.y};
   }
+  // of this workgroup's rows, in their order
+  __shared__ double2 group[ROWS];
+  if (s == 0) group[r] = in && counts ? double2{(double)loss, 1.0} : double2{0.0, 0.0};
+  __syncthreads();
+  if (t > 0) return;
+  double2 sum = group[0];
+#pragma unroll
+  for (int i = 1; i < ROWS; ++i) {
+    sum.x += group[i].x;
+    sum.y += group[i].y;
+  }
+  a.means[blockIdx.x] = sum;
 }
 
 // Block 0: the mean.  The others: 2048 elements each of xz's rows.
@@ -197,46 +234,31 @@ template <typename T>
 __device__ __forceinline__ void all_rows_block(const AllRows& a, int block) {
   const int t = threadIdx.x;
   if (block == 0) {
-    __shared__ double sums[4];
-    __shared__ int counts[4];
-    double sum = 0.0;
-    int n = 0;
-    for (int i0 = t; i0 < a.rows; i0 += 2048) {         // eight loads under way
-      float loss[8], peak[8];
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const int i = i0 + 256 * q;
-        loss[q] = i < a.rows ? a.losses[i] : 0.0f;
-        peak[q] = i < a.rows ? a.norm[i].x : INFINITY;
-      }
-#pragma unroll
-      for (int q = 0; q < 8; ++q)
-        if (peak[q] != INFINITY) {
-          sum += (double)loss[q];
-          ++n;
-        }
+    __shared__ double2 sums[4];
+    double2 sum = {0.0, 0.0};
+#pragma unroll 4
+    for (int i = t; i < a.groups; i += 256) {
+      const double2 m = a.means[i];
+      sum.x += m.x;
+      sum.y += m.y;
     }
     for (int step = 32; step > 0; step >>= 1) {
-      sum += __shfl_xor(sum, step);
-      n += __shfl_xor(n, step);
+      sum.x += __shfl_xor(sum.x, step);
+      sum.y += __shfl_xor(sum.y, step);
     }
-    if ((t & 63) == 0) {
-      sums[t >> 6] = sum;
-      counts[t >> 6] = n;
-    }
+    if ((t & 63) == 0) sums[t >> 6] = sum;
     __syncthreads();
     if (t == 0) {
-      sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-      n = counts[0] + counts[1] + counts[2] + counts[3];
-      *a.loss = n ? (float)(sum / n) : 0.0f;
-      *a.alpha = n ? a.scale / (float)n : 0.0f;
+      const double n = (sums[0].y + sums[1].y) + (sums[2].y + sums[3].y);
+      *a.loss = n > 0.0 ? (float)(((sums[0].x + sums[1].x) + (sums[2].x + sums[3].x)) / n) : 0.0f;
+      *a.alpha = n > 0.0 ? a.scale / (float)n : 0.0f;
     }
     return;
   }
   const int eights = (a.dim + 7) / 8;
   const int64_t at = (int64_t)(block - 1) * 256 + t, row = at / eights;
   const int c = (int)(at % eights) * 8;
-  if (row >= a.rows) return;
+  if (row >= a.rows || (!a.x && a.norm[row].x != INFINITY)) return;
   float v[8];
   load8((const T*)a.x + row * a.ldx + c, a.norm[row].x == INFINITY ? 0 : a.dim - c, v);
   store8((T*)a.xz + row * a.ldxz + c, 8, v);
@@ -328,34 +350,39 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const T* in, int64_t ldin
   store8(out + row * ldo + c, 8, v);
 }
 
-// 32 columns a workgroup, 8 strands of parts each, four loads under way.
-__device__ __forceinline__ void bias_block(const BiasGradient& a, int block) {
-  __shared__ double strand[8][32];
-  const int t = threadIdx.x, l = t & 31, s = t >> 5, c = block * 32 + l;
+// 32 columns a workgroup, 8 strands of parts each, or, of many parts, 8 columns and 32 strands; four loads under way.
+template <int COLS>
+__device__ __forceinline__ void bias_block(const BiasGradient& a, int block, double (&strand)[256]) {
+  constexpr int STRANDS = 256 / COLS;
+  const int t = threadIdx.x, l = t % COLS, s = t / COLS, c = block * COLS + l;
   double sum = 0.0;
   if (c < a.columns) {
     int i = s;
-    for (; i + 24 < a.parts; i += 32) {
+    for (; i + 3 * STRANDS < a.parts; i += 4 * STRANDS) {
       float v[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = a.sums[(int64_t)(i + 8 * q) * a.columns + c];
+      for (int q = 0; q < 4; ++q) v[q] = a.sums[(int64_t)(i + STRANDS * q) * a.columns + c];
       sum += ((double)v[0] + (double)v[1]) + ((double)v[2] + (double)v[3]);
     }
-    for (; i < a.parts; i += 8) sum += (double)a.sums[(int64_t)i * a.columns + c];
+    for (; i < a.parts; i += STRANDS) sum += (double)a.sums[(int64_t)i * a.columns + c];
   }
-  strand[s][l] = sum;
+  strand[t] = sum;
   __syncthreads();
   if (s > 0 || c >= a.columns) return;
   sum = (double)(long long)a.fixed[c] * (1.0 / 1099511627776.0);
-  for (int i = 0; i < 8; ++i) sum += strand[i][l];
+#pragma unroll
+  for (int i = 0; i < STRANDS; ++i) sum += strand[i * COLS + l];
   a.dbias[c] = (float)(sum * (double)*a.alpha);
 }
+__device__ __host__ __forceinline__ bool many_parts(const BiasGradient& a) { return a.parts >= 128; }
 
 // Workgroups behind the joining ones: bias_block.
 template <typename T>
 __global__ __launch_bounds__(256) void join_parts_kernel(const float* work, int parts, int rows, int cols, const float* alpha, T* out, int64_t ldo, unsigned joins, const BiasGradient bias) {
   if (blockIdx.x >= joins) {
-    bias_block(bias, blockIdx.x - joins);
+    __shared__ double strand[256];
+    if (many_parts(bias)) bias_block<8>(bias, blockIdx.x - joins, strand);
+    else bias_block<32>(bias, blockIdx.x - joins, strand);
     return;
   }
   const int quads = (cols + 3) / 4;
@@ -392,12 +419,19 @@ hipError_t launch_target_logits(int dtype, const TargetLogits& a, hipStream_t s)
   return hipGetLastError();
 }
 
+// Threads for each row of row_loss_kernel.
+static int team_of(const RowLoss& a) {
+  if (a.work) return a.classes > 512 ? 256 : 64;
+  if (a.rows <= 256) return a.spans > 512 ? 256 : 64;
+  return a.t.k > 256 ? 256 : 16;
+}
+int row_groups(const RowLoss& a) { return (int)blocks(a.rows, 256 / team_of(a)); }
 hipError_t launch_row_loss(const RowLoss& a, hipStream_t s) {
-  const int entries = a.t.top ? (a.t.k | 1) * (int)sizeof(float2) : 0;
-  const unsigned clears = a.fixed ? blocks(a.classes, 2048) : 0;
-  if (a.rows <= 256 ? a.spans > 512 : a.t.k > 256) row_loss_kernel<256><<<a.rows + clears, 256, entries, s>>>(a);
-  else if (a.rows <= 256) row_loss_kernel<64><<<blocks(a.rows, 4) + clears, 256, 4 * entries, s>>>(a);
-  else row_loss_kernel<16><<<blocks(a.rows, 16) + clears, 256, 16 * entries, s>>>(a);
+  const int team = team_of(a), entries = a.t.top ? 256 / team * (a.t.k | 1) * (int)sizeof(float2) : 0;
+  const unsigned grid = (unsigned)row_groups(a) + (a.fixed ? blocks(a.classes, 2048) : 0);
+  if (team == 256) row_loss_kernel<256><<<grid, 256, entries, s>>>(a);
+  else if (team == 64) row_loss_kernel<64><<<grid, 256, entries, s>>>(a);
+  else row_loss_kernel<16><<<grid, 256, entries, s>>>(a);
   return hipGetLastError();
 }
 
@@ -408,18 +442,23 @@ hipError_t launch_all_rows(int dtype, const AllRows& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Rows of a workgroup of kept_prob_kernel: few where there are few, so that there are workgroups.
-int kept_sum_parts(int rows) { return (int)blocks(rows, rows >= 1024 ? 64 : rows >= 128 ? 16 : 4); }
+// Rows that each wavefront of kept_prob_kernel takes: as few as make 512 workgroups (8192 x 47 24 us with 16, 8 with 4).
+static int each_of(int rows, int columns) {
+  const int64_t groups = (int64_t)blocks(columns, 512) * rows;
+  return groups >= 512 * 64 ? 16 : groups >= 512 * 16 || rows > 4096 ? 4 : 1;
+}
+int kept_sum_parts(int rows, int columns) { return (int)blocks(rows, 4 * each_of(rows, columns)); }
 
 hipError_t launch_kept_prob(const TargetFix& a, const float* z, int64_t ldz, const int32_t* labels, const AllRows* all, hipStream_t s) {
   // each workgroup looks through its rows' targets: a few of them
   const bool fix = a.t.k <= 16;
-  const unsigned grid = blocks(a.columns, 512) * (unsigned)kept_sum_parts(a.rows) + (all ? all_rows_blocks(*all) : 0);
+  const unsigned grid = blocks(a.columns, 512) * (unsigned)kept_sum_parts(a.rows, a.columns) + (all ? all_rows_blocks(*all) : 0);
   const AllRows more = all ? *all : AllRows{};
   auto launch = [&](auto type, auto each) { kept_prob_kernel<decltype(type), decltype(each)::value><<<grid, 256, 0, s>>>(a, z, ldz, labels, fix, more); };
   auto rows_of = [&](auto type) {
-    if (a.rows >= 1024) launch(type, std::integral_constant<int, 16>{});
-    else if (a.rows >= 128) launch(type, std::integral_constant<int, 4>{});
+    const int each = each_of(a.rows, a.columns);
+    if (each == 16) launch(type, std::integral_constant<int, 16>{});
+    else if (each == 4) launch(type, std::integral_constant<int, 4>{});
     else launch(type, std::integral_constant<int, 1>{});
   };
   if (a.dtype == 1) rows_of(bf16{});
@@ -448,7 +487,7 @@ hipError_t launch_pad_rows(int dtype, const void* in, int64_t ldin, int rows, in
 }
 
 hipError_t launch_join_parts(int dtype, const float* work, int parts, int rows, int cols, const float* alpha, void* out, int64_t ldo, const BiasGradient* bias, hipStream_t s) {
-  const unsigned n = blocks((int64_t)rows * ((cols + 3) / 4), 256), more = bias ? blocks(bias->columns, 32) : 0;
+  const unsigned n = blocks((int64_t)rows * ((cols + 3) / 4), 256), more = bias ? blocks(bias->columns, many_parts(*bias) ? 8 : 32) : 0;
   const BiasGradient b = bias ? *bias : BiasGradient{};
   if (dtype == 1) join_parts_kernel<bf16><<<n + more, 256, 0, s>>>(work, parts, rows, cols, alpha, (bf16*)out, ldo, n, b);
   else join_parts_kernel<float><<<n + more, 256, 0, s>>>(work, parts, rows, cols, alpha, (float*)out, ldo, n, b);

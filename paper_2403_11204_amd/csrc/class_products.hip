@@ -2,6 +2,7 @@
 //
 //   STATS  z = (x W^T + b) / T, tile by tile; a row's largest z and sum of exp(z - largest) over each wavefront's columns leave the chip, and z where it is kept
 //   PROB   z again, p = softmax(z) for a piece of the classes, row-major and transposed
+//   Z      x W^T over parts of the contraction, where there are few tiles and it is long
 //   DX     P W, a contraction over the piece's classes, split over the chip where there are few tiles
 //   DW     P^T x, over the rows
 // W lies in DX, and both operands in DW, with a row for each step of the contraction: their tiles are read transposed from LDS, so that nothing has to be
@@ -104,7 +105,7 @@ __device__ __forceinline__ void finish(const ClassProduct& g, f32x4 (&acc)[MI][N
   const int lgrp = lane >> 4, lrow = lane & 15;
   if constexpr (KIND >= PRODUCT_DX) {
     // (float32, see Side::fragments: rows that lie the other way are dealt out one by one, columns 4 NI side by side to a lane)
-    constexpr bool AROUND = sizeof(T) == 4 && KIND == PRODUCT_DW, BROUND = sizeof(T) == 4;
+    constexpr bool AROUND = sizeof(T) == 4 && KIND == PRODUCT_DW, BROUND = sizeof(T) == 4 && KIND != PRODUCT_Z;
     auto row = [&](int i) { return AROUND ? m0 + MI * lrow + i : m0 + 16 * i + lrow; };
     auto col = [&](int j) { return BROUND ? n0 + 4 * NI * lgrp + 4 * j : n0 + 16 * j + 4 * lgrp; };
     if (g.work) {
@@ -333,7 +334,7 @@ __global__ __launch_bounds__(256 * NG) void class_tile_kernel(const ClassProduct
 #if defined(__HIP_DEVICE_COMPILE__)
   extern __shared__ __attribute__((aligned(16))) unsigned char all_smem[];
   constexpr int BK = 128 / (int)sizeof(T), A_BYTES = BM * 128, STAGE = (BM + BN) * 128, NLD = (BM + BN) / 32, MI = BM / 32, NI = BN / 32;
-  constexpr bool KMA = KIND == PRODUCT_DW, KMB = KIND >= PRODUCT_DX;
+  constexpr bool KMA = KIND == PRODUCT_DW, KMB = KIND == PRODUCT_DX || KMA;
   const int group = NG > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
   unsigned char* const smem = all_smem + group * (NS * STAGE);
   int tm, tn;
@@ -419,7 +420,7 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
     const int64_t lda = g.lda * 2, ldb = g.ldb * 2, from = (int64_t)blockIdx.y * kper * 128, all = (int64_t)g.K * 2 - from, part = (int64_t)kper * 128;
     const int K = all <= 0 ? 0 : (int)(all < part ? all : part);
     const int64_t at = all <= 0 ? 0 : from;
-    constexpr bool KMA = KIND == PRODUCT_DW, KMB = KIND >= PRODUCT_DX;
+    constexpr bool KMA = KIND == PRODUCT_DW, KMB = KIND == PRODUCT_DX || KMA;
     long_tile<f32x4, false, KMA, KMB>(acc, smem, (const char*)g.a + (KMA ? at / 2 * lda + m0 * 2 : m0 * lda + at), (const char*)g.b + (KMB ? at / 2 * ldb + n0 * 2 : n0 * ldb + at), lda, ldb, g.M - m0 < 256 ? g.M - m0 : 256, g.N - n0 < 256 ? g.N - n0 : 256, K);
   }
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, wm = w & 1, wn = w >> 1, lgrp = lane >> 4, lrow = lane & 15;
@@ -641,6 +642,7 @@ hipError_t launch_type(int dtype, int kind, const ClassProduct& g, hipStream_t s
   switch (kind) {
     case PRODUCT_STATS: return launch_kind<T, PRODUCT_STATS>(dtype, g, s);
     case PRODUCT_PROB: return launch_kind<T, PRODUCT_PROB>(dtype, g, s);
+    case PRODUCT_Z: return launch_kind<T, PRODUCT_Z>(dtype, g, s);
     case PRODUCT_DX: return launch_kind<T, PRODUCT_DX>(dtype, g, s);
     default: return launch_kind<T, PRODUCT_DW>(dtype, g, s);
   }
@@ -663,6 +665,15 @@ int class_parts(int dtype, int M, int N, int K) {
   return p < 1 ? 1 : p;
 }
 
+// Parts of a contraction whose few tiles would leave most of the chip waiting for a long one, where the partial sums are few: 2 x 64 x 4096 float32 35 us in one, 6 in 16.
+int z_parts(int dtype, int M, int N, int K) {
+  const int nk = (K + (dtype == 1 ? 63 : 31)) / (dtype == 1 ? 64 : 32);
+  if (nk < 32 || tiles_of(M, N, 128, 128) >= 200) return 0;
+  int parts = class_parts(dtype, M, N, K);
+  if (parts > nk / 8) parts = nk / 8;
+  return parts < 2 || (int64_t)M * N * parts > 1 << 23 ? 0 : parts;
+}
+
 int stats_spans(int dtype, int M, int N, int K) {
   const int w = span_columns(shape_of(dtype, M, N, K));
   return (N + 2 * w - 1) / (2 * w) * 2;
@@ -675,7 +686,7 @@ int sum_parts(int dtype, int M, int N, int K) {
 hipError_t launch_class_product(int dtype, int kind, const ClassProduct& g, hipStream_t s) {
   const int64_t es = dtype == 1 ? 2 : 4;
   // a tile's rows, or an operand that lies the other way, are addressed with 32-bit offsets
-  const int64_t rows_a = kind == PRODUCT_DW ? g.K : 256, rows_b = kind >= PRODUCT_DX ? g.K : 256;
+  const int64_t rows_a = kind == PRODUCT_DW ? g.K : 256, rows_b = kind == PRODUCT_DX || kind == PRODUCT_DW ? g.K : 256;
   if (g.M <= 0 || g.N <= 0 || g.K <= 0 || rows_a * g.lda * es >= 0x7FFFFF00 || rows_b * g.ldb * es >= 0x7FFFFF00) return hipErrorInvalidValue;
   if ((((uintptr_t)g.a | (uintptr_t)g.b) & 15) || g.lda * es % 16 || g.ldb * es % 16) return hipErrorInvalidValue;
   return dtype == 1 ? launch_type<bf16>(dtype, kind, g, s) : launch_type<float>(dtype, kind, g, s);

@@ -52,8 +52,8 @@ struct Plan {
   bool copy_x, copy_w;
   int piece, kept;                      // classes of a piece; those whose logits are kept, whole pieces
   int64_t ldz;
-  int dx_parts, dw_parts, spans;
-  size_t zt, p, labels, norm, alpha, stats, xc, wc, xz, z, P, dx_work, dw_work, sums, fixed, bytes;
+  int dx_parts, dw_parts, z_parts, spans;
+  size_t zt, p, labels, norm, alpha, means, stats, xc, wc, xz, z, z_work, P, dx_work, dw_work, sums, fixed, bytes;
 };
 
 // Whether the products can read a matrix in place.
@@ -76,7 +76,8 @@ Plan plan_of(const Call& c) {
   a.piece = wanted == 1 ? c.classes : ((c.classes + wanted - 1) / wanted + 255) / 256 * 256;
   const int pieces = (c.classes + a.piece - 1) / a.piece;
   a.ldp = row_ld(a.piece, a.es);
-  if (grads) {
+  if (pieces == 1) a.z_parts = z_parts(c.dt, c.rows, c.classes, c.dim);
+  if (grads || a.z_parts) {
     const int64_t fit = kKeptBytes / ((int64_t)c.rows * 4);
     a.kept = fit >= c.classes ? c.classes : (int)(fit / a.piece) * a.piece;
     a.ldz = row_ld(a.kept, 4);
@@ -97,18 +98,21 @@ Plan plan_of(const Call& c) {
   a.labels = take(!c.t.top, r * 4);
   a.norm = take(true, r * 8);
   a.alpha = take(true, 4);
-  a.stats = take(true, (int64_t)a.spans * r * 8);
+  a.means = take(true, r * 16);
+  a.stats = take(a.z_parts == 0, (int64_t)a.spans * r * 8);
   a.xc = take(a.copy_x, r * a.ldk * a.es);
   a.wc = take(a.copy_w, (int64_t)a.piece * a.ldk * a.es);
-  a.xz = take(c.dw, r * a.ldk * a.es);
+  a.xz = a.copy_x ? a.xc : take(c.dw, r * a.ldk * a.es);
   a.z = take(a.kept > 0, r * a.ldz * 4);
+  a.z_work = take(a.z_parts > 0, a.z_parts * r * ((c.classes + 3) / 4 * 4) * 4);
   a.P = take(grads, r * a.ldp * a.es);
   a.dx_work = take(c.dx && (pieces > 1 || a.dx_parts > 1), (int64_t)a.dx_parts * r * dq * 4);
   a.dw_work = take(c.dw && a.dw_parts > 1, (int64_t)a.dw_parts * a.piece * dq * 4);
   // sums of a piece's columns, over as many parts of the rows as the widest kernel makes
   const int64_t rest = c.classes - (int64_t)(pieces - 1) * a.piece, most_sums = (int64_t)sum_parts(c.dt, c.rows, a.piece, c.dim) * a.piece;
   const int64_t rest_sums = rest > 0 ? sum_parts(c.dt, c.rows, (int)rest, c.dim) * rest : 0;      // (smaller tiles, more parts)
-  const int64_t kept_sums = (int64_t)kept_sum_parts(c.rows) * a.piece, gemm_sums = most_sums > rest_sums ? most_sums : rest_sums;
+  const int64_t kept_piece = (int64_t)kept_sum_parts(c.rows, a.piece) * a.piece, kept_rest = rest > 0 ? kept_sum_parts(c.rows, (int)rest) * rest : 0;
+  const int64_t kept_sums = kept_piece > kept_rest ? kept_piece : kept_rest, gemm_sums = most_sums > rest_sums ? most_sums : rest_sums;
   a.sums = take(c.dbias, (kept_sums > gemm_sums ? kept_sums : gemm_sums) * 4);
   a.fixed = take(c.dbias, (int64_t)c.classes * 8);
   a.bytes = at;
@@ -165,15 +169,20 @@ int run(const Call& c, void* workspace, hipStream_t s) {
       g.zcols = a.kept - first < columns ? a.kept - first : columns;
     }
     g.parts = 1;
-    HIP_TRY(launch_class_product(c.dt, PRODUCT_STATS, g, s));
+    if (a.z_parts) {                     // (one piece: all classes)
+      g.work = (float*)at(a.z_work);
+      g.parts = a.z_parts;
+    }
+    HIP_TRY(launch_class_product(c.dt, a.z_parts ? PRODUCT_Z : PRODUCT_STATS, g, s));
     stats += (int64_t)stats_spans(c.dt, c.rows, columns, c.dim) * c.rows;
   }
   unsigned long long* const all_fixed = c.dbias ? (unsigned long long*)at(a.fixed) : nullptr;
   int32_t* const labels = c.t.top ? nullptr : (int32_t*)at(a.labels);
-  HIP_TRY(launch_row_loss(RowLoss{(const float2*)at(a.stats), a.spans, c.rows, c.classes, c.t, z, a.ldz, a.kept, zt, c.temperature * c.temperature, c.lse, c.losses, norm, p, labels, all_fixed}, s));
+  const RowLoss each{(const float2*)at(a.stats), a.spans, a.z_parts ? (const float*)at(a.z_work) : nullptr, a.z_parts, c.bias, c.rows, c.classes, c.t, z, a.ldz, a.kept, zt, c.temperature * c.temperature, c.lse, c.losses, norm, p, labels, all_fixed, (double2*)at(a.means)};
+  HIP_TRY(launch_row_loss(each, s));
   // (xz: the rows that count; 0 times what others hold may be NaN)
-  const AllRows all{c.losses, norm, c.rows, c.dim, c.scale * c.temperature, c.loss, alpha, c.x, c.ldx, c.dw ? at(a.xz) : nullptr, a.ldk};
-  if (!a.kept) HIP_TRY(launch_all_rows(c.dt, all, s));
+  const AllRows all{each.means, row_groups(each), norm, c.rows, c.dim, c.scale * c.temperature, c.loss, alpha, a.copy_x ? nullptr : c.x, c.ldx, c.dw ? at(a.xz) : nullptr, a.ldk};
+  if (!a.kept || !grads) HIP_TRY(launch_all_rows(c.dt, all, s));
   if (!grads) return SLP_OK;
 
   for (int first = 0; first < c.classes; first += a.piece) {
@@ -209,7 +218,7 @@ int run(const Call& c, void* workspace, hipStream_t s) {
       HIP_TRY(launch_class_product(c.dt, PRODUCT_PROB, g, s));
       HIP_TRY(launch_target_fix(fix, s));
     }
-    const BiasGradient bias{sums, kept ? kept_sum_parts(c.rows) : sum_parts(c.dt, c.rows, columns, c.dim), columns, fixed, alpha, c.dbias + first};
+    const BiasGradient bias{sums, kept ? kept_sum_parts(c.rows, columns) : sum_parts(c.dt, c.rows, columns, c.dim), columns, fixed, alpha, c.dbias + first};
     bool bias_left = c.dbias;              // (goes along with the first joining of parts)
     auto join = [&](int dt, const float* work, int parts, int rows, void* out, int64_t ldo) -> int {
       HIP_TRY(launch_join_parts(dt, work, parts, rows, c.dim, alpha, out, ldo, bias_left ? &bias : nullptr, s));
