@@ -31,7 +31,7 @@ struct ClassProduct {
   int64_t ldz;
   int zcols;
   const float2* norm;       // [M]: the row's largest z (+infinity: the row does not count, its P is zero), 1 / its sum of exp(z - that)
-  const int32_t* labels;    // [M], may be null: class whose P is zero and is left out of the sums (the caller writes it)
+  const int32_t* labels;    // [M], may be null: class from whose probability 1 is taken
   int label0;               // column 0's class
   void* p;                  // [M][ldp], written up to the next 8 columns
   int64_t ldp;
@@ -114,7 +114,7 @@ struct AllRows {
 };
 hipError_t launch_all_rows(int dtype, const AllRows& a, hipStream_t s);
 
-// P at the targets: softmax - (the probability of all the row's entries of that class), in classes [first, first + columns)
+// A distillation's targets: softmax - (the probability of all the row's entries of that class) to P, in classes [first, first + columns)
 struct TargetFix {
   Targets t;
   int rows, classes, dtype;
@@ -124,12 +124,13 @@ struct TargetFix {
   void* P;
   int64_t ldp;
   unsigned long long* fixed;      // [columns], may be null: what the targets add to the sums of P's columns, in units of 2^-40 ...
-  float* sums;                    // ... and the sums, where that is NaN
+  float* sums;                    // ... and the sums, NaN where that is (may be null)
 };
 hipError_t launch_target_fix(const TargetFix& a, hipStream_t s);
 // P of a piece whose logits are kept, targets and all, and (all may be null) launch_all_rows on the way: rows [rows][ldz] of z from the piece's first class on; sums: as PRODUCT_PROB's, kept_sum_parts(rows) of them
 hipError_t launch_kept_prob(const TargetFix& a, const float* z, int64_t ldz, const int32_t* labels, const AllRows* all, hipStream_t s);
 int kept_sum_parts(int rows, int columns);
+bool fixes_targets(int k, int columns);       // whether it does without `fixed`
 
 // dbias[c] = alpha (sum over the parts of sums[part][c] + fixed[c] 2^-40)
 struct BiasGradient {

@@ -268,30 +268,33 @@ __global__ __launch_bounds__(256) void all_rows_kernel(const AllRows a) {
   all_rows_block<T>(a, blockIdx.x);
 }
 
-// Entry j of a row, the first of its class, where that is one of the columns [col0, col1).
-// sums: a part of the columns' sums that is there already.
-__device__ __forceinline__ void fix_target(const TargetFix& a, int64_t row, int j, int col0, int col1, float* sums) {
+// A distillation's entry j of a row, the first of its class, where that is one of the columns [col0, col1): what all entries of that class leave of the probability goes to P, and
+// what they take from it, negative, to put(col, .).
+template <typename Put>
+__device__ __forceinline__ void fix_target(const TargetFix& a, int64_t row, int j, int col0, int col1, Put put) {
   const int c = class_of(a.t, row, j, a.classes), col = c - a.first;
   if (c < 0 || col < col0 || col >= col1) return;
   const float2 norm = a.norm[row];
   if (norm.x == INFINITY) return;
-  const float given = a.t.top ? a.p[row * a.t.k + j] : 1.0f;
+  const float given = a.p[row * a.t.k + j];
   if (given < 0.0f) return;
   // the probability less what is given, to a step of the larger one; of the result where both are near 1
   const float d = a.zt[row * a.t.k + j] - norm.x, v = given > 0.5f ? expm1f(d + logf(norm.y)) + (1.0f - given) : expf(d) * norm.y - given;
   if (a.dtype == 1) ((bf16*)a.P)[row * a.ldp + col] = (bf16)v;
   else ((float*)a.P)[row * a.ldp + col] = v;
-  // (integers: the order of the additions does not matter.  One class: the column's sum has left the target out, otherwise it holds the probability.)
-  if (a.fixed) {
-    const float add = a.t.top ? -given : v;
-    if (add != add) sums[col] = NAN;
-    else atomicAdd(a.fixed + col, (unsigned long long)(long long)rint((double)add * 1099511627776.0));
-  }
+  if (a.sums) put(col, -given);
 }
+// Sums in units of 2^-40: integers, so that the order of the additions does not matter.
+__device__ __forceinline__ unsigned long long units(float x) { return (unsigned long long)(long long)rint((double)x * 1099511627776.0); }
+__device__ __forceinline__ double of_units(unsigned long long u) { return (double)(long long)u * (1.0 / 1099511627776.0); }
 
 __global__ __launch_bounds__(256) void target_fix_kernel(const TargetFix a) {
   const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at < (int64_t)a.rows * a.t.k) fix_target(a, at / a.t.k, (int)(at % a.t.k), 0, a.columns, a.sums);
+  if (at >= (int64_t)a.rows * a.t.k) return;
+  fix_target(a, at / a.t.k, (int)(at % a.t.k), 0, a.columns, [&](int col, float x) {
+    if (x != x) a.sums[col] = NAN;
+    else atomicAdd(a.fixed + col, units(x));
+  });
 }
 
 // 512 columns by 4 EACH rows a workgroup, a lane 8 columns of EACH rows; then, where fix is set, the targets among them.  Workgroups behind those: all_rows_block.  Bound by memory: 4 bytes in, 2 or 4 out.
@@ -299,12 +302,13 @@ template <typename T, int EACH>
 __global__ __launch_bounds__(256) void kept_prob_kernel(const TargetFix a, const float* z, int64_t ldz, const int32_t* labels, bool fix, const AllRows all) {
   constexpr float kLog2e = 1.44269504088896340736f;
   __shared__ float sums[4][512];
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6, wide = (a.columns + 511) / 512, high = (a.rows + 4 * EACH - 1) / (4 * EACH);
+  __shared__ unsigned long long fixed[512];
+  const int wide = (a.columns + 511) / 512, high = (a.rows + 4 * EACH - 1) / (4 * EACH);
   if ((int)blockIdx.x >= wide * high) {
     all_rows_block<T>(all, blockIdx.x - wide * high);
     return;
   }
-  const int bx = blockIdx.x % wide, by = blockIdx.x / wide, col0 = bx * 512, c = col0 + lane * 8, row0 = by * 4 * EACH;
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, bx = blockIdx.x % wide, by = blockIdx.x / wide, col0 = bx * 512, c = col0 + lane * 8, row0 = by * 4 * EACH;
   float sum[8] = {};
   if (c < a.columns) {
 #pragma unroll 4
@@ -318,25 +322,31 @@ __global__ __launch_bounds__(256) void kept_prob_kernel(const TargetFix a, const
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         p[e] = __builtin_amdgcn_exp2f((u[e / 4][e % 4] - norm.x) * kLog2e) * norm.y;
-        if (norm.x == INFINITY || c + e == label || c + e >= a.columns) p[e] = 0.0f;       // (also where the row holds NaN)
+        if (c + e == label) p[e] = expm1f(u[e / 4][e % 4] - norm.x + logf(norm.y));              // (1 less, and exact where that is near 0)
+        if (norm.x == INFINITY || c + e >= a.columns) p[e] = 0.0f;                                // (also where the row holds NaN)
         sum[e] += p[e];
       }
       store8((T*)a.P + (int64_t)row * a.ldp + c, 8, p);
     }
   }
-  if (a.sums) {
+  if (!a.sums && !fix) return;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sums[w][lane * 8 + e] = sum[e];
-  }
+  for (int e = 0; e < 8; ++e) sums[w][lane * 8 + e] = sum[e];
+  for (int i = t; i < 512; i += 256) fixed[i] = 0;
   __syncthreads();                       // (what this workgroup has written is in order from here on)
-  if (a.sums) {
-    for (int i = t; i < 512; i += 256)
-      if (col0 + i < a.columns) a.sums[(int64_t)by * a.columns + col0 + i] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+  if (fix) {
+    const int rows = a.rows - row0 < 4 * EACH ? a.rows - row0 : 4 * EACH, col1 = col0 + 512 < a.columns ? col0 + 512 : a.columns;
+    for (int i = t; i < rows * a.t.k; i += 256)
+      fix_target(a, row0 + i / a.t.k, i % a.t.k, col0, col1, [&](int col, float x) {
+        if (x != x) sums[0][col - col0] = NAN;
+        else atomicAdd(&fixed[col - col0], units(x));
+      });
     __syncthreads();
   }
-  if (!fix) return;
-  const int rows = a.rows - row0 < 4 * EACH ? a.rows - row0 : 4 * EACH, col1 = col0 + 512 < a.columns ? col0 + 512 : a.columns;
-  for (int i = t; i < rows * a.t.k; i += 256) fix_target(a, row0 + i / a.t.k, i % a.t.k, col0, col1, a.sums + (int64_t)by * a.columns);
+  if (a.sums)
+    for (int i = t; i < 512; i += 256)
+      if (col0 + i < a.columns)
+        a.sums[(int64_t)by * a.columns + col0 + i] = (float)(((double)sums[0][i] + (double)sums[1][i]) + ((double)sums[2][i] + (double)sums[3][i]) + of_units(fixed[i]));
 }
 
 template <typename T>
@@ -369,7 +379,7 @@ __device__ __forceinline__ void bias_block(const BiasGradient& a, int block, dou
   strand[t] = sum;
   __syncthreads();
   if (s > 0 || c >= a.columns) return;
-  sum = (double)(long long)a.fixed[c] * (1.0 / 1099511627776.0);
+  sum = a.fixed ? of_units(a.fixed[c]) : 0.0;
 #pragma unroll
   for (int i = 0; i < STRANDS; ++i) sum += strand[i * COLS + l];
   a.dbias[c] = (float)(sum * (double)*a.alpha);
@@ -435,6 +445,10 @@ hipError_t launch_row_loss(const RowLoss& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Whether kept_prob_kernel sees to a distillation's targets itself, without `fixed`: as long as its workgroups do not look through too many of them too often.  5184 x 512 with 9:
+// additions to `fixed` from all over the chip, 90 to a class, took 9 us more.
+bool fixes_targets(int k, int columns) { return k <= 16 || columns <= 2048; }
+
 static unsigned all_rows_blocks(const AllRows& a) { return 1 + (a.xz ? blocks((int64_t)a.rows * ((a.dim + 7) / 8), 256) : 0); }
 hipError_t launch_all_rows(int dtype, const AllRows& a, hipStream_t s) {
   if (dtype == 1) all_rows_kernel<bf16><<<all_rows_blocks(a), 256, 0, s>>>(a);
@@ -450,8 +464,8 @@ static int each_of(int rows, int columns) {
 int kept_sum_parts(int rows, int columns) { return (int)blocks(rows, 4 * each_of(rows, columns)); }
 
 hipError_t launch_kept_prob(const TargetFix& a, const float* z, int64_t ldz, const int32_t* labels, const AllRows* all, hipStream_t s) {
-  // each workgroup looks through its rows' targets: a few of them
-  const bool fix = a.t.k <= 16;
+  // (each workgroup looks through all its rows' targets: few of them, or few workgroups beside each other)
+  const bool fix = a.t.top && fixes_targets(a.t.k, a.columns);
   const unsigned grid = blocks(a.columns, 512) * (unsigned)kept_sum_parts(a.rows, a.columns) + (all ? all_rows_blocks(*all) : 0);
   const AllRows more = all ? *all : AllRows{};
   auto launch = [&](auto type, auto each) { kept_prob_kernel<decltype(type), decltype(each)::value><<<grid, 256, 0, s>>>(a, z, ldz, labels, fix, more); };
@@ -464,7 +478,7 @@ hipError_t launch_kept_prob(const TargetFix& a, const float* z, int64_t ldz, con
   if (a.dtype == 1) rows_of(bf16{});
   else rows_of(0.0f);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess || fix ? e : launch_target_fix(a, s);
+  return e != hipSuccess || fix || !a.t.top ? e : launch_target_fix(a, s);
 }
 
 hipError_t launch_target_fix(const TargetFix& a, hipStream_t s) {

@@ -98,6 +98,12 @@ __device__ __forceinline__ float fmax_of_rows(float x) {
   return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
 }
 
+// The softmax at a logit; 1 less where the class is the row's, exact where that is near 0.
+__device__ __forceinline__ float probability(float z, float2 norm, bool label) {
+  if (label) return expm1f(z - norm.x + logf(norm.y));
+  return __builtin_amdgcn_exp2f((z - norm.x) * kLog2e) * norm.y;
+}
+
 // The tail of a wavefront's (16 MI) x (16 NI) sums at row m0, column n0: lane l holds in acc[i][j] the columns n0 + 16 j + 4 (l / 16) .. + 3 of row
 // m0 + 16 i + l % 16.
 template <typename T, int KIND, int MI, int NI>
@@ -198,8 +204,8 @@ __device__ __forceinline__ void finish(const ClassProduct& g, f32x4 (&acc)[MI][N
           f32x4 p;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            p[e] = __builtin_amdgcn_exp2f((acc[i][j][e] - norm[i].x) * kLog2e) * norm[i].y;
-            if (norm[i].x == INFINITY || n + e == label[i] || n + e >= g.N) p[e] = 0.0f;       // (also where the row holds NaN)
+            p[e] = probability(acc[i][j][e], norm[i], n + e == label[i]);
+            if (norm[i].x == INFINITY || n + e >= g.N) p[e] = 0.0f;       // (also where the row holds NaN)
           }
           sum += p;
           if (m < g.M && n < last_n) {
@@ -559,8 +565,8 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float z = (acc[i][j][e] + bias[e]) * g.per_t;
-          p[e] = __builtin_amdgcn_exp2f((z - norm[i].x) * kLog2e) * norm[i].y;
-          if (norm[i].x == INFINITY || n + e == label[i] || n + e >= g.N) p[e] = 0.0f;       // (also where the row holds NaN)
+          p[e] = probability(z, norm[i], n + e == label[i]);
+          if (norm[i].x == INFINITY || n + e >= g.N) p[e] = 0.0f;       // (also where the row holds NaN)
         }
         sum += p;
         stage(i, j, p);

@@ -49,7 +49,7 @@ struct Call {
 // Where everything lies in the workspace, and in which pieces the classes are taken.
 struct Plan {
   int64_t es, ldk, ldp;                 // operands' element size; leading dimensions of copies of x and W, of P
-  bool copy_x, copy_w;
+  bool copy_x, copy_w, fix;
   int piece, kept;                      // classes of a piece; those whose logits are kept, whole pieces
   int64_t ldz;
   int dx_parts, dw_parts, z_parts, spans;
@@ -114,7 +114,9 @@ Plan plan_of(const Call& c) {
   const int64_t kept_piece = (int64_t)kept_sum_parts(c.rows, a.piece) * a.piece, kept_rest = rest > 0 ? kept_sum_parts(c.rows, (int)rest) * rest : 0;
   const int64_t kept_sums = kept_piece > kept_rest ? kept_piece : kept_rest, gemm_sums = most_sums > rest_sums ? most_sums : rest_sums;
   a.sums = take(c.dbias, (kept_sums > gemm_sums ? kept_sums : gemm_sums) * 4);
-  a.fixed = take(c.dbias, (int64_t)c.classes * 8);
+  // a distillation's targets among pieces that do not see to them while they are turned into P
+  a.fix = c.dbias && c.t.top && (a.kept < c.classes || !fixes_targets(c.t.k, a.piece));
+  a.fixed = take(a.fix, (int64_t)c.classes * 8);
   a.bytes = at;
   return a;
 }
@@ -176,7 +178,7 @@ int run(const Call& c, void* workspace, hipStream_t s) {
     HIP_TRY(launch_class_product(c.dt, a.z_parts ? PRODUCT_Z : PRODUCT_STATS, g, s));
     stats += (int64_t)stats_spans(c.dt, c.rows, columns, c.dim) * c.rows;
   }
-  unsigned long long* const all_fixed = c.dbias ? (unsigned long long*)at(a.fixed) : nullptr;
+  unsigned long long* const all_fixed = a.fix ? (unsigned long long*)at(a.fixed) : nullptr;
   int32_t* const labels = c.t.top ? nullptr : (int32_t*)at(a.labels);
   const RowLoss each{(const float2*)at(a.stats), a.spans, a.z_parts ? (const float*)at(a.z_work) : nullptr, a.z_parts, c.bias, c.rows, c.classes, c.t, z, a.ldz, a.kept, zt, c.temperature * c.temperature, c.lse, c.losses, norm, p, labels, all_fixed, (double2*)at(a.means)};
   HIP_TRY(launch_row_loss(each, s));
@@ -193,7 +195,7 @@ int run(const Call& c, void* workspace, hipStream_t s) {
     int64_t ldw = 0;
     if (!kept || c.dx) SLP_CHECK(weights(first, columns, w, ldw));
     float* const sums = c.dbias ? (float*)at(a.sums) : nullptr;
-    unsigned long long* const fixed = c.dbias ? all_fixed + first : nullptr;
+    unsigned long long* const fixed = all_fixed ? all_fixed + first : nullptr;
     const TargetFix fix{c.t, c.rows, c.classes, c.dt, zt, p, norm, first, columns, at(a.P), a.ldp, fixed, sums};
     if (kept) {
       HIP_TRY(launch_kept_prob(fix, z + first, a.ldz, labels, first == 0 ? &all : nullptr, s));
@@ -216,7 +218,7 @@ int run(const Call& c, void* workspace, hipStream_t s) {
       g.sums = sums;
       g.parts = 1;
       HIP_TRY(launch_class_product(c.dt, PRODUCT_PROB, g, s));
-      HIP_TRY(launch_target_fix(fix, s));
+      if (c.t.top) HIP_TRY(launch_target_fix(fix, s));
     }
     const BiasGradient bias{sums, kept ? kept_sum_parts(c.rows, columns) : sum_parts(c.dt, c.rows, columns, c.dim), columns, fixed, alpha, c.dbias + first};
     bool bias_left = c.dbias;              // (goes along with the first joining of parts)
