@@ -368,25 +368,26 @@ int slp_clip_gradients(const void* const* tensors /*host*/, void* const* out /*h
                        float max_norm, float* norm_out /*device, may be NULL*/, void* workspace /*device*/, size_t workspace_bytes, slp_stream stream);
 
 /* ---- losses over the classes of a linear layer --------------------------------------------------
- * z = x W^T + b for rows x[rows][dim] and weights w[classes][dim] (both of dtype dt), bias float32 [classes] or NULL; the logits z are computed in pieces of the
- * classes and never kept as a whole: beside x, w and their gradients a call takes the workspace, at most some 256 MB for the logits' gradient of a piece and as much for
- * its transpose, where [rows][classes] of them would be needed four times over.  For each row
+ * z = x W^T + b for rows x[rows][dim] and weights w[classes][dim] (both of dtype dt), bias float32 [classes] or NULL.  The logits z are computed tile by tile and do not have to
+ * fit in memory: beside its operands and outputs a call takes a workspace of at most 1 GiB for logits that it keeps in float32 until their gradient is due (the others are
+ * computed again), 256 MB for the gradient of a piece of them, and what grows with rows x dim (the rows that count, partial sums of dx) and with rows x classes / 16 at most (statistics).  For each row
  *   lse = log sum over the classes of exp(z / T)                                      (float32 [rows], of rows that do not count as well)
  * slp_linear_cross_entropy (T = 1): targets[rows] are class ids (target_bytes 4 or 8: int32 or int64).  loss = lse - z_target.
  * slp_linear_distillation: top[rows][k] (dtype top_dt) are a teacher's logits of the classes top_classes[rows][k] (class_bytes 4 or 8), in any order, k from 1 to 1024,
  *   p = softmax(top / T) over the row's entries, loss = T^2 sum of p (log p - log softmax(z / T) at the entry's class).  A class may stand in several entries of a row, whose probabilities
- *   then add up.  0.001 <= T <= 1000.
+ *   then add up in the gradient.  0.001 <= T <= 1000.
  * An id outside [0, classes) is no class: the row of a cross-entropy, the entry of a distillation does not count (padding), nor does an entry whose top is -infinity.  A row
  * without an entry that counts has the loss 0, does not enter the mean, and its x reaches no output but its own lse, whatever it holds.
  * *loss = the mean of losses[rows] over the rows that count, 0 where none does.  The gradients, each wanted where its pointer is not NULL, are those of scale * *loss:
  *   dz = scale T (softmax(z / T) - p) / (rows that count);  dx[rows][dim] = dz W, of dtype dt;  dw[classes][dim] = dz^T x, of dtype dw_dt;  dbias (float32 [classes]) = sums of dz
- * Products add in float32; dz / (scale T / n) is rounded to dt where it enters the products for dx and dw (float32 operands: exact to 2^-24 as float32 arithmetic is).  Sums are in a fixed order: the same bits every time.
- * Logits that are NaN or +infinity make their row's loss, and what it reaches, NaN; -infinity (a class that the bias masks out) is a probability of 0.  Float32 operands
- * count as infinite from 2^127 (1 + 127/128) on, and a product with an infinity as NaN.
- * Matrices may start at any element; rows of x and w on 16-byte boundaries whose dim fills them are read in place, others are copied to the workspace first.  No rows: a loss of 0, dw and dbias
- * become zeros.  The workspace is 256-byte aligned, of slp_linear_loss_workspace_bytes for the same pointers and sizes; top: k of a distillation, 0 for a cross-entropy; outputs: SLP_LOSS_* of the gradients wanted.
+ * Products add in float32; dz over its common factor is rounded to dt where it enters the products for dx and dw, not for dbias.  Float32 operands are multiplied to 2^-24 as float32 arithmetic
+ * does; above 3.39e38 they count as infinite, below 2^-102 they lose bits, and a product with an infinity is NaN.  Sums are in a fixed order, targets' in integers: the same bits every time.
+ * Logits that are NaN or +infinity make their row's loss, and what it reaches, NaN; -infinity (a class that the bias masks out) is a probability of 0.
+ * Matrices may start at any element; x and w whose rows start on 16-byte boundaries and whose dim fills them are read in place, others are copied to the workspace first.  Outputs must not overlap
+ * operands.  No rows: a loss of 0, dw and dbias become zeros.  The workspace is 256-byte aligned, of slp_linear_loss_workspace_bytes for the same pointers and sizes; top: k of a distillation, 0 for a
+ * cross-entropy; outputs: SLP_LOSS_* of the gradients wanted.
  * Errors: SLP_ERR_ARG (null pointer, negative rows, no classes or dim, unknown dtype or id size, k, T or scale out of range), SLP_ERR_SHAPE (a leading dimension below the row or, of x and w, above 2^20;
- * more than 2^20 rows or dim, 2^24 classes, 2^33 elements of x or w, 2^36 logits, 2^25 targets), SLP_ERR_ALLOC (alignment, workspace), SLP_ERR_DEVICE. */
+ * more than 2^20 rows or dim, 2^24 classes, 2^33 elements of x or w, 2^36 logits, 2^25 targets; with dw, rows of x that come to 2 GiB), SLP_ERR_ALLOC (alignment, workspace), SLP_ERR_DEVICE. */
 enum { SLP_LOSS_DX = 1, SLP_LOSS_DW = 2, SLP_LOSS_DBIAS = 4 };
 size_t slp_linear_loss_workspace_bytes(const void* x, int64_t ldx, const void* w, int64_t ldw, int dt, int rows, int classes, int dim, int top, int outputs);
 int slp_linear_cross_entropy(const void* x /*device*/, int64_t ldx, const void* w /*device*/, int64_t ldw, const float* bias /*device, may be NULL*/, int dt, int rows, int classes, int dim,

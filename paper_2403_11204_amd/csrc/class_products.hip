@@ -9,7 +9,7 @@
 // written twice.
 //
 // Float32 operands go through the bf16 matrix unit, which does 16 times the float32 one's work: each value is the sum of three bf16 values (8 bits of its 24
-// each, exact above 2^-110), and of the nine products of two values' parts the six largest are added in float32; the three left out are below 2^-26 of the product,
+// each, exact above 2^-102), and of the nine products of two values' parts the six largest are added in float32; the three left out are below 2^-26 of the product,
 // where float32 itself rounds each step by 2^-24.
 #include "class_loss.h"
 #include "eightbit_device.h"
@@ -438,9 +438,10 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int n = colW + 16 * j + 4 * lgrp + e;
-        bias[j][e] = n >= g.N ? -INFINITY : g.bias ? g.bias[n] : 0.0f;
+        bias[j][e] = g.bias && n < g.N ? g.bias[n] : 0.0f;
       }
     const int span = colW / 128;
+    const bool edge = colW + 128 > g.N;            // (uniform over the wavefront)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       f32x4 z[8];
@@ -451,6 +452,7 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           z[j][e] = (acc[i][j][e] + bias[j][e]) * g.per_t;
+          if (edge && colW + 16 * j + 4 * lgrp + e >= g.N) z[j][e] = -INFINITY;
           most = fmaxf(most, z[j][e]);
         }
       }
@@ -557,7 +559,7 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
       const int n = colW + 16 * j + 4 * lgrp;
       f32x4 bias, sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) bias[e] = n + e >= g.N ? -INFINITY : g.bias ? g.bias[n + e] : 0.0f;
+      for (int e = 0; e < 4; ++e) bias[e] = g.bias && n + e < g.N ? g.bias[n + e] : 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         asm volatile("" : "+a"(acc[i][j]));

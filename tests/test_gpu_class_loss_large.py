@@ -61,3 +61,16 @@ def test_large(rows, classes, dim, k, bias, dtype):
     if not k:
         other = api.linear_cross_entropy(x, w, ids[:, 0].contiguous(), bias=b, dtype=api.F32 if dtype == "bf16" else api.BF16)
         assert torch.equal(other.dw.bfloat16(), r.dw.bfloat16())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,classes,dim,k,bias", [(3, 64, 4096, 0, True), (130, 94, 5282, 3, True), (1, 1000, 8192, 0, False), (70, 3000, 3001, 40, True), (300, 500, 4103, 0, True)])
+def test_few_tiles_of_long_contractions(rows, classes, dim, k, bias, dtype):
+    """Logits from parts of the contraction."""
+    test_large(rows, classes, dim, k, bias, dtype)
+
+
+@pytest.mark.parametrize("rows,classes,dim,k,dtype", [(5200, 512, 64, 9, "bf16"), (8200, 47, 60, 40, "bf16"), (2100, 47, 60, 0, "fp32"), (1030, 2500, 40, 33, "fp32")])
+def test_many_rows_of_few_classes(rows, classes, dim, k, dtype):
+    """Many targets of the same class, sums of columns over many parts."""
+    test_large(rows, classes, dim, k, True, dtype)
