@@ -389,12 +389,15 @@ __global__ __launch_bounds__(256 * NG) void class_tile_kernel(const ClassProduct
       for (int i = 0; i < MI * NI; ++i) sums[((group - 1) * MI * NI + i) * 256] = acc[i / NI][i % NI];
     }
     __syncthreads();
-    if (group > 0) return;
+    if (group == 0) {
 #pragma unroll
-    for (int v = 0; v < NG - 1; ++v)
+      for (int v = 0; v < NG - 1; ++v)
 #pragma unroll
-      for (int i = 0; i < MI * NI; ++i) acc[i / NI][i % NI] += sums[(v * MI * NI + i) * 256];
+        for (int i = 0; i < MI * NI; ++i) acc[i / NI][i % NI] += sums[(v * MI * NI + i) * 256];
+    }
   }
+  __syncthreads();                               // nobody reads LDS any more
+  if (NG > 1 && group > 0) return;
   if constexpr (sizeof(T) == 4 && KMB) {
     // the columns that a lane holds lie side by side: 4 NI of them, element e of fragment j the (NI e + j)-th
 #pragma unroll
@@ -406,6 +409,36 @@ __global__ __launch_bounds__(256 * NG) void class_tile_kernel(const ClassProduct
         for (int r = 0; r < 4; ++r) v[q][r] = acc[i][(4 * q + r) % NI][(4 * q + r) / NI];
 #pragma unroll
       for (int q = 0; q < NI; ++q) acc[i][q] = v[q];
+    }
+  }
+  if constexpr (sizeof(T) == 2 && (KIND == PRODUCT_DX || KIND == PRODUCT_DW) && MI * NI >= 2) {
+    if (!g.work && g.out_dtype == 1) {
+      // bf16 leaves as whole row segments: each wavefront's part through LDS, rows of 2 NI pieces of 16 bytes, piece c of row r at c ^ (r mod 2 NI)
+      constexpr int PIECES = 2 * NI, EACH = 64 / PIECES;
+      const int lgrp = lane >> 4, lrow = lane & 15;
+      const float alpha = *g.alpha;
+      unsigned char* const st = smem + w * (MI * NI * 512);
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          const f32x4 v = acc[i][j] * alpha;
+          const bf16x4 o = {(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+          *(u32x2*)(st + (16 * i + lrow) * (PIECES * 16) + (((2 * j + (lgrp >> 1)) ^ (lrow & (PIECES - 1))) << 4) + (lgrp & 1) * 8) = __builtin_bit_cast(u32x2, o);
+        }
+      const int c = lane % PIECES, n = n0 + wn * (BN / 2) + 8 * c;
+#pragma unroll
+      for (int q = 0; q < MI * NI / 2; ++q) {
+        const int r = q * EACH + lane / PIECES, m = m0 + wm * (BM / 2) + r;
+        const bf16x8 o = *(const bf16x8*)(st + r * (PIECES * 16) + ((c ^ (r & (PIECES - 1))) << 4));
+        if (m < g.M && n < g.N) {
+          bf16* const to = (bf16*)g.out + (int64_t)m * g.ldo + n;
+          if (n + 8 <= g.N) ((AnyBf16x8*)to)->v = o;
+          else
+            for (int e = 0; e < g.N - n; ++e) to[e] = o[e];
+        }
+      }
+      return;
     }
   }
   finish<T, KIND, MI, NI>(g, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), lane);
@@ -593,11 +626,12 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
 int64_t tiles_of(int M, int N, int BM, int BN) { return (int64_t)((M + BM - 1) / BM) * ((N + BN - 1) / BN); }
 
 enum Tile { kLong, k128, k128x64, k64, k64by2, k32x64, k32x64by2, k32, k32by4 };
-// parts: of the contraction, which share the chip
+// parts: of the contraction, which share the chip.  Short contractions with a large output (dW of few rows) are all stores, which two workgroups a compute unit overlap: 16 x
+// 131072 x 4096 on 256x256 / 128x128 411 / 323 us, 64 x 32768 x 4096 109 / 80, 128 x 65536 x 2048 127 / 109, 256 x 32768 x 4096 161 / 172, 512 218 / 281.
 Tile shape_of(int dtype, int M, int N, int K, int parts = 1) {
   const int64_t nk = ((int64_t)K * (dtype == 1 ? 2 : 4) + 127) / 128 / parts;
   const int64_t t256 = tiles_of(M, N, 256, 256) * parts, t128 = tiles_of(M, N, 128, 128) * parts, t64 = tiles_of(M, N, 64, 64) * parts;
-  if (dtype == 1 && t256 >= 200) return kLong;
+  if (dtype == 1 && t256 >= 200 && nk > 2) return kLong;
   if (t128 >= 384) return k128;
   if (tiles_of(M, N, 128, 64) * parts >= 480) return k128x64;
   if (tiles_of(M, N, 32, 32) * parts <= 256) return nk >= 11 ? k32by4 : k32;
