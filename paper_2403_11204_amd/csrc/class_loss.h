@@ -51,6 +51,8 @@ int z_parts(int dtype, int M, int N, int K);      // 0: PRODUCT_STATS
 int stats_spans(int dtype, int M, int N, int K);
 int sum_parts(int dtype, int M, int N, int K);
 hipError_t launch_class_product(int dtype, int kind, const ClassProduct& g, hipStream_t s);
+// dX, and dW with it (`together`) where both are a few small tiles
+hipError_t launch_class_gradients(int dtype, const ClassProduct& x, const ClassProduct& w, bool& together, hipStream_t s);
 
 // The rows' targets: class ids (a class id outside [0, classes) is none), and for a distillation the teacher's logits of them.
 struct Targets {

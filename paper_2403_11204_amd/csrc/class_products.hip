@@ -107,7 +107,7 @@ __device__ __forceinline__ float probability(float z, float2 norm, bool label) {
 // The tail of a wavefront's (16 MI) x (16 NI) sums at row m0, column n0: lane l holds in acc[i][j] the columns n0 + 16 j + 4 (l / 16) .. + 3 of row
 // m0 + 16 i + l % 16.
 template <typename T, int KIND, int MI, int NI>
-__device__ __forceinline__ void finish(const ClassProduct& g, f32x4 (&acc)[MI][NI], int m0, int n0, int lane) {
+__device__ __forceinline__ void finish(const ClassProduct& g, f32x4 (&acc)[MI][NI], int m0, int n0, int lane, int part) {
   const int lgrp = lane >> 4, lrow = lane & 15;
   if constexpr (KIND >= PRODUCT_DX) {
     // (float32, see Side::fragments: rows that lie the other way are dealt out one by one, columns 4 NI side by side to a lane)
@@ -123,7 +123,7 @@ __device__ __forceinline__ void finish(const ClassProduct& g, f32x4 (&acc)[MI][N
         for (int i = 0; i < MI; ++i) {
           const int m = row(i);
           if (m < g.M && n < g.N) {
-            f32x4* const to = (f32x4*)(g.work + ((int64_t)blockIdx.y * g.M + m) * ldw + n);
+            f32x4* const to = (f32x4*)(g.work + ((int64_t)part * g.M + m) * ldw + n);
             *to = g.add ? *to + acc[i][j] : acc[i][j];
           }
         }
@@ -226,8 +226,8 @@ __device__ __forceinline__ void finish(const ClassProduct& g, f32x4 (&acc)[MI][N
 }
 
 // workgroup -> tile: consecutive workgroups go round the XCDs; each XCD walks a contiguous run of tiles, 8 tile rows high.
-__device__ __forceinline__ void tile_of(int tilesM, int tilesN, int& tm, int& tn) {
-  const int total = tilesM * tilesN, pid = blockIdx.x, xcd = pid % kXcds, q = pid / kXcds, base = total / kXcds, rem = total % kXcds;
+__device__ __forceinline__ void tile_of(int pid, int tilesM, int tilesN, int& tm, int& tn) {
+  const int total = tilesM * tilesN, xcd = pid % kXcds, q = pid / kXcds, base = total / kXcds, rem = total % kXcds;
   const int tid = xcd * base + (xcd < rem ? xcd : rem) + q;
   constexpr int kGroup = 8;
   const int width = kGroup * tilesN, first = tid / width * kGroup, rows = tilesM - first < kGroup ? tilesM - first : kGroup;
@@ -334,20 +334,19 @@ struct Side {
 };
 
 // BM x BN tile, 4 wavefronts in a 2 x 2 grid, NS LDS stages of a k-tile of 128 bytes each, one barrier a k-tile.  NG such groups of wavefronts take a part of the
-// contraction each (kper k-tiles) and are added up in order at the end.  blockIdx.y: part of the contraction of a whole workgroup.
+// contraction each (kper k-tiles) and are added up in order at the end.  part: of the contraction, of a whole workgroup.
 template <typename T, int KIND, int BM, int BN, int NS, int NG>
-__global__ __launch_bounds__(256 * NG) void class_tile_kernel(const ClassProduct g, int kper) {
+__device__ __forceinline__ void class_tile(const ClassProduct& g, int kper, int pid, int part, unsigned char* all_smem) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  extern __shared__ __attribute__((aligned(16))) unsigned char all_smem[];
   constexpr int BK = 128 / (int)sizeof(T), A_BYTES = BM * 128, STAGE = (BM + BN) * 128, NLD = (BM + BN) / 32, MI = BM / 32, NI = BN / 32;
   constexpr bool KMA = KIND == PRODUCT_DW, KMB = KIND == PRODUCT_DX || KMA;
   const int group = NG > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
   unsigned char* const smem = all_smem + group * (NS * STAGE);
   int tm, tn;
-  tile_of((g.M + BM - 1) / BM, (g.N + BN - 1) / BN, tm, tn);
+  tile_of(pid, (g.M + BM - 1) / BM, (g.N + BN - 1) / BN, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
   const int t = threadIdx.x & 255, lane = t & 63, w = t >> 6, wm = w & 1, wn = w >> 1;
-  const int nk = (g.K + BK - 1) / BK, k0 = (blockIdx.y * NG + group) * kper, k1 = k0 + kper < nk ? k0 + kper : nk;
+  const int nk = (g.K + BK - 1) / BK, k0 = (part * NG + group) * kper, k1 = k0 + kper < nk ? k0 + kper : nk;
   Side<T, BM, KMA> A;
   Side<T, BN, KMB> B;
   A.init(g.a, g.lda, m0, g.M - m0 < BM ? g.M - m0 : BM, g.K, t);
@@ -441,8 +440,21 @@ __global__ __launch_bounds__(256 * NG) void class_tile_kernel(const ClassProduct
       return;
     }
   }
-  finish<T, KIND, MI, NI>(g, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), lane);
+  finish<T, KIND, MI, NI>(g, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), lane, part);
 #endif
+}
+template <typename T, int KIND, int BM, int BN, int NS, int NG>
+__global__ __launch_bounds__(256 * NG) void class_tile_kernel(const ClassProduct g, int kper) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char all_smem[];
+  class_tile<T, KIND, BM, BN, NS, NG>(g, kper, blockIdx.x, blockIdx.y, all_smem);
+}
+// Both gradients of P in one launch, where each takes a few small tiles: `xtiles` times x.parts workgroups on dX, the others on dW.
+template <typename T, int NX, int NW>
+__global__ __launch_bounds__(256) void class_pair_kernel(const ClassProduct x, int xper, int xtiles, int xblocks, const ClassProduct w, int wper, int wtiles) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char all_smem[];
+  const int at = blockIdx.x;
+  if (at < xblocks) class_tile<T, PRODUCT_DX, 32, NX, 3, 1>(x, xper, at % xtiles, at / xtiles, all_smem);
+  else class_tile<T, PRODUCT_DW, 32, NW, 3, 1>(w, wper, (at - xblocks) % wtiles, (at - xblocks) / wtiles, all_smem);
 }
 
 // Large bf16 products (long_tile.h).  What the epilogues of the tiles above do, with the accumulators taken out of the AGPRs a block at a time; bf16 outputs leave as whole
@@ -664,6 +676,19 @@ hipError_t launch_long(const ClassProduct& g, hipStream_t s) {
   class_long_kernel<KIND><<<dim3((unsigned)tiles_of(g.M, g.N, 256, 256), parts), 256, kLongSmem, s>>>(g, kper);
   return hipGetLastError();
 }
+template <typename T, int NX, int NW>
+hipError_t launch_pair(const ClassProduct& x, const ClassProduct& w, hipStream_t s) {
+  constexpr int smem = 3 * (32 + (NX > NW ? NX : NW)) * 128, BK = 128 / (int)sizeof(T);
+  auto per = [](const ClassProduct& g) { const int nk = (g.K + BK - 1) / BK, parts = g.work ? g.parts : 1; return (nk + parts - 1) / parts; };
+  const int xtiles = (int)tiles_of(x.M, x.N, 32, NX), wtiles = (int)tiles_of(w.M, w.N, 32, NW), xblocks = xtiles * (x.work ? x.parts : 1), wblocks = wtiles * (w.work ? w.parts : 1);
+  class_pair_kernel<T, NX, NW><<<xblocks + wblocks, 256, smem, s>>>(x, per(x), xtiles, xblocks, w, per(w), wtiles);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_pair(bool x64, bool w64, const ClassProduct& x, const ClassProduct& w, hipStream_t s) {
+  if (x64) return w64 ? launch_pair<T, 64, 64>(x, w, s) : launch_pair<T, 64, 32>(x, w, s);
+  return w64 ? launch_pair<T, 32, 64>(x, w, s) : launch_pair<T, 32, 32>(x, w, s);
+}
 template <typename T, int KIND>
 hipError_t launch_kind(int dtype, const ClassProduct& g, hipStream_t s) {
   switch (shape_of(dtype, g.M, g.N, g.K, g.work ? g.parts : 1)) {
@@ -725,13 +750,24 @@ int sum_parts(int dtype, int M, int N, int K) {
   return (M + 2 * w - 1) / (2 * w) * 2;
 }
 
-hipError_t launch_class_product(int dtype, int kind, const ClassProduct& g, hipStream_t s) {
+static bool addressable(int dtype, int kind, const ClassProduct& g) {
   const int64_t es = dtype == 1 ? 2 : 4;
   // a tile's rows, or an operand that lies the other way, are addressed with 32-bit offsets
   const int64_t rows_a = kind == PRODUCT_DW ? g.K : 256, rows_b = kind == PRODUCT_DX || kind == PRODUCT_DW ? g.K : 256;
-  if (g.M <= 0 || g.N <= 0 || g.K <= 0 || rows_a * g.lda * es >= 0x7FFFFF00 || rows_b * g.ldb * es >= 0x7FFFFF00) return hipErrorInvalidValue;
-  if ((((uintptr_t)g.a | (uintptr_t)g.b) & 15) || g.lda * es % 16 || g.ldb * es % 16) return hipErrorInvalidValue;
+  if (g.M <= 0 || g.N <= 0 || g.K <= 0 || rows_a * g.lda * es >= 0x7FFFFF00 || rows_b * g.ldb * es >= 0x7FFFFF00) return false;
+  return !((((uintptr_t)g.a | (uintptr_t)g.b) & 15) || g.lda * es % 16 || g.ldb * es % 16);
+}
+hipError_t launch_class_product(int dtype, int kind, const ClassProduct& g, hipStream_t s) {
+  if (!addressable(dtype, kind, g)) return hipErrorInvalidValue;
   return dtype == 1 ? launch_type<bf16>(dtype, kind, g, s) : launch_type<float>(dtype, kind, g, s);
+}
+hipError_t launch_class_gradients(int dtype, const ClassProduct& x, const ClassProduct& w, bool& together, hipStream_t s) {
+  auto shape = [&](const ClassProduct& g) { return shape_of(dtype, g.M, g.N, g.K, g.work ? g.parts : 1); };
+  const Tile sx = shape(x), sw = shape(w);
+  together = (sx == k32 || sx == k32x64) && (sw == k32 || sw == k32x64);
+  if (!together) return launch_class_product(dtype, PRODUCT_DX, x, s);
+  if (!addressable(dtype, PRODUCT_DX, x) || !addressable(dtype, PRODUCT_DW, w)) return hipErrorInvalidValue;
+  return dtype == 1 ? launch_pair<bf16>(sx == k32x64, sw == k32x64, x, w, s) : launch_pair<float>(sx == k32x64, sw == k32x64, x, w, s);
 }
 
 }  // namespace slp

@@ -227,49 +227,51 @@ int run(const Call& c, void* workspace, hipStream_t s) {
       bias_left = false;
       return SLP_OK;
     };
+    ClassProduct dx{}, dw{};
     if (c.dx) {
-      ClassProduct o{};
-      o.a = at(a.P);
-      o.lda = a.ldp;
-      o.b = w;
-      o.ldb = ldw;
-      o.M = c.rows;
-      o.N = c.dim;
-      o.K = columns;
-      o.alpha = alpha;
-      o.parts = a.dx_parts;
+      dx.a = at(a.P);
+      dx.lda = a.ldp;
+      dx.b = w;
+      dx.ldb = ldw;
+      dx.M = c.rows;
+      dx.N = c.dim;
+      dx.K = columns;
+      dx.alpha = alpha;
+      dx.parts = a.dx_parts;
       if (a.dx_parts > 1 || a.piece < c.classes) {
-        o.work = (float*)at(a.dx_work);
-        o.add = first > 0;
+        dx.work = (float*)at(a.dx_work);
+        dx.add = first > 0;
       } else {
-        o.out = c.dx;
-        o.ldo = c.lddx;
-        o.out_dtype = c.dt;
+        dx.out = c.dx;
+        dx.ldo = c.lddx;
+        dx.out_dtype = c.dt;
       }
-      HIP_TRY(launch_class_product(c.dt, PRODUCT_DX, o, s));
-      if (o.work && last) SLP_CHECK(join(c.dt, o.work, o.parts, c.rows, c.dx, c.lddx));
     }
     if (c.dw) {
-      char* const dw = (char*)c.dw + (int64_t)first * c.lddw * (int64_t)size_of(c.dw_dt);
-      ClassProduct o{};
-      o.a = at(a.P);
-      o.lda = a.ldp;
-      o.b = at(a.xz);
-      o.ldb = a.ldk;
-      o.M = columns;
-      o.N = c.dim;
-      o.K = c.rows;
-      o.alpha = alpha;
-      o.parts = a.dw_parts;
+      dw.a = at(a.P);
+      dw.lda = a.ldp;
+      dw.b = at(a.xz);
+      dw.ldb = a.ldk;
+      dw.M = columns;
+      dw.N = c.dim;
+      dw.K = c.rows;
+      dw.alpha = alpha;
+      dw.parts = a.dw_parts;
       if (a.dw_parts > 1) {
-        o.work = (float*)at(a.dw_work);
+        dw.work = (float*)at(a.dw_work);
       } else {
-        o.out = dw;
-        o.ldo = c.lddw;
-        o.out_dtype = c.dw_dt;
+        dw.out = (char*)c.dw + (int64_t)first * c.lddw * (int64_t)size_of(c.dw_dt);
+        dw.ldo = c.lddw;
+        dw.out_dtype = c.dw_dt;
       }
-      HIP_TRY(launch_class_product(c.dt, PRODUCT_DW, o, s));
-      if (o.work) SLP_CHECK(join(c.dw_dt, o.work, o.parts, columns, dw, c.lddw));
+    }
+    bool together = false;
+    if (c.dx && c.dw) HIP_TRY(launch_class_gradients(c.dt, dx, dw, together, s));
+    else if (c.dx) HIP_TRY(launch_class_product(c.dt, PRODUCT_DX, dx, s));
+    if (dx.work && last) SLP_CHECK(join(c.dt, dx.work, dx.parts, c.rows, c.dx, c.lddx));
+    if (c.dw) {
+      if (!together) HIP_TRY(launch_class_product(c.dt, PRODUCT_DW, dw, s));
+      if (dw.work) SLP_CHECK(join(c.dw_dt, dw.work, dw.parts, columns, (char*)c.dw + (int64_t)first * c.lddw * (int64_t)size_of(c.dw_dt), c.lddw));
     }
     if (bias_left) SLP_CHECK(join(c.dt, nullptr, 0, 0, nullptr, 0));
   }
