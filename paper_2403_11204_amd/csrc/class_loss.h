@@ -97,6 +97,7 @@ struct RowLoss {
   int32_t* labels;          // [rows], may be null: the row's class or -1
   unsigned long long* fixed;      // [classes], may be null: cleared on the way
   double2* means;           // [row_groups(this)]: sum of the losses and number of the rows that count, of a group of rows
+  float* loss;              // may be null: their mean, where there is one group
 };
 hipError_t launch_row_loss(const RowLoss& a, hipStream_t s);
 int row_groups(const RowLoss& a);

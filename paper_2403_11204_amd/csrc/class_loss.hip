@@ -28,12 +28,12 @@ __device__ __forceinline__ float teacher(const Targets& t, int64_t row, int j, i
   return (t.top_dtype == 1 ? (float)((const bf16*)t.top)[at] : ((const float*)t.top)[at]) * t.per_t;
 }
 
-// One wavefront for each target: the dot product of a row of x and the row of W that is its class.  Bound by reading those rows of W: 4096 x 64
-// targets of 4096 bf16 are 2.1 GB.
-template <typename T>
+// The dot product of a row of x and the row of W that is its class, one wavefront for each target; a workgroup where they are few and each waits for its own loads (1 target of
+// 4096 bf16 8 us on a wavefront, see below).  Many are bound by reading those rows of W: 4096 x 64 targets of 4096 bf16 are 2.1 GB.
+template <typename T, int TEAM>
 __global__ __launch_bounds__(256) void target_logits_kernel(const TargetLogits a) {
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * (256 / TEAM) + threadIdx.x / TEAM;
+  const int lane = threadIdx.x % TEAM;
   if (at >= (int64_t)a.rows * a.t.k) return;
   const int64_t row = at / a.t.k;
   const int c = class_of(a.t, row, (int)(at % a.t.k), a.classes);
@@ -41,7 +41,7 @@ __global__ __launch_bounds__(256) void target_logits_kernel(const TargetLogits a
   const T* const x = (const T*)a.x + row * a.ldx;
   const T* const w = (const T*)a.w + (int64_t)c * a.ldw;
   float sum = 0.0f;
-  for (int d = lane * 8; d < a.dim; d += 512) {
+  for (int d = lane * 8; d < a.dim; d += TEAM * 8) {
     float u[8], v[8];
     load8(x + d, a.dim - d, u);
     load8(w + d, a.dim - d, v);
@@ -49,6 +49,12 @@ __global__ __launch_bounds__(256) void target_logits_kernel(const TargetLogits a
     for (int e = 0; e < 8; ++e) sum += u[e] * v[e];
   }
   sum = sum_of_64(sum);
+  if constexpr (TEAM == 256) {
+    __shared__ float part[4];
+    if ((lane & 63) == 0) part[lane >> 6] = sum;
+    __syncthreads();
+    sum = (part[0] + part[1]) + (part[2] + part[3]);
+  }
   if (lane == 0) a.zt[at] = (sum + (a.bias ? a.bias[c] : 0.0f)) * a.t.per_t;
 }
 
@@ -227,6 +233,7 @@ __global__ __launch_bounds__(256) void row_loss_kernel(const RowLoss a) {
     sum.y += group[i].y;
   }
   a.means[blockIdx.x] = sum;
+  if (a.loss) *a.loss = sum.y > 0.0 ? (float)(sum.x / sum.y) : 0.0f;
 }
 
 // Block 0: the mean.  The others: 2048 elements each of xz's rows.
@@ -423,9 +430,13 @@ unsigned blocks(int64_t n, int each) { return (unsigned)((n + each - 1) / each);
 }  // namespace
 
 hipError_t launch_target_logits(int dtype, const TargetLogits& a, hipStream_t s) {
-  const unsigned n = blocks((int64_t)a.rows * a.t.k, 4);
-  if (dtype == 1) target_logits_kernel<bf16><<<n, 256, 0, s>>>(a);
-  else target_logits_kernel<float><<<n, 256, 0, s>>>(a);
+  const int64_t targets = (int64_t)a.rows * a.t.k;
+  const unsigned n = blocks(targets, 4);
+  if (targets <= 1024) {
+    if (dtype == 1) target_logits_kernel<bf16, 256><<<(unsigned)targets, 256, 0, s>>>(a);
+    else target_logits_kernel<float, 256><<<(unsigned)targets, 256, 0, s>>>(a);
+  } else if (dtype == 1) target_logits_kernel<bf16, 64><<<n, 256, 0, s>>>(a);
+  else target_logits_kernel<float, 64><<<n, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

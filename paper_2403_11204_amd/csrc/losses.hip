@@ -180,11 +180,13 @@ int run(const Call& c, void* workspace, hipStream_t s) {
   }
   unsigned long long* const all_fixed = a.fix ? (unsigned long long*)at(a.fixed) : nullptr;
   int32_t* const labels = c.t.top ? nullptr : (int32_t*)at(a.labels);
-  const RowLoss each{(const float2*)at(a.stats), a.spans, a.z_parts ? (const float*)at(a.z_work) : nullptr, a.z_parts, c.bias, c.rows, c.classes, c.t, z, a.ldz, a.kept, zt, c.temperature * c.temperature, c.lse, c.losses, norm, p, labels, all_fixed, (double2*)at(a.means)};
+  RowLoss each{(const float2*)at(a.stats), a.spans, a.z_parts ? (const float*)at(a.z_work) : nullptr, a.z_parts, c.bias, c.rows, c.classes, c.t, z, a.ldz, a.kept, zt, c.temperature * c.temperature, c.lse, c.losses, norm, p, labels, all_fixed, (double2*)at(a.means), nullptr};
+  const bool alone = !grads && row_groups(each) == 1;
+  if (alone) each.loss = c.loss;
   HIP_TRY(launch_row_loss(each, s));
   // (xz: the rows that count; 0 times what others hold may be NaN)
   const AllRows all{each.means, row_groups(each), norm, c.rows, c.dim, c.scale * c.temperature, c.loss, alpha, a.copy_x ? nullptr : c.x, c.ldx, c.dw ? at(a.xz) : nullptr, a.ldk};
-  if (!a.kept || !grads) HIP_TRY(launch_all_rows(c.dt, all, s));
+  if ((!a.kept || !grads) && !alone) HIP_TRY(launch_all_rows(c.dt, all, s));
   if (!grads) return SLP_OK;
 
   for (int first = 0; first < c.classes; first += a.piece) {
