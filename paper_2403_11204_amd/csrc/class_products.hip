@@ -638,12 +638,20 @@ __global__ __launch_bounds__(256) void class_long_kernel(const ClassProduct g, i
 int64_t tiles_of(int M, int N, int BM, int BN) { return (int64_t)((M + BM - 1) / BM) * ((N + BN - 1) / BN); }
 
 enum Tile { kLong, k128, k128x64, k64, k64by2, k32x64, k32x64by2, k32, k32by4 };
-// parts: of the contraction, which share the chip.  Short contractions with a large output (dW of few rows) are all stores, which two workgroups a compute unit overlap: 16 x
-// 131072 x 4096 on 256x256 / 128x128 411 / 323 us, 64 x 32768 x 4096 109 / 80, 128 x 65536 x 2048 127 / 109, 256 x 32768 x 4096 161 / 172, 512 218 / 281.
-Tile shape_of(int dtype, int M, int N, int K, int parts = 1) {
+// parts: of the contraction, which share the chip.
+// 256x256 tiles have one workgroup a compute unit, which waits for its own stores and loads.  Where those are all there is, two or more of 128 or 64 rows do better:
+//   short contractions with a large output (dW of few rows), on 256x256 / 128x128: 16 x 131072 x 4096 411 / 323 us, 64 x 32768 x 4096 109 / 80, 128 x 65536 x 2048
+//   127 / 109; 256 x 32768 x 4096 161 / 172, 512 218 / 281;
+//   few rows (logits), on 256x256 / 128x128 / 64x64: 1 x 131072 x 4096 216 / 180 / 170, 64 x 131072 x 1024 62 / 47 / 42, 128 x 131072 x 4096 249 / 200 / 320, 256 x
+//   131072 x 1024 71 / 93 / 128; few classes (dW): 8192 x 47 x 4096 24 / 19 / 16, 128 32 / 24 / 27;
+//   few rows of dX, whose W is read across: 1 x 131072 x 4096 225 / 238 / 184, 16 229 / 239 / 204, 64 252 / 270 / 255, 128 275 / 286 / 391; 64 x 131072 x 1024 62 / 62 /
+//   75, 128 x 65536 x 2048 73 / 66 / 102, 128 x 32768 x 2048 46 / 36 / 42.
+Tile shape_of(int kind, int dtype, int M, int N, int K, int parts = 1) {
   const int64_t nk = ((int64_t)K * (dtype == 1 ? 2 : 4) + 127) / 128 / parts;
   const int64_t t256 = tiles_of(M, N, 256, 256) * parts, t128 = tiles_of(M, N, 128, 128) * parts, t64 = tiles_of(M, N, 64, 64) * parts;
-  if (dtype == 1 && t256 >= 200 && nk > 2) return kLong;
+  const bool few = M <= (kind == PRODUCT_DX ? 16 : 64);
+  if (dtype == 1 && t256 >= 200 && nk > 2 && !few && (M > 128 || M <= 64)) return kLong;
+  if (few && t64 >= 512) return k64;
   if (t128 >= 384) return k128;
   if (tiles_of(M, N, 128, 64) * parts >= 480) return k128x64;
   if (tiles_of(M, N, 32, 32) * parts <= 256) return nk >= 11 ? k32by4 : k32;
@@ -691,7 +699,7 @@ hipError_t launch_pair(bool x64, bool w64, const ClassProduct& x, const ClassPro
 }
 template <typename T, int KIND>
 hipError_t launch_kind(int dtype, const ClassProduct& g, hipStream_t s) {
-  switch (shape_of(dtype, g.M, g.N, g.K, g.work ? g.parts : 1)) {
+  switch (shape_of(KIND, dtype, g.M, g.N, g.K, g.work ? g.parts : 1)) {
     case kLong:
       if constexpr (sizeof(T) == 2) return launch_long<KIND>(g, s);
     case k128: return launch_tile<T, KIND, 128, 128, 2, 1>(g, s);
@@ -742,11 +750,11 @@ int z_parts(int dtype, int M, int N, int K) {
 }
 
 int stats_spans(int dtype, int M, int N, int K) {
-  const int w = span_columns(shape_of(dtype, M, N, K));
+  const int w = span_columns(shape_of(PRODUCT_STATS, dtype, M, N, K));
   return (N + 2 * w - 1) / (2 * w) * 2;
 }
 int sum_parts(int dtype, int M, int N, int K) {
-  const int w = span_rows(shape_of(dtype, M, N, K));
+  const int w = span_rows(shape_of(PRODUCT_PROB, dtype, M, N, K));
   return (M + 2 * w - 1) / (2 * w) * 2;
 }
 
@@ -762,8 +770,8 @@ hipError_t launch_class_product(int dtype, int kind, const ClassProduct& g, hipS
   return dtype == 1 ? launch_type<bf16>(dtype, kind, g, s) : launch_type<float>(dtype, kind, g, s);
 }
 hipError_t launch_class_gradients(int dtype, const ClassProduct& x, const ClassProduct& w, bool& together, hipStream_t s) {
-  auto shape = [&](const ClassProduct& g) { return shape_of(dtype, g.M, g.N, g.K, g.work ? g.parts : 1); };
-  const Tile sx = shape(x), sw = shape(w);
+  auto shape = [&](int kind, const ClassProduct& g) { return shape_of(kind, dtype, g.M, g.N, g.K, g.work ? g.parts : 1); };
+  const Tile sx = shape(PRODUCT_DX, x), sw = shape(PRODUCT_DW, w);
   together = (sx == k32 || sx == k32x64) && (sw == k32 || sw == k32x64);
   if (!together) return launch_class_product(dtype, PRODUCT_DX, x, s);
   if (!addressable(dtype, PRODUCT_DX, x) || !addressable(dtype, PRODUCT_DW, w)) return hipErrorInvalidValue;
