@@ -74,3 +74,18 @@ def test_few_tiles_of_long_contractions(rows, classes, dim, k, bias, dtype):
 def test_many_rows_of_few_classes(rows, classes, dim, k, dtype):
     """Many targets of the same class, sums of columns over many parts."""
     test_large(rows, classes, dim, k, True, dtype)
+
+
+@pytest.mark.parametrize("rows,classes,dim,k,dtype", [(5, 40000, 264, 0, "bf16"), (16, 66000, 128, 2, "bf16"), (33, 40008, 2056, 0, "bf16"), (64, 33000, 135, 3, "bf16"), (100, 34001, 520, 0, "bf16"),
+                                                      (128, 33000, 128, 5, "bf16"), (129, 33000, 136, 0, "bf16"), (16500, 47, 4104, 0, "bf16"), (9000, 100, 2050, 2, "bf16"),
+                                                      (5, 40000, 264, 2, "fp32"), (64, 33001, 132, 0, "fp32"), (70, 33000, 100, 3, "fp32")])
+def test_few_rows_or_classes(rows, classes, dim, k, dtype):
+    """Tiles that most of the rows' or classes' side does not fill; gradients of weights whose contraction is short."""
+    test_large(rows, classes, dim, k, True, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,classes,dim,k", [(64, 1000, 512, 8), (600, 47, 512, 0), (600, 300, 512, 3), (300, 150, 256, 0), (500, 70, 250, 2)])
+def test_both_gradients_together(rows, classes, dim, k, dtype):
+    """Few small tiles of each gradient, with a contraction in one part and in several."""
+    test_large(rows, classes, dim, k, True, dtype)
