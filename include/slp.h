@@ -333,7 +333,7 @@ int slp_product(const void* a /*device*/, int64_t lda, const void* a_scales, int
  * slp_quantize_integers: q = round(127 x / max|x|) over each row, ties to even, of the real quotient; scale = max|x| / 127.  A row of zeros has the scale 0, one that holds an
  * infinity or a NaN zeros and the scale NaN.  Written up to the next multiple of 16 columns.
  * slp_product_integers: out[M][N] = act(a_scales[m] b_scales[n] sum over k of A[m][k] B[n][k] + bias[n]), out of dtype dt; the sums are exact, K up to 131071 (any signed byte may stand
- * in A and B); scales, bias and ReLU (where relu is not 0; a NaN stays one) in float32.  The workspace holds parts of a contraction that is split over the chip; 256-byte aligned, 0 for most large products.
+ * in A and B); scales, bias and ReLU (where relu is not 0; a NaN stays one) in float32.  The workspace holds parts of a contraction that is split over the chip; 256-byte aligned, 0 for most large products, and no other call's that may run at the same time.
  * Limits and errors as for 8-bit matrices; SLP_ERR_SHAPE also for a longer contraction. */
 int slp_quantize_integers(const void* x /*device*/, int64_t ldx, int dt, int rows, int cols, void* q /*device*/, int64_t ldq, float* scales /*device*/, slp_stream stream);
 size_t slp_product_integers_workspace_bytes(int M, int N, int K);
@@ -384,7 +384,7 @@ int slp_clip_gradients(const void* const* tensors /*host*/, void* const* out /*h
  * does; above 3.39e38 they count as infinite, below 2^-102 they lose bits, and a product with an infinity is NaN.  Sums are in a fixed order, targets' in integers: the same bits every time.
  * Logits that are NaN or +infinity make their row's loss, and what it reaches, NaN; -infinity (a class that the bias masks out) is a probability of 0.
  * Matrices may start at any element; x and w whose rows start on 16-byte boundaries and whose dim fills them are read in place, others are copied to the workspace first.  Outputs must not overlap
- * operands.  No rows: a loss of 0, dw and dbias become zeros.  The workspace is 256-byte aligned, of slp_linear_loss_workspace_bytes for the same pointers and sizes; top: k of a distillation, 0 for a
+ * operands.  No rows: a loss of 0, dw and dbias become zeros.  The workspace is 256-byte aligned, of slp_linear_loss_workspace_bytes for the same pointers and sizes, and of no other call that may run at the same time; top: k of a distillation, 0 for a
  * cross-entropy; outputs: SLP_LOSS_* of the gradients wanted.
  * Errors: SLP_ERR_ARG (null pointer, negative rows, no classes or dim, unknown dtype or id size, k, T or scale out of range), SLP_ERR_SHAPE (a leading dimension below the row or, of x and w, above 2^20;
  * more than 2^20 rows or dim, 2^24 classes, 2^33 elements of x or w, 2^36 logits, 2^25 targets; with dw, rows of x that come to 2 GiB), SLP_ERR_ALLOC (alignment, workspace), SLP_ERR_DEVICE. */

@@ -304,7 +304,8 @@ __global__ __launch_bounds__(256) void target_fix_kernel(const TargetFix a) {
   });
 }
 
-// 512 columns by 4 EACH rows a workgroup, a lane 8 columns of EACH rows; then, where fix is set, the targets among them.  Workgroups behind those: all_rows_block.  Bound by memory: 4 bytes in, 2 or 4 out.
+// 512 columns by 4 EACH rows a workgroup, a lane 8 columns of EACH rows; then, where fix is set, the targets among them.  Workgroups behind those: all_rows_block.  Bound by memory, 4 bytes in, 2 or 4 out:
+// 2048 x 32000 bf16 78 us (5.0 TB/s), 1000 x 50001 58 (5.2).
 template <typename T, int EACH>
 __global__ __launch_bounds__(256) void kept_prob_kernel(const TargetFix a, const float* z, int64_t ldz, const int32_t* labels, bool fix, const AllRows all) {
   constexpr float kLog2e = 1.44269504088896340736f;

