@@ -5,6 +5,8 @@
 //   Z      x W^T over parts of the contraction, where there are few tiles and it is long
 //   DX     P W, a contraction over the piece's classes, split over the chip where there are few tiles
 //   DW     P^T x, over the rows
+// P leaves PROB (or kept_prob_kernel) rounded to the operands' type, bf16 by half a step of 2^-8, as the gradient of any layer in bf16 is: in two parts it would be twice the work of
+// both products.  Its common factor T scale / n, and 1 less at a row's own class, are applied in float32 around that.
 // W lies in DX, and both operands in DW, with a row for each step of the contraction: their tiles are read transposed from LDS, so that nothing has to be
 // written twice.
 //
