@@ -49,6 +49,8 @@ struct ClassProduct {
 int class_parts(int dtype, int M, int N, int K);
 int z_parts(int dtype, int M, int N, int K);      // 0: PRODUCT_STATS
 int stats_spans(int dtype, int M, int N, int K);
+// of `classes`, as many as one launch of PRODUCT_STATS or PRODUCT_DW had better take; others: rows and dim, or dim and rows
+int whole_rounds(int dtype, int kind, int classes, int others, int K);
 int sum_parts(int dtype, int M, int N, int K);
 hipError_t launch_class_product(int dtype, int kind, const ClassProduct& g, hipStream_t s);
 // dX, and dW with it (`together`) where both are a few small tiles

@@ -647,7 +647,10 @@ int64_t tiles_of(int M, int N, int BM, int BN) { return (int64_t)((M + BM - 1) /
 
 enum Tile { kLong, k128, k128x64, k64, k64by2, k32x64, k32x64by2, k32, k32by4 };
 // parts: of the contraction, which share the chip.
-// 256x256 tiles have one workgroup a compute unit, which waits for its own stores and loads.  Where those are all there is, two or more of 128 or 64 rows do better:
+// 256x256 tiles where they keep half of the compute units busy, long contractions sooner, of which more than 512 of 128x128 (two a compute unit) take two rounds: dW of 8192 x 9300 x 1024
+// (148 tiles) 192 us / 355 on 128x128, of 8192 x 2500 x 4096 (160) 205 / 333, of 1000 x 9000 x 1024 (144) 33 / 46, logits of it 39 / 41; short ones, logits of 1000 x 9000 x 256 (144)
+// 25.6 / 21.0, of 4096 x 2600 x 512 (176) 30 / 28.
+// They have one workgroup a compute unit, which waits for its own stores and loads.  Where those are all there is, two or more of 128 or 64 rows do better:
 //   short contractions with a large output (dW of few rows), on 256x256 / 128x128: 16 x 131072 x 4096 411 / 323 us, 64 x 32768 x 4096 109 / 80, 128 x 65536 x 2048
 //   127 / 109; 256 x 32768 x 4096 161 / 172, 512 218 / 281;
 //   few rows (logits), on 256x256 / 128x128 / 64x64: 1 x 131072 x 4096 216 / 180 / 170, 64 x 131072 x 1024 62 / 47 / 42, 128 x 131072 x 4096 249 / 200 / 320, 256 x
@@ -658,7 +661,7 @@ Tile shape_of(int kind, int dtype, int M, int N, int K, int parts = 1) {
   const int64_t nk = ((int64_t)K * (dtype == 1 ? 2 : 4) + 127) / 128 / parts;
   const int64_t t256 = tiles_of(M, N, 256, 256) * parts, t128 = tiles_of(M, N, 128, 128) * parts, t64 = tiles_of(M, N, 64, 64) * parts;
   const bool few = M <= (kind == PRODUCT_DX ? 16 : 64);
-  if (dtype == 1 && t256 >= 200 && nk > 2 && !few && (M > 128 || M <= 64)) return kLong;
+  if (dtype == 1 && t256 >= (nk >= 16 ? 130 : 200) && nk > 2 && !few && (M > 128 || M <= 64)) return kLong;
   if (few && t64 >= 512) return k64;
   if (t128 >= 384) return k128;
   if (tiles_of(M, N, 128, 64) * parts >= 480) return k128x64;
@@ -757,6 +760,15 @@ int z_parts(int dtype, int M, int N, int K) {
   return parts < 2 || (int64_t)M * N * parts > 1 << 23 ? 0 : parts;
 }
 
+// Tiles of 256x256 go round by round of 256; few of them behind a few whole rounds keep most of the chip waiting, and go on smaller tiles in a launch of their own.  In one / two: logits of
+// 1000 x 50001 x 1500 (784 tiles) 227 / 205 us, 2048 x 17000 x 4096 (536) 321 / 283, 4096 x 4300 x 4096 (272) 188 / 145, dW of it 183 / 156; with more rounds or more tiles left they run into each
+// other anyway: dW of 2048 x 17000 x 4096 (1072) 294 / 298, 18300 (1152) 306 / 325.
+int whole_rounds(int dtype, int kind, int classes, int others, int K) {
+  const int M = kind == PRODUCT_DW ? classes : others, N = kind == PRODUCT_DW ? others : classes;
+  const int64_t tiles = tiles_of(M, N, 256, 256), rounds = tiles / 256, across = (others + 255) / 256;
+  if (shape_of(kind, dtype, M, N, K) != kLong || rounds < 1 || rounds > 3 || tiles % 256 == 0 || tiles % 256 > 64 || across > 64) return classes;
+  return (int)(rounds * 256 / across) * 256;
+}
 int stats_spans(int dtype, int M, int N, int K) {
   const int w = span_columns(shape_of(PRODUCT_STATS, dtype, M, N, K));
   return (N + 2 * w - 1) / (2 * w) * 2;

@@ -59,6 +59,12 @@ struct Plan {
 // Whether the products can read a matrix in place.
 bool in_place(const void* p, int64_t ld, int rows, int dim, int64_t es) { return !off(p, 16) && (rows == 1 || ld * es % 16 == 0) && dim * es % 16 == 0; }
 
+// Classes from `first` on whose logits a launch takes: no more than the copy of W holds, and whole rounds of the chip where those are few.
+int stats_columns(const Call& c, const Plan& a, int first) {
+  const int left = a.copy_w ? a.piece - first % a.piece : c.classes, most = c.classes - first < left ? c.classes - first : left;
+  return whole_rounds(c.dt, PRODUCT_STATS, most, c.rows, c.dim);
+}
+
 Plan plan_of(const Call& c) {
   Plan a{};
   const bool grads = c.dx || c.dw || c.dbias;
@@ -84,8 +90,10 @@ Plan plan_of(const Call& c) {
   }
   a.dx_parts = class_parts(c.dt, c.rows, c.dim, a.piece);
   a.dw_parts = class_parts(c.dt, a.piece, c.dim, c.rows);
-  for (int first = 0; first < c.classes; first += a.copy_w ? a.piece : c.classes)
-    a.spans += stats_spans(c.dt, c.rows, a.copy_w && c.classes - first > a.piece ? a.piece : c.classes - first, c.dim);
+  for (int first = 0, columns; first < c.classes; first += columns) {
+    columns = stats_columns(c, a, first);
+    a.spans += stats_spans(c.dt, c.rows, columns, c.dim);
+  }
   size_t at = 0;
   auto take = [&](bool wanted, int64_t bytes) {
     const size_t here = at;
@@ -153,10 +161,12 @@ int run(const Call& c, void* workspace, hipStream_t s) {
   if (a.kept < c.classes) HIP_TRY(launch_target_logits(c.dt, TargetLogits{c.x, c.w, c.ldx, c.ldw, c.bias, c.rows, c.classes, c.dim, a.kept, c.t, zt}, s));
   float* const z = a.kept ? (float*)at(a.z) : nullptr;
   float2* stats = (float2*)at(a.stats);
-  for (int first = 0; first < c.classes; first += a.copy_w ? a.piece : c.classes) {
-    const int left = c.classes - first, columns = a.copy_w && left > a.piece ? a.piece : left;
+  for (int first = 0, columns; first < c.classes; first += columns) {
+    columns = a.z_parts ? c.classes : stats_columns(c, a, first);
     ClassProduct g{};
-    SLP_CHECK(weights(first, columns, g.b, g.ldb));
+    const int from = a.copy_w ? first % a.piece : 0, held = c.classes - (first - from) < a.piece ? c.classes - (first - from) : a.piece;
+    SLP_CHECK(weights(first - from, held, g.b, g.ldb));
+    g.b = (const char*)g.b + (a.copy_w ? (int64_t)from * g.ldb * a.es : 0);
     g.a = x;
     g.lda = ldx;
     g.M = c.rows;
@@ -272,7 +282,17 @@ int run(const Call& c, void* workspace, hipStream_t s) {
     else if (c.dx) HIP_TRY(launch_class_product(c.dt, PRODUCT_DX, dx, s));
     if (dx.work && last) SLP_CHECK(join(c.dt, dx.work, dx.parts, c.rows, c.dx, c.lddx));
     if (c.dw) {
-      if (!together) HIP_TRY(launch_class_product(c.dt, PRODUCT_DW, dw, s));
+      const int most = dw.work ? columns : whole_rounds(c.dt, PRODUCT_DW, columns, c.dim, c.rows);
+      if (!together) {
+        dw.M = most;
+        HIP_TRY(launch_class_product(c.dt, PRODUCT_DW, dw, s));
+        if (most < columns) {
+          dw.a = (const char*)dw.a + most * a.es;
+          dw.out = (char*)dw.out + (int64_t)most * c.lddw * (int64_t)size_of(c.dw_dt);
+          dw.M = columns - most;
+          HIP_TRY(launch_class_product(c.dt, PRODUCT_DW, dw, s));
+        }
+      }
       if (dw.work) SLP_CHECK(join(c.dw_dt, dw.work, dw.parts, columns, (char*)c.dw + (int64_t)first * c.lddw * (int64_t)size_of(c.dw_dt), c.lddw));
     }
     if (bias_left) SLP_CHECK(join(c.dt, nullptr, 0, 0, nullptr, 0));

@@ -89,3 +89,9 @@ def test_few_rows_or_classes(rows, classes, dim, k, dtype):
 def test_both_gradients_together(rows, classes, dim, k, dtype):
     """Few small tiles of each gradient, with a contraction in one part and in several."""
     test_large(rows, classes, dim, k, True, dtype)
+
+
+@pytest.mark.parametrize("rows,classes,dim,k,dtype", [(1000, 16900, 264, 3, "bf16"), (1030, 13400, 1100, 0, "bf16"), (1100, 4400, 4136, 2, "bf16"), (1021, 16645, 129, 0, "bf16")])
+def test_tiles_left_behind_whole_rounds(rows, classes, dim, k, dtype):
+    """Classes on two sizes of tiles: of the logits, and of the weights' gradient."""
+    test_large(rows, classes, dim, k, True, dtype)
