@@ -1,5 +1,8 @@
 """The operators of a last layer over many classes put together: trained, distilled from a teacher served in integers, as a frozen right partition, joined."""
 
+import os
+import re
+
 import numpy as np
 import pytest
 import torch
@@ -113,3 +116,25 @@ def test_right_partition():
     assert torch.equal(z, torch.cat([right.forward(left.forward(X[a:a + 64])) for a in range(0, 150, 64)]))
     hits = pipeline.accuracy([left, right], X, y, batch=64)
     assert hits == (_np(z).argmax(1) == y.cpu().numpy()).mean()                    # (numpy's is the first among equals)
+
+
+def test_the_readmes_example():
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    block = re.search(r"\n\n((?:    .*\n)*    r = api\.linear_cross_entropy(?:.*\n)(?:    .*\n)*)", text).group(1)
+    x, V, b = _rows(21, 70, 200), _rows(22, 500, 200) / 16, _rows(23, 1, 500)[0].float()
+    y = torch.randint(-40, 500, (70,), dtype=torch.int32, generator=torch.Generator().manual_seed(24)).cuda()
+    teacher = _rows(25, 70, 500)
+    have = {"api": api, "x": x, "V": V, "b": b, "y": y, "teacher_logits": teacher}
+    exec(re.sub(r"^    ", "", block, flags=re.M), have)
+    top, ids = teacher.topk(32, 1)
+    o = class_loss.loss(_np(x), _np(V), y.cpu().numpy()[:, None], bias=_np(b))
+    od = class_loss.loss(_np(x), _np(V), ids.cpu().numpy(), _np(top), _np(b), 2.0)
+    # logits below 16: 200 additions' 2^-24 of it come to 2e-4 at the most, of random sign to 1.4e-5; twice that, 4 times with the temperature squared
+    assert abs(float(have["r"].loss) - o["loss"]) < 1e-4 and abs(float(have["d"].loss) - od["loss"]) < 1e-4
+    _off(have["r"].dx, o["dx"], 1.05 * 2.0 ** -8 * (np.abs(o["dz"]) @ np.abs(_np(V))) + 1.01 * 2.0 ** -8 * np.abs(o["dx"]) + 1e-8)
+    # an integer is half a scale off
+    X, W = _np(x), _np(V)
+    sx, sw = np.abs(X).max(1)[:, None] / 127, np.abs(W).max(1)[:, None] / 127
+    tol = (sx / 2 * np.abs(W).sum(1) + np.abs(X).sum(1)[:, None] * sw.T / 2 + 200 * sx * sw.T / 4) * (1 + 2.0 ** -20)
+    z = X @ W.T + _np(b)
+    _off(have["z"], z, tol * (1 + 2.0 ** -8) + 1.01 * 2.0 ** -8 * np.abs(z))
