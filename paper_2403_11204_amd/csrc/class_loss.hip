@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void target_logits_kernel(const TargetLogits a
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum += u[e] * v[e];
   }
-  sum = sum_of_64(sum);
+  sum = TEAM == 16 ? sum_of_16(sum) : sum_of_64(sum);
   if constexpr (TEAM == 256) {
     __shared__ float part[4];
     if ((lane & 63) == 0) part[lane >> 6] = sum;
@@ -187,14 +187,16 @@ __global__ __launch_bounds__(256) void row_loss_kernel(const RowLoss a) {
     float2 top = {-INFINITY, 0.0f};
     for (int j = s; j < k; j += TEAM) {
       const float t = teacher(a.t, row, j, a.classes);
+      entries[r * (k | 1) + j] = float2{__builtin_bit_cast(float, class_of(a.t, row, j, a.classes)), t};      // (read again by this thread alone)
       if (t != -INFINITY) top = joined(top, float2{t, 1.0f});
     }
     top = all(top);
     counts = top.y != 0.0f;               // (a NaN counts)
     const float log_sum = logf(top.y);
     for (int j = s; j < k; j += TEAM) {
-      const int c = class_of(a.t, row, j, a.classes);
-      const float t = teacher(a.t, row, j, a.classes), z = c >= 0 ? logit(j, c) : 0.0f;
+      const float2 e = entries[r * (k | 1) + j];
+      const int c = __builtin_bit_cast(int, e.x);
+      const float t = e.y, z = c >= 0 ? logit(j, c) : 0.0f;
       const float logp = t - top.x - log_sum, p = counts && t != -INFINITY ? expf(t - top.x) / top.y : 0.0f;
       entries[r * (k | 1) + j] = float2{__builtin_bit_cast(float, c), p};
       if (p != 0.0f) loss += p * (logp + log_all + (mine.x - z));
@@ -206,6 +208,7 @@ __global__ __launch_bounds__(256) void row_loss_kernel(const RowLoss a) {
       const int c = __builtin_bit_cast(int, entries[r * (k | 1) + j].x);
       float sum = 0.0f;
       bool first = true;
+#pragma unroll 8
       for (int i = 0; i < k; ++i) {
         const float2 e = entries[r * (k | 1) + i];
         if (__builtin_bit_cast(int, e.x) == c) {
@@ -436,6 +439,10 @@ hipError_t launch_target_logits(int dtype, const TargetLogits& a, hipStream_t s)
   if (targets <= 1024) {
     if (dtype == 1) target_logits_kernel<bf16, 256><<<(unsigned)targets, 256, 0, s>>>(a);
     else target_logits_kernel<float, 256><<<(unsigned)targets, 256, 0, s>>>(a);
+  } else if (a.dim <= 512) {
+    const unsigned few = blocks(targets, 16);
+    if (dtype == 1) target_logits_kernel<bf16, 16><<<few, 256, 0, s>>>(a);
+    else target_logits_kernel<float, 16><<<few, 256, 0, s>>>(a);
   } else if (dtype == 1) target_logits_kernel<bf16, 64><<<n, 256, 0, s>>>(a);
   else target_logits_kernel<float, 64><<<n, 256, 0, s>>>(a);
   return hipGetLastError();

@@ -109,41 +109,22 @@ __device__ __forceinline__ float probability(float z, float2 norm, bool label) {
 // The tail of a wavefront's (16 MI) x (16 NI) sums at row m0, column n0: lane l holds in acc[i][j] the columns n0 + 16 j + 4 (l / 16) .. + 3 of row
 // m0 + 16 i + l % 16.
 template <typename T, int KIND, int MI, int NI>
-__device__ __forceinline__ void finish(const ClassProduct& g, f32x4 (&acc)[MI][NI], int m0, int n0, int lane, int part) {
+__device__ __forceinline__ void finish(const ClassProduct& g, f32x4 (&acc)[MI][NI], int m0, int n0, int lane) {
   const int lgrp = lane >> 4, lrow = lane & 15;
   if constexpr (KIND >= PRODUCT_DX) {
     // (float32, see Side::fragments: rows that lie the other way are dealt out one by one, columns 4 NI side by side to a lane)
     constexpr bool AROUND = sizeof(T) == 4 && KIND == PRODUCT_DW, BROUND = sizeof(T) == 4 && KIND != PRODUCT_Z;
     auto row = [&](int i) { return AROUND ? m0 + MI * lrow + i : m0 + 16 * i + lrow; };
     auto col = [&](int j) { return BROUND ? n0 + 4 * NI * lgrp + 4 * j : n0 + 16 * j + 4 * lgrp; };
-    if (g.work) {
-      const int64_t ldw = (g.N + 3) & ~3;
+    // (to bf16; float32 has gone through LDS, and the bf16 of larger bf16 tiles)
+    const float alpha = *g.alpha;
 #pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        const int n = col(j);
+    for (int j = 0; j < NI; ++j) {
+      const int n = col(j);
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
-          const int m = row(i);
-          if (m < g.M && n < g.N) {
-            f32x4* const to = (f32x4*)(g.work + ((int64_t)part * g.M + m) * ldw + n);
-            *to = g.add ? *to + acc[i][j] : acc[i][j];
-          }
-        }
-      }
-    } else {
-      const float alpha = *g.alpha;
-#pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        const int n = col(j);
-#pragma unroll
-        for (int i = 0; i < MI; ++i) {
-          const int m = row(i);
-          if (m < g.M && n < g.N) {
-            const int64_t at = (int64_t)m * g.ldo + n;
-            if (g.out_dtype == 1) store4((bf16*)g.out + at, g.N - n, acc[i][j] * alpha);
-            else store4((float*)g.out + at, g.N - n, acc[i][j] * alpha);
-          }
-        }
+      for (int i = 0; i < MI; ++i) {
+        const int m = row(i);
+        if (m < g.M && n < g.N) store4((bf16*)g.out + (int64_t)m * g.ldo + n, g.N - n, acc[i][j] * alpha);
       }
     }
   } else {
@@ -444,7 +425,40 @@ __device__ __forceinline__ void class_tile(const ClassProduct& g, int kper, int 
       return;
     }
   }
-  finish<T, KIND, MI, NI>(g, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), lane, part);
+  if constexpr (KIND >= PRODUCT_DX) {
+    if (g.work || g.out_dtype == 0) {
+      // float32 the same, rows of 4 NI pieces: lanes hold 4 consecutive columns, which alone would leave 16 bytes at a time
+      constexpr int PIECES = 4 * NI, EACH = 64 / PIECES;
+      constexpr bool AROUND = sizeof(T) == 4 && KMA, BROUND = sizeof(T) == 4 && KMB;
+      static_assert(MI * NI * 4096 <= NS * STAGE, "room for the wavefronts' parts");
+      auto key = [](int r) { return (AROUND ? r / MI : r) & (PIECES - 1); };
+      const int lgrp = lane >> 4, lrow = lane & 15;
+      const float alpha = g.work ? 1.0f : *g.alpha;
+      unsigned char* const st = smem + w * (MI * NI * 1024);
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          const int r = AROUND ? MI * lrow + i : 16 * i + lrow, c = BROUND ? NI * lgrp + j : 4 * j + lgrp;
+          *(f32x4*)(st + r * (PIECES * 16) + ((c ^ key(r)) << 4)) = acc[i][j] * alpha;
+        }
+      const int64_t ld = g.work ? (g.N + 3) & ~3 : g.ldo;
+      float* const out = g.work ? g.work + (int64_t)part * g.M * ld : (float*)g.out;
+      const int c = lane % PIECES, n = n0 + wn * (BN / 2) + 4 * c, left = g.work ? 4 : g.N - n;
+#pragma unroll
+      for (int q = 0; q < MI * NI; ++q) {
+        const int r = q * EACH + lane / PIECES, m = m0 + wm * (BM / 2) + r;
+        f32x4 v = *(const f32x4*)(st + r * (PIECES * 16) + ((c ^ key(r)) << 4));
+        if (m < g.M && n < g.N) {
+          float* const to = out + (int64_t)m * ld + n;
+          if (g.work && g.add) v += *(const f32x4*)to;
+          store4(to, left, v);
+        }
+      }
+      return;
+    }
+  }
+  finish<T, KIND, MI, NI>(g, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), lane);
 #endif
 }
 template <typename T, int KIND, int BM, int BN, int NS, int NG>
