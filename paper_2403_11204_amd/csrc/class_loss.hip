@@ -23,13 +23,13 @@ __device__ __forceinline__ int class_of(const Targets& t, int64_t row, int j, in
 }
 // The teacher's logit over the temperature; -infinity for an entry that does not count.
 __device__ __forceinline__ float teacher(const Targets& t, int64_t row, int j, int classes) {
-  if (class_of(t, row, j, classes) < 0) return -INFINITY;
   const int64_t at = row * t.ldtop + j;
-  return (t.top_dtype == 1 ? (float)((const bf16*)t.top)[at] : ((const float*)t.top)[at]) * t.per_t;
+  const float z = (t.top_dtype == 1 ? (float)((const bf16*)t.top)[at] : ((const float*)t.top)[at]) * t.per_t;
+  return class_of(t, row, j, classes) < 0 ? -INFINITY : z;
 }
 
 // The dot product of a row of x and the row of W that is its class, one wavefront for each target; a workgroup where they are few and each waits for its own loads (1 target of
-// 4096 bf16 8.2 us on a wavefront, 5 on a workgroup).  Many are bound by reading those rows of W: 4096 x 64 targets of 4096 bf16 are 2.1 GB.
+// 4096 bf16 8.2 us on a wavefront, 5 on a workgroup), 16 lanes where rows are short (6146 x 25 targets of 170 46 / 18).  Many are bound by reading those rows of W: 4096 x 64 targets of 4096 bf16 are 2.1 GB.
 template <typename T, int TEAM>
 __global__ __launch_bounds__(256) void target_logits_kernel(const TargetLogits a) {
   const int64_t at = (int64_t)blockIdx.x * (256 / TEAM) + threadIdx.x / TEAM;
@@ -185,6 +185,7 @@ __global__ __launch_bounds__(256) void row_loss_kernel(const RowLoss a) {
   } else {
     const int k = in ? a.t.k : 0;
     float2 top = {-INFINITY, 0.0f};
+#pragma unroll 4
     for (int j = s; j < k; j += TEAM) {
       const float t = teacher(a.t, row, j, a.classes);
       entries[r * (k | 1) + j] = float2{__builtin_bit_cast(float, class_of(a.t, row, j, a.classes)), t};      // (read again by this thread alone)
@@ -208,13 +209,23 @@ __global__ __launch_bounds__(256) void row_loss_kernel(const RowLoss a) {
       const int c = __builtin_bit_cast(int, entries[r * (k | 1) + j].x);
       float sum = 0.0f;
       bool first = true;
-#pragma unroll 8
-      for (int i = 0; i < k; ++i) {
-        const float2 e = entries[r * (k | 1) + i];
-        if (__builtin_bit_cast(int, e.x) == c) {
-          sum += e.y;
-          first &= i >= j;
+      int i = 0;
+      for (; i + 8 <= k; i += 8) {       // eight reads under way
+        float2 e[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) e[q] = entries[r * (k | 1) + i + q];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const bool same = __builtin_bit_cast(int, e[q].x) == c;
+          sum += same ? e[q].y : 0.0f;
+          first &= !same || i + q >= j;
         }
+      }
+      for (; i < k; ++i) {
+        const float2 e = entries[r * (k | 1) + i];
+        const bool same = __builtin_bit_cast(int, e.x) == c;
+        sum += same ? e.y : 0.0f;
+        first &= !same || i >= j;
       }
       a.p[row * k + j] = first ? sum : -1.0f;
     }

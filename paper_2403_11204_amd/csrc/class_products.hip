@@ -427,7 +427,7 @@ __device__ __forceinline__ void class_tile(const ClassProduct& g, int kper, int 
   }
   if constexpr (KIND >= PRODUCT_DX) {
     if (g.work || g.out_dtype == 0) {
-      // float32 the same, rows of 4 NI pieces: lanes hold 4 consecutive columns, which alone would leave 16 bytes at a time
+      // float32 the same, rows of 4 NI pieces: lanes hold 4 consecutive columns, which would leave 16 bytes at a time (dW of 21 x 81199 x 2048 468 us, in whole segments 167)
       constexpr int PIECES = 4 * NI, EACH = 64 / PIECES;
       constexpr bool AROUND = sizeof(T) == 4 && KMA, BROUND = sizeof(T) == 4 && KMB;
       static_assert(MI * NI * 4096 <= NS * STAGE, "room for the wavefronts' parts");
