@@ -318,7 +318,7 @@ struct Side {
 
 // BM x BN tile, 4 wavefronts in a 2 x 2 grid, NS LDS stages of a k-tile of 128 bytes each, one barrier a k-tile.  NG such groups of wavefronts take a part of the
 // contraction each (kper k-tiles) and are added up in order at the end.  part: of the contraction, of a whole workgroup.
-// Bound by LDS and conversions between barriers: float32 (six products) 333 x 5001 x 777 34 to 38 us each (70 to 75 TFLOP/s, 420 to 450 of products), 4096 x 4096 x 4096 all three 171 to 177;
+// Bound by LDS and conversions between barriers: float32 (six products) 333 x 5001 x 777 34 to 37 us each (70 to 75 TFLOP/s, 420 to 450 of products), 4096 x 4096 x 4096 all three 171 to 177;
 // where W is read once and little else happens, by memory: logits of 1 x 131072 x 4096 bf16 170 us, 6.3 TB/s.
 template <typename T, int KIND, int BM, int BN, int NS, int NG>
 __device__ __forceinline__ void class_tile(const ClassProduct& g, int kper, int pid, int part, unsigned char* all_smem) {
