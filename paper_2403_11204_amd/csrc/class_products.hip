@@ -670,13 +670,15 @@ enum Tile { kLong, k128, k128x64, k64, k64by2, k32x64, k32x64by2, k32, k32by4 };
 //   few rows (logits), on 256x256 / 128x128 / 64x64: 1 x 131072 x 4096 216 / 180 / 170, 64 x 131072 x 1024 62 / 47 / 42, 128 x 131072 x 4096 249 / 200 / 320, 256 x
 //   131072 x 1024 71 / 93 / 128; few classes (dW): 8192 x 47 x 4096 24 / 19 / 16, 128 32 / 24 / 27;
 //   few rows of dX, whose W is read across: 1 x 131072 x 4096 225 / 238 / 184, 16 229 / 239 / 204, 64 252 / 270 / 255, 128 275 / 286 / 391; 64 x 131072 x 1024 62 / 62 /
-//   75, 128 x 65536 x 2048 73 / 66 / 102, 128 x 32768 x 2048 46 / 36 / 42.
+//   75, 128 x 65536 x 2048 73 / 66 / 102, 128 x 32768 x 2048 46 / 36 / 42;
+//   float32, which multiplies six times, on 64x64 / 32x64: logits of 8 x 131072 x 3180 572 / 430, of 21 x 81199 x 2048 290 / 261, dX of
+//   8 x 131072 x 2048 368 / 274; of 21 x 81199 x 2048 on 128x128 / 32x64 290 / 175.
 Tile shape_of(int kind, int dtype, int M, int N, int K, int parts = 1) {
   const int64_t nk = ((int64_t)K * (dtype == 1 ? 2 : 4) + 127) / 128 / parts;
   const int64_t t256 = tiles_of(M, N, 256, 256) * parts, t128 = tiles_of(M, N, 128, 128) * parts, t64 = tiles_of(M, N, 64, 64) * parts;
-  const bool few = M <= (kind == PRODUCT_DX ? 16 : 64);
+  const bool few = M <= (kind != PRODUCT_DX ? 64 : dtype == 1 ? 16 : 32);
   if (dtype == 1 && t256 >= (nk >= 16 ? 130 : 200) && nk > 2 && !few && (M > 128 || M <= 64)) return kLong;
-  if (few && t64 >= 512) return k64;
+  if (few && t64 >= 512) return dtype == 0 && M <= 32 ? k32x64 : k64;
   if (t128 >= 384) return k128;
   if (tiles_of(M, N, 128, 64) * parts >= 480) return k128x64;
   if (tiles_of(M, N, 32, 32) * parts <= 256) return nk >= 11 ? k32by4 : k32;

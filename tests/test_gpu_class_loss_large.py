@@ -78,7 +78,7 @@ def test_many_rows_of_few_classes(rows, classes, dim, k, dtype):
 
 @pytest.mark.parametrize("rows,classes,dim,k,dtype", [(5, 40000, 264, 0, "bf16"), (16, 66000, 128, 2, "bf16"), (33, 40008, 2056, 0, "bf16"), (64, 33000, 135, 3, "bf16"), (100, 34001, 520, 0, "bf16"),
                                                       (128, 33000, 128, 5, "bf16"), (129, 33000, 136, 0, "bf16"), (16500, 47, 4104, 0, "bf16"), (9000, 100, 2050, 2, "bf16"),
-                                                      (5, 40000, 264, 2, "fp32"), (64, 33001, 132, 0, "fp32"), (70, 33000, 100, 3, "fp32")])
+                                                      (5, 40000, 264, 2, "fp32"), (64, 33001, 132, 0, "fp32"), (70, 33000, 100, 3, "fp32"), (27, 33005, 388, 0, "fp32"), (32, 40000, 2052, 2, "fp32")])
 def test_few_rows_or_classes(rows, classes, dim, k, dtype):
     """Tiles that most of the rows' or classes' side does not fill; gradients of weights whose contraction is short."""
     test_large(rows, classes, dim, k, True, dtype)
