@@ -384,7 +384,7 @@ int slp_clip_gradients(const void* const* tensors /*host*/, void* const* out /*h
  * does; above 3.39e38 they count as infinite, below 2^-102 they lose bits, and a product with an infinity is NaN.  Sums are in a fixed order, targets' in integers: the same bits every time.
  * Logits that are NaN or +infinity make their row's loss, and what it reaches, NaN; -infinity (a class that the bias masks out) is a probability of 0.
  * Matrices may start at any element; x and w whose rows start on 16-byte boundaries and whose dim fills them are read in place, others are copied to the workspace first.  Outputs must not overlap
- * operands.  No rows: a loss of 0, dw and dbias become zeros.  The workspace is 256-byte aligned, of slp_linear_loss_workspace_bytes for the same pointers and sizes, and of no other call that may run at the same time; top: k of a distillation, 0 for a
+ * operands.  No rows: a loss of 0, dw and dbias become zeros.  The workspace is 256-byte aligned, of slp_linear_loss_workspace_bytes for the same pointers and sizes (0 for those that the calls refuse), and of no other call that may run at the same time; top: k of a distillation, 0 for a
  * cross-entropy; outputs: SLP_LOSS_* of the gradients wanted.
  * Errors: SLP_ERR_ARG (null pointer, negative rows, no classes or dim, unknown dtype or id size, k, T or scale out of range), SLP_ERR_SHAPE (a leading dimension below the row or, of x and w, above 2^20;
  * more than 2^20 rows or dim, 2^24 classes, 2^33 elements of x or w, 2^36 logits, 2^25 targets; with dw, rows of x that come to 2 GiB), SLP_ERR_ALLOC (alignment, workspace), SLP_ERR_DEVICE. */

@@ -300,13 +300,26 @@ int run(const Call& c, void* workspace, hipStream_t s) {
   return SLP_OK;
 }
 
-int check_call(const char* who, const Call& c) {
-  if (!known(c.dt) || (c.dw && !known(c.dw_dt))) return fail(SLP_ERR_ARG, "%s: unknown dtype %d", who, known(c.dt) ? c.dw_dt : c.dt);
+// Sizes and leading dimensions that plan_of takes: it divides by them.
+int check_sizes(const char* who, const Call& c) {
   if (c.rows < 0 || c.classes <= 0 || c.dim <= 0) return fail(SLP_ERR_ARG, "%s: rows %d, classes %d, dim %d", who, c.rows, c.classes, c.dim);
   if (c.rows > kMaxRows || c.classes > kMaxSide || c.dim > kMaxDim)
     return fail(SLP_ERR_SHAPE, "%s: up to %d rows, %d classes and a width of %d (got %d, %d, %d)", who, kMaxRows, kMaxSide, kMaxDim, c.rows, c.classes, c.dim);
   if ((int64_t)c.classes * c.dim > kMaxWeights || (int64_t)c.rows * c.dim > kMaxWeights || (int64_t)c.rows * c.classes > kMaxLogits || (int64_t)c.rows * c.t.k > kMaxTargets)
     return fail(SLP_ERR_SHAPE, "%s: %d rows of %d and %d classes, %d targets a row", who, c.rows, c.dim, c.classes, c.t.k);
+  return SLP_OK;
+}
+int check_rows(const char* who, const Call& c) {
+  SLP_CHECK(check_dense(who, "x", c.x, c.ldx, c.dim, c.dt));
+  SLP_CHECK(check_dense(who, "w", c.w, c.ldw, c.dim, c.dt));
+  if (c.dw && c.rows * row_ld(c.dim, (int64_t)size_of(c.dt)) * (int64_t)size_of(c.dt) >= kAcross) return fail(SLP_ERR_SHAPE, "%s: %d rows of %d come to 2 GiB", who, c.rows, c.dim);
+  if ((c.rows > 1 && c.ldx > kMaxPiece) || (c.classes > 1 && c.ldw > kMaxPiece)) return fail(SLP_ERR_SHAPE, "%s: rows of x and w lie at most %d elements apart", who, kMaxPiece);
+  return SLP_OK;
+}
+
+int check_call(const char* who, const Call& c) {
+  if (!known(c.dt) || (c.dw && !known(c.dw_dt))) return fail(SLP_ERR_ARG, "%s: unknown dtype %d", who, known(c.dt) ? c.dw_dt : c.dt);
+  SLP_CHECK(check_sizes(who, c));
   if (!(c.scale == c.scale) || c.scale - c.scale != 0.0f) return fail(SLP_ERR_ARG, "%s: the gradients' scale must be finite", who);
   if (!c.loss) return fail(SLP_ERR_ARG, "%s: null pointer", who);
   if (off(c.loss, 4) || off(c.losses, 4) || off(c.lse, 4) || off(c.bias, 4) || off(c.dbias, 4))
@@ -314,11 +327,8 @@ int check_call(const char* who, const Call& c) {
   if (c.dw) SLP_CHECK(check_dense(who, "dw", c.dw, c.lddw, c.dim, c.dw_dt));
   if (c.rows == 0) return SLP_OK;
   if (!c.x || !c.w || !c.t.ids || !c.losses || !c.lse) return fail(SLP_ERR_ARG, "%s: null pointer", who);
-  SLP_CHECK(check_dense(who, "x", c.x, c.ldx, c.dim, c.dt));
-  SLP_CHECK(check_dense(who, "w", c.w, c.ldw, c.dim, c.dt));
+  SLP_CHECK(check_rows(who, c));
   if (c.dx) SLP_CHECK(check_dense(who, "dx", c.dx, c.lddx, c.dim, c.dt));
-  if (c.dw && c.rows * row_ld(c.dim, (int64_t)size_of(c.dt)) * (int64_t)size_of(c.dt) >= kAcross) return fail(SLP_ERR_SHAPE, "%s: %d rows of %d come to 2 GiB", who, c.rows, c.dim);
-  if ((c.rows > 1 && c.ldx > kMaxPiece) || (c.classes > 1 && c.ldw > kMaxPiece)) return fail(SLP_ERR_SHAPE, "%s: rows of x and w lie at most %d elements apart", who, kMaxPiece);
   if (off(c.t.ids, c.t.ids64 ? 8 : 4)) return fail(SLP_ERR_ALLOC, "%s: class ids are not on an element's boundary", who);
   return SLP_OK;
 }
@@ -342,7 +352,8 @@ int loss_call(const char* who, const Call& c, void* workspace, size_t workspace_
 extern "C" {
 
 size_t slp_linear_loss_workspace_bytes(const void* x, int64_t ldx, const void* w, int64_t ldw, int dt, int rows, int classes, int dim, int top, int outputs) {
-  if (!known(dt) || rows <= 0 || classes <= 0 || dim <= 0 || rows > kMaxRows || classes > kMaxSide || dim > kMaxDim || top < 0 || top > kMaxTop) return 0;
+  const char* const who = "slp_linear_loss_workspace_bytes";
+  if (!known(dt) || rows <= 0 || top < 0 || top > kMaxTop) return 0;
   static char given;
   Call c{};
   c.x = x;
@@ -358,7 +369,8 @@ size_t slp_linear_loss_workspace_bytes(const void* x, int64_t ldx, const void* w
   c.dx = outputs & SLP_LOSS_DX ? &given : nullptr;
   c.dw = outputs & SLP_LOSS_DW ? &given : nullptr;
   c.dbias = outputs & SLP_LOSS_DBIAS ? (float*)&given : nullptr;
-  return plan_of(c).bytes;
+  // (the binding asks for the workspace before the call that reports what is out of range)
+  return check_sizes(who, c) || check_rows(who, c) ? 0 : plan_of(c).bytes;
 }
 
 int slp_linear_cross_entropy(const void* x, int64_t ldx, const void* w, int64_t ldw, const float* bias, int dt, int rows, int classes, int dim, const void* targets,
