@@ -333,7 +333,7 @@ int slp_product(const void* a /*device*/, int64_t lda, const void* a_scales, int
  * slp_quantize_integers: q = round(127 x / max|x|) over each row, ties to even, of the real quotient; scale = max|x| / 127.  A row of zeros has the scale 0, one that holds an
  * infinity or a NaN zeros and the scale NaN.  Written up to the next multiple of 16 columns.
  * slp_product_integers: out[M][N] = act(a_scales[m] b_scales[n] sum over k of A[m][k] B[n][k] + bias[n]), out of dtype dt; the sums are exact, K up to 131071 (any signed byte may stand
- * in A and B); scales, bias and ReLU (where relu is not 0; a NaN stays one) in float32.  The workspace holds parts of a contraction that is split over the chip; 256-byte aligned, 0 for most large products, and no other call's that may run at the same time.
+ * in A and B); scales, bias and ReLU (where relu is not 0; a NaN stays one) in float32, of which no step on the way leaves the range where the result does not.  The workspace holds parts of a contraction that is split over the chip; 256-byte aligned, 0 for most large products, and no other call's that may run at the same time.
  * Limits and errors as for 8-bit matrices; SLP_ERR_SHAPE also for a longer contraction. */
 int slp_quantize_integers(const void* x /*device*/, int64_t ldx, int dt, int rows, int cols, void* q /*device*/, int64_t ldq, float* scales /*device*/, slp_stream stream);
 size_t slp_product_integers_workspace_bytes(int M, int N, int K);
