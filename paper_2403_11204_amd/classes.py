@@ -8,6 +8,9 @@ Of api.Segment's calls the class has step, input_grad and forward, so it can be 
 (pipeline.train_epochs), be the frozen right partition of pipeline.recovery_epochs, and be joined (pipeline.joined_forward,
 pipeline.accuracy).  forward computes in integers: it is the serving form.
 
+A new layer is ready on every stream.  step, distil and refresh write the parameters and their copies (bf16, integers) on the current stream; input_grad and forward
+only read them, on any number of streams at once, which wait for the last of those writes as for any tensor's.
+
     right = ClassLayer(width=512, classes=50000)
     losses = pipeline.train_epochs(right, stored, y, epochs=3, batch=1024)         # stored: bf16 [N, 512], y: int32 [N]
     top, ids = teacher.forward(x).topk(32, 1)                                      # another ClassLayer, say, on rows x
@@ -28,11 +31,12 @@ class ClassLayer:
         self.w, self.b = (torch.nn.Parameter(torch.from_numpy(a).to(device)) for a in (w, b))
         self.optimizer = torch.optim.SGD([self.w, self.b], lr=lr, momentum=momentum)
         self.refresh()
+        torch.cuda.current_stream(self.w.device).synchronize()
 
     def refresh(self):
-        """The copies of the weights that the products read, after the float32 ones have changed."""
+        """The copies of the weights that the products read, after the float32 ones have changed: here, not in the first call that needs them, whose stream others do not wait for."""
         self.w16 = self.w.data.bfloat16()
-        self._w8 = None
+        self._w8 = api.quantize_integers(self.w.data)
 
     def _update(self, r):
         self.w.grad, self.b.grad = r.dw, r.dbias
@@ -58,6 +62,4 @@ class ClassLayer:
 
     def forward(self, X, out=None):
         """The logits, in bf16 (or of out's type): rows and weights as integers with a scale each."""
-        if self._w8 is None:
-            self._w8 = api.quantize_integers(self.w.data)
         return api.product_integers(api.quantize_integers(X), self._w8, bias=self.b.data, out=out)
