@@ -257,9 +257,11 @@ def product(a, b, bias=None, relu=False, dtype=BF16, out=None, float32_sums=Fals
 Integers = collections.namedtuple("Integers", "q scales")
 
 
-def quantize_integers(x):
-    """slp_quantize_integers: the rows of x (tokens, or the output channels of a weight matrix) as integers from -127 to 127, each with its own scale."""
-    return Integers(*_outputs(_binding().quantize_integers(x)))
+def quantize_integers(x, out=None):
+    """slp_quantize_integers: the rows of x (tokens, or the output channels of a weight matrix) as integers from -127 to 127, each with its own scale (into `out`, an Integers
+    of its shape whose rows have room up to the next multiple of 16 columns, where that is given)."""
+    q, scales = out or (None, None)
+    return Integers(*_outputs(_binding().quantize_integers(x, q, scales)))
 
 
 def product_integers(a, b, bias=None, relu=False, dtype=BF16, out=None):

@@ -9,7 +9,8 @@ Of api.Segment's calls the class has step, input_grad and forward, so it can be 
 pipeline.accuracy).  forward computes in integers: it is the serving form.
 
 A new layer is ready on every stream.  step, distil and refresh write the parameters and their copies (bf16, integers) on the current stream; input_grad and forward
-only read them, on any number of streams at once, which wait for the last of those writes as for any tensor's.
+only read them, on any number of streams at once, which wait for the last of those writes as for any tensor's.  All of these stay where they are for as long as the layer
+lives, so that a captured call works on the parameters of the time of its replay; what a captured step calculates with besides, lr among it, is that of its capture.
 
     right = ClassLayer(width=512, classes=50000)
     losses = pipeline.train_epochs(right, stored, y, epochs=3, batch=1024)         # stored: bf16 [N, 512], y: int32 [N]
@@ -30,13 +31,16 @@ class ClassLayer:
         (w, b), = datagen.uniform_weights(self.widths, seed)
         self.w, self.b = (torch.nn.Parameter(torch.from_numpy(a).to(device)) for a in (w, b))
         self.optimizer = torch.optim.SGD([self.w, self.b], lr=lr, momentum=momentum)
-        self.refresh()
+        if momentum:                       # from zeros the first step is like the others, also where it is a captured one
+            for p in (self.w, self.b):
+                self.optimizer.state[p]["momentum_buffer"] = torch.zeros_like(p.data)
+        self.w16, self._w8 = self.w.data.bfloat16(), api.quantize_integers(self.w.data)
         torch.cuda.current_stream(self.w.device).synchronize()
 
     def refresh(self):
         """The copies of the weights that the products read, after the float32 ones have changed: here, not in the first call that needs them, whose stream others do not wait for."""
-        self.w16 = self.w.data.bfloat16()
-        self._w8 = api.quantize_integers(self.w.data)
+        self.w16.copy_(self.w.data)
+        api.quantize_integers(self.w.data, out=self._w8)
 
     def _update(self, r):
         self.w.grad, self.b.grad = r.dw, r.dbias

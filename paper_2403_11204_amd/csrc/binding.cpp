@@ -243,19 +243,6 @@ PyObject* product(PyObject* const* a) {
   return wrapped(out);
 }
 
-// x
-PyObject* quantize_integers(PyObject* const* a) {
-  const at::Tensor& x = tensor(a[0]);
-  const int64_t ldx = leading(x), m = x.size(0), n = x.size(1), ld = eight_ld(m, n);
-  const int dt = dtype_of(x);
-  const On on(x.device());
-  Room room(x.device(), Room::padded((size_t)(m * ld)) + Room::padded(4 * m), 0);
-  const at::Tensor q = room.take({m, ld}, at::kChar), scales = room.take({m}, at::kFloat);
-  if (ld != n) q.unsafeGetTensorImpl()->set_sizes_and_strides(at::IntArrayRef({m, n}), at::IntArrayRef({ld, 1}));
-  const int rc = slp_quantize_integers(x.data_ptr(), ldx, dt, side(m), side(n), q.data_ptr(), ld, (float*)scales.data_ptr(), on.stream());
-  return rc ? code(rc) : tuple({q, scales});
-}
-
 // A matrix of integers: its leading dimension and scales.
 const float* integers_given(PyObject* q, PyObject* scales, int64_t cols, int64_t& ld) {
   const at::Tensor& t = tensor(q);
@@ -264,6 +251,31 @@ const float* integers_given(PyObject* q, PyObject* scales, int64_t cols, int64_t
   ld = t.size(0) <= 1 ? (cols + 15) / 16 * 16 : t.stride(0);
   require(given(scales), "scales of float32, one a row, are wanted");
   return vector(scales, t.size(0), t);
+}
+
+// x, out's values, scales
+PyObject* quantize_integers(PyObject* const* a) {
+  const at::Tensor& x = tensor(a[0]);
+  const int64_t ldx = leading(x), m = x.size(0), n = x.size(1), end = (n + 15) / 16 * 16;
+  const int dt = dtype_of(x);
+  const On on(x.device());
+  int64_t ld = eight_ld(m, n);
+  at::Tensor q, scales;
+  if (given(a[1])) {
+    integers_given(a[1], a[2], n, ld);
+    q = tensor(a[1]);
+    scales = tensor(a[2]);
+    require(q.size(0) == m && q.device() == x.device(), "an output of the matrix's shape is wanted");
+    // (rows are written up to the next multiple of 16)
+    require(m == 0 || n == 0 || q.storage_offset() + (m - 1) * ld + end <= (int64_t)q.storage().nbytes(), "an output whose rows have room for whole 16 bytes is wanted");
+  } else {
+    Room room(x.device(), Room::padded((size_t)(m * ld)) + Room::padded(4 * m), 0);
+    q = room.take({m, ld}, at::kChar);
+    scales = room.take({m}, at::kFloat);
+    if (ld != n) q.unsafeGetTensorImpl()->set_sizes_and_strides(at::IntArrayRef({m, n}), at::IntArrayRef({ld, 1}));
+  }
+  const int rc = slp_quantize_integers(x.data_ptr(), ldx, dt, side(m), side(n), q.data_ptr(), ld, (float*)scales.data_ptr(), on.stream());
+  return rc ? code(rc) : tuple({q, scales});
 }
 
 // a's values, scales, b's, bias, relu, dtype, out
@@ -498,7 +510,7 @@ PyMethodDef method(const char* name) {
 
 PyMethodDef methods[] = {method<quantize, 6>("quantize"),           method<product, 11>("product"), method<rmsnorm, 6>("rmsnorm"), method<rmsnorm_backward, 6>("rmsnorm_backward"),
                          method<gradient_norm, 1>("gradient_norm"), method<clip_gradients, 3>("clip_gradients"),
-                         method<quantize_integers, 1>("quantize_integers"), method<product_integers, 8>("product_integers"),
+                         method<quantize_integers, 3>("quantize_integers"), method<product_integers, 8>("product_integers"),
                          method<linear_cross_entropy, 8>("linear_cross_entropy"), method<linear_distillation, 10>("linear_distillation"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
