@@ -369,8 +369,13 @@ int slp_clip_gradients(const void* const* tensors /*host*/, void* const* out /*h
 
 /* ---- losses over the classes of a linear layer --------------------------------------------------
  * z = x W^T + b for rows x[rows][dim] and weights w[classes][dim] (both of dtype dt), bias float32 [classes] or NULL.  The logits z are computed tile by tile and do not have to
- * fit in memory: beside its operands and outputs a call takes a workspace of at most 1 GiB for logits that it keeps in float32 until their gradient is due (the others are
- * computed again), 256 MB for the gradient of a piece of them, and what grows with rows x dim (the rows that count, partial sums of dx) and with rows x classes / 16 at most (statistics).  For each row
+ * fit in memory.  Beside its operands and outputs a call takes a workspace of, at most,
+ *   1 GiB for logits that are kept in float32 until their gradient is due (the others are computed again; none where no gradient is wanted), 256 MB for the gradient of a piece of the
+ *   classes, or 256 classes of every row where that is more (1 GiB for 2^20 rows in float32); rows of both are padded by up to 256 bytes;
+ *   x once more for dw, or where it cannot be read in place, and up to 2 GiB of w where that cannot, their rows padded as well;
+ *   partial sums: 68 MB, or float32 [rows][dim] where that is more, for dx, 68 MB for dw, 20 MB for dbias, 64 MB for logits of few tiles;
+ *   8 bytes for each row and 16 classes (and 64 of these a row), for each class (dbias of a distillation) and for each entry of a row, 32 for each row, 4 KB.
+ * For each row
  *   lse = log sum over the classes of exp(z / T)                                      (float32 [rows], of rows that do not count as well)
  * slp_linear_cross_entropy (T = 1): targets[rows] are class ids (target_bytes 4 or 8: int32 or int64).  loss = lse - z_target.
  * slp_linear_distillation: top[rows][k] (dtype top_dt) are a teacher's logits of the classes top_classes[rows][k] (class_bytes 4 or 8), in any order, k from 1 to 1024,

@@ -10,9 +10,9 @@ using namespace slp;
 namespace {
 
 constexpr int kMaxRows = 1 << 20, kMaxDim = 1 << 20, kMaxTop = 1024;
-// P of a piece of the classes takes this much at most.
+// P of a piece of the classes takes this much at most, or what 256 classes take (the width of a tile), and the padding of its rows.
 constexpr int64_t kPieceBytes = 256 << 20;
-// Logits that are kept in float32 between the loss and the gradient, where they are wanted: what fits here.  A piece of others is computed twice, which takes the third of three products
+// Logits that are kept in float32 between the loss and the gradient, where they are wanted: what fits here without the padding of their rows.  A piece of others is computed twice, which takes the third of three products
 // again.
 constexpr int64_t kKeptBytes = (int64_t)1 << 30;
 // A tile of 256 rows is addressed with 32-bit offsets: rows of x, W and P lie at most this many elements apart.
