@@ -44,3 +44,38 @@ def test_labels_of_one_piece(dtype, dim):
         off = (r.dx.double() - G @ W).abs() - (err @ W.abs() + 6 * classes ** 0.5 * 2.0 ** -24 * (G.abs() @ W.abs()) + 1.01 * half * (G @ W).abs() + 1e-30)
         assert off.max() <= 0, (first, float(off.max()))
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype,dim,k", [("bf16", 264, 0), ("bf16", 264, 2), ("bf16", 40, 0), ("fp32", 68, 0), ("bf16", 261, 0)])
+def test_padding_and_masked_classes(dtype, dim, k):
+    """Rows that do not count hold anything, classes that the bias leaves out have no gradient, a row with a NaN reaches its own, in all pieces; and the same bits every time."""
+    from paper_2403_11204_amd import api
+    rows, classes, masked = 5003, 60001, torch.tensor([0, 5, 20223, 20224, 45000, 59999, 60000], device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn(rows, dim, device="cuda", generator=g).to(large.DT[dtype])
+    w = (torch.randn(classes, dim, device="cuda", generator=g) * (2.5 / dim ** 0.5)).to(large.DT[dtype])
+    b = torch.randn(classes, device="cuda", generator=g)
+    b[masked] = -float("inf")
+    ids = torch.randint(6, 20000, (rows, max(k, 1)), device="cuda", generator=g)
+    ids[2500:] += 25000                                                    # (the second and the third piece; none of the masked)
+    ids[ids == 45000] += 1
+    padding = torch.arange(0, rows, 17, device="cuda")
+    ids[padding] = -1
+    top = torch.randn(rows, k, device="cuda", generator=g) if k else None
+    call = lambda x: api.linear_distillation(x, w, top, ids, bias=b, temperature=2.0) if k else api.linear_cross_entropy(x, w, ids[:, 0].contiguous(), bias=b)  # noqa: E731
+    r = call(x)
+    assert all(torch.isfinite(t).all() for t in r)
+    assert not r.dw[masked].any() and not r.dbias[masked].any() and not r.dx[padding].any() and not r.losses[padding].any()
+    for value in (float("nan"), float("inf")):
+        y = x.clone()
+        y[padding] = value
+        again = call(y)
+        for name in ("loss", "losses", "dx", "dw", "dbias"):
+            assert torch.equal(getattr(r, name), getattr(again, name)), name
+    assert all(torch.equal(u, v) for u, v in zip(r, call(x)))
+    x[1, 3] = float("nan")                                                 # a row that counts
+    bad = call(x)
+    others = torch.arange(rows, device="cuda") != 1
+    assert bad.loss.isnan() and bad.dx[1].isnan().all() and bad.dw.isnan().all() and bad.dbias.isnan().all()
+    assert torch.equal(bad.dx[others], r.dx[others]) and torch.equal(bad.losses[others], r.losses[others])
+    torch.cuda.empty_cache()
