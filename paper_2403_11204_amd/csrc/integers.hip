@@ -162,7 +162,7 @@ __device__ __forceinline__ void store4(const IntegerProductArgs& g, int m, int n
 
 // BM x BN tile, 4 wavefronts in a 2 x 2 grid, NS LDS stages of a k-tile of 128 each, one barrier a k-tile.  NG such groups of wavefronts
 // take a part of the contraction each (kper k-tiles) and are added up at the end.  blockIdx.y: part of the contraction of a whole workgroup; several parts
-// leave partial sums for integer_join_kernel.  48 x 4096 x 8192 10.8 us (3.1 TB/s of B, 2.5 of them the launch), 1000 x 3001 x 1500 float32 13.9: three workgroups a
+// leave partial sums for integer_join_kernel.  48 x 4096 x 8192 10.7 us (3.1 TB/s of B, 2.5 of them the launch), 1000 x 3001 x 1500 float32 13.8: three workgroups a
 // compute unit, loads, barriers and LDS in turn, 12 MB of output.
 template <int BM, int BN, int NS, int NG>
 __global__ __launch_bounds__(256 * NG) void integer_tile_kernel(const IntegerProductArgs g, int kper) {
@@ -310,7 +310,7 @@ __global__ __launch_bounds__(256 * NG) void integer_tile_kernel(const IntegerPro
 
 // Few rows: bound by reading B once.  A workgroup takes 16 rows of B, its wavefronts take turns along the contraction, STEP k-tiles at a time whose loads are
 // all under way together, from memory straight into the fragments' registers; the parts are added up at the end.  MF fragments of 16 rows of A.
-// 1 x 4096 x 4096 5.7 us, 2.5 of them the launch.
+// 1 x 4096 x 4096 5.4 us, 2.5 of them the launch.
 template <int MF, int STEP>
 __global__ __launch_bounds__(1024) void integer_rows_kernel(const IntegerProductArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)
